@@ -419,6 +419,79 @@ SAMP_API int samp_embed_ln(const samp_embedding_t *emb, const int32_t *token_ids
 SAMP_API int samp_pack_rows(const uint16_t *hidden, const int32_t *mask, int32_t B, int32_t S, int32_t H, float s_x,
                             void *packed, int32_t *cu_seqlens, int32_t *row_map, void *stream);
 
+/* ---- attention block of an 8-bit decoder -------------------------------------------------------------
+ * Operators for causal models whose activations bring their own steps, without calibration: a projection in 8-bit
+ * integers with a step for each token and each channel, a paged int8 cache of keys and values, attention of new tokens over
+ * that cache, and attention of whole prompts.  Activations are fp16 or bfloat16 (`type`), results are of the same type.
+ *
+ * Quantiser of a row (Appendix B with the row's own absmax in the place of a calibrated one): step = absmax / 127 in binary32, code = 127 x / absmax rounded half to even,
+ * decided exactly.  A row without a value of at least 2^-60 has step 1 and codes 0; a row that holds an infinity or NaN has codes
+ * 0 and a step of NaN, so that what is computed from it is NaN.
+ *
+ * Packed rows: sequence b has rows cu[b] .. cu[b+1] - 1 of the tensors (dev int32 [batch + 1]), any number of them, none included; cu
+ * NULL: max_new (max_rows, max_len) rows each.  The host's maximum must be no less than the longest; of a longer sequence only that many
+ * rows are computed.  Rows behind the last sequence are left as they were, as are those that an offset puts outside the tensors.  Device memory is not
+ * checked by the host.
+ * `ld...` is the distance of consecutive rows in values (a multiple of 8); inside a row the heads follow each other without a gap.     */
+enum { SAMP_TYPE_F16 = 0, SAMP_TYPE_BF16 = 1 };
+#define SAMP_MAX_ROW (1 << 22)
+#define SAMP_MAX_HEADS 1024
+
+/* codes dev int8 [M,K] and steps dev float [M] of x [M,K]; K % 8 == 0.                              */
+SAMP_API int samp_quantize_tokens(const uint16_t *x, int64_t ldx, int32_t type, int32_t M, int32_t K, int8_t *codes, float *steps, void *stream);
+
+/* out[m,n] = act(steps[m] * s_w[n] * sum_k codes[m,k] W[n,k] + bias[n]) as 16-bit [M,N]; Wp from samp_pack_weight_i8, s_w dev float [N], bias dev
+ * float [N] or NULL, act = GELU (erf) if gelu.  The sum is exact.  N % 16 == 0, K % 64 == 0, K <= 131072, N * K < 2^31.              */
+SAMP_API int samp_gemm_i8_tokens_packed(const int8_t *codes, const float *steps, const int8_t *Wp, const float *s_w, const float *bias, int32_t gelu,
+                                        uint16_t *out, int32_t type, int32_t M, int32_t N, int32_t K, void *stream);
+
+/* The two in one call, x [M,K] -> out [M,N]: the bytes that samp_quantize_tokens and samp_gemm_i8_tokens_packed give.
+ * workspace dev, 256-byte aligned; calls that share one must be stream-ordered.                      */
+SAMP_API size_t samp_linear_i8_tokens_workspace_bytes(int32_t M, int32_t K);
+SAMP_API int samp_linear_i8_tokens(const uint16_t *x, int64_t ldx, int32_t type, const int8_t *Wp, const float *s_w, const float *bias, int32_t gelu,
+                                   uint16_t *out, int32_t M, int32_t N, int32_t K, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A paged cache: codes dev int8 [pages, kv_heads, page_len, head_dim] and steps dev float [pages, kv_heads, page_len] of keys and of values;
+ * page_len a power of two from 16 to 1024, head_dim 64 or 128.  A sequence's page table is a row of `width` page numbers: position p lies
+ * in page table[b * width + p / page_len], at p % page_len.  A number that is none of the cache's pages (-1 for instance) is never followed: what would be written there is dropped, what would
+ * be read there is zeros, and attention does not see those positions.  Pages may be shared by sequences that read them; one that a call writes must belong to one
+ * sequence of the call, otherwise what it holds afterwards is undefined.                              */
+typedef struct {
+    int8_t *k, *v;
+    float *k_step, *v_step;
+    int32_t pages, kv_heads, page_len, head_dim;
+} samp_kv_cache_t;
+
+/* Writes the packed rows k, v [rows, kv_heads, head_dim] as the last cu[b+1] - cu[b] of the lens[b] positions of each sequence (lens dev
+ * int32 [batch], the new ones counted).                                                              */
+SAMP_API int samp_cache_write(const samp_kv_cache_t *cache, const uint16_t *k, int64_t ldk, const uint16_t *v, int64_t ldv, int32_t type,
+                              const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows,
+                              void *stream);
+
+/* Reads the last cu[b+1] - cu[b] of the lens[b] positions of each sequence back into packed k, v [rows, kv_heads, head_dim]: code * step,
+ * rounded once.                                                                                      */
+SAMP_API int samp_cache_read(const samp_kv_cache_t *cache, uint16_t *k, uint16_t *v, int32_t type, const int32_t *table, int32_t width, const int32_t *cu,
+                             const int32_t *lens, int32_t batch, int32_t max_rows, int32_t rows, void *stream);
+
+/* out [rows, heads, head_dim] = softmax(scale q K^T) V of the new tokens q [rows, heads, head_dim] over the cache, in which samp_cache_write has put
+ * their own keys and values: new token i of n sees the positions up to its own, lens[b] - n + i.  heads is a multiple of kv_heads; query head h reads
+ * key head h / (heads / kv_heads).  tree (dev uint64 [rows], or NULL): the new tokens are drafts; each sees all positions in front of the first draft, and draft j of its sequence
+ * if bit j of its word is set (its own bit like any other), up to 64 drafts.  A token that sees nothing gets zeros.
+ * max_len: the longest context that the host expects; it only decides how the work is cut.  workspace dev, 256-byte aligned; calls that share one must be
+ * stream-ordered.                                                                                    */
+SAMP_API size_t samp_attention_cache_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_new,
+                                                     int32_t max_len);
+SAMP_API int samp_attention_cache(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const int32_t *table,
+                                  int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t max_len, int32_t rows,
+                                  float scale, const uint64_t *tree, uint16_t *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* out [rows, heads, head_dim] = softmax(scale q K^T) V of whole prompts: q [rows, heads, head_dim], k and v [rows, kv_heads, head_dim], a query sees the
+ * keys of its sequence up to its own.  What a query does not see has no part in its result, infinities and NaN included.
+ * head_dim 64 or 128, heads a multiple of kv_heads.                                                   */
+SAMP_API int samp_attention_causal(const uint16_t *q, int64_t ldq, const uint16_t *k, int64_t ldk, const uint16_t *v, int64_t ldv, int32_t type,
+                                   int32_t heads, int32_t kv_heads, int32_t head_dim, const int32_t *cu, int32_t batch, int32_t max_len, int32_t rows,
+                                   float scale, uint16_t *out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

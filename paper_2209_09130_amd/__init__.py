@@ -10,3 +10,6 @@ from .binding import (  # noqa: F401
     gemm_i8_i32, gemm_i8_requant, gemm_i8_gelu_quant, gemm_i8_gelu_quant_packed, gemm_i8_requant_packed, pack_weight_i8, gelu_table_build, gemm_f16, gemm_f16_packed, pack_weight_f16, attention_i8, qkv_attention_i8, qkv_attention_i8_packed, qkv_attention_f16, qkv_attention_f16_packed, attention_f16, add_ln,
     quantize_weight, quantize_f16_i8, pack_rows, gelu_quant, set_gemm_config, allocate_decay_aware, recommend, code_histogram, classify, probe_mfma_rate, probe_copy_rate, probe_feed_rate,
 )
+from .decoder import (  # noqa: F401
+    KVCache, quantize_tokens, gemm_i8_tokens_packed, linear_i8_tokens, cache_write, cache_read, attention_cache, attention_causal,
+)

@@ -2,6 +2,7 @@
 // per-layer kernel sequence of Section 3.2 (seven kernels per layer plus entry / exit handling).
 #include "../../include/samp.h"
 #include "samp_common.h"
+#include "api_common.h"
 #include "side_streams.h"
 #include "gemm_rules.h"
 
@@ -15,11 +16,9 @@
 
 using namespace samp;
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
-
-int fail(int code, const char *fmt, ...)
+int samp::fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -28,15 +27,10 @@ int fail(int code, const char *fmt, ...)
     return code;
 }
 
-#define HIP_TRY(expr)                                                                               \
-    do {                                                                                            \
-        hipError_t e_ = (expr);                                                                     \
-        if (e_ != hipSuccess) return fail(SAMP_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_));    \
-    } while (0)
+namespace {
 
 constexpr size_t ALIGN = 256;
 size_t up(size_t v) { return (v + ALIGN - 1) / ALIGN * ALIGN; }
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool good_scale(float s) { return std::isfinite(s) && s > 0.0f; }
 // An int8 score is at most 64 * 127 * 127 in magnitude, so with the multiplier bounded like this the argument of
 // the softmax exponential stays above -2^30, the range its integer exponent arithmetic is good for.

@@ -1,0 +1,336 @@
+// Attention of a few new tokens per sequence over the int8 cache: O = softmax(scale q K^T) V with K = step_k[key] codes, V = step_v[key] codes.
+//
+// What bounds it is HBM: 2 (head_dim + 4) bytes per token and key head, against which the products are small.  So the loop is a stream: every wave
+// takes key tiles of its own (32 keys) straight from the pages into registers, there is no LDS and no barrier before its end, and the
+// query heads of a group (and the new tokens of a sequence) share what was read as the columns of the matrix products.  Long contexts are cut into
+// pieces (splits), each with a partial result, which a second kernel joins.
+//
+// Products are 16 x 16 x 32 in binary16, in which int8 codes are exact: 1024 + (code + 128) is a code's byte under the exponent byte 0x64, and one packed
+// addition takes 1152 off again.  S^T = K Q^T: a lane gets four keys of one query, two such tiles are the eight keys that it needs as the operand of
+// O^T += V^T P^T.  V^T is formed on the way: a lane holds head_dim / 16 neighbouring channels of eight keys, and the byte permute that widens codes takes
+// the two halves of a dword from two keys.  The steps of the keys multiply scores (K) and probabilities (V) in binary32.
+//
+// Softmax in one pass with a running reference m per query that bounds log2(p step_v): exponent(step_v) + score, so that p step_v fits binary16 (at most
+// 2^9) whatever the steps.  m moves (and the sums are scaled) only when a score exceeds it by 2^8, not for every new maximum.  Rounding p step_v to
+// binary16 is off by 2^-11 of each, below the rounding of the result.  Queries of bfloat16 are scaled by a power of two per row into binary16's range.
+#include "decoder.h"
+#include "divisor.h"
+
+namespace samp {
+namespace {
+
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+constexpr float LOWEST = -3.0e38f, SLACK = 8.0f;
+constexpr int TILE = 32;                                              // keys of a wave's step
+
+// halves 1024 + 128 + code from the dword whose bytes 0 and 2 are codes and 1 and 3 are zero; codes as binary16
+__device__ __forceinline__ int to_halves(unsigned bytes)
+{
+    const v2h biased = __builtin_bit_cast(v2h, bytes ^ 0x64806480u);
+    return __builtin_bit_cast(int, biased - v2h{(_Float16)1152.0f, (_Float16)1152.0f});
+}
+
+template <int D> struct KeyTile {
+    v4i k[2][D / 64];                                                 // two rows (keys r, 16 + r), 16 codes of each 64
+    int v[8][D / 64];                                                 // eight keys, D / 16 codes
+    v4f ks[2], vs[2];                                                 // steps of keys 4 g .. 4 g + 3 and 16 + 4 g ..
+    unsigned known;                                                   // bit h: the page of keys 16 h .. 16 h + 15 is one of the cache's
+};
+
+template <int D>
+__device__ __forceinline__ KeyTile<D> load_tile(const KvCache &c, const int *table, int head, int j0, int last, int r, int g)
+{
+    KeyTile<D> t;
+    t.known = 0;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        const int pos = min(j0 + 16 * h, last);                       // 16 keys lie in one page; past the end the last ones are read again, and masked
+        int page = table[pos >> c.page_shift];
+        const bool ok = (unsigned)page < (unsigned)c.pages;
+        t.known |= (unsigned)ok << h;
+        page = ok ? page : 0;
+        const size_t row = (((size_t)page * c.kv_heads + head) << c.page_shift) + (pos & ((1 << c.page_shift) - 1) & ~15);
+        const int8_t *k = c.k + row * D, *v = c.v + row * D;
+#pragma unroll
+        for (int i = 0; i < D / 64; i++) t.k[h][i] = *reinterpret_cast<const v4i *>(k + r * D + 64 * i + 16 * g);
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int8_t *at = v + (4 * g + u) * D + r * (D / 16);
+            if constexpr (D == 128) {
+                const v2i two = *reinterpret_cast<const v2i *>(at);
+                t.v[4 * h + u][0] = two[0];
+                t.v[4 * h + u][1] = two[1];
+            } else t.v[4 * h + u][0] = *reinterpret_cast<const int *>(at);
+        }
+        t.ks[h] = *reinterpret_cast<const v4f *>(c.k_step + row + 4 * g);
+        t.vs[h] = *reinterpret_cast<const v4f *>(c.v_step + row + 4 * g);
+    }
+    return t;
+}
+
+// One block: sequence, key head, 16 QT rows (row = new token x query heads of the group + head in the group) and one split's key tiles, which its
+// four waves take in turn.  partials: per row of the call and split head_dim sums, then the rows' (reference, sum of exponentials).
+template <bool BF, int D, int QT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
+void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, KvRows rows, int group, int chunks, int splits, float scale,
+                             const uint64_t *__restrict__ tree, float *__restrict__ partials, char *__restrict__ out)
+{
+    constexpr int QR = 16 * QT, DV = D / 16;
+    __shared__ __attribute__((aligned(16))) float so[4][QR][D + 4];
+    __shared__ float sm[4][QR], sl[4][QR];
+    int item = blockIdx.x;
+    const int chunk = item % chunks;
+    item /= chunks;
+    const int split = item % splits;
+    item /= splits;
+    const int head = item % c.kv_heads, b = item / c.kv_heads;
+    const SeqRows s = seq_rows(rows, b, c.page_shift);
+    const int r0 = chunk * QR, all = s.todo * group;
+    if (r0 >= all) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    const int heads = c.kv_heads * group, len = max(s.len, 0);
+    const int first = rows.lens[b] - s.n;                             // position of the first new token (negative: more new tokens than positions)
+    const int *table = rows.table + (size_t)b * rows.width;
+
+    // queries: operand step (i, half) holds channels 64 i + 16 g + 8 half .. + 7
+    v8h qf[QT][D / 32];
+    float factor[QT];                                                 // of a row's scores, as exponents of two
+    int limit[QT];                                                    // positions below it are seen; from `first` on the word's bits decide if there are drafts
+    uint64_t word[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        const int row = min(r0 + 16 * qt + r, all - 1), token = row / group, h = head * group + row - token * group;
+        const char *from = Q + 2 * ((size_t)(s.first_row + token) * ldq + h * D + 16 * g);
+        limit[qt] = min(tree ? len : first + token + 1, len);
+        word[qt] = tree ? tree[s.first_row + token] : ~0ull;
+        factor[qt] = scale * 1.44269504088896341f;
+        if constexpr (BF) {
+            float x[D / 32][8], top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) {
+                widen8<true>(*reinterpret_cast<const v4i *>(from + 128 * (i >> 1) + 16 * (i & 1)), x[i]);
+#pragma unroll
+                for (int e = 0; e < 8; e++) top = __builtin_fmaxf(top, __builtin_fabsf(x[i][e]));
+            }
+            top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+            const int shift = top > 0.0f && top < INFINITY ? min(14 - ilogbf(top), 120) : 0;
+            factor[qt] = ldexpf(factor[qt], -shift);
+#pragma unroll
+            for (int i = 0; i < D / 32; i++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) qf[qt][i][e] = (_Float16)ldexpf(x[i][e], shift);
+        } else {
+#pragma unroll
+            for (int i = 0; i < D / 32; i++) qf[qt][i] = __builtin_bit_cast(v8h, *reinterpret_cast<const v4i *>(from + 128 * (i >> 1) + 16 * (i & 1)));
+        }
+    }
+    v4f o[QT][DV];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        m[qt] = LOWEST;
+        l[qt] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < DV; j++) o[qt][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const int tiles = (len + TILE - 1) / TILE, per = (tiles + splits - 1) / splits, end = min((split + 1) * per, tiles);
+    const int whole = min(first, len) / TILE;                         // tiles below it are seen by every row
+    for (int t = split * per + w; t < end; t += 4) {
+        const KeyTile<D> kt = load_tile<D>(c, table, head, t * TILE, (len - 1) & ~15, r, g);
+        v8h kf[2][D / 32];
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int i = 0; i < D / 64; i++)
+#pragma unroll
+                for (int half = 0; half < 2; half++) {
+                    v4i x;
+#pragma unroll
+                    for (int e = 0; e < 2; e++) {
+                        const unsigned four = (unsigned)kt.k[h][i][2 * half + e];
+                        x[2 * e] = to_halves(__builtin_amdgcn_perm(0u, four, 0x0c010c00u));
+                        x[2 * e + 1] = to_halves(__builtin_amdgcn_perm(0u, four, 0x0c030c02u));
+                    }
+                    kf[h][2 * i + half] = __builtin_bit_cast(v8h, x);
+                }
+        float ev[2][4];                                               // step_v <= 2^ev
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) ev[h][e] = (float)__builtin_amdgcn_frexp_expf(kt.vs[h][e]);
+        v8h pf[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            float sc[2][4], top = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                v4f acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < D / 32; i++) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h][i], qf[qt][i], acc, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; e++) sc[h][e] = acc[e] * (kt.ks[h][e] * factor[qt]);
+            }
+            unsigned masked = 0;                                      // bit 4 h + e
+            if (t >= whole || kt.known != 3u) {
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const int pos = t * TILE + 16 * h + 4 * g + e, draft = pos - first;
+                        const bool seen = pos < limit[qt] && (kt.known >> h & 1u) && (draft < 0 || (draft < 64 ? (word[qt] >> draft) & 1 : tree == nullptr));
+                        if (!seen) sc[h][e] = -INFINITY;
+                        masked |= (unsigned)!seen << (4 * h + e);
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) top = __builtin_fmaxf(top, sc[h][e] + ev[h][e]);
+            if (__any(top > m[qt] + SLACK)) {
+                top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
+                top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+                const float to = top > m[qt] + SLACK ? top : m[qt], down = __builtin_amdgcn_exp2f(m[qt] - to);
+                m[qt] = to;
+                l[qt] *= down;
+#pragma unroll
+                for (int j = 0; j < DV; j++) o[qt][j] *= down;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const float p = __builtin_amdgcn_exp2f(sc[h][e] - m[qt]);
+                    l[qt] += p;
+                    pf[qt][4 * h + e] = (_Float16)(masked >> (4 * h + e) & 1u ? 0.0f : p * kt.vs[h][e]);
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < DV; j++) {
+            constexpr unsigned PICK[4] = {0x0c040c00u, 0x0c050c01u, 0x0c060c02u, 0x0c070c03u};
+            v4i x;
+#pragma unroll
+            for (int u = 0; u < 4; u++) x[u] = to_halves(__builtin_amdgcn_perm((unsigned)kt.v[2 * u + 1][j >> 2], (unsigned)kt.v[2 * u][j >> 2], PICK[j & 3]));
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++) o[qt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), pf[qt], o[qt][j], 0, 0, 0);
+        }
+    }
+
+    // the waves' parts meet: the lane's channels are DV (4 g + e) + j of query r
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        l[qt] += __shfl_xor(l[qt], 16, 64);
+        l[qt] += __shfl_xor(l[qt], 32, 64);
+        if (g == 0) {
+            sm[w][16 * qt + r] = m[qt];
+            sl[w][16 * qt + r] = l[qt];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+#pragma unroll
+            for (int j = 0; j < DV; j += 4)
+                *reinterpret_cast<v4f *>(&so[w][16 * qt + r][DV * (4 * g + e) + j]) = v4f{o[qt][j][e], o[qt][j + 1][e], o[qt][j + 2][e], o[qt][j + 3][e]};
+    }
+    __syncthreads();
+    constexpr int LANES = D / 8;                                      // lanes of a row, eight channels each
+    for (int at = tid / LANES; at < QR && r0 + at < all; at += 256 / LANES) {
+        const int row = r0 + at, token = row / group, h = head * group + row - token * group, d = tid % LANES * 8;
+        float top = sm[0][at], sum = 0.0f, f[4], y[8];
+#pragma unroll
+        for (int u = 1; u < 4; u++) top = __builtin_fmaxf(top, sm[u][at]);
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            f[u] = __builtin_amdgcn_exp2f(sm[u][at] - top);
+            sum += sl[u][at] * f[u];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            y[e] = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 4; u++) y[e] += so[u][at][d + e] * f[u];
+        }
+        const size_t to = (size_t)(s.first_row + token) * heads + h;
+        if (splits == 1) {
+            const float by = sum != 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;        // a row that sees nothing is zeros
+            const v4i packed = {narrow2<BF>(y[0] * by, y[1] * by), narrow2<BF>(y[2] * by, y[3] * by), narrow2<BF>(y[4] * by, y[5] * by),
+                                narrow2<BF>(y[6] * by, y[7] * by)};
+            *reinterpret_cast<v4i *>(out + 2 * (to * D + d)) = packed;
+        } else {
+            float *p = partials + (to * splits + split) * D + d;
+            *reinterpret_cast<v4f *>(p) = v4f{y[0], y[1], y[2], y[3]};
+            *reinterpret_cast<v4f *>(p + 4) = v4f{y[4], y[5], y[6], y[7]};
+            if (d == 0) {
+                float *ml = partials + (size_t)rows.rows * heads * splits * D + 2 * (to * splits + split);
+                ml[0] = top;
+                ml[1] = sum;
+            }
+        }
+    }
+}
+
+// joins the splits' parts, D / 8 lanes a row
+template <bool BF, int D>
+__global__ __launch_bounds__(256) void join_splits_kernel(KvRows rows, int heads, int splits, int page_shift, const float *__restrict__ partials,
+                                                          char *__restrict__ out)
+{
+    constexpr int LANES = D / 8;
+    const SeqRows s = seq_rows(rows, blockIdx.y, page_shift);
+    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d = threadIdx.x % LANES * 8;
+    if (row >= s.todo * heads) return;
+    const size_t at = (size_t)s.first_row * heads + row;
+    const float *ml = partials + (size_t)rows.rows * heads * splits * D + 2 * at * splits, *p = partials + at * splits * D + d;
+    float top = LOWEST, sum = 0.0f, y[8] = {};
+    for (int i = 0; i < splits; i++) top = __builtin_fmaxf(top, ml[2 * i]);
+    for (int i = 0; i < splits; i++) {
+        const float f = __builtin_amdgcn_exp2f(ml[2 * i] - top);
+        const v4f a = *reinterpret_cast<const v4f *>(p + (size_t)i * D), b = *reinterpret_cast<const v4f *>(p + (size_t)i * D + 4);
+        sum += ml[2 * i + 1] * f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            y[e] += a[e] * f;
+            y[4 + e] += b[e] * f;
+        }
+    }
+    const float by = sum != 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
+    *reinterpret_cast<v4i *>(out + 2 * (at * D + d)) = v4i{narrow2<BF>(y[0] * by, y[1] * by), narrow2<BF>(y[2] * by, y[3] * by),
+                                                           narrow2<BF>(y[4] * by, y[5] * by), narrow2<BF>(y[6] * by, y[7] * by)};
+}
+
+int row_tiles(int rows) { return rows > 16 ? 2 : 1; }
+
+template <bool BF, int D>
+hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree, int splits,
+                            float *partials, void *out, hipStream_t st)
+{
+    const int group = heads / c.kv_heads, most = rows.max_rows * group, qt = row_tiles(most), chunks = (most + 16 * qt - 1) / (16 * qt);
+    auto kern = qt == 1 ? cached_attention_kernel<BF, D, 1> : cached_attention_kernel<BF, D, 2>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)rows.batch * c.kv_heads * splits * chunks), dim3(256), 0, st, (const char *)q, ldq, c, rows, group, chunks, splits,
+                       scale, tree, partials, (char *)out);
+    if (splits > 1)
+        hipLaunchKernelGGL((join_splits_kernel<BF, D>), dim3((unsigned)((rows.max_rows * heads + 2048 / D - 1) / (2048 / D)), (unsigned)rows.batch), dim3(256), 0, st,
+                           rows, heads, splits, c.page_shift, partials, (char *)out);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int cached_attention_splits(int batch, int heads, int kv_heads, int, int max_new, int max_len)
+{
+    const int most = max_new * (heads / kv_heads), qt = row_tiles(most);
+    const long items = (long)batch * kv_heads * ((most + 16 * qt - 1) / (16 * qt)), tiles = (max_len + TILE - 1) / TILE;
+    long splits = (1024 + items - 1) / items;
+    if (splits > tiles / 8) splits = tiles / 8;
+    return splits < 1 ? 1 : (int)splits;
+}
+
+hipError_t launch_cached_attention(const void *q, long ldq, bool bf16, int heads, int D, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree,
+                                   int splits, float *partials, void *out, hipStream_t st)
+{
+    if (D == 128) return bf16 ? cached_attention<true, 128>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st)
+                              : cached_attention<false, 128>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st);
+    return bf16 ? cached_attention<true, 64>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st)
+                : cached_attention<false, 64>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st);
+}
+
+}  // namespace samp

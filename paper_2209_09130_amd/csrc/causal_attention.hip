@@ -1,0 +1,255 @@
+// Causal attention over packed prompts with grouped heads: O = softmax(scale q K^T) V, a query sees the keys of its sequence up to itself.
+//
+// What bounds it is the matrix cores, with the softmax's vector work close behind: 4 head_dim operations per (query, key) pair on the one side, some ten
+// vector operations and an exponential on the other.  A wave owns 32 queries for the whole loop and keeps them, their output (as O^T) and the softmax in
+// registers: S^T = K Q^T leaves a lane one query and 32 of a tile's 64 keys, and what it makes of them is, as it stands, the operand of
+// O^T += V^T P^T.  The key tiles (64 keys, K and V) are shared by the block's waves: direct loads into one half of LDS while the other is worked on, V
+// transposed by the reads.  One pass, with a reference per query that moves (and rescales) only when a score exceeds it by 2^8.
+// Rounding a probability to 16 bits is off by half a step of each, as the result's own rounding is.
+//
+// A key that a query does not see has no part in its result, whatever it holds.  On the diagonal the product multiplies such keys' V by a probability of 0,
+// which an infinity or NaN survives; so a block with a result that is not finite goes over its tiles again, with V's infinities and NaN left out of the
+// product on the diagonal and added to the queries that see them.
+#include "decoder.h"
+#include "mfma_tile.h"
+
+namespace samp {
+namespace {
+
+constexpr float LOWEST = -3.0e38f, SLACK = 8.0f;
+constexpr int KEYS = 64;
+
+template <bool BF> __device__ __forceinline__ v16f mma32(const v4i &a, const v4i &b, const v16f &c)
+{
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
+}
+
+// Positions of 16-byte chunks inside a row of a tile in LDS (D * 2 bytes a row).  K is read 16 bytes a lane, eight rows at a time over all banks; V by
+// transposing reads, four rows of 64 bytes at a time.
+template <int D> __device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : swz<128>(row); }
+template <int D> __device__ __forceinline__ int swz_v(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+
+typedef __attribute__((address_space(3))) v4s *LdsHalves;
+
+// Of two halves: bits 15 and 31 where one is an infinity or NaN (the exponent's carry); the pair with zeros in their place
+template <bool BF> __device__ __forceinline__ unsigned odd_halves(int two)
+{ return (((unsigned)two & 0x7fff7fffu) + (BF ? 0x00800080u : 0x04000400u)) & 0x80008000u; }
+template <bool BF> __device__ __forceinline__ v4i without_odd(v4i v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const unsigned odd = odd_halves<BF>(v[i]);
+        if (odd & 0x8000u) v[i] &= (int)0xffff0000u;
+        if (odd >> 16) v[i] &= 0xffff;
+    }
+    return v;
+}
+
+template <int D, int NW> struct CausalTile {
+    static constexpr int ROW = 2 * D, TILE = KEYS * ROW, STAGE = 2 * TILE;            // bytes; K then V
+    static constexpr int LOADS = TILE / 1024 / NW;                                  // direct loads of a wave per tile and matrix
+    static constexpr int OUT = 32 * (ROW + 16) * NW;                              // the output tile takes the ring's place
+    static constexpr int LDS = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+};
+
+template <bool BF, int D, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
+void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict__ K, const char *__restrict__ V, long ldq, long ldk, long ldv,
+                             const int *__restrict__ cu, int rows, int max_len, int heads, int group, int pairs, int strips, float scale, char *__restrict__ out)
+{
+    typedef CausalTile<D, NW> T;
+    constexpr int QB = 32 * NW, KS = D / 16, DB = D / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
+
+    // strips of queries from the last (longest) to the first; the (sequence, key head) pair runs fastest, so that where pairs are a multiple of eight an
+    // XCD's L2 holds the keys of its own pairs
+    const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, strip = strips - 1 - rest / group;
+    const int kv_heads = heads / group, b = pair / kv_heads, kvh = pair - b * kv_heads, head = kvh * group + rest % group;
+    const int t0 = cu ? cu[b] : b * max_len;
+    int n = (cu ? cu[b + 1] : t0 + max_len) - t0;
+    if (t0 < 0 || n < 0 || t0 > rows - n) return;                          // rows that the tensors do not have
+    n = min(n, max_len);
+    const int q0 = strip * QB;
+    if (q0 >= n) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, g = lane >> 5;
+    const int qw = q0 + 32 * w;                                           // the wave's first query
+    const unsigned ldkb = 2 * (unsigned)ldk, ldvb = 2 * (unsigned)ldv;
+    const char *kbase = K + (size_t)t0 * ldkb + kvh * T::ROW, *vbase = V + (size_t)t0 * ldvb + kvh * T::ROW;
+
+    v4i qf[KS];
+    {
+        const char *from = Q + 2 * ((size_t)(t0 + min(qw + r, n - 1)) * ldq + (size_t)head * D + 8 * g);
+#pragma unroll
+        for (int i = 0; i < KS; i++) qf[i] = *reinterpret_cast<const v4i *>(from + 32 * i);
+    }
+    // direct loads: a wave's j-th fills 1 KB, 1024 / ROW rows; past the sequence the descriptor makes them zeros
+    constexpr int CH = T::ROW / 16, RPL = 64 / CH;                        // chunks of a row; rows of a load
+    unsigned offk[T::LOADS], offv[T::LOADS];
+#pragma unroll
+    for (int j = 0; j < T::LOADS; j++) {
+        const int row = (w * T::LOADS + j) * RPL + lane / CH, chunk = lane % CH;
+        offk[j] = row * ldkb + ((chunk ^ swz_k<D>(row)) << 4);
+        offv[j] = row * ldvb + ((chunk ^ swz_v<D>(row)) << 4);
+    }
+    auto request = [&](int tile, int buffer) {
+        const int j0 = tile * KEYS, left = min(n - j0, KEYS);              // rows of the tile that are there
+        const auto kr = buffer_of(kbase + (size_t)j0 * ldkb, (int)((left - 1) * ldkb + T::ROW));
+        const auto vr = buffer_of(vbase + (size_t)j0 * ldvb, (int)((left - 1) * ldvb + T::ROW));
+        char *to = lds + buffer * T::STAGE + w * T::LOADS * 1024;
+#pragma unroll
+        for (int j = 0; j < T::LOADS; j++) buffer_to_lds128(kr, offk[j], 0, to + j * 1024);
+#pragma unroll
+        for (int j = 0; j < T::LOADS; j++) buffer_to_lds128(vr, offv[j], 0, to + T::TILE + j * 1024);
+    };
+    // a lane's V^T reads: key 4 g + (lane >> 2 & 3) of a group of eight, channels 16 (lane >> 4 & 1) + 4 (lane & 3) of 32
+    const int vkey = 4 * g + ((lane >> 2) & 3), vchunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+
+    const float factor = scale * 1.44269504088896341f;
+    const int tiles = (min(n, q0 + QB) + KEYS - 1) / KEYS;
+    v16f o[DB];
+    float m, l;
+    auto sweep = [&](bool careful) {
+#pragma unroll
+    for (int i = 0; i < DB; i++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) o[i][e] = 0.0f;
+    m = LOWEST;
+    l = 0.0f;
+    request(0, 0);
+    for (int t = 0; t < tiles; t++) {
+        wait_vm_and_barrier<0>();                                         // tile t is there, and tile t - 1 has been read by all
+        if (t + 1 < tiles) request(t + 1, (t + 1) & 1);
+        const int j0 = t * KEYS;
+        if (j0 > qw + 31) continue;                                       // (wave-uniform) keys behind all of the wave's queries
+        const char *kt = lds + (t & 1) * T::STAGE, *vt = kt + T::TILE;
+        float sc[2][16], top = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            v16f acc;
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[e] = 0.0f;
+            const int row = 32 * h + r;
+#pragma unroll
+            for (int i = 0; i < KS; i++)
+                acc = mma32<BF>(*reinterpret_cast<const v4i *>(kt + row * T::ROW + (((2 * i + g) ^ swz_k<D>(row)) << 4)), qf[i], acc);
+#pragma unroll
+            for (int e = 0; e < 16; e++) sc[h][e] = acc[e] * factor;
+        }
+        const bool edge = j0 + KEYS - 1 > qw;                             // the diagonal crosses the tile (the sequence's end lies behind it)
+        if (edge) {
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int e = 0; e < 16; e++)
+                    if (j0 + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3) > qw + r) sc[h][e] = -INFINITY;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) top = __builtin_fmaxf(top, sc[h][e]);
+        if (__any(top > m + SLACK)) {
+            top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+            const float to = top > m + SLACK ? top : m, down = __builtin_amdgcn_exp2f(m - to);   // (a query's result does not depend on the wave's others)
+            m = to;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < DB; i++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) o[i][e] *= down;
+        }
+        v4i pf[4];
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float p0 = __builtin_amdgcn_exp2f(sc[h][e] - m), p1 = __builtin_amdgcn_exp2f(sc[h][e + 1] - m);
+                l += p0 + p1;
+                pf[2 * h + (e >> 3)][(e & 7) >> 1] = narrow2<BF>(p0, p1);
+            }
+#pragma unroll
+        for (int u = 0; u < 4; u++)                                       // keys 16 u + 4 g + (0..3, 8..11)
+#pragma unroll
+            for (int i = 0; i < DB; i++) {
+                const int key = 16 * u + vkey;
+                const char *p = vt + key * T::ROW + (((4 * i + vchunk) ^ swz_v<D>(key)) << 4) + 8 * (lane & 1);
+                const v2i lo = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalves)p));
+                const v2i hi = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalves)(p + 8 * T::ROW)));
+                v4i vf = {lo[0], lo[1], hi[0], hi[1]};
+                if (careful && edge) vf = without_odd<BF>(vf);
+                o[i] = mma32<BF>(vf, pf[u], o[i]);
+            }
+        if (careful && edge)
+            for (int key = 0; key < KEYS && j0 + key < n; key++) {
+                const char *row = vt + key * T::ROW;
+                if (!__any(odd_halves<BF>(*reinterpret_cast<const int *>(row + 4 * (lane % (D / 2)))))) continue;
+                const bool sees = j0 + key <= qw + r;
+#pragma unroll
+                for (int i = 0; i < DB; i++)
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {                     // channels 32 i + 2 e + 4 g + (0..3)
+                        const v2i four = *reinterpret_cast<const v2i *>(row + (((4 * i + (e >> 2)) ^ swz_v<D>(key)) << 4) + 8 * g);
+#pragma unroll
+                        for (int c = 0; c < 4; c++) {
+                            const unsigned half = (unsigned)four[c >> 1] >> (16 * (c & 1)) & 0xffffu;
+                            if (sees && odd_halves<BF>((int)half)) o[i][e + c] += BF ? __uint_as_float(half << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)half);
+                        }
+                    }
+            }
+    }
+    };
+    sweep(false);
+    {
+        float all = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DB; i++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) all = __builtin_fmaf(o[i][e], 0.0f, all);
+        if (__syncthreads_or(!(all == 0.0f))) {                           // (the same for all waves; behind it the tiles have been read)
+            sweep(true);
+            __syncthreads();
+        }
+    }
+    l += __shfl_xor(l, 32, 64);
+    const float by = l != 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
+    __syncthreads();
+    char *mine = lds + w * 32 * (T::ROW + 16);
+#pragma unroll
+    for (int i = 0; i < DB; i++)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<v2i *>(mine + r * (T::ROW + 16) + 2 * (32 * i + 2 * e + 4 * g)) =
+                v2i{narrow2<BF>(o[i][e] * by, o[i][e + 1] * by), narrow2<BF>(o[i][e + 2] * by, o[i][e + 3] * by)};
+    wait_lds();
+#pragma unroll
+    for (int p = 0; p < 32 / RPL; p++) {
+        const int row = p * RPL + lane / CH;
+        if (qw + row < n)
+            *reinterpret_cast<v4i *>(out + 2 * ((size_t)(t0 + qw + row) * heads + head) * D + lane % CH * 16) =
+                *reinterpret_cast<const v4i *>(mine + row * (T::ROW + 16) + lane % CH * 16);
+    }
+}
+
+template <bool BF, int D>
+hipError_t causal_attention(const void *q, long ldq, const void *k, long ldk, const void *v, long ldv, int heads, int kv_heads, const int *cu, int batch,
+                            int max_len, int rows, float scale, void *out, hipStream_t st)
+{
+    constexpr int NW = 4;
+    const int strips = (max_len + 32 * NW - 1) / (32 * NW), pairs = batch * kv_heads;
+    hipLaunchKernelGGL((causal_attention_kernel<BF, D, NW>), dim3((unsigned)strips * heads * batch), dim3(64 * NW), 0, st, (const char *)q, (const char *)k,
+                       (const char *)v, ldq, ldk, ldv, cu, rows, max_len, heads, heads / kv_heads, pairs, strips, scale, (char *)out);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_causal_attention(const void *q, long ldq, const void *k, long ldk, const void *v, long ldv, bool bf16, int heads, int kv_heads, int D,
+                                   const int *cu, int batch, int max_len, int rows, float scale, void *out, hipStream_t st)
+{
+    if (D == 128) return bf16 ? causal_attention<true, 128>(q, ldq, k, ldk, v, ldv, heads, kv_heads, cu, batch, max_len, rows, scale, out, st)
+                              : causal_attention<false, 128>(q, ldq, k, ldk, v, ldv, heads, kv_heads, cu, batch, max_len, rows, scale, out, st);
+    return bf16 ? causal_attention<true, 64>(q, ldq, k, ldk, v, ldv, heads, kv_heads, cu, batch, max_len, rows, scale, out, st)
+                : causal_attention<false, 64>(q, ldq, k, ldk, v, ldv, heads, kv_heads, cu, batch, max_len, rows, scale, out, st);
+}
+
+}  // namespace samp

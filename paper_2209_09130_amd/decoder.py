@@ -1,0 +1,252 @@
+"""ctypes binding of the decoder's entry points in include/samp.h (same names, argument marshalling only).
+
+Every call runs on the current stream of its tensors' device, allocates its output (and workspace, where the C entry takes one) from
+torch's allocator, and raises SampError for what the library refuses.  Activations are fp16 or bfloat16 tensors on the GPU.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import math
+from typing import Optional, Tuple
+
+import torch
+
+from .binding import SampError, lib
+
+_TYPES = {torch.float16: 0, torch.bfloat16: 1}
+_P, _I, _L, _F, _Z = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
+_SIGNATURES = {
+    "samp_quantize_tokens": (_P, _L, _I, _I, _I, _P, _P, _P),
+    "samp_gemm_i8_tokens_packed": (_P, _P, _P, _P, _P, _I, _P, _I, _I, _I, _I, _P),
+    "samp_linear_i8_tokens_workspace_bytes": (_I, _I),
+    "samp_linear_i8_tokens": (_P, _L, _I, _P, _P, _P, _I, _P, _I, _I, _I, _P, _Z, _P),
+    "samp_cache_write": (_P, _P, _L, _P, _L, _I, _P, _I, _P, _P, _I, _I, _I, _P),
+    "samp_cache_read": (_P, _P, _P, _I, _P, _I, _P, _P, _I, _I, _I, _P),
+    "samp_attention_cache_workspace_bytes": (_I,) * 7,
+    "samp_attention_cache": (_P, _L, _I, _I, _P, _P, _I, _P, _P, _I, _I, _I, _I, _F, _P, _P, _P, _Z, _P),
+    "samp_attention_causal": (_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _P, _I, _I, _I, _F, _P, _P),
+}
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L = lib()
+        for name, types in _SIGNATURES.items():
+            f = getattr(L, name)
+            f.argtypes = types
+            f.restype = _Z if name.endswith("_bytes") else C.c_int
+        _ready = L
+    return _ready
+
+
+def _refuse(why: str):
+    raise SampError(-1, why)
+
+
+def _bytes(need: int) -> int:
+    if need == 0:
+        raise SampError(-2, lib().samp_last_error().decode())
+    return need
+
+
+def _on(device: torch.device, *tensors):
+    if device.type != "cuda":
+        _refuse(f"tensors must be on the GPU ({device})")
+    for t in tensors:
+        if t is not None and t.device != device:
+            _refuse(f"tensors on different devices: {t.device}, {device}")
+
+
+def _flat(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, size: Optional[int] = None) -> int:
+    """The address of a contiguous tensor of one type (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or not t.is_contiguous() or (size is not None and t.numel() != size):
+        _refuse(f"{what}: a contiguous {dtype} tensor{'' if size is None else f' of {size} elements'} is needed, not {t.dtype} {tuple(t.shape)} {t.stride()}")
+    return t.data_ptr()
+
+
+def _heads(what: str, t: torch.Tensor) -> Tuple[int, int]:
+    """Address and row distance of [rows, heads, head_dim] whose heads lie next to each other."""
+    if t.dim() != 3 or t.dtype not in _TYPES:
+        _refuse(f"{what}: fp16 or bfloat16 [rows, heads, head_dim] is needed, not {t.dtype} {tuple(t.shape)}")
+    rows, heads, dim = t.shape
+    row, head, one = t.stride()
+    if one != 1 or (head != dim and heads > 1):
+        _refuse(f"{what}: the heads of a row must lie next to each other (strides {t.stride()})")
+    return t.data_ptr(), row if rows > 1 else heads * dim
+
+
+def _call(device: torch.device, name: str, *args):
+    f = getattr(_lib(), name)
+    if device.index is not None and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            rc = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        rc = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    if rc:
+        raise SampError(rc, lib().samp_last_error().decode())
+
+
+def _rows2(what: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
+    """Address, row distance, rows and width of a matrix with dense rows."""
+    if x.dim() != 2 or x.dtype not in _TYPES or (x.stride(1) != 1 and x.shape[1] > 1):
+        _refuse(f"{what}: an fp16 or bfloat16 matrix with dense rows is needed, not {x.dtype} {tuple(x.shape)} {x.stride()}")
+    M, K = x.shape
+    return x.data_ptr(), x.stride(0) if M > 1 else K, M, K
+
+
+def quantize_tokens(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """samp_quantize_tokens: int8 codes [M, K] and float32 steps [M] of the rows of x (step = the row's absmax / 127)."""
+    _on(x.device)
+    at, ld, M, K = _rows2("x", x)
+    codes = torch.empty((M, K), dtype=torch.int8, device=x.device)
+    steps = torch.empty(M, dtype=torch.float32, device=x.device)
+    if M:
+        _call(x.device, "samp_quantize_tokens", at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr())
+    return codes, steps
+
+
+def gemm_i8_tokens_packed(codes: torch.Tensor, steps: torch.Tensor, Wp: torch.Tensor, s_w: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                          gelu: bool = False, dtype: torch.dtype = torch.float16) -> torch.Tensor:
+    """samp_gemm_i8_tokens_packed: [M, N] of `dtype` from int8 codes [M, K] with a step for each row and weights that pack_weight_i8 packed, with a
+    step for each channel."""
+    _on(codes.device, steps, Wp, s_w, bias)
+    if codes.dim() != 2 or dtype not in _TYPES:
+        _refuse("codes must be a matrix, and the result's type fp16 or bfloat16")
+    M, K = codes.shape
+    N = s_w.numel()
+    out = torch.empty((M, N), dtype=dtype, device=codes.device)
+    args = (_flat("codes", codes, torch.int8), _flat("steps", steps, torch.float32, M), _flat("Wp", Wp, torch.int8, N * K), _flat("s_w", s_w, torch.float32),
+            _flat("bias", bias, torch.float32, N), int(bool(gelu)), out.data_ptr(), _TYPES[dtype], M, N, K)
+    if M:
+        _call(codes.device, "samp_gemm_i8_tokens_packed", *args)
+    return out
+
+
+def linear_i8_tokens(x: torch.Tensor, Wp: torch.Tensor, s_w: torch.Tensor, bias: Optional[torch.Tensor] = None, gelu: bool = False) -> torch.Tensor:
+    """samp_linear_i8_tokens: quantize_tokens and gemm_i8_tokens_packed in one call, x [M, K] -> [M, N] of x's type."""
+    device = x.device
+    _on(device, Wp, s_w, bias)
+    at, ld, M, K = _rows2("x", x)
+    N = s_w.numel()
+    out = torch.empty((M, N), dtype=x.dtype, device=device)
+    w, s, b = _flat("Wp", Wp, torch.int8, N * K), _flat("s_w", s_w, torch.float32), _flat("bias", bias, torch.float32, N)
+    if M:
+        need = _bytes(_lib().samp_linear_i8_tokens_workspace_bytes(M, K))
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        _call(device, "samp_linear_i8_tokens", at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws.data_ptr(), need)
+    return out
+
+
+class _CacheStruct(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_step", "v_step")] + [(n, C.c_int32) for n in ("pages", "kv_heads", "page_len", "head_dim")]
+
+
+class KVCache:
+    """A paged int8 cache: codes k, v [pages, kv_heads, page_len, head_dim] and float32 steps k_step, v_step [pages, kv_heads, page_len] (contiguous,
+    kept alive by this object), and the samp_kv_cache_t that points at them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_step: torch.Tensor, v_step: torch.Tensor):
+        _on(k.device, v, k_step, v_step)
+        if k.dim() != 4 or v.shape != k.shape or k_step.shape != k.shape[:3] or v_step.shape != k.shape[:3]:
+            _refuse(f"a cache is codes [pages, kv_heads, page_len, head_dim] and steps [pages, kv_heads, page_len], not {tuple(k.shape)} {tuple(v.shape)} "
+                    f"{tuple(k_step.shape)} {tuple(v_step.shape)}")
+        self.k, self.v, self.k_step, self.v_step = k, v, k_step, v_step
+        self.device = k.device
+        self.pages, self.kv_heads, self.page_len, self.head_dim = k.shape
+        self.struct = _CacheStruct(_flat("k", k, torch.int8), _flat("v", v, torch.int8), _flat("k_step", k_step, torch.float32),
+                                   _flat("v_step", v_step, torch.float32), *k.shape)
+        self.address = C.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, page_len: int, head_dim: int, device="cuda") -> "KVCache":
+        """A cache of zeros (what a sequence has not written is never seen)."""
+        codes = [torch.zeros((pages, kv_heads, page_len, head_dim), dtype=torch.int8, device=device) for _ in range(2)]
+        return cls(*codes, *(torch.zeros((pages, kv_heads, page_len), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _places(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor):
+    _on(cache.device, table, cu, lens)
+    if table.dim() != 2:
+        _refuse("the page table is [sequences, pages of a sequence]")
+    B, width = table.shape
+    return _flat("table", table, torch.int32), width, _flat("cu", cu, torch.int32, B + 1), _flat("lens", lens, torch.int32, B), B
+
+
+def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int) -> None:
+    """samp_cache_write: the packed rows k, v [rows, kv_heads, head_dim] become the last cu[b + 1] - cu[b] of the lens[b] positions of each sequence.
+    table int32 [B, width]; cu int32 [B + 1] or None (max_new rows each); lens int32 [B], the new positions counted."""
+    _on(cache.device, k, v)
+    (pk, ldk), (pv, ldv) = _heads("k", k), _heads("v", v)
+    if k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (cache.kv_heads, cache.head_dim):
+        _refuse(f"k and v must be [rows, {cache.kv_heads}, {cache.head_dim}] of one type, not {tuple(k.shape)} and {tuple(v.shape)}")
+    t, width, pcu, plens, B = _places(cache, table, cu, lens)
+    if k.shape[0] and B:
+        _call(cache.device, "samp_cache_write", cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, max_new, k.shape[0])
+
+
+def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_rows: int, rows: int,
+               dtype: torch.dtype = torch.float16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """samp_cache_read: k, v [rows, kv_heads, head_dim] of `dtype`, sequence b's rows the last cu[b + 1] - cu[b] of its lens[b] positions."""
+    if dtype not in _TYPES:
+        _refuse("the result's type must be fp16 or bfloat16")
+    t, width, pcu, plens, B = _places(cache, table, cu, lens)
+    if out is None:
+        out = tuple(torch.empty((rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device) for _ in range(2))
+    _on(cache.device, *out)
+    k, v = (_flat("out", o, dtype, rows * cache.kv_heads * cache.head_dim) for o in out)
+    if rows and B:
+        _call(cache.device, "samp_cache_read", cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, max_rows, rows)
+    return out
+
+
+def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int,
+                    max_len: Optional[int] = None, scale: Optional[float] = None, tree: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """samp_attention_cache: [rows, heads, head_dim] of the new tokens q over the cache that holds their keys and values already.
+    max_len: the longest context expected (None: what the page table has room for).  scale: None for 1 / sqrt(head_dim).  tree: int64 words [rows]."""
+    device = cache.device
+    _on(device, q, tree, out)
+    at, ld = _heads("q", q)
+    rows, heads, dim = q.shape
+    if dim != cache.head_dim:
+        _refuse(f"q has heads of {dim}, the cache of {cache.head_dim}")
+    t, width, pcu, plens, B = _places(cache, table, cu, lens)
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=device)
+    to, words = _flat("out", out, q.dtype, rows * heads * dim), _flat("tree", tree, torch.int64, rows)
+    if rows and B:
+        if max_len is None:
+            max_len = width * cache.page_len
+        need = _bytes(_lib().samp_attention_cache_workspace_bytes(rows, B, heads, cache.kv_heads, dim, max_new, max_len))
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        _call(device, "samp_attention_cache", at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
+              1.0 / math.sqrt(dim) if scale is None else scale, words, to, ws.data_ptr(), need)
+    return out
+
+
+def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Optional[torch.Tensor], max_len: int, scale: Optional[float] = None,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """samp_attention_causal: [rows, heads, head_dim] from q [rows, heads, head_dim] and k, v [rows, kv_heads, head_dim] (views into a fused
+    projection's rows are read in place).  cu int32 [B + 1], or None for sequences of max_len rows each."""
+    device = q.device
+    _on(device, k, v, cu, out)
+    (pq, ldq), (pk, ldk), (pv, ldv) = _heads("q", q), _heads("k", k), _heads("v", v)
+    rows, heads, dim = q.shape
+    if k.shape != v.shape or k.shape[0] != rows or k.shape[2] != dim or k.dtype != q.dtype or v.dtype != q.dtype:
+        _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
+    if out is None:
+        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=device)
+    to = _flat("out", out, q.dtype, rows * heads * dim)
+    if rows == 0:
+        return out
+    if cu is None and (max_len < 1 or rows % max_len):
+        _refuse("without sequence offsets every sequence has max_len rows")
+    B = rows // max_len if cu is None else cu.numel() - 1
+    if B:
+        _call(device, "samp_attention_causal", pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, B + 1), B, max_len,
+              rows, 1.0 / math.sqrt(dim) if scale is None else scale, to)
+    return out
