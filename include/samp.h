@@ -446,7 +446,8 @@ SAMP_API int samp_gemm_i8_tokens_packed(const int8_t *codes, const float *steps,
                                         uint16_t *out, int32_t type, int32_t M, int32_t N, int32_t K, void *stream);
 
 /* The two in one call, x [M,K] -> out [M,N]: the bytes that samp_quantize_tokens and samp_gemm_i8_tokens_packed give.
- * workspace dev, 256-byte aligned; calls that share one must be stream-ordered.                      */
+ * workspace dev, 256-byte aligned; calls that share one must be stream-ordered.  Bytes: 0 where none is needed (NULL will do), and for arguments that the
+ * call refuses.                                                                                      */
 SAMP_API size_t samp_linear_i8_tokens_workspace_bytes(int32_t M, int32_t K);
 SAMP_API int samp_linear_i8_tokens(const uint16_t *x, int64_t ldx, int32_t type, const int8_t *Wp, const float *s_w, const float *bias, int32_t gelu,
                                    uint16_t *out, int32_t M, int32_t N, int32_t K, void *workspace, size_t workspace_bytes, void *stream);
@@ -477,8 +478,7 @@ SAMP_API int samp_cache_read(const samp_kv_cache_t *cache, uint16_t *k, uint16_t
  * their own keys and values: new token i of n sees the positions up to its own, lens[b] - n + i.  heads is a multiple of kv_heads; query head h reads
  * key head h / (heads / kv_heads).  tree (dev uint64 [rows], or NULL): the new tokens are drafts; each sees all positions in front of the first draft, and draft j of its sequence
  * if bit j of its word is set (its own bit like any other), up to 64 drafts.  A token that sees nothing gets zeros.
- * max_len: the longest context that the host expects; it only decides how the work is cut.  workspace dev, 256-byte aligned; calls that share one must be
- * stream-ordered.                                                                                    */
+ * max_len: the longest context that the host expects; it only decides how the work is cut.  workspace as in samp_linear_i8_tokens.                       */
 SAMP_API size_t samp_attention_cache_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_new,
                                                      int32_t max_len);
 SAMP_API int samp_attention_cache(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const int32_t *table,

@@ -106,7 +106,7 @@ int samp_gemm_i8_tokens_packed(const int8_t *codes, const float *steps, const in
 
 size_t samp_linear_i8_tokens_workspace_bytes(int32_t M, int32_t K)
 {
-    if (check_tokens(M, 16, K)) return 0;
+    if (check_tokens(M, 16, K) || linear_tokens_is_fused(M, K)) return 0;
     return up((size_t)M * K) + up((size_t)M * sizeof(float));
 }
 
@@ -117,8 +117,12 @@ int samp_linear_i8_tokens(const uint16_t *x, int64_t ldx, int32_t type, const in
     if (int rc = check_tokens(M, N, K)) return rc;
     if (int rc = check_product(Wp, s_w, bias, out)) return rc;
     if (int rc = check_rows("x", x, ldx, K)) return rc;
-    if (!workspace || !aligned(workspace, ALIGN) || workspace_bytes < samp_linear_i8_tokens_workspace_bytes(M, K))
-        return fail(SAMP_ERR_SPACE, "a 256-byte aligned workspace of %zu bytes is needed", samp_linear_i8_tokens_workspace_bytes(M, K));
+    if (linear_tokens_is_fused(M, K)) {
+        HIP_TRY(launch_linear_few(x, ldx, type == SAMP_TYPE_BF16, Wp, s_w, bias, gelu != 0, out, M, N, K, (hipStream_t)stream));
+        return SAMP_OK;
+    }
+    const size_t need = samp_linear_i8_tokens_workspace_bytes(M, K);
+    if (!workspace || !aligned(workspace, ALIGN) || workspace_bytes < need) return fail(SAMP_ERR_SPACE, "a 256-byte aligned workspace of %zu bytes is needed", need);
     int8_t *codes = static_cast<int8_t *>(workspace);
     float *steps = reinterpret_cast<float *>(codes + up((size_t)M * K));
     HIP_TRY(launch_quantize_tokens(x, ldx, type == SAMP_TYPE_BF16, M, K, codes, steps, (hipStream_t)stream));
@@ -166,8 +170,8 @@ static int check_cached(int32_t rows, int32_t batch, int32_t heads, int32_t kv_h
 size_t samp_attention_cache_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_new, int32_t max_len)
 {
     if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len)) return 0;
-    const size_t splits = cached_attention_splits(batch, heads, kv_heads, head_dim, max_new, max_len);
-    return splits == 1 ? ALIGN : up((size_t)rows * heads * splits * (head_dim + 2) * sizeof(float));
+    const size_t splits = cached_attention_cut(batch, heads, kv_heads, max_new, max_len).splits;
+    return splits == 1 ? 0 : up((size_t)rows * heads * splits * (head_dim + 2) * sizeof(float));
 }
 
 int samp_attention_cache(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const int32_t *table, int32_t width,
@@ -186,9 +190,10 @@ int samp_attention_cache(const uint16_t *q, int64_t ldq, int32_t type, int32_t h
     if (tree && max_new > 64) return fail(SAMP_ERR_SHAPE, "a tree has at most 64 drafted tokens (max_new %d)", max_new);
     if (tree && !aligned(tree, 8)) return fail(SAMP_ERR_ARG, "tree must be 8-byte aligned");
     const size_t need = samp_attention_cache_workspace_bytes(rows, batch, heads, c.kv_heads, cache->head_dim, max_new, max_len);
-    if (!workspace || !aligned(workspace, ALIGN) || workspace_bytes < need) return fail(SAMP_ERR_SPACE, "a 256-byte aligned workspace of %zu bytes is needed", need);
-    const int splits = cached_attention_splits(batch, heads, c.kv_heads, cache->head_dim, max_new, max_len);
-    HIP_TRY(launch_cached_attention(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, r, scale, tree, splits, static_cast<float *>(workspace), out,
+    if (need && (!workspace || !aligned(workspace, ALIGN) || workspace_bytes < need))
+        return fail(SAMP_ERR_SPACE, "a 256-byte aligned workspace of %zu bytes is needed", need);
+    const Cut cut = cached_attention_cut(batch, heads, c.kv_heads, max_new, max_len);
+    HIP_TRY(launch_cached_attention(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, r, scale, tree, cut, static_cast<float *>(workspace), out,
                                     (hipStream_t)stream));
     return SAMP_OK;
 }

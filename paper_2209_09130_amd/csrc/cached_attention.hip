@@ -12,7 +12,8 @@
 //
 // Softmax in one pass with a running reference m per query that bounds log2(p step_v): exponent(step_v) + score, so that p step_v fits binary16 (at most
 // 2^9) whatever the steps.  m moves (and the sums are scaled) only when a score exceeds it by 2^8, not for every new maximum.  Rounding p step_v to
-// binary16 is off by 2^-11 of each, below the rounding of the result.  Queries of bfloat16 are scaled by a power of two per row into binary16's range.
+// binary16 is off by 2^-11 of each, well below a bfloat16 result's rounding; for an fp16 result, where it would be as much again, what was rounded off is multiplied as
+// well (the matrix cores are idle most of the time).  Queries of bfloat16 are scaled by a power of two per row into binary16's range.
 #include "decoder.h"
 #include "divisor.h"
 
@@ -68,11 +69,14 @@ __device__ __forceinline__ KeyTile<D> load_tile(const KvCache &c, const int *tab
     return t;
 }
 
+// A context of more than `piece` tiles is cut into pieces of so many, at most `splits` of them (the last takes what is left); the parts of one that is not are the result
+__device__ __forceinline__ int pieces_of(int tiles, int piece, int splits) { return min(max((tiles + piece - 1) / piece, 1), splits); }
+
 // One block: sequence, key head, 16 QT rows (row = new token x query heads of the group + head in the group) and one split's key tiles, which its
 // four waves take in turn.  partials: per row of the call and split head_dim sums, then the rows' (reference, sum of exponentials).
 template <bool BF, int D, int QT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2)))
-void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, KvRows rows, int group, int chunks, int splits, float scale,
+void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, KvRows rows, int group, int chunks, int splits, int piece, float scale,
                              const uint64_t *__restrict__ tree, float *__restrict__ partials, char *__restrict__ out)
 {
     constexpr int QR = 16 * QT, DV = D / 16;
@@ -85,8 +89,8 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
     item /= splits;
     const int head = item % c.kv_heads, b = item / c.kv_heads;
     const SeqRows s = seq_rows(rows, b, c.page_shift);
-    const int r0 = chunk * QR, all = s.todo * group;
-    if (r0 >= all) return;
+    const int r0 = chunk * QR, all = s.todo * group, tiles = (max(s.len, 0) + TILE - 1) / TILE, pieces = pieces_of(tiles, piece, splits);
+    if (r0 >= all || split >= pieces) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int heads = c.kv_heads * group, len = max(s.len, 0);
     const int first = rows.lens[b] - s.n;                             // position of the first new token (negative: more new tokens than positions)
@@ -135,9 +139,9 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
         for (int j = 0; j < DV; j++) o[qt][j] = v4f{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int tiles = (len + TILE - 1) / TILE, per = (tiles + splits - 1) / splits, end = min((split + 1) * per, tiles);
+    const int end = split == pieces - 1 ? tiles : (split + 1) * piece;
     const int whole = min(first, len) / TILE;                         // tiles below it are seen by every row
-    for (int t = split * per + w; t < end; t += 4) {
+    for (int t = split * piece + w; t < end; t += 4) {
         const KeyTile<D> kt = load_tile<D>(c, table, head, t * TILE, (len - 1) & ~15, r, g);
         v8h kf[2][D / 32];
 #pragma unroll
@@ -160,7 +164,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
         for (int h = 0; h < 2; h++)
 #pragma unroll
             for (int e = 0; e < 4; e++) ev[h][e] = (float)__builtin_amdgcn_frexp_expf(kt.vs[h][e]);
-        v8h pf[QT];
+        v8h pf[QT], pl[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
             float sc[2][4], top = -INFINITY;
@@ -203,7 +207,9 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
                 for (int e = 0; e < 4; e++) {
                     const float p = __builtin_amdgcn_exp2f(sc[h][e] - m[qt]);
                     l[qt] += p;
-                    pf[qt][4 * h + e] = (_Float16)(masked >> (4 * h + e) & 1u ? 0.0f : p * kt.vs[h][e]);
+                    const float pv = masked >> (4 * h + e) & 1u ? 0.0f : p * kt.vs[h][e];
+                    pf[qt][4 * h + e] = to_half(pv);
+                    if (!BF) pl[qt][4 * h + e] = (_Float16)(pv - (float)pf[qt][4 * h + e]);
                 }
         }
 #pragma unroll
@@ -213,7 +219,10 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
 #pragma unroll
             for (int u = 0; u < 4; u++) x[u] = to_halves(__builtin_amdgcn_perm((unsigned)kt.v[2 * u + 1][j >> 2], (unsigned)kt.v[2 * u][j >> 2], PICK[j & 3]));
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++) o[qt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), pf[qt], o[qt][j], 0, 0, 0);
+            for (int qt = 0; qt < QT; qt++) {
+                o[qt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), pf[qt], o[qt][j], 0, 0, 0);
+                if (!BF) o[qt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), pl[qt], o[qt][j], 0, 0, 0);
+            }
         }
     }
 
@@ -251,7 +260,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
             for (int u = 0; u < 4; u++) y[e] += so[u][at][d + e] * f[u];
         }
         const size_t to = (size_t)(s.first_row + token) * heads + h;
-        if (splits == 1) {
+        if (pieces == 1) {
             const float by = sum != 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;        // a row that sees nothing is zeros
             const v4i packed = {narrow2<BF>(y[0] * by, y[1] * by), narrow2<BF>(y[2] * by, y[3] * by), narrow2<BF>(y[4] * by, y[5] * by),
                                 narrow2<BF>(y[6] * by, y[7] * by)};
@@ -269,68 +278,95 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
     }
 }
 
-// joins the splits' parts, D / 8 lanes a row
+// Joins the pieces of the sequences that have several: a wave per row, D / 8 lanes of eight channels, the others of the wave taking pieces of their own.
+constexpr int MAX_SPLITS = 64;
 template <bool BF, int D>
-__global__ __launch_bounds__(256) void join_splits_kernel(KvRows rows, int heads, int splits, int page_shift, const float *__restrict__ partials,
+__global__ __launch_bounds__(256) void join_pieces_kernel(KvRows rows, int heads, int splits, int piece, int page_shift, const float *__restrict__ partials,
                                                           char *__restrict__ out)
 {
-    constexpr int LANES = D / 8;
+    constexpr int LANES = D / 8, AT_ONCE = 64 / LANES;
     const SeqRows s = seq_rows(rows, blockIdx.y, page_shift);
-    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d = threadIdx.x % LANES * 8;
-    if (row >= s.todo * heads) return;
+    const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = lane % LANES * 8;
+    const int pieces = pieces_of((max(s.len, 0) + TILE - 1) / TILE, piece, splits);
+    if (row >= s.todo * heads || pieces == 1) return;
     const size_t at = (size_t)s.first_row * heads + row;
     const float *ml = partials + (size_t)rows.rows * heads * splits * D + 2 * at * splits, *p = partials + at * splits * D + d;
-    float top = LOWEST, sum = 0.0f, y[8] = {};
-    for (int i = 0; i < splits; i++) top = __builtin_fmaxf(top, ml[2 * i]);
-    for (int i = 0; i < splits; i++) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * i] - top);
-        const v4f a = *reinterpret_cast<const v4f *>(p + (size_t)i * D), b = *reinterpret_cast<const v4f *>(p + (size_t)i * D + 4);
-        sum += ml[2 * i + 1] * f;
+    const float m = lane < pieces ? ml[2 * lane] : LOWEST, l = lane < pieces ? ml[2 * lane + 1] : 0.0f;
+    constexpr int BATCH = 4;
+    float y[8] = {}, factor = 0.0f, sum = 0.0f;
+    for (int i0 = 0; i0 < pieces; i0 += BATCH * AT_ONCE) {
+        v4f a[BATCH][2];
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            y[e] += a[e] * f;
-            y[4 + e] += b[e] * f;
+        for (int u = 0; u < BATCH; u++) {
+            const float *from = p + (size_t)min(i0 + u * AT_ONCE + lane / LANES, pieces - 1) * D;
+            a[u][0] = *reinterpret_cast<const v4f *>(from);
+            a[u][1] = *reinterpret_cast<const v4f *>(from + 4);
+        }
+        if (i0 == 0) {
+            factor = __builtin_amdgcn_exp2f(m - wave_max(m));
+            sum = l * factor;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        }
+#pragma unroll
+        for (int u = 0; u < BATCH; u++) {
+            const int i = i0 + u * AT_ONCE + lane / LANES;
+            const float f = __shfl(factor, min(i, pieces - 1), 64);
+            if (i < pieces) {
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    y[e] += a[u][0][e] * f;
+                    y[4 + e] += a[u][1][e] * f;
+                }
+            }
         }
     }
+#pragma unroll
+    for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+        for (int e = 0; e < 8; e++) y[e] += __shfl_xor(y[e], o, 64);
     const float by = sum != 0.0f ? __fdiv_rn(1.0f, sum) : 0.0f;
-    *reinterpret_cast<v4i *>(out + 2 * (at * D + d)) = v4i{narrow2<BF>(y[0] * by, y[1] * by), narrow2<BF>(y[2] * by, y[3] * by),
-                                                           narrow2<BF>(y[4] * by, y[5] * by), narrow2<BF>(y[6] * by, y[7] * by)};
+    if (lane < LANES)
+        *reinterpret_cast<v4i *>(out + 2 * (at * D + d)) = v4i{narrow2<BF>(y[0] * by, y[1] * by), narrow2<BF>(y[2] * by, y[3] * by),
+                                                               narrow2<BF>(y[4] * by, y[5] * by), narrow2<BF>(y[6] * by, y[7] * by)};
 }
 
 int row_tiles(int rows) { return rows > 16 ? 2 : 1; }
 
 template <bool BF, int D>
-hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree, int splits,
+hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree, Cut cut,
                             float *partials, void *out, hipStream_t st)
 {
     const int group = heads / c.kv_heads, most = rows.max_rows * group, qt = row_tiles(most), chunks = (most + 16 * qt - 1) / (16 * qt);
     auto kern = qt == 1 ? cached_attention_kernel<BF, D, 1> : cached_attention_kernel<BF, D, 2>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)rows.batch * c.kv_heads * splits * chunks), dim3(256), 0, st, (const char *)q, ldq, c, rows, group, chunks, splits,
-                       scale, tree, partials, (char *)out);
-    if (splits > 1)
-        hipLaunchKernelGGL((join_splits_kernel<BF, D>), dim3((unsigned)((rows.max_rows * heads + 2048 / D - 1) / (2048 / D)), (unsigned)rows.batch), dim3(256), 0, st,
-                           rows, heads, splits, c.page_shift, partials, (char *)out);
+    hipLaunchKernelGGL(kern, dim3((unsigned)rows.batch * c.kv_heads * cut.splits * chunks), dim3(256), 0, st, (const char *)q, ldq, c, rows, group, chunks, cut.splits,
+                       cut.piece, scale, tree, partials, (char *)out);
+    if (cut.splits > 1)
+        hipLaunchKernelGGL((join_pieces_kernel<BF, D>), dim3((unsigned)((most * c.kv_heads + 3) / 4), (unsigned)rows.batch), dim3(256), 0, st,
+                           rows, heads, cut.splits, cut.piece, c.page_shift, partials, (char *)out);
     return hipGetLastError();
 }
 
 }  // namespace
 
-int cached_attention_splits(int batch, int heads, int kv_heads, int, int max_new, int max_len)
+Cut cached_attention_cut(int batch, int heads, int kv_heads, int max_new, int max_len)
 {
     const int most = max_new * (heads / kv_heads), qt = row_tiles(most);
-    const long items = (long)batch * kv_heads * ((most + 16 * qt - 1) / (16 * qt)), tiles = (max_len + TILE - 1) / TILE;
-    long splits = (1024 + items - 1) / items;
-    if (splits > tiles / 8) splits = tiles / 8;
-    return splits < 1 ? 1 : (int)splits;
+    const long items = (long)batch * kv_heads * ((most + 16 * qt - 1) / (16 * qt)), tiles = (max_len + (long)TILE - 1) / TILE;
+    const long wanted = (1024 + items - 1) / items;
+    long piece = (tiles + wanted - 1) / wanted;
+    if (piece < 8) piece = 8;
+    if (piece < (tiles + MAX_SPLITS - 1) / MAX_SPLITS) piece = (tiles + MAX_SPLITS - 1) / MAX_SPLITS;
+    return Cut{(int)((tiles + piece - 1) / piece), (int)piece};
 }
 
 hipError_t launch_cached_attention(const void *q, long ldq, bool bf16, int heads, int D, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree,
-                                   int splits, float *partials, void *out, hipStream_t st)
+                                   Cut cut, float *partials, void *out, hipStream_t st)
 {
-    if (D == 128) return bf16 ? cached_attention<true, 128>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st)
-                              : cached_attention<false, 128>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st);
-    return bf16 ? cached_attention<true, 64>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st)
-                : cached_attention<false, 64>(q, ldq, heads, c, rows, scale, tree, splits, partials, out, st);
+    if (D == 128) return bf16 ? cached_attention<true, 128>(q, ldq, heads, c, rows, scale, tree, cut, partials, out, st)
+                              : cached_attention<false, 128>(q, ldq, heads, c, rows, scale, tree, cut, partials, out, st);
+    return bf16 ? cached_attention<true, 64>(q, ldq, heads, c, rows, scale, tree, cut, partials, out, st)
+                : cached_attention<false, 64>(q, ldq, heads, c, rows, scale, tree, cut, partials, out, st);
 }
 
 }  // namespace samp

@@ -95,13 +95,18 @@ __device__ __forceinline__ SeqRows seq_rows(const KvRows &r, int b, int page_shi
 hipError_t launch_quantize_tokens(const void *x, long ldx, bool bf16, int M, int K, int8_t *codes, float *steps, hipStream_t st);
 hipError_t launch_gemm_i8_tokens(const int8_t *codes, const float *steps, const int8_t *Wp, const float *s_w, const float *bias, bool gelu, void *out,
                                  bool bf16, int M, int N, int K, hipStream_t st);
+// few rows: both in one launch
+bool linear_tokens_is_fused(int M, int K);
+hipError_t launch_linear_few(const void *x, long ldx, bool bf16, const int8_t *Wp, const float *s_w, const float *bias, bool gelu, void *out, int M, int N, int K,
+                             hipStream_t st);
 hipError_t launch_cache_write(const KvCache &cache, const void *k, long ldk, const void *v, long ldv, bool bf16, int head_dim, const KvRows &rows,
                               hipStream_t st);
 hipError_t launch_cache_read(const KvCache &cache, void *k, void *v, bool bf16, int head_dim, const KvRows &rows, hipStream_t st);
-// the pieces that a call cuts the sequences into (each a partial result in the workspace if more than one)
-int cached_attention_splits(int batch, int heads, int kv_heads, int head_dim, int max_new, int max_len);
+// how a call cuts contexts: pieces of so many tiles of 32 keys, at most `splits` of them, each with a partial result in the workspace if there are several
+struct Cut { int splits, piece; };
+Cut cached_attention_cut(int batch, int heads, int kv_heads, int max_new, int max_len);
 hipError_t launch_cached_attention(const void *q, long ldq, bool bf16, int heads, int head_dim, const KvCache &cache, const KvRows &rows, float scale,
-                                   const uint64_t *tree, int splits, float *partials, void *out, hipStream_t st);
+                                   const uint64_t *tree, Cut cut, float *partials, void *out, hipStream_t st);
 hipError_t launch_causal_attention(const void *q, long ldq, const void *k, long ldk, const void *v, long ldv, bool bf16, int heads, int kv_heads,
                                    int head_dim, const int *cu, int batch, int max_len, int rows, float scale, void *out, hipStream_t st);
 

@@ -26,12 +26,13 @@ template <bool BF> __device__ __forceinline__ v2i finish4(const v4i &acc, float 
 // N need only be a multiple of 16: a wave's blocks past the last one repeat it and are not stored.
 template <bool BF, int MT, int NTW, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void gemm_tokens_kernel(const char *__restrict__ A, const char *__restrict__ Wp, int M, int N, int K, int tiles_m, int tiles_n, TokensEpi epi, char *__restrict__ out)
+void gemm_tokens_kernel(const char *__restrict__ A, const char *__restrict__ Wp, int M, int N, int K, int tiles_m, int tiles_n, int band, TokensEpi epi, char *__restrict__ out)
 {
     constexpr int BM = 16 * MT, BN = 64 * NTW, NLDA = stream_loads<false, MT>(), STRIDE = BN * 2 + 16;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    const int tile = xcd_contiguous(blockIdx.x, tiles_m * tiles_n);
-    const int m0 = tile / tiles_n * BM, n0 = tile % tiles_n * BN;
+    // tiles in bands of `band` row tiles, in a band column by column
+    const int tile = xcd_contiguous(blockIdx.x, tiles_m * tiles_n), first = tile / (band * tiles_n) * band, high = min(band, tiles_m - first);
+    const int in_band = tile - first * tiles_n, m0 = (first + in_band % high) * BM, n0 = in_band / high * BN;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, q = lane >> 4;
 
@@ -101,7 +102,7 @@ void gemm_tokens_kernel(const char *__restrict__ A, const char *__restrict__ Wp,
 }
 
 template <bool BF, int MT, int NTW, int D>
-hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, hipStream_t st)
+hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, int band, hipStream_t st)
 {
     constexpr int RING = stream_ring_bytes<false, MT, D>(), OUT = 16 * MT * (64 * NTW * 2 + 16), LDS = RING > OUT ? RING : OUT;
     auto kern = gemm_tokens_kernel<BF, MT, NTW, D>;
@@ -114,14 +115,139 @@ hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, 
         }
     }
     const int tm = (M + 16 * MT - 1) / (16 * MT), tn = (N + 64 * NTW - 1) / (64 * NTW);
-    hipLaunchKernelGGL(kern, dim3((unsigned)tm * tn), dim3(256), LDS, st, (const char *)A, (const char *)Wp, M, N, K, tm, tn, epi, (char *)out);
+    hipLaunchKernelGGL(kern, dim3((unsigned)tm * tn), dim3(256), LDS, st, (const char *)A, (const char *)Wp, M, N, K, tm, tn, band, epi, (char *)out);
     return hipGetLastError();
+}
+
+// ---- up to sixteen rows ------------------------------------------------------------------------------
+// One token tile; what it costs is the weights' way from HBM and the latencies around it.  A block owns 16 channels and splits K over its eight waves, so that
+// all of its weights (KB blocks of 1 KB a wave) are requested before anything else happens; the int32 partial tiles meet in LDS.  FUSED: the rows come in 16
+// bits and every block quantises them for itself while its weights are on the way, into LDS (rows 16 bytes more than K apart, so that the sixteen rows of an
+// operand read lie in different banks), which saves a launch.  Eight, four, two or one waves share a row, the fewer the more rows there are.
+constexpr int FEW_WAVES = 8;
+struct FewRows { const void *x; long ld; const float *steps; };        // FUSED: 16-bit rows, ld values apart; else codes, K apart, and their steps
+template <bool BF, bool FUSED, int KB>
+__global__ __launch_bounds__(64 * FEW_WAVES) void gemm_tokens_few_kernel(const char *__restrict__ Wp, int K, int N, int M, int sharers, FewRows in, TokensEpi epi,
+                                                                           char *__restrict__ out)
+{
+    extern __shared__ __attribute__((aligned(16))) char lds[];             // FUSED: codes
+    __shared__ unsigned tops[FEW_WAVES];
+    __shared__ float row_steps[16];
+    __shared__ __attribute__((aligned(16))) v4i part[FEW_WAVES][64];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4, kblocks = K >> 6;
+    const auto weights = buffer_of(Wp + (size_t)blockIdx.x * 16 * K, 16 * K);
+    const int row = min(r, M - 1);
+    v4i wf[KB], f[KB];
+    auto request_weights = [&]() {                                          // past the end: zeros
+#pragma unroll
+        for (int i = 0; i < KB; i++) wf[i] = __builtin_amdgcn_raw_buffer_load_b128(weights, (w + FEW_WAVES * i) * 1024 + 16 * lane, 0, 0);
+    };
+    // the lane of the result: token r, channels 4 q .. 4 q + 3
+    const int chan = blockIdx.x * 16 + 4 * q;
+    v4f sw = {0.f, 0.f, 0.f, 0.f}, bb = sw;
+    auto request_tables = [&]() {
+        if (w) return;
+        sw = *reinterpret_cast<const v4f *>(epi.s_w + chan);
+        if (epi.bias) bb = *reinterpret_cast<const v4f *>(epi.bias + chan);
+    };
+    float step = 1.0f;
+    if constexpr (FUSED) {
+        const int pitch = K + 16, rows_at_once = FEW_WAVES / sharers, first = (w & (sharers - 1)) * 64 + lane, stride = 64 * sharers;
+        for (int m0 = 0; m0 < M; m0 += rows_at_once) {                      // (one round where waves share a row)
+            const int m = m0 + w / sharers;
+            const auto from = buffer_of((const char *)in.x + 2 * (size_t)min(m, M - 1) * in.ld, m < M ? 2 * K : 0);
+            v4i x[KB];
+#pragma unroll
+            for (int i = 0; i < KB; i++) x[i] = __builtin_amdgcn_raw_buffer_load_b128(from, 16 * (first + i * stride), 0, 0);
+            if (m0 == 0) {
+                request_weights();
+                request_tables();
+            }
+            unsigned top = 0;
+#pragma unroll
+            for (int i = 0; i < KB; i++) top = max(top, bits_max16(x[i]));
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o, 64));
+            if (sharers > 1) {
+                if (lane == 0) tops[w] = top;
+                __syncthreads();
+                for (int u = 0; u < sharers; u++) top = max(top, tops[(w & ~(sharers - 1)) + u]);
+            }
+            const RowQuant rq = row_quant<BF>(top);
+            if (m < M) {
+#pragma unroll
+                for (int i = 0; i < KB; i++) {
+                    float v[8];
+                    widen8<BF>(x[i], v);
+                    if (8 * (first + i * stride) < K) *reinterpret_cast<v2i *>(lds + m * pitch + 8 * (first + i * stride)) = quant8(v, rq);
+                }
+                if (first == 0) row_steps[m] = rq.step;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KB; i++) f[i] = *reinterpret_cast<const v4i *>(lds + row * pitch + min(w + FEW_WAVES * i, kblocks - 1) * 64 + 16 * q);
+        step = row_steps[row];
+    } else {
+        const auto codes = buffer_of(in.x, M * K);
+#pragma unroll
+        for (int i = 0; i < KB; i++)
+            f[i] = __builtin_amdgcn_raw_buffer_load_b128(codes, row * K + min(w + FEW_WAVES * i, kblocks - 1) * 64 + 16 * q, 0, 0);
+        request_weights();
+        request_tables();
+        if (w == 0) step = in.steps[row];
+    }
+    v4i acc = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < KB; i++) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[i], f[i], acc, 0, 0, 0);
+    part[w][lane] = acc;
+    __syncthreads();
+    if (w || r >= M) return;
+#pragma unroll
+    for (int u = 1; u < FEW_WAVES; u++) acc += part[u][lane];
+    *reinterpret_cast<v2i *>(out + 2 * ((size_t)r * N + chan)) = finish4<BF>(acc, step, sw, bb, epi.gelu);
+}
+
+// K: sixteen blocks of weights a wave.  The codes of a fused call: what leaves a block below 64 KB of LDS
+constexpr int FEW_ROWS = 16, FEW_K = 16 * 64 * FEW_WAVES, FEW_CODES = 54 << 10;
+template <bool BF, bool FUSED>
+hipError_t launch_few(const FewRows &in, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, hipStream_t st)
+{
+    const int kb = (K / 64 + FEW_WAVES - 1) / FEW_WAVES, sharers = M == 1 ? 8 : M == 2 ? 4 : M <= 4 ? 2 : 1;
+    auto kern = kb <= 2 ? gemm_tokens_few_kernel<BF, FUSED, 2> : kb <= 4 ? gemm_tokens_few_kernel<BF, FUSED, 4> : kb <= 8 ? gemm_tokens_few_kernel<BF, FUSED, 8>
+                        : gemm_tokens_few_kernel<BF, FUSED, 16>;
+    hipLaunchKernelGGL(kern, dim3(N / 16), dim3(64 * FEW_WAVES), FUSED ? M * (K + 16) : 0, st, (const char *)Wp, K, N, M, sharers, in, epi, (char *)out);
+    return hipGetLastError();
+}
+
+// ---- which kernel ------------------------------------------------------------------------------------
+// The tile whose cost is least: its time for K = 4096 where the chip is full of it, times the rounds of blocks (the mean of whole rounds and their fraction).
+struct TokensTile { int mt, ntw; float us; };
+constexpr TokensTile TOKENS_TILES[] = {{2, 1, 7.3f}, {4, 1, 7.8f}, {4, 2, 13.0f}, {8, 2, 17.0f}, {8, 3, 23.0f}};
+int tokens_tile(int M, int N)
+{
+    int best = 0;
+    float least = 0.0f;
+    for (int i = 0; i < 5; i++) {
+        const long bm = 16 * TOKENS_TILES[i].mt, bn = 64 * TOKENS_TILES[i].ntw, blocks = (M + bm - 1) / bm * ((N + bn - 1) / bn);
+        const float rounds = blocks <= 256 ? 1.0f : 0.5f * ((float)((blocks + 255) / 256) + (float)blocks / 256.0f), cost = rounds * TOKENS_TILES[i].us;
+        if (i == 0 || cost < least) { best = i; least = cost; }
+    }
+    return best;
 }
 
 template <bool BF>
 hipError_t gemm_tokens(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, hipStream_t st)
 {
-    return launch_tile<BF, 2, 1, 2>(A, Wp, epi, out, M, N, K, st);
+    if (M <= FEW_ROWS && K <= FEW_K) return launch_few<BF, false>(FewRows{A, K, epi.steps}, Wp, epi, out, M, N, K, st);
+    const bool deep = K >= 512 && K % 512 < 256;                     // four stages in flight instead of two, if no more is left over
+    switch (tokens_tile(M, N)) {
+    case 0: return deep ? launch_tile<BF, 2, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 2, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
+    case 1: return deep ? launch_tile<BF, 4, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 4, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
+    case 2: return deep ? launch_tile<BF, 4, 2, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 4, 2, 2>(A, Wp, epi, out, M, N, K, 8, st);
+    case 3: return launch_tile<BF, 8, 2, 2>(A, Wp, epi, out, M, N, K, 8, st);
+    }
+    return launch_tile<BF, 8, 3, 2>(A, Wp, epi, out, M, N, K, 4, st);
 }
 
 }  // namespace
@@ -131,6 +257,15 @@ hipError_t launch_gemm_i8_tokens(const int8_t *codes, const float *steps, const 
 {
     const TokensEpi epi{steps, s_w, bias, gelu};
     return bf16 ? gemm_tokens<true>(codes, Wp, epi, out, M, N, K, st) : gemm_tokens<false>(codes, Wp, epi, out, M, N, K, st);
+}
+
+bool linear_tokens_is_fused(int M, int K) { return M <= FEW_ROWS && K <= FEW_K && M * (K + 16) <= FEW_CODES; }
+hipError_t launch_linear_few(const void *x, long ldx, bool bf16, const int8_t *Wp, const float *s_w, const float *bias, bool gelu, void *out, int M, int N, int K,
+                             hipStream_t st)
+{
+    const TokensEpi epi{nullptr, s_w, bias, gelu};
+    const FewRows in{x, ldx, nullptr};
+    return bf16 ? launch_few<true, true>(in, Wp, epi, out, M, N, K, st) : launch_few<false, true>(in, Wp, epi, out, M, N, K, st);
 }
 
 }  // namespace samp

@@ -26,50 +26,48 @@ _SIGNATURES = {
     "samp_attention_cache": (_P, _L, _I, _I, _P, _P, _I, _P, _P, _I, _I, _I, _I, _F, _P, _P, _P, _Z, _P),
     "samp_attention_causal": (_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _P, _I, _I, _I, _F, _P, _P),
 }
-_ready = None
+_entry = {}
 
 
-def _lib():
-    global _ready
-    if _ready is None:
-        L = lib()
-        for name, types in _SIGNATURES.items():
-            f = getattr(L, name)
-            f.argtypes = types
-            f.restype = _Z if name.endswith("_bytes") else C.c_int
-        _ready = L
-    return _ready
+def _fn(name: str):
+    f = _entry.get(name)
+    if f is None:
+        f = getattr(lib(), name)
+        f.argtypes = _SIGNATURES[name]
+        f.restype = _Z if name.endswith("_bytes") else C.c_int
+        _entry[name] = f
+    return f
 
 
 def _refuse(why: str):
     raise SampError(-1, why)
 
 
-def _bytes(need: int) -> int:
-    if need == 0:
-        raise SampError(-2, lib().samp_last_error().decode())
-    return need
+def _device(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        _refuse(f"tensors must be on the GPU ({t.device})")
+    return t.get_device()
 
 
-def _on(device: torch.device, *tensors):
-    if device.type != "cuda":
-        _refuse(f"tensors must be on the GPU ({device})")
-    for t in tensors:
-        if t is not None and t.device != device:
-            _refuse(f"tensors on different devices: {t.device}, {device}")
+def _elsewhere(t: torch.Tensor, device: int):
+    _refuse(f"tensors on different devices: {t.device}, cuda:{device}")
 
 
-def _flat(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, size: Optional[int] = None) -> int:
+def _flat(what: str, t: Optional[torch.Tensor], dtype: torch.dtype, device: int, size: Optional[int] = None) -> int:
     """The address of a contiguous tensor of one type (0 for None)."""
     if t is None:
         return 0
-    if t.dtype != dtype or not t.is_contiguous() or (size is not None and t.numel() != size):
+    if t.get_device() != device:
+        _elsewhere(t, device)
+    if t.dtype is not dtype or not t.is_contiguous() or (size is not None and t.numel() != size):
         _refuse(f"{what}: a contiguous {dtype} tensor{'' if size is None else f' of {size} elements'} is needed, not {t.dtype} {tuple(t.shape)} {t.stride()}")
     return t.data_ptr()
 
 
-def _heads(what: str, t: torch.Tensor) -> Tuple[int, int]:
+def _heads(what: str, t: torch.Tensor, device: int) -> Tuple[int, int]:
     """Address and row distance of [rows, heads, head_dim] whose heads lie next to each other."""
+    if t.get_device() != device:
+        _elsewhere(t, device)
     if t.dim() != 3 or t.dtype not in _TYPES:
         _refuse(f"{what}: fp16 or bfloat16 [rows, heads, head_dim] is needed, not {t.dtype} {tuple(t.shape)}")
     rows, heads, dim = t.shape
@@ -77,17 +75,6 @@ def _heads(what: str, t: torch.Tensor) -> Tuple[int, int]:
     if one != 1 or (head != dim and heads > 1):
         _refuse(f"{what}: the heads of a row must lie next to each other (strides {t.stride()})")
     return t.data_ptr(), row if rows > 1 else heads * dim
-
-
-def _call(device: torch.device, name: str, *args):
-    f = getattr(_lib(), name)
-    if device.index is not None and device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            rc = f(*args, torch.cuda.current_stream(device).cuda_stream)
-    else:
-        rc = f(*args, torch.cuda.current_stream(device).cuda_stream)
-    if rc:
-        raise SampError(rc, lib().samp_last_error().decode())
 
 
 def _rows2(what: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
@@ -98,14 +85,24 @@ def _rows2(what: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
     return x.data_ptr(), x.stride(0) if M > 1 else K, M, K
 
 
+def _call(device: int, name: str, *args):
+    stream = torch._C._cuda_getCurrentRawStream(device)              # torch.cuda.current_stream(device).cuda_stream, without the objects
+    if torch._C._cuda_getDevice() == device:
+        rc = _fn(name)(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            rc = _fn(name)(*args, stream)
+    if rc:
+        raise SampError(rc, lib().samp_last_error().decode())
+
+
 def quantize_tokens(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """samp_quantize_tokens: int8 codes [M, K] and float32 steps [M] of the rows of x (step = the row's absmax / 127)."""
-    _on(x.device)
+    device = _device(x)
     at, ld, M, K = _rows2("x", x)
-    codes = torch.empty((M, K), dtype=torch.int8, device=x.device)
-    steps = torch.empty(M, dtype=torch.float32, device=x.device)
+    codes, steps = x.new_empty((M, K), dtype=torch.int8), x.new_empty((M,), dtype=torch.float32)
     if M:
-        _call(x.device, "samp_quantize_tokens", at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr())
+        _call(device, "samp_quantize_tokens", at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr())
     return codes, steps
 
 
@@ -113,31 +110,30 @@ def gemm_i8_tokens_packed(codes: torch.Tensor, steps: torch.Tensor, Wp: torch.Te
                           gelu: bool = False, dtype: torch.dtype = torch.float16) -> torch.Tensor:
     """samp_gemm_i8_tokens_packed: [M, N] of `dtype` from int8 codes [M, K] with a step for each row and weights that pack_weight_i8 packed, with a
     step for each channel."""
-    _on(codes.device, steps, Wp, s_w, bias)
+    device = _device(codes)
     if codes.dim() != 2 or dtype not in _TYPES:
         _refuse("codes must be a matrix, and the result's type fp16 or bfloat16")
     M, K = codes.shape
     N = s_w.numel()
-    out = torch.empty((M, N), dtype=dtype, device=codes.device)
-    args = (_flat("codes", codes, torch.int8), _flat("steps", steps, torch.float32, M), _flat("Wp", Wp, torch.int8, N * K), _flat("s_w", s_w, torch.float32),
-            _flat("bias", bias, torch.float32, N), int(bool(gelu)), out.data_ptr(), _TYPES[dtype], M, N, K)
+    out = codes.new_empty((M, N), dtype=dtype)
+    args = (_flat("codes", codes, torch.int8, device), _flat("steps", steps, torch.float32, device, M), _flat("Wp", Wp, torch.int8, device, N * K),
+            _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N), int(bool(gelu)), out.data_ptr(), _TYPES[dtype], M, N, K)
     if M:
-        _call(codes.device, "samp_gemm_i8_tokens_packed", *args)
+        _call(device, "samp_gemm_i8_tokens_packed", *args)
     return out
 
 
 def linear_i8_tokens(x: torch.Tensor, Wp: torch.Tensor, s_w: torch.Tensor, bias: Optional[torch.Tensor] = None, gelu: bool = False) -> torch.Tensor:
     """samp_linear_i8_tokens: quantize_tokens and gemm_i8_tokens_packed in one call, x [M, K] -> [M, N] of x's type."""
-    device = x.device
-    _on(device, Wp, s_w, bias)
+    device = _device(x)
     at, ld, M, K = _rows2("x", x)
     N = s_w.numel()
-    out = torch.empty((M, N), dtype=x.dtype, device=device)
-    w, s, b = _flat("Wp", Wp, torch.int8, N * K), _flat("s_w", s_w, torch.float32), _flat("bias", bias, torch.float32, N)
+    w, s, b = _flat("Wp", Wp, torch.int8, device, N * K), _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N)
+    out = x.new_empty((M, N))
     if M:
-        need = _bytes(_lib().samp_linear_i8_tokens_workspace_bytes(M, K))
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-        _call(device, "samp_linear_i8_tokens", at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws.data_ptr(), need)
+        need = _fn("samp_linear_i8_tokens_workspace_bytes")(M, K)
+        ws = x.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
+        _call(device, "samp_linear_i8_tokens", at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws, need)
     return out
 
 
@@ -150,15 +146,15 @@ class KVCache:
     kept alive by this object), and the samp_kv_cache_t that points at them."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_step: torch.Tensor, v_step: torch.Tensor):
-        _on(k.device, v, k_step, v_step)
+        device = _device(k)
         if k.dim() != 4 or v.shape != k.shape or k_step.shape != k.shape[:3] or v_step.shape != k.shape[:3]:
             _refuse(f"a cache is codes [pages, kv_heads, page_len, head_dim] and steps [pages, kv_heads, page_len], not {tuple(k.shape)} {tuple(v.shape)} "
                     f"{tuple(k_step.shape)} {tuple(v_step.shape)}")
         self.k, self.v, self.k_step, self.v_step = k, v, k_step, v_step
-        self.device = k.device
+        self.device = device
         self.pages, self.kv_heads, self.page_len, self.head_dim = k.shape
-        self.struct = _CacheStruct(_flat("k", k, torch.int8), _flat("v", v, torch.int8), _flat("k_step", k_step, torch.float32),
-                                   _flat("v_step", v_step, torch.float32), *k.shape)
+        self.struct = _CacheStruct(_flat("k", k, torch.int8, device), _flat("v", v, torch.int8, device), _flat("k_step", k_step, torch.float32, device),
+                                   _flat("v_step", v_step, torch.float32, device), *k.shape)
         self.address = C.addressof(self.struct)
 
     @classmethod
@@ -168,24 +164,23 @@ class KVCache:
         return cls(*codes, *(torch.zeros((pages, kv_heads, page_len), dtype=torch.float32, device=device) for _ in range(2)))
 
 
-def _places(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor):
-    _on(cache.device, table, cu, lens)
+def _places(device: int, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor):
     if table.dim() != 2:
         _refuse("the page table is [sequences, pages of a sequence]")
     B, width = table.shape
-    return _flat("table", table, torch.int32), width, _flat("cu", cu, torch.int32, B + 1), _flat("lens", lens, torch.int32, B), B
+    return _flat("table", table, torch.int32, device), width, _flat("cu", cu, torch.int32, device, B + 1), _flat("lens", lens, torch.int32, device, B), B
 
 
 def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int) -> None:
     """samp_cache_write: the packed rows k, v [rows, kv_heads, head_dim] become the last cu[b + 1] - cu[b] of the lens[b] positions of each sequence.
     table int32 [B, width]; cu int32 [B + 1] or None (max_new rows each); lens int32 [B], the new positions counted."""
-    _on(cache.device, k, v)
-    (pk, ldk), (pv, ldv) = _heads("k", k), _heads("v", v)
+    device = cache.device
+    (pk, ldk), (pv, ldv) = _heads("k", k, device), _heads("v", v, device)
     if k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (cache.kv_heads, cache.head_dim):
         _refuse(f"k and v must be [rows, {cache.kv_heads}, {cache.head_dim}] of one type, not {tuple(k.shape)} and {tuple(v.shape)}")
-    t, width, pcu, plens, B = _places(cache, table, cu, lens)
+    t, width, pcu, plens, B = _places(device, table, cu, lens)
     if k.shape[0] and B:
-        _call(cache.device, "samp_cache_write", cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, max_new, k.shape[0])
+        _call(device, "samp_cache_write", cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, max_new, k.shape[0])
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_rows: int, rows: int,
@@ -193,13 +188,15 @@ def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], 
     """samp_cache_read: k, v [rows, kv_heads, head_dim] of `dtype`, sequence b's rows the last cu[b + 1] - cu[b] of its lens[b] positions."""
     if dtype not in _TYPES:
         _refuse("the result's type must be fp16 or bfloat16")
-    t, width, pcu, plens, B = _places(cache, table, cu, lens)
+    device = cache.device
+    t, width, pcu, plens, B = _places(device, table, cu, lens)
     if out is None:
-        out = tuple(torch.empty((rows, cache.kv_heads, cache.head_dim), dtype=dtype, device=cache.device) for _ in range(2))
-    _on(cache.device, *out)
-    k, v = (_flat("out", o, dtype, rows * cache.kv_heads * cache.head_dim) for o in out)
+        shape = (rows, cache.kv_heads, cache.head_dim)
+        out = cache.k.new_empty(shape, dtype=dtype), cache.k.new_empty(shape, dtype=dtype)
+    size = rows * cache.kv_heads * cache.head_dim
+    k, v = _flat("out", out[0], dtype, device, size), _flat("out", out[1], dtype, device, size)
     if rows and B:
-        _call(cache.device, "samp_cache_read", cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, max_rows, rows)
+        _call(device, "samp_cache_read", cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, max_rows, rows)
     return out
 
 
@@ -209,22 +206,21 @@ def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Op
     """samp_attention_cache: [rows, heads, head_dim] of the new tokens q over the cache that holds their keys and values already.
     max_len: the longest context expected (None: what the page table has room for).  scale: None for 1 / sqrt(head_dim).  tree: int64 words [rows]."""
     device = cache.device
-    _on(device, q, tree, out)
-    at, ld = _heads("q", q)
+    at, ld = _heads("q", q, device)
     rows, heads, dim = q.shape
     if dim != cache.head_dim:
         _refuse(f"q has heads of {dim}, the cache of {cache.head_dim}")
-    t, width, pcu, plens, B = _places(cache, table, cu, lens)
+    t, width, pcu, plens, B = _places(device, table, cu, lens)
     if out is None:
-        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=device)
-    to, words = _flat("out", out, q.dtype, rows * heads * dim), _flat("tree", tree, torch.int64, rows)
+        out = q.new_empty((rows, heads, dim))
+    to, words = _flat("out", out, q.dtype, device, rows * heads * dim), _flat("tree", tree, torch.int64, device, rows)
     if rows and B:
         if max_len is None:
             max_len = width * cache.page_len
-        need = _bytes(_lib().samp_attention_cache_workspace_bytes(rows, B, heads, cache.kv_heads, dim, max_new, max_len))
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        need = _fn("samp_attention_cache_workspace_bytes")(rows, B, heads, cache.kv_heads, dim, max_new, max_len)
+        ws = q.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
         _call(device, "samp_attention_cache", at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
-              1.0 / math.sqrt(dim) if scale is None else scale, words, to, ws.data_ptr(), need)
+              1.0 / math.sqrt(dim) if scale is None else scale, words, to, ws, need)
     return out
 
 
@@ -232,21 +228,20 @@ def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Opti
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """samp_attention_causal: [rows, heads, head_dim] from q [rows, heads, head_dim] and k, v [rows, kv_heads, head_dim] (views into a fused
     projection's rows are read in place).  cu int32 [B + 1], or None for sequences of max_len rows each."""
-    device = q.device
-    _on(device, k, v, cu, out)
-    (pq, ldq), (pk, ldk), (pv, ldv) = _heads("q", q), _heads("k", k), _heads("v", v)
+    device = _device(q)
+    (pq, ldq), (pk, ldk), (pv, ldv) = _heads("q", q, device), _heads("k", k, device), _heads("v", v, device)
     rows, heads, dim = q.shape
     if k.shape != v.shape or k.shape[0] != rows or k.shape[2] != dim or k.dtype != q.dtype or v.dtype != q.dtype:
         _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
     if out is None:
-        out = torch.empty((rows, heads, dim), dtype=q.dtype, device=device)
-    to = _flat("out", out, q.dtype, rows * heads * dim)
+        out = q.new_empty((rows, heads, dim))
+    to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows == 0:
         return out
     if cu is None and (max_len < 1 or rows % max_len):
         _refuse("without sequence offsets every sequence has max_len rows")
     B = rows // max_len if cu is None else cu.numel() - 1
     if B:
-        _call(device, "samp_attention_causal", pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, B + 1), B, max_len,
+        _call(device, "samp_attention_causal", pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, device, B + 1), B, max_len,
               rows, 1.0 / math.sqrt(dim) if scale is None else scale, to)
     return out

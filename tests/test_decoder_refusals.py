@@ -14,7 +14,9 @@ def L():
     if not os.path.exists(P.lib_path()):
         from paper_2209_09130_amd import build as B
         B.build(force=True)
-    return D._lib()
+    for name in D._SIGNATURES:
+        D._fn(name)
+    return P.lib()
 
 
 _mem = (C.c_char * 8192)()
@@ -57,14 +59,14 @@ def test_products(L):
               ({"N": 24}, SHAPE, b"N=24"), ({"N": 0}, SHAPE, b"N=0"), ({"K": 96}, SHAPE, b"K=96"), ({"K": 131136}, SHAPE, b"K <="), ({"N": 1 << 20, "K": 4096}, SHAPE, b"2^31"),
               ({"Wp": AT + 8}, ARG, b"aligned"), ({"s_w": AT + 4}, ARG, b"aligned"), ({"bias": AT + 4}, ARG, b"aligned"), ({"out": AT + 2}, ARG, b"aligned")]
     refusals(L.samp_gemm_i8_tokens_packed, base, shared + [({"codes": None}, ARG, b"NULL"), ({"steps": None}, ARG, b"NULL"), ({"codes": AT + 8}, ARG, b"aligned")])
-    need = L.samp_linear_i8_tokens_workspace_bytes(2, 128)
-    assert need >= 2 * 128 + 8
-    assert L.samp_linear_i8_tokens_workspace_bytes(0, 128) == 0 and L.samp_linear_i8_tokens_workspace_bytes(2, 100) == 0
+    need = L.samp_linear_i8_tokens_workspace_bytes(100, 128)
+    assert need >= 100 * 128 + 400
+    assert L.samp_linear_i8_tokens_workspace_bytes(0, 128) == 0 and L.samp_linear_i8_tokens_workspace_bytes(100, 100) == 0
     base = [("x", AT), ("ldx", 128), ("type", 0), ("Wp", AT), ("s_w", AT), ("bias", None), ("gelu", 0), ("out", AT), ("M", 2), ("N", 64), ("K", 128),
             ("workspace", AT), ("bytes", need), ("stream", None)]
     refusals(L.samp_linear_i8_tokens, base, shared + [
-        ({"x": None}, ARG, b"NULL"), ({"ldx": 120}, SHAPE, b"leading"), ({"workspace": None}, SPACE, b"workspace"), ({"workspace": AT + 16}, SPACE, b"workspace"),
-        ({"bytes": need - 1}, SPACE, b"workspace")])
+        ({"x": None}, ARG, b"NULL"), ({"ldx": 120}, SHAPE, b"leading"), ({"M": 100, "workspace": None}, SPACE, b"workspace"),
+        ({"M": 100, "workspace": AT + 16}, SPACE, b"workspace"), ({"M": 100, "bytes": need - 1}, SPACE, b"workspace")])
 
 
 BAD_CACHES = [(dict(k=None), ARG, b"NULL"), (dict(v_step=None), ARG, b"NULL"), (dict(v=AT + 8), ARG, b"aligned"), (dict(head_dim=96), SHAPE, b"head_dim"),
@@ -94,7 +96,7 @@ def test_cache_write_and_read(L):
 
 def test_attention_cache(L):
     ok = cache()
-    need = L.samp_attention_cache_workspace_bytes(5, 2, 4, 2, 64, 3, 32)
+    need = L.samp_attention_cache_workspace_bytes(5, 2, 4, 2, 64, 3, 4096)
     assert need > 0
     assert L.samp_attention_cache_workspace_bytes(5, 2, 3, 2, 64, 3, 32) == 0 and L.samp_attention_cache_workspace_bytes(5, 2, 4, 2, 80, 3, 32) == 0
     base = [("q", AT), ("ldq", 256), ("type", 0), ("heads", 4), ("cache", C.addressof(ok)), ("table", AT), ("width", 2), ("cu", AT), ("lens", AT), ("batch", 2),
@@ -104,8 +106,8 @@ def test_attention_cache(L):
         ({"q": None}, ARG, b"q is NULL"), ({"ldq": 248}, SHAPE, b"q: "), ({"heads": 3}, SHAPE, b"multiple"), ({"heads": 0}, SHAPE, b"multiple"), ({"heads": 1026}, SHAPE, b"1024"),
         ({"max_len": 0}, SHAPE, b"max_len"), ({"scale": 0.0}, SCALE, b"scale"), ({"scale": -1.0}, SCALE, b"scale"), ({"scale": float("nan")}, SCALE, b"scale"),
         ({"scale": float("inf")}, SCALE, b"scale"), ({"out": None}, ARG, b"out"), ({"out": AT + 8}, ARG, b"out"), ({"tree": AT + 4}, ARG, b"tree"),
-        ({"tree": AT, "rows": 100, "max_new": 65}, SHAPE, b"64"), ({"workspace": None}, SPACE, b"workspace"), ({"bytes": need - 1}, SPACE, b"workspace"),
-        ({"rows": 1 << 22, "max_new": 1 << 22, "batch": 1000, "heads": 1024}, SHAPE, b"2^31")])
+        ({"tree": AT, "rows": 100, "max_new": 65}, SHAPE, b"64"), ({"max_len": 4096, "workspace": None}, SPACE, b"workspace"),
+        ({"max_len": 4096, "bytes": need - 1}, SPACE, b"workspace"), ({"max_len": 4096, "workspace": AT + 8}, SPACE, b"workspace"), ({"rows": 1 << 22, "max_new": 1 << 22, "batch": 1000, "heads": 1024}, SHAPE, b"2^31")])
 
 
 def test_attention_causal(L):
@@ -128,11 +130,13 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     f = torch.zeros(2, 4, 64, dtype=torch.float16)
     for t, why in ((f.float(), "bfloat16"), (f[0], "rows, heads"), (f.transpose(0, 1).contiguous().transpose(0, 1), "next to each other"), (f[..., ::2], "next to each other")):
         with pytest.raises(P.SampError, match=why):
-            D._heads("q", t)
-    assert D._heads("q", f[:, 1:3])[1] == 256 and D._heads("q", f[:1])[1] == 256
+            D._heads("q", t, -1)
+    assert D._heads("q", f[:, 1:3], -1)[1] == 256 and D._heads("q", f[:1], -1)[1] == 256
     with pytest.raises(P.SampError, match="dense rows"):
         D._rows2("x", h.t())
     with pytest.raises(P.SampError, match="contiguous"):
-        D._flat("t", h.t(), torch.float16)
+        D._flat("t", h.t(), torch.float16, -1)
+    with pytest.raises(P.SampError, match="different devices"):
+        D._flat("t", h, torch.float16, 0)
     with pytest.raises(P.SampError, match="elements"):
-        D._flat("t", h, torch.float16, 3)
+        D._flat("t", h, torch.float16, -1, 3)
