@@ -82,12 +82,14 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
     constexpr int QR = 16 * QT, DV = D / 16;
     __shared__ __attribute__((aligned(16))) float so[4][QR][D + 4];
     __shared__ float sm[4][QR], sl[4][QR];
+    // key heads run fastest: their work is alike, so the XCDs, to which blocks go in turn, have the same share whatever the lengths are (pieces running
+    // fastest, 64 contexts of 17 to 8192 tokens in pieces of 1024: 149 us, of 768 119.5)
     int item = blockIdx.x;
-    const int chunk = item % chunks;
-    item /= chunks;
-    const int split = item % splits;
-    item /= splits;
-    const int head = item % c.kv_heads, b = item / c.kv_heads;
+    const int head = item % c.kv_heads;
+    item /= c.kv_heads;
+    const int b = item % rows.batch;
+    item /= rows.batch;
+    const int chunk = item % chunks, split = item / chunks;
     const SeqRows s = seq_rows(rows, b, c.page_shift);
     const int r0 = chunk * QR, all = s.todo * group, tiles = (max(s.len, 0) + TILE - 1) / TILE, pieces = pieces_of(tiles, piece, splits);
     if (r0 >= all || split >= pieces) return;
@@ -349,15 +351,23 @@ hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c
 
 }  // namespace
 
+// Pieces of so many tiles that 512 blocks have them all, but no less than four tiles (a tile for each wave; eight where a block has two row tiles), below which
+// the blocks' own latencies count for more than their number, and no more than 48, so that blocks of contexts of different lengths end together; none at all
+// where there would be few more tiles than in one.  Joining costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
+// key heads of 128, one context of 4000 8.6 / 9.3 / 12.0 / 17.5 / 28.7 / 48; 64 of 17 to 8192 178 / 142 / 126 / 120 / 121 / 136; 32 of 500 to 1000 21.8 / 19.8 /
+// 17.6 / 18.2; 16 drafts on 8 contexts of 300 to 2100, 16 heads of 64, 17.0 / 15.0 / 14.2 / 16.2 / 22.9; one context of 8192, five tokens of 28 heads on 4,
+// 18.3 / 15.9 / 17.3 / 22.7 / 34.4; 64 contexts of 100 to 300, 12 heads of 64, 15.1 / 13.0 / - / - / - / 10.1
 Cut cached_attention_cut(int batch, int heads, int kv_heads, int max_new, int max_len)
 {
     const int most = max_new * (heads / kv_heads), qt = row_tiles(most);
     const long items = (long)batch * kv_heads * ((most + 16 * qt - 1) / (16 * qt)), tiles = (max_len + (long)TILE - 1) / TILE;
-    const long wanted = (1024 + items - 1) / items;
-    long piece = (tiles + wanted - 1) / wanted;
-    if (piece < 8) piece = 8;
-    if (piece < (tiles + MAX_SPLITS - 1) / MAX_SPLITS) piece = (tiles + MAX_SPLITS - 1) / MAX_SPLITS;
-    return Cut{(int)((tiles + piece - 1) / piece), (int)piece};
+    long piece = tiles * items / 512;
+    if (piece > 48) piece = 48;
+    if (piece < 4 * qt) piece = 4 * qt;
+    if (2 * tiles <= 3 * piece) return Cut{1, (int)tiles};
+    long splits = (tiles + piece - 1) / piece;
+    if (splits > MAX_SPLITS) splits = MAX_SPLITS;
+    return Cut{(int)splits, (int)((tiles + splits - 1) / splits)};
 }
 
 hipError_t launch_cached_attention(const void *q, long ldq, bool bf16, int heads, int D, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree,

@@ -30,7 +30,12 @@ template <bool BF> __device__ __forceinline__ v16f mma32(const v4i &a, const v4i
 template <int D> __device__ __forceinline__ int swz_k(int row) { return D == 128 ? row & 15 : swz<128>(row); }
 template <int D> __device__ __forceinline__ int swz_v(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
 
-typedef __attribute__((address_space(3))) v4s *LdsHalves;
+template <int OFFSET> __device__ __forceinline__ v2i lds_read_tr64(unsigned addr)
+{
+    v2i v;
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFFSET));
+    return v;
+}
 
 // Of two halves: bits 15 and 31 where one is an infinity or NaN (the exponent's carry); the pair with zeros in their place
 template <bool BF> __device__ __forceinline__ unsigned odd_halves(int two)
@@ -56,16 +61,20 @@ template <int D, int NW> struct CausalTile {
 template <bool BF, int D, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict__ K, const char *__restrict__ V, long ldq, long ldk, long ldv,
-                             const int *__restrict__ cu, int rows, int max_len, int heads, int group, int pairs, int strips, float scale, char *__restrict__ out)
+                             const int *__restrict__ cu, int rows, int max_len, int heads, int group, int batch, int strips, float scale, char *__restrict__ out)
 {
     typedef CausalTile<D, NW> T;
     constexpr int QB = 32 * NW, KS = D / 16, DB = D / 32;
     __shared__ __attribute__((aligned(1024))) char lds[T::LDS];
 
-    // strips of queries from the last (longest) to the first; the (sequence, key head) pair runs fastest, so that where pairs are a multiple of eight an
-    // XCD's L2 holds the keys of its own pairs
-    const int pair = blockIdx.x % pairs, rest = blockIdx.x / pairs, strip = strips - 1 - rest / group;
-    const int kv_heads = heads / group, b = pair / kv_heads, kvh = pair - b * kv_heads, head = kvh * group + rest % group;
+    // Strips of queries from the last (longest) to the first; a strip's heads, which have the same work, follow each other, so that the XCDs and their shader engines, to
+    // which blocks go in turn, have the same share (sequences following each other, eight of 300 to 2048 tokens: 230 us, the engine that gets the long one's
+    // blocks holds the others up).  Key heads run fastest: where they are a multiple of eight an XCD's L2 holds the keys of its own.
+    const int kv_heads = heads / group, kvh = blockIdx.x % kv_heads;
+    int rest = blockIdx.x / kv_heads;
+    const int head = kvh * group + rest % group;
+    rest /= group;
+    const int b = rest % batch, strip = strips - 1 - rest / batch;
     const int t0 = cu ? cu[b] : b * max_len;
     int n = (cu ? cu[b + 1] : t0 + max_len) - t0;
     if (t0 < 0 || n < 0 || t0 > rows - n) return;                          // rows that the tensors do not have
@@ -102,103 +111,134 @@ void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict_
 #pragma unroll
         for (int j = 0; j < T::LOADS; j++) buffer_to_lds128(vr, offv[j], 0, to + T::TILE + j * 1024);
     };
-    // a lane's V^T reads: key 4 g + (lane >> 2 & 3) of a group of eight, channels 16 (lane >> 4 & 1) + 4 (lane & 3) of 32
+    // A lane's operand reads, as LDS addresses in a stage: K row r (+ 32), chunk 2 i + g at address ^ (i << 5); V key vkey of a group of eight, channels 16 (lane >> 4 & 1)
+    // + 4 (lane & 3) of 32 at address ^ (i << 6) for the i-th 32.  (The reads are asm with waits of their own, as in the GEMMs: the compiler would wait for the direct
+    // loads of the next tile in front of every read of this one, which costs a memory latency per tile: two documents of 8192 tokens 1150 us.)
     const int vkey = 4 * g + ((lane >> 2) & 3), vchunk = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+    const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const unsigned kat = lds_base + r * T::ROW + ((g ^ swz_k<D>(r)) << 4);
+    const unsigned vat = lds_base + T::TILE + vkey * T::ROW + ((vchunk ^ swz_v<D>(vkey)) << 4) + 8 * (lane & 1);
 
     const float factor = scale * 1.44269504088896341f;
     const int tiles = (min(n, q0 + QB) + KEYS - 1) / KEYS;
     v16f o[DB];
     float m, l;
-    auto sweep = [&](bool careful) {
+    auto sweep = [&](auto careful_tag) {
+        constexpr bool CAREFUL = decltype(careful_tag)::value;
 #pragma unroll
-    for (int i = 0; i < DB; i++)
+        for (int i = 0; i < DB; i++)
 #pragma unroll
-        for (int e = 0; e < 16; e++) o[i][e] = 0.0f;
-    m = LOWEST;
-    l = 0.0f;
-    request(0, 0);
-    for (int t = 0; t < tiles; t++) {
-        wait_vm_and_barrier<0>();                                         // tile t is there, and tile t - 1 has been read by all
-        if (t + 1 < tiles) request(t + 1, (t + 1) & 1);
-        const int j0 = t * KEYS;
-        if (j0 > qw + 31) continue;                                       // (wave-uniform) keys behind all of the wave's queries
-        const char *kt = lds + (t & 1) * T::STAGE, *vt = kt + T::TILE;
-        float sc[2][16], top = -INFINITY;
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            v16f acc;
-#pragma unroll
-            for (int e = 0; e < 16; e++) acc[e] = 0.0f;
-            const int row = 32 * h + r;
-#pragma unroll
-            for (int i = 0; i < KS; i++)
-                acc = mma32<BF>(*reinterpret_cast<const v4i *>(kt + row * T::ROW + (((2 * i + g) ^ swz_k<D>(row)) << 4)), qf[i], acc);
-#pragma unroll
-            for (int e = 0; e < 16; e++) sc[h][e] = acc[e] * factor;
-        }
-        const bool edge = j0 + KEYS - 1 > qw;                             // the diagonal crosses the tile (the sequence's end lies behind it)
-        if (edge) {
+            for (int e = 0; e < 16; e++) o[i][e] = 0.0f;
+        m = LOWEST;
+        l = 0.0f;
+        request(0, 0);
+        for (int t = 0; t < tiles; t++) {
+            wait_vm_and_barrier<0>();                                     // tile t is there, and tile t - 1 has been read by all
+            if (t + 1 < tiles) request(t + 1, (t + 1) & 1);
+            const int j0 = t * KEYS;
+            if (j0 > qw + 31) continue;                                   // (wave-uniform) keys behind all of the wave's queries
+            const unsigned stage = (t & 1) * T::STAGE, ka = kat + stage, va = vat + stage;
+            // scores: four fragments of K on their way while four are multiplied
+            constexpr int HALF = KS / 2;                                  // fragments of a step; steps (h, first or second half of the channels)
+            v16f sc[2];
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int e = 0; e < 16; e++)
-                    if (j0 + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3) > qw + r) sc[h][e] = -INFINITY;
-        }
+                for (int e = 0; e < 16; e++) sc[h][e] = 0.0f;
+            v4i kf[2][HALF];
+            auto fetch_k = [&](auto step_tag) {
+                constexpr int S = decltype(step_tag)::value;
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+                for (int i = 0; i < HALF; i++) kf[S & 1][i] = lds_read128<(S >> 1) * 32 * T::ROW>(ka ^ (((S & 1) * HALF + i) << 5));
+            };
+            v2i vf[2][DB][2];
+            auto fetch_v = [&](auto u_tag) {                              // keys 16 u + 4 g + (0..3, 8..11)
+                constexpr int U = decltype(u_tag)::value;
 #pragma unroll
-            for (int e = 0; e < 16; e++) top = __builtin_fmaxf(top, sc[h][e]);
-        if (__any(top > m + SLACK)) {
-            top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-            const float to = top > m + SLACK ? top : m, down = __builtin_amdgcn_exp2f(m - to);   // (a query's result does not depend on the wave's others)
-            m = to;
-            l *= down;
+                for (int i = 0; i < DB; i++) {
+                    vf[U & 1][i][0] = lds_read_tr64<U * 16 * T::ROW>(va ^ (i << 6));
+                    vf[U & 1][i][1] = lds_read_tr64<U * 16 * T::ROW + 8 * T::ROW>(va ^ (i << 6));
+                }
+            };
+            constexpr std::integral_constant<int, 0> c0;
+            fetch_k(c0);
+            each_index([&](auto step_tag) {
+                constexpr int S = decltype(step_tag)::value, HB = S >> 1;
+                if constexpr (S < 3) fetch_k(std::integral_constant<int, S + 1>());
+                else fetch_v(c0);
+                wait_lds_reads<S < 3 ? HALF : 2 * DB>();
+                tie(kf[S & 1], std::make_integer_sequence<int, HALF>());
 #pragma unroll
-            for (int i = 0; i < DB; i++)
+                for (int i = 0; i < HALF; i++) sc[HB] = mma32<BF>(kf[S & 1][i], qf[(S & 1) * HALF + i], sc[HB]);
+            }, std::make_integer_sequence<int, 4>());
+            const bool edge = j0 + KEYS - 1 > qw;                         // the diagonal crosses the tile (the sequence's end lies behind it)
+            if (edge) {
 #pragma unroll
-                for (int e = 0; e < 16; e++) o[i][e] *= down;
-        }
-        v4i pf[4];
+                for (int h = 0; h < 2; h++)
 #pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-                const float p0 = __builtin_amdgcn_exp2f(sc[h][e] - m), p1 = __builtin_amdgcn_exp2f(sc[h][e + 1] - m);
-                l += p0 + p1;
-                pf[2 * h + (e >> 3)][(e & 7) >> 1] = narrow2<BF>(p0, p1);
+                    for (int e = 0; e < 16; e++)
+                        if (j0 + 32 * h + 8 * (e >> 2) + 4 * g + (e & 3) > qw + r) sc[h][e] = -INFINITY;
             }
+            float top = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < 4; u++)                                       // keys 16 u + 4 g + (0..3, 8..11)
+            for (int h = 0; h < 2; h++)
 #pragma unroll
-            for (int i = 0; i < DB; i++) {
-                const int key = 16 * u + vkey;
-                const char *p = vt + key * T::ROW + (((4 * i + vchunk) ^ swz_v<D>(key)) << 4) + 8 * (lane & 1);
-                const v2i lo = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalves)p));
-                const v2i hi = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalves)(p + 8 * T::ROW)));
-                v4i vf = {lo[0], lo[1], hi[0], hi[1]};
-                if (careful && edge) vf = without_odd<BF>(vf);
-                o[i] = mma32<BF>(vf, pf[u], o[i]);
-            }
-        if (careful && edge)
-            for (int key = 0; key < KEYS && j0 + key < n; key++) {
-                const char *row = vt + key * T::ROW;
-                if (!__any(odd_halves<BF>(*reinterpret_cast<const int *>(row + 4 * (lane % (D / 2)))))) continue;
-                const bool sees = j0 + key <= qw + r;
+                for (int e = 0; e < 16; e++) top = __builtin_fmaxf(top, sc[h][e]);
+            top *= factor;
+            if (__any(top > m + SLACK)) {
+                top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
+                const float to = top > m + SLACK ? top : m, down = __builtin_amdgcn_exp2f(m - to);   // (a query's result does not depend on the wave's others)
+                m = to;
+                l *= down;
 #pragma unroll
                 for (int i = 0; i < DB; i++)
 #pragma unroll
-                    for (int e = 0; e < 16; e += 4) {                     // channels 32 i + 2 e + 4 g + (0..3)
-                        const v2i four = *reinterpret_cast<const v2i *>(row + (((4 * i + (e >> 2)) ^ swz_v<D>(key)) << 4) + 8 * g);
-#pragma unroll
-                        for (int c = 0; c < 4; c++) {
-                            const unsigned half = (unsigned)four[c >> 1] >> (16 * (c & 1)) & 0xffffu;
-                            if (sees && odd_halves<BF>((int)half)) o[i][e + c] += BF ? __uint_as_float(half << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)half);
-                        }
-                    }
+                    for (int e = 0; e < 16; e++) o[i][e] *= down;
             }
-    }
+            v4i pf[4];
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h][e], factor, -m)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h][e + 1], factor, -m));
+                    l += p0 + p1;
+                    pf[2 * h + (e >> 3)][(e & 7) >> 1] = narrow2<BF>(p0, p1);
+                }
+            each_index([&](auto u_tag) {
+                constexpr int U = decltype(u_tag)::value;
+                if constexpr (U < 3) fetch_v(std::integral_constant<int, U + 1>());
+                wait_lds_reads<U < 3 ? 2 * DB : 0>();
+#pragma unroll
+                for (int i = 0; i < DB; i++) {
+                    asm volatile("" : "+v"(vf[U & 1][i][0]), "+v"(vf[U & 1][i][1]));          // (read from here on)
+                    v4i v = {vf[U & 1][i][0][0], vf[U & 1][i][0][1], vf[U & 1][i][1][0], vf[U & 1][i][1][1]};
+                    if (CAREFUL && edge) v = without_odd<BF>(v);
+                    o[i] = mma32<BF>(v, pf[U], o[i]);
+                }
+            }, std::make_integer_sequence<int, 4>());
+            if (CAREFUL && edge) {
+                const char *vt = lds + stage + T::TILE;
+                for (int key = 0; key < KEYS && j0 + key < n; key++) {
+                    const char *row = vt + key * T::ROW;
+                    if (!__any(odd_halves<BF>(*reinterpret_cast<const int *>(row + 4 * (lane % (D / 2)))))) continue;
+                    const bool sees = j0 + key <= qw + r;
+#pragma unroll
+                    for (int i = 0; i < DB; i++)
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) {                 // channels 32 i + 2 e + 4 g + (0..3)
+                            const v2i four = *reinterpret_cast<const v2i *>(row + (((4 * i + (e >> 2)) ^ swz_v<D>(key)) << 4) + 8 * g);
+#pragma unroll
+                            for (int c = 0; c < 4; c++) {
+                                const unsigned half = (unsigned)four[c >> 1] >> (16 * (c & 1)) & 0xffffu;
+                                if (sees && odd_halves<BF>((int)half))
+                                    o[i][e + c] += BF ? __uint_as_float(half << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)half);
+                            }
+                        }
+                }
+            }
+        }
     };
-    sweep(false);
+    sweep(std::false_type());
     {
         float all = 0.0f;
 #pragma unroll
@@ -206,7 +246,7 @@ void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict_
 #pragma unroll
             for (int e = 0; e < 16; e++) all = __builtin_fmaf(o[i][e], 0.0f, all);
         if (__syncthreads_or(!(all == 0.0f))) {                           // (the same for all waves; behind it the tiles have been read)
-            sweep(true);
+            sweep(std::true_type());
             __syncthreads();
         }
     }
@@ -235,9 +275,9 @@ hipError_t causal_attention(const void *q, long ldq, const void *k, long ldk, co
                             int max_len, int rows, float scale, void *out, hipStream_t st)
 {
     constexpr int NW = 4;
-    const int strips = (max_len + 32 * NW - 1) / (32 * NW), pairs = batch * kv_heads;
+    const int strips = (max_len + 32 * NW - 1) / (32 * NW);
     hipLaunchKernelGGL((causal_attention_kernel<BF, D, NW>), dim3((unsigned)strips * heads * batch), dim3(64 * NW), 0, st, (const char *)q, (const char *)k,
-                       (const char *)v, ldq, ldk, ldv, cu, rows, max_len, heads, heads / kv_heads, pairs, strips, scale, (char *)out);
+                       (const char *)v, ldq, ldk, ldv, cu, rows, max_len, heads, heads / kv_heads, batch, strips, scale, (char *)out);
     return hipGetLastError();
 }
 

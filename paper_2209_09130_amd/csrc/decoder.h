@@ -3,6 +3,8 @@
 #pragma once
 #include "samp_common.h"
 
+#include <type_traits>
+
 namespace samp {
 
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -22,14 +24,13 @@ template <bool BF> __device__ __forceinline__ void widen8(const v4i &raw, float 
         }
     }
 }
-template <bool BF> __device__ __forceinline__ unsigned short narrow(float v)
+template <bool BF> __device__ __forceinline__ int narrow2(float lo, float hi)
 {
-    if constexpr (BF) {
-        asm("" : "+v"(v));
-        return __builtin_bit_cast(unsigned short, (__bf16)v);
-    } else return __builtin_bit_cast(unsigned short, to_half(v));
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef typename std::conditional<BF, __bf16, _Float16>::type half2 __attribute__((ext_vector_type(2)));
+    asm("" : "+v"(lo), "+v"(hi));
+    return __builtin_bit_cast(int, __builtin_convertvector((v2f{lo, hi}), half2));          // one instruction
 }
-template <bool BF> __device__ __forceinline__ int narrow2(float lo, float hi) { return (int)(narrow<BF>(lo) | (unsigned)narrow<BF>(hi) << 16); }
 
 // The larger of two magnitudes of 16-bit values, by their bits: infinities come above every number and NaN above them
 __device__ __forceinline__ unsigned bits_max16(const v4i &raw)
