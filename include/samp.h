@@ -436,6 +436,7 @@ SAMP_API int samp_pack_rows(const uint16_t *hidden, const int32_t *mask, int32_t
 enum { SAMP_TYPE_F16 = 0, SAMP_TYPE_BF16 = 1 };
 #define SAMP_MAX_ROW (1 << 22)
 #define SAMP_MAX_HEADS 1024
+#define SAMP_MAX_CACHE_ROWS (1 << 20)      /* rows of one sequence in a call on a cache */
 
 /* codes dev int8 [M,K] and steps dev float [M] of x [M,K]; K % 8 == 0.                              */
 SAMP_API int samp_quantize_tokens(const uint16_t *x, int64_t ldx, int32_t type, int32_t M, int32_t K, int8_t *codes, float *steps, void *stream);

@@ -63,6 +63,7 @@ int check_kv_rows(const KvRows &r, const char *most)
     if (r.batch < 1 || r.batch > SAMP_MAX_BATCH) return fail(SAMP_ERR_SHAPE, "1 to %d sequences are supported (%d)", SAMP_MAX_BATCH, r.batch);
     if (r.width < 1 || r.max_rows < 1 || r.rows < 1 || r.rows > SAMP_MAX_TOKENS)
         return fail(SAMP_ERR_SHAPE, "a table width, %s and rows of at least 1 are needed, rows up to %d", most, SAMP_MAX_TOKENS);
+    if (r.max_rows > SAMP_MAX_CACHE_ROWS) return fail(SAMP_ERR_SHAPE, "%s is %d, %d at most are supported", most, r.max_rows, SAMP_MAX_CACHE_ROWS);
     if (r.max_rows > r.rows) return fail(SAMP_ERR_SHAPE, "%s is %d, but there are %d rows", most, r.max_rows, r.rows);
     if (!r.cu && (long long)r.batch * r.max_rows != r.rows)
         return fail(SAMP_ERR_SHAPE, "without offsets every sequence has %s rows: %d x %d are not %d", most, r.batch, r.max_rows, r.rows);

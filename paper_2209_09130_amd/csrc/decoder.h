@@ -32,18 +32,36 @@ template <bool BF> __device__ __forceinline__ int narrow2(float lo, float hi)
     return __builtin_bit_cast(int, __builtin_convertvector((v2f{lo, hi}), half2));          // one instruction
 }
 
-// The larger of two magnitudes of 16-bit values, by their bits: infinities come above every number and NaN above them
+// The largest magnitude of 16-bit values, by their bits (two running maxima, in the halves of a dword): infinities come above every number and NaN above them
+typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned max_halves(unsigned a, unsigned b)
+{ return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(v2u16, a), __builtin_bit_cast(v2u16, b))); }
 __device__ __forceinline__ unsigned bits_max16(const v4i &raw)
 {
-    unsigned m = 0;
-#pragma unroll
-    for (int i = 0; i < 4; i++) m = max(m, max((unsigned)raw[i] & 0x7fffu, ((unsigned)raw[i] >> 16) & 0x7fffu));
-    return m;
+    const unsigned M = 0x7fff7fffu;
+    return max_halves(max_halves((unsigned)raw[0] & M, (unsigned)raw[1] & M), max_halves((unsigned)raw[2] & M, (unsigned)raw[3] & M));
+}
+// over sixteen lanes (row rotations) or all 64 of the wave; then of the two halves
+__device__ __forceinline__ unsigned max_of_16_lanes(unsigned top)
+{
+    top = max_halves(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x128, 0xf, 0xf, true));
+    top = max_halves(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x124, 0xf, 0xf, true));
+    top = max_halves(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x122, 0xf, 0xf, true));
+    top = max_halves(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x121, 0xf, 0xf, true));
+    return max(top & 0xffffu, top >> 16);
+}
+__device__ __forceinline__ unsigned max_of_wave(unsigned top)
+{
+    top = max_of_16_lanes(top);
+    top = max(top, (unsigned)__shfl_xor((int)top, 16, 64));
+    return max(top, (unsigned)__shfl_xor((int)top, 32, 64));
 }
 
 // The quantiser of a row that brings its own step: step = absmax / 127 and code = 127 x / absmax rounded half to even, decided exactly.  127 x / absmax is
-// a quotient of short integers: where it is no tie it is further than 2^-12 from one, so a product with error 2^-40 that is rounded to binary32
-// lies on the right side, and a tie is a binary32 number, to which it rounds.  The reciprocal therefore comes in two parts.
+// a quotient of short integers: where it is no tie it is further than 2^-12 from one, so a product with error 2^-28 that is rounded to binary32
+// lies on the right side, and a tie is a binary32 number, to which it rounds.  The reciprocal therefore comes in two parts, an approximate one and what it
+// leaves; so does 1 / 127 (quotients by 127 have bits of period seven: none is near a rounding boundary).  True divisions in their place made the cache's
+// writing 30 % longer: every lane of a row forms them.
 // A row without a number of at least 2^-60 is a row of zeros (step 1, as for a weight row of zeros); a row with an infinity or NaN has codes 0 and a step of
 // NaN, so that what is computed from it is NaN as well.
 struct RowQuant { float step, hi, lo; bool finite; };
@@ -53,12 +71,13 @@ template <bool BF> __device__ __forceinline__ RowQuant row_quant(unsigned absmax
     RowQuant q;
     q.finite = absmax_bits < (BF ? 0x7f80u : 0x7c00u);
     const bool some = q.finite && top >= 0x1p-60f;
-    const float t = some ? top : 1.0f;
-    q.hi = __fdiv_rn(127.0f, t);
-    q.lo = __fdiv_rn(__builtin_fmaf(-q.hi, t, 127.0f), t);
-    q.hi = some ? q.hi : 0.0f;
-    q.lo = some ? q.lo : 0.0f;
-    q.step = !q.finite ? __builtin_nanf("") : some ? __fdiv_rn(top, 127.0f) : 1.0f;
+    const float t = some ? top : 1.0f, m = __builtin_amdgcn_frexp_mantf(t), inverse = __builtin_amdgcn_rcpf(m), hi = 127.0f * inverse;
+    const int down = -__builtin_amdgcn_frexp_expf(t);
+    q.hi = some ? __builtin_amdgcn_ldexpf(hi, down) : 0.0f;
+    q.lo = some ? __builtin_amdgcn_ldexpf(__builtin_fmaf(-hi, m, 127.0f) * inverse, down) : 0.0f;
+    constexpr double C = 1.0 / 127.0;
+    constexpr float CH = (float)C, CL = (float)(C - (double)CH);
+    q.step = !q.finite ? __builtin_nanf("") : some ? __builtin_fmaf(top, CH, top * CL) : 1.0f;
     return q;
 }
 // eight codes; |127 x / absmax| <= 127, so adding 1.5 * 2^23 leaves the code in the low byte without a clamp

@@ -165,9 +165,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_tokens_few_kernel(const c
             }
             unsigned top = 0;
 #pragma unroll
-            for (int i = 0; i < KB; i++) top = max(top, bits_max16(x[i]));
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o, 64));
+            for (int i = 0; i < KB; i++) top = max_halves(top, bits_max16(x[i]));
+            top = max_of_wave(top);
             if (sharers > 1) {
                 if (lane == 0) tops[w] = top;
                 __syncthreads();

@@ -25,9 +25,8 @@ __global__ __launch_bounds__(256) void quantize_tokens_kernel(const char *__rest
         raw[c] = at < chunks ? *reinterpret_cast<const v4i *>(from + 16 * (size_t)at) : v4i{0, 0, 0, 0};
     }
 #pragma unroll
-    for (int c = 0; c < C; c++) top = max(top, bits_max16(raw[c]));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o, 64));
+    for (int c = 0; c < C; c++) top = max_halves(top, bits_max16(raw[c]));
+    top = max_of_wave(top);
     if constexpr (WPR > 1) {
         if (lane == 0) tops[w] = top;
         __syncthreads();
@@ -55,9 +54,8 @@ __global__ __launch_bounds__(256) void quantize_tokens_long_kernel(const char *_
     const int tid = threadIdx.x, row = blockIdx.x, chunks = K >> 3;
     const char *from = x + 2 * (size_t)row * ldx;
     unsigned top = 0;
-    for (int at = tid; at < chunks; at += 256) top = max(top, bits_max16(*reinterpret_cast<const v4i *>(from + 16 * (size_t)at)));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o, 64));
+    for (int at = tid; at < chunks; at += 256) top = max_halves(top, bits_max16(*reinterpret_cast<const v4i *>(from + 16 * (size_t)at)));
+    top = max_of_wave(top);
     if ((tid & 63) == 0) tops[tid >> 6] = top;
     __syncthreads();
     const RowQuant q = row_quant<BF>(max(max(tops[0], tops[1]), max(tops[2], tops[3])));
@@ -85,14 +83,15 @@ hipError_t quantize_tokens(const void *x, long ldx, int M, int K, int8_t *codes,
 
 // ---- cache -----------------------------------------------------------------------------------------
 // Sixteen lanes a row of head_dim values; a block's sixteen rows are 2^TOKENS_LOG2 tokens of 16 >> TOKENS_LOG2 of the 2 kv_heads keys and values, so
-// that a page's neighbouring rows and steps are written together and a block of a decode step (one token) is not left idle.
+// that a page's neighbouring rows and steps are written together and a block of a decode step (one token) is not left idle.  PASSES: so many times that many
+// tokens, all requested before the first is worked on.  Heads run fastest over the blocks, so that those at work at a time read whole rows of the tensors.
 struct RowAt { int token, head; bool is_v; };
-__device__ __forceinline__ RowAt row_at(int tokens_log2, int kv_heads)
+template <int PASSES> __device__ __forceinline__ RowAt row_at(int tokens_log2, int kv_heads)
 {
     const int group = threadIdx.x >> 4;
     RowAt a;
-    a.token = (blockIdx.x << tokens_log2) + (group & ((1 << tokens_log2) - 1));
-    const int part = blockIdx.y * (16 >> tokens_log2) + (group >> tokens_log2);
+    a.token = ((int)blockIdx.y * PASSES << tokens_log2) + (group & ((1 << tokens_log2) - 1));
+    const int part = blockIdx.x * (16 >> tokens_log2) + (group >> tokens_log2);
     a.is_v = part >= kv_heads;
     a.head = a.is_v ? part - kv_heads : part;
     return a;
@@ -105,64 +104,86 @@ __device__ __forceinline__ int page_of(const KvRows &r, const KvCache &c, int b,
     return (unsigned)p < (unsigned)c.pages ? p : -1;
 }
 
-template <bool BF, int D>
+template <bool BF, int D, int PASSES>
 __global__ __launch_bounds__(256) void cache_write_kernel(KvCache c, const char *__restrict__ k, long ldk, const char *__restrict__ v, long ldv, KvRows r,
                                                           int tokens_log2)
 {
     constexpr int PER = D / 16;                                       // values of a lane
     const SeqRows s = seq_rows(r, blockIdx.z, c.page_shift);
-    const RowAt a = row_at(tokens_log2, c.kv_heads);
+    const RowAt a = row_at<PASSES>(tokens_log2, c.kv_heads);
     if (a.token >= s.todo || a.head >= c.kv_heads) return;
-    const int pos = r.lens[blockIdx.z] - s.n + a.token, page = page_of(r, c, blockIdx.z, pos), lane = threadIdx.x & 15;
-    if (page < 0) return;
-    const char *from = (a.is_v ? v : k) + 2 * ((size_t)(s.first_row + a.token) * (a.is_v ? ldv : ldk) + a.head * D + lane * PER);
-    v4i raw = {0, 0, 0, 0};
-    if constexpr (PER == 8) raw = *reinterpret_cast<const v4i *>(from);
-    else {
-        const v2i half = *reinterpret_cast<const v2i *>(from);
-        raw[0] = half[0];
-        raw[1] = half[1];
-    }
-    unsigned top = bits_max16(raw);
+    const int lane = threadIdx.x & 15;
+    const char *from = (a.is_v ? v : k) + 2 * ((size_t)s.first_row * (a.is_v ? ldv : ldk) + a.head * D + lane * PER);
+    const size_t ld = 2 * (size_t)(a.is_v ? ldv : ldk);
+    v4i raw[PASSES];
+    int pos[PASSES], page[PASSES];
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o, 16));
-    const RowQuant q = row_quant<BF>(top);
-    float x[8];
-    widen8<BF>(raw, x);
-    const v2i code = quant8(x, q);
-    const size_t row = (((size_t)page * c.kv_heads + a.head) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
-    int8_t *to = (a.is_v ? c.v : c.k) + row * D + lane * PER;
-    if constexpr (PER == 8) *reinterpret_cast<v2i *>(to) = code;
-    else *reinterpret_cast<int *>(to) = code[0];
-    if (lane == 0) (a.is_v ? c.v_step : c.k_step)[row] = q.step;
+    for (int i = 0; i < PASSES; i++) {
+        const int token = a.token + (i << tokens_log2);
+        raw[i] = v4i{0, 0, 0, 0};
+        page[i] = -1;
+        if (token >= s.todo) continue;
+        pos[i] = r.lens[blockIdx.z] - s.n + token;
+        page[i] = page_of(r, c, blockIdx.z, pos[i]);
+        if constexpr (PER == 8) raw[i] = *reinterpret_cast<const v4i *>(from + token * ld);
+        else {
+            const v2i half = *reinterpret_cast<const v2i *>(from + token * ld);
+            raw[i][0] = half[0];
+            raw[i][1] = half[1];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PASSES; i++) {
+        const unsigned top = max_of_16_lanes(bits_max16(raw[i]));
+        if (page[i] < 0) continue;
+        const RowQuant q = row_quant<BF>(top);
+        float x[8];
+        widen8<BF>(raw[i], x);
+        const v2i code = quant8(x, q);
+        const size_t row = (((size_t)page[i] * c.kv_heads + a.head) << c.page_shift) + (pos[i] & ((1 << c.page_shift) - 1));
+        int8_t *to = (a.is_v ? c.v : c.k) + row * D + lane * PER;
+        if constexpr (PER == 8) *reinterpret_cast<v2i *>(to) = code;
+        else *reinterpret_cast<int *>(to) = code[0];
+        if (lane == 0) (a.is_v ? c.v_step : c.k_step)[row] = q.step;
+    }
 }
 
-template <bool BF, int D>
+template <bool BF, int D, int PASSES>
 __global__ __launch_bounds__(256) void cache_read_kernel(KvCache c, char *__restrict__ k, char *__restrict__ v, KvRows r, int tokens_log2)
 {
     constexpr int PER = D / 16;
     const SeqRows s = seq_rows(r, blockIdx.z, c.page_shift);
-    const RowAt a = row_at(tokens_log2, c.kv_heads);
+    const RowAt a = row_at<PASSES>(tokens_log2, c.kv_heads);
     if (a.token >= s.todo || a.head >= c.kv_heads) return;
-    const int pos = r.lens[blockIdx.z] - s.n + a.token, page = page_of(r, c, blockIdx.z, pos), lane = threadIdx.x & 15;
-    v2i code = {0, 0};
-    float step = 0.0f;
-    if (page >= 0) {
+    const int lane = threadIdx.x & 15;
+    v2i code[PASSES];
+    float step[PASSES];
+#pragma unroll
+    for (int i = 0; i < PASSES; i++) {
+        const int token = a.token + (i << tokens_log2), pos = r.lens[blockIdx.z] - s.n + token, page = token < s.todo ? page_of(r, c, blockIdx.z, pos) : -1;
+        code[i] = v2i{0, 0};
+        step[i] = 0.0f;
+        if (page < 0) continue;
         const size_t row = (((size_t)page * c.kv_heads + a.head) << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
         const int8_t *from = (a.is_v ? c.v : c.k) + row * D + lane * PER;
-        if constexpr (PER == 8) code = *reinterpret_cast<const v2i *>(from);
-        else code[0] = *reinterpret_cast<const int *>(from);
-        step = (a.is_v ? c.v_step : c.k_step)[row];
+        if constexpr (PER == 8) code[i] = *reinterpret_cast<const v2i *>(from);
+        else code[i][0] = *reinterpret_cast<const int *>(from);
+        step[i] = (a.is_v ? c.v_step : c.k_step)[row];
     }
-    v4i out;
 #pragma unroll
-    for (int i = 0; i < PER / 2; i++) {
-        const int two = code[i >> 1] >> (16 * (i & 1));
-        out[i] = narrow2<BF>((float)(int8_t)two * step, (float)(int8_t)(two >> 8) * step);
+    for (int i = 0; i < PASSES; i++) {
+        const int token = a.token + (i << tokens_log2);
+        if (token >= s.todo) continue;
+        v4i out;
+#pragma unroll
+        for (int e = 0; e < PER / 2; e++) {
+            const int two = code[i][e >> 1] >> (16 * (e & 1));
+            out[e] = narrow2<BF>((float)(int8_t)two * step[i], (float)(int8_t)(two >> 8) * step[i]);
+        }
+        char *to = (a.is_v ? v : k) + 2 * (((size_t)(s.first_row + token) * c.kv_heads + a.head) * D + lane * PER);
+        if constexpr (PER == 8) *reinterpret_cast<v4i *>(to) = out;
+        else *reinterpret_cast<v2i *>(to) = v2i{out[0], out[1]};
     }
-    char *to = (a.is_v ? v : k) + 2 * (((size_t)(s.first_row + a.token) * c.kv_heads + a.head) * D + lane * PER);
-    if constexpr (PER == 8) *reinterpret_cast<v4i *>(to) = out;
-    else *reinterpret_cast<v2i *>(to) = v2i{out[0], out[1]};
 }
 
 int tokens_log2_for(int max_rows)
@@ -171,9 +192,30 @@ int tokens_log2_for(int max_rows)
     while (n < 4 && (1 << n) < max_rows) n++;
     return n;
 }
-dim3 cache_grid(const KvCache &c, const KvRows &r, int log2)
+dim3 cache_grid(const KvCache &c, const KvRows &r, int log2, int passes)
 {
-    return dim3((unsigned)((r.max_rows + (1 << log2) - 1) >> log2), (unsigned)((2 * c.kv_heads + (16 >> log2) - 1) / (16 >> log2)), (unsigned)r.batch);
+    const int tokens = passes << log2;
+    return dim3((unsigned)((2 * c.kv_heads + (16 >> log2) - 1) / (16 >> log2)), (unsigned)((r.max_rows + tokens - 1) / tokens), (unsigned)r.batch);
+}
+// Four rows a lane group where there are blocks enough
+int cache_passes(const KvCache &c, const KvRows &r) { return (long)r.rows * c.kv_heads >= 32768 ? 4 : 1; }
+
+template <bool BF, int D>
+hipError_t cache_write(const KvCache &c, const void *k, long ldk, const void *v, long ldv, const KvRows &r, hipStream_t st)
+{
+    const int n = tokens_log2_for(r.max_rows), passes = cache_passes(c, r);
+    auto kern = passes == 4 ? cache_write_kernel<BF, D, 4> : cache_write_kernel<BF, D, 1>;
+    hipLaunchKernelGGL(kern, cache_grid(c, r, n, passes), dim3(256), 0, st, c, (const char *)k, ldk, (const char *)v, ldv, r, n);
+    return hipGetLastError();
+}
+
+template <bool BF, int D>
+hipError_t cache_read(const KvCache &c, void *k, void *v, const KvRows &r, hipStream_t st)
+{
+    const int n = tokens_log2_for(r.max_rows), passes = cache_passes(c, r);
+    auto kern = passes == 4 ? cache_read_kernel<BF, D, 4> : cache_read_kernel<BF, D, 1>;
+    hipLaunchKernelGGL(kern, cache_grid(c, r, n, passes), dim3(256), 0, st, c, (char *)k, (char *)v, r, n);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -185,20 +227,14 @@ hipError_t launch_quantize_tokens(const void *x, long ldx, bool bf16, int M, int
 
 hipError_t launch_cache_write(const KvCache &c, const void *k, long ldk, const void *v, long ldv, bool bf16, int D, const KvRows &r, hipStream_t st)
 {
-    const int n = tokens_log2_for(r.max_rows);
-    auto kern = D == 128 ? (bf16 ? cache_write_kernel<true, 128> : cache_write_kernel<false, 128>)
-                         : (bf16 ? cache_write_kernel<true, 64> : cache_write_kernel<false, 64>);
-    hipLaunchKernelGGL(kern, cache_grid(c, r, n), dim3(256), 0, st, c, (const char *)k, ldk, (const char *)v, ldv, r, n);
-    return hipGetLastError();
+    if (D == 128) return bf16 ? cache_write<true, 128>(c, k, ldk, v, ldv, r, st) : cache_write<false, 128>(c, k, ldk, v, ldv, r, st);
+    return bf16 ? cache_write<true, 64>(c, k, ldk, v, ldv, r, st) : cache_write<false, 64>(c, k, ldk, v, ldv, r, st);
 }
 
 hipError_t launch_cache_read(const KvCache &c, void *k, void *v, bool bf16, int D, const KvRows &r, hipStream_t st)
 {
-    const int n = tokens_log2_for(r.max_rows);
-    auto kern = D == 128 ? (bf16 ? cache_read_kernel<true, 128> : cache_read_kernel<false, 128>)
-                         : (bf16 ? cache_read_kernel<true, 64> : cache_read_kernel<false, 64>);
-    hipLaunchKernelGGL(kern, cache_grid(c, r, n), dim3(256), 0, st, c, (char *)k, (char *)v, r, n);
-    return hipGetLastError();
+    if (D == 128) return bf16 ? cache_read<true, 128>(c, k, v, r, st) : cache_read<false, 128>(c, k, v, r, st);
+    return bf16 ? cache_read<true, 64>(c, k, v, r, st) : cache_read<false, 64>(c, k, v, r, st);
 }
 
 }  // namespace samp

@@ -33,8 +33,7 @@ def _fn(name: str):
     f = _entry.get(name)
     if f is None:
         f = getattr(lib(), name)
-        f.argtypes = _SIGNATURES[name]
-        f.restype = _Z if name.endswith("_bytes") else C.c_int
+        f.argtypes, f.restype = _SIGNATURES[name], _Z if name.endswith("_bytes") else C.c_int
         _entry[name] = f
     return f
 
@@ -68,9 +67,10 @@ def _heads(what: str, t: torch.Tensor, device: int) -> Tuple[int, int]:
     """Address and row distance of [rows, heads, head_dim] whose heads lie next to each other."""
     if t.get_device() != device:
         _elsewhere(t, device)
-    if t.dim() != 3 or t.dtype not in _TYPES:
-        _refuse(f"{what}: fp16 or bfloat16 [rows, heads, head_dim] is needed, not {t.dtype} {tuple(t.shape)}")
-    rows, heads, dim = t.shape
+    shape = t.shape
+    if len(shape) != 3 or t.dtype not in _TYPES:
+        _refuse(f"{what}: fp16 or bfloat16 [rows, heads, head_dim] is needed, not {t.dtype} {tuple(shape)}")
+    rows, heads, dim = shape
     row, head, one = t.stride()
     if one != 1 or (head != dim and heads > 1):
         _refuse(f"{what}: the heads of a row must lie next to each other (strides {t.stride()})")
@@ -85,13 +85,16 @@ def _rows2(what: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
     return x.data_ptr(), x.stride(0) if M > 1 else K, M, K
 
 
-def _call(device: int, name: str, *args):
-    stream = torch._C._cuda_getCurrentRawStream(device)              # torch.cuda.current_stream(device).cuda_stream, without the objects
-    if torch._C._cuda_getDevice() == device:
-        rc = _fn(name)(*args, stream)
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice   # torch.cuda.current_stream(device).cuda_stream without the objects
+
+
+def _call(device: int, f, *args) -> None:
+    """The entry point on `device`, which its stream, the last of its arguments, belongs to."""
+    if _current_device() == device:
+        rc = f(*args)
     else:
         with torch.cuda.device(device):
-            rc = _fn(name)(*args, stream)
+            rc = f(*args)
     if rc:
         raise SampError(rc, lib().samp_last_error().decode())
 
@@ -102,7 +105,7 @@ def quantize_tokens(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     at, ld, M, K = _rows2("x", x)
     codes, steps = x.new_empty((M, K), dtype=torch.int8), x.new_empty((M,), dtype=torch.float32)
     if M:
-        _call(device, "samp_quantize_tokens", at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr())
+        _call(device, _fn("samp_quantize_tokens"), at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr(), _raw_stream(device))
     return codes, steps
 
 
@@ -119,7 +122,7 @@ def gemm_i8_tokens_packed(codes: torch.Tensor, steps: torch.Tensor, Wp: torch.Te
     args = (_flat("codes", codes, torch.int8, device), _flat("steps", steps, torch.float32, device, M), _flat("Wp", Wp, torch.int8, device, N * K),
             _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N), int(bool(gelu)), out.data_ptr(), _TYPES[dtype], M, N, K)
     if M:
-        _call(device, "samp_gemm_i8_tokens_packed", *args)
+        _call(device, _fn("samp_gemm_i8_tokens_packed"), *args, _raw_stream(device))
     return out
 
 
@@ -133,7 +136,7 @@ def linear_i8_tokens(x: torch.Tensor, Wp: torch.Tensor, s_w: torch.Tensor, bias:
     if M:
         need = _fn("samp_linear_i8_tokens_workspace_bytes")(M, K)
         ws = x.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
-        _call(device, "samp_linear_i8_tokens", at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws, need)
+        _call(device, _fn("samp_linear_i8_tokens"), at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws, need, _raw_stream(device))
     return out
 
 
@@ -180,7 +183,7 @@ def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.T
         _refuse(f"k and v must be [rows, {cache.kv_heads}, {cache.head_dim}] of one type, not {tuple(k.shape)} and {tuple(v.shape)}")
     t, width, pcu, plens, B = _places(device, table, cu, lens)
     if k.shape[0] and B:
-        _call(device, "samp_cache_write", cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, max_new, k.shape[0])
+        _call(device, _fn("samp_cache_write"), cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, max_new, k.shape[0], _raw_stream(device))
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_rows: int, rows: int,
@@ -191,12 +194,13 @@ def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], 
     device = cache.device
     t, width, pcu, plens, B = _places(device, table, cu, lens)
     if out is None:
-        shape = (rows, cache.kv_heads, cache.head_dim)
-        out = cache.k.new_empty(shape, dtype=dtype), cache.k.new_empty(shape, dtype=dtype)
-    size = rows * cache.kv_heads * cache.head_dim
-    k, v = _flat("out", out[0], dtype, device, size), _flat("out", out[1], dtype, device, size)
+        out = cache.k.new_empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
+        k, v = out[0].data_ptr(), out[1].data_ptr()
+    else:
+        size = rows * cache.kv_heads * cache.head_dim
+        k, v = _flat("out", out[0], dtype, device, size), _flat("out", out[1], dtype, device, size)
     if rows and B:
-        _call(device, "samp_cache_read", cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, max_rows, rows)
+        _call(device, _fn("samp_cache_read"), cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, max_rows, rows, _raw_stream(device))
     return out
 
 
@@ -211,16 +215,19 @@ def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Op
     if dim != cache.head_dim:
         _refuse(f"q has heads of {dim}, the cache of {cache.head_dim}")
     t, width, pcu, plens, B = _places(device, table, cu, lens)
+    words = _flat("tree", tree, torch.int64, device, rows)
     if out is None:
         out = q.new_empty((rows, heads, dim))
-    to, words = _flat("out", out, q.dtype, device, rows * heads * dim), _flat("tree", tree, torch.int64, device, rows)
+        to = out.data_ptr()
+    else:
+        to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows and B:
         if max_len is None:
             max_len = width * cache.page_len
         need = _fn("samp_attention_cache_workspace_bytes")(rows, B, heads, cache.kv_heads, dim, max_new, max_len)
         ws = q.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
-        _call(device, "samp_attention_cache", at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
-              1.0 / math.sqrt(dim) if scale is None else scale, words, to, ws, need)
+        _call(device, _fn("samp_attention_cache"), at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
+              1.0 / math.sqrt(dim) if scale is None else scale, words, to, ws, need, _raw_stream(device))
     return out
 
 
@@ -235,13 +242,15 @@ def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Opti
         _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
     if out is None:
         out = q.new_empty((rows, heads, dim))
-    to = _flat("out", out, q.dtype, device, rows * heads * dim)
+        to = out.data_ptr()
+    else:
+        to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows == 0:
         return out
     if cu is None and (max_len < 1 or rows % max_len):
         _refuse("without sequence offsets every sequence has max_len rows")
     B = rows // max_len if cu is None else cu.numel() - 1
     if B:
-        _call(device, "samp_attention_causal", pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, device, B + 1), B, max_len,
-              rows, 1.0 / math.sqrt(dim) if scale is None else scale, to)
+        _call(device, _fn("samp_attention_causal"), pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, device, B + 1), B, max_len,
+              rows, 1.0 / math.sqrt(dim) if scale is None else scale, to, _raw_stream(device))
     return out
