@@ -429,8 +429,8 @@ SAMP_API int samp_pack_rows(const uint16_t *hidden, const int32_t *mask, int32_t
  * 0 and a step of NaN, so that what is computed from it is NaN.
  *
  * Packed rows: sequence b has rows cu[b] .. cu[b+1] - 1 of the tensors (dev int32 [batch + 1]), any number of them, none included; cu
- * NULL: max_new (max_rows, max_len) rows each.  The host's maximum must be no less than the longest; of a longer sequence only that many
- * rows are computed.  Rows behind the last sequence are left as they were, as are those that an offset puts outside the tensors.  Device memory is not
+ * NULL: max_new (max_rows, max_len) rows each.  The host's maximum should be no less than the longest, and may be more; of a longer sequence only that many
+ * rows are computed.  Results must not overlap inputs.  Rows behind the last sequence are left as they were, as are those that an offset puts outside the tensors.  Device memory is not
  * checked by the host.
  * `ld...` is the distance of consecutive rows in values (a multiple of 8); inside a row the heads follow each other without a gap.     */
 enum { SAMP_TYPE_F16 = 0, SAMP_TYPE_BF16 = 1 };
@@ -456,8 +456,8 @@ SAMP_API int samp_linear_i8_tokens(const uint16_t *x, int64_t ldx, int32_t type,
 /* A paged cache: codes dev int8 [pages, kv_heads, page_len, head_dim] and steps dev float [pages, kv_heads, page_len] of keys and of values;
  * page_len a power of two from 16 to 1024, head_dim 64 or 128.  A sequence's page table is a row of `width` page numbers: position p lies
  * in page table[b * width + p / page_len], at p % page_len.  A number that is none of the cache's pages (-1 for instance) is never followed: what would be written there is dropped, what would
- * be read there is zeros, and attention does not see those positions.  Pages may be shared by sequences that read them; one that a call writes must belong to one
- * sequence of the call, otherwise what it holds afterwards is undefined.                              */
+ * be read there is zeros, and attention does not see those positions.  Pages may be shared by sequences that read them; a position that a call writes must be
+ * written once, or what it holds afterwards is undefined.                              */
 typedef struct {
     int8_t *k, *v;
     float *k_step, *v_step;

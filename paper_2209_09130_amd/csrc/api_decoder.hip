@@ -57,16 +57,17 @@ int check_cache(const samp_kv_cache_t *c, KvCache *to)
     return SAMP_OK;
 }
 
-int check_kv_rows(const KvRows &r, const char *most)
+// (a maximum above the number of rows, as of a program that passes its largest batch, counts as that number)
+int check_kv_rows(KvRows &r, const char *most)
 {
     if (!r.table || !r.lens) return fail(SAMP_ERR_ARG, "the page table or the lengths are NULL");
     if (r.batch < 1 || r.batch > SAMP_MAX_BATCH) return fail(SAMP_ERR_SHAPE, "1 to %d sequences are supported (%d)", SAMP_MAX_BATCH, r.batch);
     if (r.width < 1 || r.max_rows < 1 || r.rows < 1 || r.rows > SAMP_MAX_TOKENS)
         return fail(SAMP_ERR_SHAPE, "a table width, %s and rows of at least 1 are needed, rows up to %d", most, SAMP_MAX_TOKENS);
-    if (r.max_rows > SAMP_MAX_CACHE_ROWS) return fail(SAMP_ERR_SHAPE, "%s is %d, %d at most are supported", most, r.max_rows, SAMP_MAX_CACHE_ROWS);
-    if (r.max_rows > r.rows) return fail(SAMP_ERR_SHAPE, "%s is %d, but there are %d rows", most, r.max_rows, r.rows);
     if (!r.cu && (long long)r.batch * r.max_rows != r.rows)
         return fail(SAMP_ERR_SHAPE, "without offsets every sequence has %s rows: %d x %d are not %d", most, r.batch, r.max_rows, r.rows);
+    if (r.max_rows > r.rows) r.max_rows = r.rows;
+    if (r.max_rows > SAMP_MAX_CACHE_ROWS) return fail(SAMP_ERR_SHAPE, "%s is %d, %d at most are supported", most, r.max_rows, SAMP_MAX_CACHE_ROWS);
     return SAMP_OK;
 }
 
@@ -135,7 +136,7 @@ int samp_cache_write(const samp_kv_cache_t *cache, const uint16_t *k, int64_t ld
                      int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows, void *stream)
 {
     KvCache c;
-    const KvRows r{table, width, cu, lens, batch, max_new, rows};
+    KvRows r{table, width, cu, lens, batch, max_new, rows};
     if (int rc = check_type(type)) return rc;
     if (int rc = check_cache(cache, &c)) return rc;
     if (int rc = check_kv_rows(r, "max_new")) return rc;
@@ -149,7 +150,7 @@ int samp_cache_read(const samp_kv_cache_t *cache, uint16_t *k, uint16_t *v, int3
                     const int32_t *lens, int32_t batch, int32_t max_rows, int32_t rows, void *stream)
 {
     KvCache c;
-    const KvRows r{table, width, cu, lens, batch, max_rows, rows};
+    KvRows r{table, width, cu, lens, batch, max_rows, rows};
     if (int rc = check_type(type)) return rc;
     if (int rc = check_cache(cache, &c)) return rc;
     if (int rc = check_kv_rows(r, "max_rows")) return rc;
@@ -158,21 +159,23 @@ int samp_cache_read(const samp_kv_cache_t *cache, uint16_t *k, uint16_t *v, int3
     return SAMP_OK;
 }
 
-static int check_cached(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_new, int32_t max_len)
+static int check_cached(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_new, int32_t max_len, Cut *cut)
 {
     if (int rc = check_heads(heads, kv_heads, 1.0f)) return rc;
     if (head_dim != 64 && head_dim != 128) return fail(SAMP_ERR_SHAPE, "head_dim must be 64 or 128 (%d)", head_dim);
-    if (batch < 1 || batch > SAMP_MAX_BATCH || max_new < 1 || max_len < 1 || rows < 1 || rows > SAMP_MAX_TOKENS || max_new > rows)
-        return fail(SAMP_ERR_SHAPE, "1 to %d sequences, 1 to %d rows, max_new of 1 to the rows and max_len >= 1 needed", SAMP_MAX_BATCH, SAMP_MAX_TOKENS);
-    if ((double)batch * heads * max_new > 2147483647.0) return fail(SAMP_ERR_SHAPE, "batch x heads x max_new is past 2^31");
+    if (batch < 1 || batch > SAMP_MAX_BATCH || max_new < 1 || max_len < 1 || rows < 1 || rows > SAMP_MAX_TOKENS)
+        return fail(SAMP_ERR_SHAPE, "1 to %d sequences, 1 to %d rows, max_new >= 1 and max_len >= 1 needed", SAMP_MAX_BATCH, SAMP_MAX_TOKENS);
+    if (max_new > rows) max_new = rows;
+    *cut = cached_attention_cut(batch, heads, kv_heads, max_new, max_len);
+    if ((double)batch * heads * max_new * cut->splits > 2147483647.0) return fail(SAMP_ERR_SHAPE, "batch x heads x max_new, times the pieces of a context, is past 2^31");
     return SAMP_OK;
 }
 
 size_t samp_attention_cache_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t max_new, int32_t max_len)
 {
-    if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len)) return 0;
-    const size_t splits = cached_attention_cut(batch, heads, kv_heads, max_new, max_len).splits;
-    return splits == 1 ? 0 : up((size_t)rows * heads * splits * (head_dim + 2) * sizeof(float));
+    Cut cut;
+    if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len, &cut)) return 0;
+    return cut.splits == 1 ? 0 : up((size_t)rows * heads * cut.splits * (head_dim + 2) * sizeof(float));
 }
 
 int samp_attention_cache(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const int32_t *table, int32_t width,
@@ -180,20 +183,20 @@ int samp_attention_cache(const uint16_t *q, int64_t ldq, int32_t type, int32_t h
                          const uint64_t *tree, uint16_t *out, void *workspace, size_t workspace_bytes, void *stream)
 {
     KvCache c;
-    const KvRows r{table, width, cu, lens, batch, max_new, rows};
+    KvRows r{table, width, cu, lens, batch, max_new, rows};
     if (int rc = check_type(type)) return rc;
     if (int rc = check_cache(cache, &c)) return rc;
     if (int rc = check_kv_rows(r, "max_new")) return rc;
     if (int rc = check_heads(heads, c.kv_heads, scale)) return rc;
-    if (int rc = check_cached(rows, batch, heads, c.kv_heads, cache->head_dim, max_new, max_len)) return rc;
+    Cut cut;
+    if (int rc = check_cached(rows, batch, heads, c.kv_heads, cache->head_dim, max_new, max_len, &cut)) return rc;
     if (int rc = check_rows("q", q, ldq, (int64_t)heads * cache->head_dim)) return rc;
     if (!out || !aligned(out, 16)) return fail(SAMP_ERR_ARG, "out must be 16-byte aligned and not NULL");
-    if (tree && max_new > 64) return fail(SAMP_ERR_SHAPE, "a tree has at most 64 drafted tokens (max_new %d)", max_new);
+    if (tree && r.max_rows > 64) return fail(SAMP_ERR_SHAPE, "a tree has at most 64 drafted tokens (max_new %d)", max_new);
     if (tree && !aligned(tree, 8)) return fail(SAMP_ERR_ARG, "tree must be 8-byte aligned");
     const size_t need = samp_attention_cache_workspace_bytes(rows, batch, heads, c.kv_heads, cache->head_dim, max_new, max_len);
     if (need && (!workspace || !aligned(workspace, ALIGN) || workspace_bytes < need))
         return fail(SAMP_ERR_SPACE, "a 256-byte aligned workspace of %zu bytes is needed", need);
-    const Cut cut = cached_attention_cut(batch, heads, c.kv_heads, max_new, max_len);
     HIP_TRY(launch_cached_attention(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, r, scale, tree, cut, static_cast<float *>(workspace), out,
                                     (hipStream_t)stream));
     return SAMP_OK;
@@ -206,9 +209,10 @@ int samp_attention_causal(const uint16_t *q, int64_t ldq, const uint16_t *k, int
     if (int rc = check_type(type)) return rc;
     if (int rc = check_heads(heads, kv_heads, scale)) return rc;
     if (head_dim != 64 && head_dim != 128) return fail(SAMP_ERR_SHAPE, "head_dim must be 64 or 128 (%d)", head_dim);
-    if (batch < 1 || batch > SAMP_MAX_BATCH || rows < 1 || rows > SAMP_MAX_TOKENS || max_len < 1 || max_len > rows)
-        return fail(SAMP_ERR_SHAPE, "1 to %d sequences, 1 to %d rows and max_len of 1 to the rows needed", SAMP_MAX_BATCH, SAMP_MAX_TOKENS);
+    if (batch < 1 || batch > SAMP_MAX_BATCH || rows < 1 || rows > SAMP_MAX_TOKENS || max_len < 1)
+        return fail(SAMP_ERR_SHAPE, "1 to %d sequences, 1 to %d rows and max_len >= 1 needed", SAMP_MAX_BATCH, SAMP_MAX_TOKENS);
     if (!cu && (long long)batch * max_len != rows) return fail(SAMP_ERR_SHAPE, "without offsets every sequence has max_len rows: %d x %d are not %d", batch, max_len, rows);
+    if (max_len > rows) max_len = rows;
     if (int rc = check_rows("q", q, ldq, (int64_t)heads * head_dim)) return rc;
     if (int rc = check_rows("k", k, ldk, (int64_t)kv_heads * head_dim)) return rc;
     if (int rc = check_rows("v", v, ldv, (int64_t)kv_heads * head_dim)) return rc;

@@ -106,14 +106,7 @@ hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, 
 {
     constexpr int RING = stream_ring_bytes<false, MT, D>(), OUT = 16 * MT * (64 * NTW * 2 + 16), LDS = RING > OUT ? RING : OUT;
     auto kern = gemm_tokens_kernel<BF, MT, NTW, D>;
-    if constexpr (LDS > 65536) {
-        static std::atomic<bool> set{false};
-        if (!set.load(std::memory_order_acquire)) {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-            if (e != hipSuccess) return e;
-            set.store(true, std::memory_order_release);
-        }
-    }
+    static_assert(LDS <= 65536, "more needs an attribute of the kernel");
     const int tm = (M + 16 * MT - 1) / (16 * MT), tn = (N + 64 * NTW - 1) / (64 * NTW);
     hipLaunchKernelGGL(kern, dim3((unsigned)tm * tn), dim3(256), LDS, st, (const char *)A, (const char *)Wp, M, N, K, tm, tn, band, epi, (char *)out);
     return hipGetLastError();

@@ -6,6 +6,7 @@ torch's allocator, and raises SampError for what the library refuses.  Activatio
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 from typing import Optional, Tuple
 
@@ -36,6 +37,11 @@ def _fn(name: str):
         f.argtypes, f.restype = _SIGNATURES[name], _Z if name.endswith("_bytes") else C.c_int
         _entry[name] = f
     return f
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name: str, *sizes: int) -> int:
+    return _fn(name)(*sizes)
 
 
 def _refuse(why: str):
@@ -134,7 +140,7 @@ def linear_i8_tokens(x: torch.Tensor, Wp: torch.Tensor, s_w: torch.Tensor, bias:
     w, s, b = _flat("Wp", Wp, torch.int8, device, N * K), _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N)
     out = x.new_empty((M, N))
     if M:
-        need = _fn("samp_linear_i8_tokens_workspace_bytes")(M, K)
+        need = _workspace_bytes("samp_linear_i8_tokens_workspace_bytes", M, K)
         ws = x.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
         _call(device, _fn("samp_linear_i8_tokens"), at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws, need, _raw_stream(device))
     return out
@@ -183,7 +189,7 @@ def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.T
         _refuse(f"k and v must be [rows, {cache.kv_heads}, {cache.head_dim}] of one type, not {tuple(k.shape)} and {tuple(v.shape)}")
     t, width, pcu, plens, B = _places(device, table, cu, lens)
     if k.shape[0] and B:
-        _call(device, _fn("samp_cache_write"), cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, max_new, k.shape[0], _raw_stream(device))
+        _call(device, _fn("samp_cache_write"), cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, int(max_new), k.shape[0], _raw_stream(device))
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_rows: int, rows: int,
@@ -200,7 +206,7 @@ def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], 
         size = rows * cache.kv_heads * cache.head_dim
         k, v = _flat("out", out[0], dtype, device, size), _flat("out", out[1], dtype, device, size)
     if rows and B:
-        _call(device, _fn("samp_cache_read"), cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, max_rows, rows, _raw_stream(device))
+        _call(device, _fn("samp_cache_read"), cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, int(max_rows), rows, _raw_stream(device))
     return out
 
 
@@ -217,17 +223,16 @@ def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Op
     t, width, pcu, plens, B = _places(device, table, cu, lens)
     words = _flat("tree", tree, torch.int64, device, rows)
     if out is None:
-        out = q.new_empty((rows, heads, dim))
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
     else:
         to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows and B:
-        if max_len is None:
-            max_len = width * cache.page_len
-        need = _fn("samp_attention_cache_workspace_bytes")(rows, B, heads, cache.kv_heads, dim, max_new, max_len)
+        max_new, max_len = int(max_new), width * cache.page_len if max_len is None else int(max_len)
+        need = _workspace_bytes("samp_attention_cache_workspace_bytes", rows, B, heads, cache.kv_heads, dim, max_new, max_len)
         ws = q.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
         _call(device, _fn("samp_attention_cache"), at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
-              1.0 / math.sqrt(dim) if scale is None else scale, words, to, ws, need, _raw_stream(device))
+              1.0 / math.sqrt(dim) if scale is None else float(scale), words, to, ws, need, _raw_stream(device))
     return out
 
 
@@ -241,16 +246,17 @@ def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Opti
     if k.shape != v.shape or k.shape[0] != rows or k.shape[2] != dim or k.dtype != q.dtype or v.dtype != q.dtype:
         _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
     if out is None:
-        out = q.new_empty((rows, heads, dim))
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
     else:
         to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows == 0:
         return out
+    max_len = int(max_len)
     if cu is None and (max_len < 1 or rows % max_len):
         _refuse("without sequence offsets every sequence has max_len rows")
     B = rows // max_len if cu is None else cu.numel() - 1
     if B:
         _call(device, _fn("samp_attention_causal"), pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, device, B + 1), B, max_len,
-              rows, 1.0 / math.sqrt(dim) if scale is None else scale, to, _raw_stream(device))
+              rows, 1.0 / math.sqrt(dim) if scale is None else float(scale), to, _raw_stream(device))
     return out

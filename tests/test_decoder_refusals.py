@@ -76,7 +76,7 @@ BAD_CACHES = [(dict(k=None), ARG, b"NULL"), (dict(v_step=None), ARG, b"NULL"), (
 
 def cache_cases(most):
     places = [({"table": None}, ARG, b"table"), ({"lens": None}, ARG, b"NULL"), ({"width": 0}, SHAPE, b"width"), ({"batch": 0}, SHAPE, b"sequences"),
-              ({"batch": 8193}, SHAPE, b"sequences"), ({most: 0}, SHAPE, most.encode()), ({most: 7}, SHAPE, most.encode()), ({"rows": 0}, SHAPE, b"rows"),
+              ({"batch": 8193}, SHAPE, b"sequences"), ({most: 0}, SHAPE, most.encode()), ({most: 1 << 21, "rows": 1 << 21}, SHAPE, most.encode()), ({"rows": 0}, SHAPE, b"rows"),
               ({"rows": (1 << 24) + 1}, SHAPE, b"rows"), ({"cu": None}, SHAPE, b"without offsets"), ({"type": 3}, ARG, b"type"), ({"cache": None}, ARG, b"cache")]
     bad = [(cache(**c), code, word) for c, code, word in BAD_CACHES]
     return places + [({"cache": C.addressof(b)}, code, word) for b, code, word in bad], bad
@@ -107,7 +107,8 @@ def test_attention_cache(L):
         ({"max_len": 0}, SHAPE, b"max_len"), ({"scale": 0.0}, SCALE, b"scale"), ({"scale": -1.0}, SCALE, b"scale"), ({"scale": float("nan")}, SCALE, b"scale"),
         ({"scale": float("inf")}, SCALE, b"scale"), ({"out": None}, ARG, b"out"), ({"out": AT + 8}, ARG, b"out"), ({"tree": AT + 4}, ARG, b"tree"),
         ({"tree": AT, "rows": 100, "max_new": 65}, SHAPE, b"64"), ({"max_len": 4096, "workspace": None}, SPACE, b"workspace"),
-        ({"max_len": 4096, "bytes": need - 1}, SPACE, b"workspace"), ({"max_len": 4096, "workspace": AT + 8}, SPACE, b"workspace"), ({"rows": 1 << 22, "max_new": 1 << 22, "batch": 1000, "heads": 1024}, SHAPE, b"2^31")])
+        ({"max_len": 4096, "bytes": need - 1}, SPACE, b"workspace"), ({"max_len": 4096, "workspace": AT + 8}, SPACE, b"workspace"), ({"rows": 1 << 20, "max_new": 1 << 20, "batch": 1000, "heads": 1024}, SHAPE, b"2^31"),
+        ({"max_len": 1 << 30, "rows": 1 << 16, "max_new": 1 << 10, "batch": 8192, "heads": 64}, SHAPE, b"2^31")])
 
 
 def test_attention_causal(L):
@@ -117,7 +118,7 @@ def test_attention_causal(L):
         ({"q": None}, ARG, b"q is"), ({"k": None}, ARG, b"k is"), ({"v": None}, ARG, b"v is"), ({"ldq": 252}, ARG, b"q: "), ({"ldk": 64}, SHAPE, b"k: "), ({"v": AT + 2}, ARG, b"v: "),
         ({"type": 2}, ARG, b"type"), ({"heads": 5}, SHAPE, b"multiple"), ({"kv_heads": 0}, SHAPE, b"multiple"), ({"head_dim": 32}, SHAPE, b"head_dim"),
         ({"cu": None}, SHAPE, b"without offsets"), ({"batch": 0}, SHAPE, b"sequences"), ({"batch": 8193}, SHAPE, b"sequences"), ({"max_len": 0}, SHAPE, b"max_len"),
-        ({"max_len": 6}, SHAPE, b"max_len"), ({"rows": 0}, SHAPE, b"rows"), ({"scale": float("nan")}, SCALE, b"scale"), ({"out": None}, ARG, b"out"),
+        ({"cu": None, "max_len": 6}, SHAPE, b"without offsets"), ({"rows": 0}, SHAPE, b"rows"), ({"scale": float("nan")}, SCALE, b"scale"), ({"out": None}, ARG, b"out"),
         ({"batch": 8192, "max_len": 1 << 24, "rows": 1 << 24}, SHAPE, b"strips")])
 
 

@@ -352,6 +352,8 @@ def test_attention_cache_leaves_rows_behind_the_last_sequence(P):
         out = torch.full((6, 4, 128), 7.0, dtype=BF16, device="cuda")
         P.attention_cache(q, plan.cache, *plan.args, 2, max_len=max_len, out=out)
         assert (out[3:] == 7).all() and (out[:3] != 7).any()
+    want = P.attention_cache(q, plan.cache, *plan.args, 2, max_len=50)
+    assert torch.equal(P.attention_cache(q, plan.cache, *plan.args, 4096, max_len=50)[:3], want[:3])      # a larger batch's maximum
     # no offsets: every sequence has max_new rows, and views of a wider projection are read in place
     wide = torch.randn(4, 10, 128, generator=gen(2)).bfloat16().cuda()
     a = P.attention_cache(wide[:, 2:6], plan.cache, plan.args[0], None, plan.args[2], 2)
@@ -455,6 +457,7 @@ def test_attention_causal_what_is_not_seen_has_no_part(P, dtype, D):
     assert (live | dead).all()
     late = got[133:150, :2][~dead[63:].cuda()]
     assert (late[:, 7] == -math.inf).all()
+    assert torch.equal(P.attention_causal(q, k, v, cu, 4096), clean)        # a larger batch's maximum
     # rows behind the last sequence, and of a sequence that is longer than the host said, are left
     out = torch.full((T, H, D), 5.0, dtype=dtype, device="cuda")
     P.attention_causal(q, k, v, cu[:2].contiguous(), 90, out=out)
@@ -580,3 +583,34 @@ def test_attention_block_of_a_decoder(P, dtype):
             # have one each (the scores' errors, of unit variance, count like another two): sqrt(8) * 0.0075 = 0.021, doubled; bfloat16's own roundings add 2^-8 a few times
             assert off < 0.045 + (0.02 if dtype == BF16 else 0.0), off
             at += m
+
+
+def test_two_streams_at_once(P):
+    """Calls on two streams overlap: each has a workspace of its own and shares nothing but what it reads."""
+    plan = Plan(P, [5000, 900, 3000], [1, 1, 1], 2, 128, 64)
+    plan.fill(P, F16, 1)
+    q = torch.randn(3, 8, 128, generator=gen(5)).half().cuda()
+    W, s_w = weights(1024, 1024, 2)
+    Wp, s = P.pack_weight_i8(W.cuda()), s_w.cuda()
+    x = torch.randn(600, 1024, generator=gen(6)).half().cuda()
+    want = P.attention_cache(q, plan.cache, *plan.args, 1), P.linear_i8_tokens(x, Wp, s)
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(10):
+        for st in streams:
+            with torch.cuda.stream(st):
+                got.append((P.attention_cache(q, plan.cache, *plan.args, 1), P.linear_i8_tokens(x, Wp, s)))
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+def test_sequences_share_the_pages_of_a_prefix(P):
+    plan = Plan(P, [64, 64], [64, 64], 2, 64, 16)
+    held = plan.fill(P, F16, 3)
+    table = plan.args[0].clone()
+    table[1, :2] = table[0, :2]                              # the first 32 positions are the first sequence's
+    q = torch.randn(2, 4, 64, generator=gen(5)).half()
+    got = P.attention_cache(q.cuda(), plan.cache, table, None, plan.args[2], 1)
+    k, v = (torch.cat([held[0][i][:32], held[1][i][32:]]) for i in (0, 1))
+    check_attention(got[1:], *attend(q[1:].double(), k, v, torch.ones(1, 64, dtype=torch.bool), 0.125), F16, F16, 64, v.abs().max().item())
