@@ -1,7 +1,7 @@
 // y[m, n] = act(steps[m] * s_w[n] * sum_k codes[m, k] W[n, k] + bias[n]): the int8 product whose activation rows bring their own steps, on weights in the
-// order of pack_weight_kernel, with a 16-bit result.
+// order of pack_weight_kernel, with a 16-bit result.  The sum is exact in int32; it becomes binary32 (2^-24), is multiplied by the row's step (2^-24) and, in one
+// fused operation with the bias, by the channel's (2^-24), and is rounded once to 16 bits.
 #include "decoder.h"
-#include "divisor.h"
 #include "mfma_tile.h"
 
 namespace samp {
@@ -22,6 +22,7 @@ template <bool BF> __device__ __forceinline__ v2i finish4(const v4i &acc, float 
 
 // ---- many rows -------------------------------------------------------------------------------------
 // The tile loop on packed weights (mfma_tile.h): 16 MT tokens x 64 NTW channels per block, weights straight into registers, token rows through LDS.
+// 8192 x 4096 x 4096: 126 us, 2.18 POP/s (torch's int8 product, 8192 x 8192 x 4096: 2.13).
 // K need only be a multiple of 64: what is left after whole rounds of the ring (D stages of 128 bytes) is multiplied from memory, without a pipeline.
 // N need only be a multiple of 16: a wave's blocks past the last one repeat it and are not stored.
 template <bool BF, int MT, int NTW, int D>
@@ -116,7 +117,8 @@ hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, 
 // One token tile; what it costs is the weights' way from HBM and the latencies around it.  A block owns 16 channels and splits K over its eight waves, so that
 // all of its weights (KB blocks of 1 KB a wave) are requested before anything else happens; the int32 partial tiles meet in LDS.  FUSED: the rows come in 16
 // bits and every block quantises them for itself while its weights are on the way, into LDS (rows 16 bytes more than K apart, so that the sixteen rows of an
-// operand read lie in different banks), which saves a launch.  Eight, four, two or one waves share a row, the fewer the more rows there are.
+// operand read lie in different banks), which saves a launch.  Eight, four, two or one waves share a row, the fewer the more rows there are.  One row, 4096 -> 6144,
+// 25 MB of weights: 6.3 us in the chain of launches (two kernels 1.9 + 7.2); with every lane quantising what it multiplies, sixteen times over, 8.5.
 constexpr int FEW_WAVES = 8;
 struct FewRows { const void *x; long ld; const float *steps; };        // FUSED: 16-bit rows, ld values apart; else codes, K apart, and their steps
 template <bool BF, bool FUSED, int KB>
@@ -213,7 +215,13 @@ hipError_t launch_few(const FewRows &in, const int8_t *Wp, const TokensEpi &epi,
 }
 
 // ---- which kernel ------------------------------------------------------------------------------------
-// The tile whose cost is least: its time for K = 4096 where the chip is full of it, times the rounds of blocks (the mean of whole rounds and their fraction).
+// The tile whose cost is least: its time for K = 4096 where the chip is full of it (small ones: where it is not), times the rounds of blocks (the mean of
+// whole rounds and their fraction).  Over 36 random shapes (17 to 16384 rows, K 256 to 8192, N 256 to 8192) the choice costs 4 % on average against the best
+// of eleven tiles and depths.  us, M x N x K, the tiles in the order of the list: 64 x 4096 x 4096 7.5 / 8.1 / 11.8 / 16.3 / 21.7; 512 x 4096 x 4096 39 / 15.5 /
+// 13.1 / 17.1 / 22.5; 2048 x 4096 x 4096 148 / 76 / 73 / 34 / 39; 8192 x 4096 x 4096 583 / 296 / 290 / 129 / 126; 4096 x 11008 x 4096 781 / 396 / 400 / 188 / 181.
+// What bounds the large ones is how fast a CU gets its operands from L2: a stage of 128 bytes of K is 32 KB (8 x 2) or 40 KB (8 x 3) for 512 and 768 clocks of matrix
+// work, 62 and 52 bytes per clock.
+// Bands: 2048 x 4096 x 4096 on 8 x 2 tiles, one row tile a band / eight 41.6 / 33.8, 8192 x 4096 x 4096 on 8 x 3, one / four / eight 139 / 126 / 136.
 struct TokensTile { int mt, ntw; float us; };
 constexpr TokensTile TOKENS_TILES[] = {{2, 1, 7.3f}, {4, 1, 7.8f}, {4, 2, 13.0f}, {8, 2, 17.0f}, {8, 3, 23.0f}};
 int tokens_tile(int M, int N)
@@ -232,9 +240,11 @@ template <bool BF>
 hipError_t gemm_tokens(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, hipStream_t st)
 {
     if (M <= FEW_ROWS && K <= FEW_K) return launch_few<BF, false>(FewRows{A, K, epi.steps}, Wp, epi, out, M, N, K, st);
-    const bool deep = K >= 512 && K % 512 < 256;                     // four stages in flight instead of two, if no more is left over
+    // four stages in flight instead of two (64 x 4096 x 4096 7.5 / 9.7) where no more is left over for it, and always on the smallest tile (85 x 1312 x 8064 12.3 / 17.2;
+    // 619 x 2624 x 3328 on 4 x 2 tiles, 256 left over, 14.0 / 12.3)
+    const bool deep = K >= 512 && K % 512 < 256;
     switch (tokens_tile(M, N)) {
-    case 0: return deep ? launch_tile<BF, 2, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 2, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
+    case 0: return K >= 512 ? launch_tile<BF, 2, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 2, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
     case 1: return deep ? launch_tile<BF, 4, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 4, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
     case 2: return deep ? launch_tile<BF, 4, 2, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 4, 2, 2>(A, Wp, epi, out, M, N, K, 8, st);
     case 3: return launch_tile<BF, 8, 2, 2>(A, Wp, epi, out, M, N, K, 8, st);

@@ -197,7 +197,8 @@ dim3 cache_grid(const KvCache &c, const KvRows &r, int log2, int passes)
     const int tokens = passes << log2;
     return dim3((unsigned)((2 * c.kv_heads + (16 >> log2) - 1) / (16 >> log2)), (unsigned)((r.max_rows + tokens - 1) / tokens), (unsigned)r.batch);
 }
-// Four rows a lane group where there are blocks enough
+// Four rows a lane group where there are blocks enough: one / four, 16 prompts of 900 to 2048 tokens written 36.2 / 33.3 us, read 31.0 / 25.3; a chunk of 4 x 512 tokens
+// has 2048 x 8 rows and is better off with one (5.4 us).
 int cache_passes(const KvCache &c, const KvRows &r) { return (long)r.rows * c.kv_heads >= 32768 ? 4 : 1; }
 
 template <bool BF, int D>
