@@ -40,18 +40,18 @@ template <int D> struct KeyTile {
     unsigned known;                                                   // bit h: the page of keys 16 h .. 16 h + 15 is one of the cache's
 };
 
+// entries: the table's, of the tile's two groups of 16 keys (which lie in one page each)
 template <int D>
-__device__ __forceinline__ KeyTile<D> load_tile(const KvCache &c, const int *table, int head, int j0, int last, int r, int g)
+__device__ __forceinline__ KeyTile<D> load_tile(const KvCache &c, const int (&entries)[2], int head, int j0, int last, int r, int g)
 {
     KeyTile<D> t;
     t.known = 0;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        const int pos = min(j0 + 16 * h, last);                       // 16 keys lie in one page; past the end the last ones are read again, and masked
-        int page = table[pos >> c.page_shift];
-        const bool ok = (unsigned)page < (unsigned)c.pages;
+        const int pos = min(j0 + 16 * h, last);                       // past the end the last keys are read again, and masked
+        const bool ok = (unsigned)entries[h] < (unsigned)c.pages;
         t.known |= (unsigned)ok << h;
-        page = ok ? page : 0;
+        const int page = ok ? entries[h] : 0;
         const size_t row = (((size_t)page * c.kv_heads + head) << c.page_shift) + (pos & ((1 << c.page_shift) - 1) & ~15);
         const int8_t *k = c.k + row * D, *v = c.v + row * D;
 #pragma unroll
@@ -100,6 +100,15 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
     const int first = rows.lens[b] - s.n;                             // position of the first new token (negative: more new tokens than positions)
     const int *table = rows.table + (size_t)b * rows.width;
 
+    // Table entries of the wave's tiles, 32 at a time (lane 2 i + h: group h of its i-th tile): looked up one by one, each would stand in front of its tile's loads
+    const int end = split == pieces - 1 ? tiles : (split + 1) * piece, last = (len - 1) & ~15;
+    int t = split * piece + w, entries = -1;
+    auto look_up = [&]() {
+        const int pos = min((t + 4 * (lane >> 1)) * TILE + 16 * (lane & 1), last);
+        entries = table[max(pos, 0) >> c.page_shift];
+    };
+    look_up();
+
     // queries: operand step (i, half) holds channels 64 i + 16 g + 8 half .. + 7
     v8h qf[QT][D / 32];
     float factor[QT];                                                 // of a row's scores, as exponents of two
@@ -143,10 +152,14 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
         for (int j = 0; j < DV; j++) o[qt][j] = v4f{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int end = split == pieces - 1 ? tiles : (split + 1) * piece;
     const int whole = min(first, len) / TILE;                         // tiles below it are seen by every row
-    for (int t = split * piece + w; t < end; t += 4) {
-        const KeyTile<D> kt = load_tile<D>(c, table, head, t * TILE, (len - 1) & ~15, r, g);
+    for (int i = 0; t < end; t += 4, i++) {
+        if (i == 32) {
+            look_up();
+            i = 0;
+        }
+        const int mine[2] = {__builtin_amdgcn_readlane(entries, 2 * i), __builtin_amdgcn_readlane(entries, 2 * i + 1)};
+        const KeyTile<D> kt = load_tile<D>(c, mine, head, t * TILE, last, r, g);
         v8h kf[2][D / 32];
 #pragma unroll
         for (int h = 0; h < 2; h++)
@@ -355,10 +368,10 @@ hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c
 
 // Pieces of so many tiles that 512 blocks have them all, but no less than four tiles (a tile for each wave; eight where a block has two row tiles), below which
 // the blocks' own latencies count for more than their number, and no more than 48, so that blocks of contexts of different lengths end together; none at all
-// where there would be few more tiles than in one.  Joining costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
-// key heads of 128, one context of 4000 8.6 / 9.3 / 12.0 / 17.5 / 28.7 / 48; 64 of 17 to 8192 178 / 142 / 126 / 120 / 121 / 136; 32 of 500 to 1000 21.8 / 19.8 /
-// 17.6 / 18.2; 16 drafts on 8 contexts of 300 to 2100, 16 heads of 64, 17.0 / 15.0 / 14.2 / 16.2 / 22.9; one context of 8192, five tokens of 28 heads on 4,
-// 18.3 / 15.9 / 17.3 / 22.7 / 34.4; 64 contexts of 100 to 300, 12 heads of 64, 15.1 / 13.0 / - / - / - / 10.1
+// where a context has at most sixteen tiles more than a piece.  Joining costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
+// key heads of 128, one context of 4000 8.5 / 9.2 / 11.7 / 16.0 / 23.9 / 36; 64 of 17 to 8192 176 / 139 / 124 / 120 / 121 / 131; 32 of 500 to 1000 21.7 / 19.4 /
+// 18.0 / 15.3 (uncut); 16 drafts on 8 contexts of 300 to 2100, 16 heads of 64, 17.3 / 14.4 / 14.0 / 15.6 / 21.7; one context of 8192, five tokens of 28 heads on 4,
+// 18.1 / 15.3 / 16.6 / 21.6 / 32.0 / 91; 64 contexts of 100 to 300, 12 heads of 64, 15.8 / 13.8 / 10.0 (uncut)
 Cut cached_attention_cut(int batch, int heads, int kv_heads, int max_new, int max_len)
 {
     const int most = max_new * (heads / kv_heads), qt = row_tiles(most);
@@ -366,7 +379,7 @@ Cut cached_attention_cut(int batch, int heads, int kv_heads, int max_new, int ma
     long piece = tiles * items / 512;
     if (piece > 48) piece = 48;
     if (piece < 4 * qt) piece = 4 * qt;
-    if (2 * tiles <= 3 * piece) return Cut{1, (int)tiles};
+    if (tiles <= piece + 16) return Cut{1, (int)tiles};
     long splits = (tiles + piece - 1) / piece;
     if (splits > MAX_SPLITS) splits = MAX_SPLITS;
     return Cut{(int)splits, (int)((tiles + splits - 1) / splits)};

@@ -312,7 +312,7 @@ def test_attention_cache_long_contexts_are_cut_and_joined(P, dtype):
     run_cached(P, [4100], [40], 4, 4, 64, 16, dtype, seed=2)
     # the host's guess of the longest context decides the cut, not the result's meaning
     run_cached(P, [900, 40], [1, 1], 8, 1, 128, 32, dtype, seed=3, max_len=100000)
-    run_cached(P, [3000, 40], [1, 1], 8, 1, 128, 32, dtype, seed=4, max_len=1)
+    run_cached(P, [9000, 40], [1, 1], 8, 1, 128, 32, dtype, seed=4, max_len=1)
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
