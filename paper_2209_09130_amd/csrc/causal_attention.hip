@@ -257,7 +257,6 @@ void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict_
     }
     l += __shfl_xor(l, 32, 64);
     const float by = l != 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
-    __syncthreads();
     char *mine = lds + w * 32 * (T::ROW + 16);
 #pragma unroll
     for (int i = 0; i < DB; i++)
