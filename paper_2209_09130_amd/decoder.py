@@ -7,7 +7,6 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-import math
 from typing import Optional, Tuple
 
 import torch
@@ -91,27 +90,31 @@ def _rows2(what: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
     return x.data_ptr(), x.stride(0) if M > 1 else K, M, K
 
 
-_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice   # torch.cuda.current_stream(device).cuda_stream without the objects
+# torch.cuda.current_stream(device).cuda_stream and torch.cuda.current_device() without their objects; a call on another device than the current one is made again
+# with that device current
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _call(device: int, f, *args) -> None:
-    """The entry point on `device`, which its stream, the last of its arguments, belongs to."""
-    if _current_device() == device:
-        rc = f(*args)
-    else:
-        with torch.cuda.device(device):
-            rc = f(*args)
-    if rc:
-        raise SampError(rc, lib().samp_last_error().decode())
+def _on(device: int, f, *args, **kwargs):
+    with torch.cuda.device(device):
+        return f(*args, **kwargs)
+
+
+def _raise(rc: int):
+    raise SampError(rc, lib().samp_last_error().decode())
 
 
 def quantize_tokens(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """samp_quantize_tokens: int8 codes [M, K] and float32 steps [M] of the rows of x (step = the row's absmax / 127)."""
     device = _device(x)
+    if device != _current_device():
+        return _on(device, quantize_tokens, x)
     at, ld, M, K = _rows2("x", x)
     codes, steps = x.new_empty((M, K), dtype=torch.int8), x.new_empty((M,), dtype=torch.float32)
     if M:
-        _call(device, _fn("samp_quantize_tokens"), at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr(), _raw_stream(device))
+        rc = _fn("samp_quantize_tokens")(at, ld, _TYPES[x.dtype], M, K, codes.data_ptr(), steps.data_ptr(), _raw_stream(device))
+        if rc:
+            _raise(rc)
     return codes, steps
 
 
@@ -120,29 +123,38 @@ def gemm_i8_tokens_packed(codes: torch.Tensor, steps: torch.Tensor, Wp: torch.Te
     """samp_gemm_i8_tokens_packed: [M, N] of `dtype` from int8 codes [M, K] with a step for each row and weights that pack_weight_i8 packed, with a
     step for each channel."""
     device = _device(codes)
+    if device != _current_device():
+        return _on(device, gemm_i8_tokens_packed, codes, steps, Wp, s_w, bias, gelu, dtype)
     if codes.dim() != 2 or dtype not in _TYPES:
         _refuse("codes must be a matrix, and the result's type fp16 or bfloat16")
     M, K = codes.shape
     N = s_w.numel()
+    c, st, w = _flat("codes", codes, torch.int8, device), _flat("steps", steps, torch.float32, device, M), _flat("Wp", Wp, torch.int8, device, N * K)
+    sw, b = _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N)
     out = codes.new_empty((M, N), dtype=dtype)
-    args = (_flat("codes", codes, torch.int8, device), _flat("steps", steps, torch.float32, device, M), _flat("Wp", Wp, torch.int8, device, N * K),
-            _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N), int(bool(gelu)), out.data_ptr(), _TYPES[dtype], M, N, K)
     if M:
-        _call(device, _fn("samp_gemm_i8_tokens_packed"), *args, _raw_stream(device))
+        rc = _fn("samp_gemm_i8_tokens_packed")(c, st, w, sw, b, int(bool(gelu)), out.data_ptr(), _TYPES[dtype], M, N, K, _raw_stream(device))
+        if rc:
+            _raise(rc)
     return out
 
 
 def linear_i8_tokens(x: torch.Tensor, Wp: torch.Tensor, s_w: torch.Tensor, bias: Optional[torch.Tensor] = None, gelu: bool = False) -> torch.Tensor:
     """samp_linear_i8_tokens: quantize_tokens and gemm_i8_tokens_packed in one call, x [M, K] -> [M, N] of x's type."""
     device = _device(x)
+    if device != _current_device():
+        return _on(device, linear_i8_tokens, x, Wp, s_w, bias, gelu)
     at, ld, M, K = _rows2("x", x)
     N = s_w.numel()
     w, s, b = _flat("Wp", Wp, torch.int8, device, N * K), _flat("s_w", s_w, torch.float32, device), _flat("bias", bias, torch.float32, device, N)
     out = x.new_empty((M, N))
     if M:
         need = _workspace_bytes("samp_linear_i8_tokens_workspace_bytes", M, K)
-        ws = x.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
-        _call(device, _fn("samp_linear_i8_tokens"), at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws, need, _raw_stream(device))
+        ws = x.new_empty((need,), dtype=torch.uint8) if need else None
+        rc = _fn("samp_linear_i8_tokens")(at, ld, _TYPES[x.dtype], w, s, b, int(bool(gelu)), out.data_ptr(), M, N, K, ws.data_ptr() if need else 0, need,
+                                          _raw_stream(device))
+        if rc:
+            _raise(rc)
     return out
 
 
@@ -174,30 +186,40 @@ class KVCache:
 
 
 def _places(device: int, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor):
-    if table.dim() != 2:
+    shape = table.shape
+    if len(shape) != 2:
         _refuse("the page table is [sequences, pages of a sequence]")
-    B, width = table.shape
-    return _flat("table", table, torch.int32, device), width, _flat("cu", cu, torch.int32, device, B + 1), _flat("lens", lens, torch.int32, device, B), B
+    B, width = shape
+    return (_flat("table", table, torch.int32, device), width, _flat("cu", cu, torch.int32, device, B + 1) if cu is not None else 0,
+            _flat("lens", lens, torch.int32, device, B), B)
 
 
 def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int) -> None:
     """samp_cache_write: the packed rows k, v [rows, kv_heads, head_dim] become the last cu[b + 1] - cu[b] of the lens[b] positions of each sequence.
     table int32 [B, width]; cu int32 [B + 1] or None (max_new rows each); lens int32 [B], the new positions counted."""
     device = cache.device
+    if device != _current_device():
+        return _on(device, cache_write, cache, k, v, table, cu, lens, max_new)
     (pk, ldk), (pv, ldv) = _heads("k", k, device), _heads("v", v, device)
-    if k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (cache.kv_heads, cache.head_dim):
+    shape = k.shape
+    if shape != v.shape or k.dtype is not v.dtype or shape[1] != cache.kv_heads or shape[2] != cache.head_dim:
         _refuse(f"k and v must be [rows, {cache.kv_heads}, {cache.head_dim}] of one type, not {tuple(k.shape)} and {tuple(v.shape)}")
     t, width, pcu, plens, B = _places(device, table, cu, lens)
-    if k.shape[0] and B:
-        _call(device, _fn("samp_cache_write"), cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, int(max_new), k.shape[0], _raw_stream(device))
+    rows = shape[0]
+    if rows and B:
+        rc = _fn("samp_cache_write")(cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, int(max_new), rows, _raw_stream(device))
+        if rc:
+            _raise(rc)
 
 
 def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_rows: int, rows: int,
                dtype: torch.dtype = torch.float16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """samp_cache_read: k, v [rows, kv_heads, head_dim] of `dtype`, sequence b's rows the last cu[b + 1] - cu[b] of its lens[b] positions."""
+    device = cache.device
+    if device != _current_device():
+        return _on(device, cache_read, cache, table, cu, lens, max_rows, rows, dtype, out)
     if dtype not in _TYPES:
         _refuse("the result's type must be fp16 or bfloat16")
-    device = cache.device
     t, width, pcu, plens, B = _places(device, table, cu, lens)
     if out is None:
         out = cache.k.new_empty((2, rows, cache.kv_heads, cache.head_dim), dtype=dtype).unbind()
@@ -206,7 +228,9 @@ def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], 
         size = rows * cache.kv_heads * cache.head_dim
         k, v = _flat("out", out[0], dtype, device, size), _flat("out", out[1], dtype, device, size)
     if rows and B:
-        _call(device, _fn("samp_cache_read"), cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, int(max_rows), rows, _raw_stream(device))
+        rc = _fn("samp_cache_read")(cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, int(max_rows), rows, _raw_stream(device))
+        if rc:
+            _raise(rc)
     return out
 
 
@@ -216,12 +240,14 @@ def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Op
     """samp_attention_cache: [rows, heads, head_dim] of the new tokens q over the cache that holds their keys and values already.
     max_len: the longest context expected (None: what the page table has room for).  scale: None for 1 / sqrt(head_dim).  tree: int64 words [rows]."""
     device = cache.device
+    if device != _current_device():
+        return _on(device, attention_cache, q, cache, table, cu, lens, max_new, max_len, scale, tree, out)
     at, ld = _heads("q", q, device)
     rows, heads, dim = q.shape
     if dim != cache.head_dim:
         _refuse(f"q has heads of {dim}, the cache of {cache.head_dim}")
     t, width, pcu, plens, B = _places(device, table, cu, lens)
-    words = _flat("tree", tree, torch.int64, device, rows)
+    words = _flat("tree", tree, torch.int64, device, rows) if tree is not None else 0
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
@@ -230,9 +256,11 @@ def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Op
     if rows and B:
         max_new, max_len = int(max_new), width * cache.page_len if max_len is None else int(max_len)
         need = _workspace_bytes("samp_attention_cache_workspace_bytes", rows, B, heads, cache.kv_heads, dim, max_new, max_len)
-        ws = q.new_empty((need,), dtype=torch.uint8).data_ptr() if need else 0
-        _call(device, _fn("samp_attention_cache"), at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
-              1.0 / math.sqrt(dim) if scale is None else float(scale), words, to, ws, need, _raw_stream(device))
+        ws = q.new_empty((need,), dtype=torch.uint8) if need else None
+        rc = _fn("samp_attention_cache")(at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
+                                         dim ** -0.5 if scale is None else float(scale), words, to, ws.data_ptr() if need else 0, need, _raw_stream(device))
+        if rc:
+            _raise(rc)
     return out
 
 
@@ -241,22 +269,29 @@ def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Opti
     """samp_attention_causal: [rows, heads, head_dim] from q [rows, heads, head_dim] and k, v [rows, kv_heads, head_dim] (views into a fused
     projection's rows are read in place).  cu int32 [B + 1], or None for sequences of max_len rows each."""
     device = _device(q)
+    if device != _current_device():
+        return _on(device, attention_causal, q, k, v, cu, max_len, scale, out)
     (pq, ldq), (pk, ldk), (pv, ldv) = _heads("q", q, device), _heads("k", k, device), _heads("v", v, device)
-    rows, heads, dim = q.shape
-    if k.shape != v.shape or k.shape[0] != rows or k.shape[2] != dim or k.dtype != q.dtype or v.dtype != q.dtype:
+    (rows, heads, dim), shape, dtype = q.shape, k.shape, q.dtype
+    if shape != v.shape or shape[0] != rows or shape[2] != dim or k.dtype is not dtype or v.dtype is not dtype:
         _refuse(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not belong together")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
     else:
-        to = _flat("out", out, q.dtype, device, rows * heads * dim)
+        to = _flat("out", out, dtype, device, rows * heads * dim)
     if rows == 0:
         return out
     max_len = int(max_len)
-    if cu is None and (max_len < 1 or rows % max_len):
-        _refuse("without sequence offsets every sequence has max_len rows")
-    B = rows // max_len if cu is None else cu.numel() - 1
+    if cu is not None:
+        B, pcu = cu.numel() - 1, _flat("cu", cu, torch.int32, device)
+    else:
+        if max_len < 1 or rows % max_len:
+            _refuse("without sequence offsets every sequence has max_len rows")
+        B, pcu = rows // max_len, 0
     if B:
-        _call(device, _fn("samp_attention_causal"), pq, ldq, pk, ldk, pv, ldv, _TYPES[q.dtype], heads, k.shape[1], dim, _flat("cu", cu, torch.int32, device, B + 1), B, max_len,
-              rows, 1.0 / math.sqrt(dim) if scale is None else float(scale), to, _raw_stream(device))
+        rc = _fn("samp_attention_causal")(pq, ldq, pk, ldk, pv, ldv, _TYPES[dtype], heads, shape[1], dim, pcu, B, max_len, rows,
+                                          dim ** -0.5 if scale is None else float(scale), to, _raw_stream(device))
+        if rc:
+            _raise(rc)
     return out
