@@ -12,6 +12,7 @@
  * is int8; dequantise + bias + residual + LayerNorm + quantise are one kernel;
  * the softmax output is quantised (Section 4.2, Appendix B); the last kernel of
  * a layer emits floating point when its consumer is not quantised.
+ * The last section holds the operators of an 8-bit decoder's attention block.
  *
  * Conventions
  *   - All `dev` pointers are device memory of the current HIP device, owned by

@@ -87,7 +87,7 @@ void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict_
     const int q0 = strip * QB;
     if (q0 >= n) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 31, g = lane >> 5;
-    const int qw = q0 + 32 * w;                                           // the wave's first query
+    const int qw = q0 + 32 * w, wave_end = qw < n ? qw + 31 : -1;          // the wave's first query; its last, -1 if the sequence ends before it
     const unsigned ldkb = 2 * (unsigned)ldk, ldvb = 2 * (unsigned)ldv;
     const char *kbase = K + (size_t)t0 * ldkb + kvh * T::ROW, *vbase = V + (size_t)t0 * ldvb + kvh * T::ROW;
 
@@ -141,7 +141,7 @@ void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict_
             wait_vm_and_barrier<0>();                                     // tile t is there, and tile t - 1 has been read by all
             if (t + 1 < tiles) request(t + 1, (t + 1) & 1);
             const int j0 = t * KEYS;
-            if (j0 > qw + 31) continue;                                   // (wave-uniform) keys behind all of the wave's queries
+            if (j0 > wave_end) continue;                                  // (wave-uniform) keys behind all of the wave's queries
             const unsigned stage = (t & 1) * T::STAGE, ka = kat + stage, va = vat + stage;
             // scores: four fragments of K on their way while four are multiplied
             constexpr int HALF = KS / 2;                                  // fragments of a step; steps (h, first or second half of the channels)

@@ -157,6 +157,9 @@ def test_linear_rows_that_are_not_finite_stay_alone(P):
     ok = torch.ones(40, dtype=torch.bool)
     ok[[7, 20]] = False
     assert torch.isnan(got[~ok.cuda()]).all() and torch.equal(got[ok.cuda()], want[ok.cuda()])
+    for rows in ([7], [6, 7, 8], [20, 21], list(range(5, 15))):              # few rows, in one launch
+        few = P.linear_i8_tokens(x[rows].cuda(), Wp, s)
+        assert torch.equal(torch.isnan(few), torch.isnan(got[rows])) and torch.equal(torch.nan_to_num(few), torch.nan_to_num(got[rows]))
 
 
 def test_linear_of_no_rows_and_of_rows_in_place(P):
@@ -198,9 +201,6 @@ class Plan:
             c, s = quantised(x)
             held.append((c * s[..., None]).split(self.lens))
         return list(zip(*held))
-
-
-LENS = [(1, [1]), (5, [40, 7, 0, 129, 16]), (3, [300, 257, 64])]
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
