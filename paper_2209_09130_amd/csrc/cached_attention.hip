@@ -8,22 +8,26 @@
 // tile's loads ahead of this one's work (64 contexts +-0, 16 drafts +3 %: other waves hide it, and it costs one of three per SIMD); the last block of a row joining the
 // pieces behind a fence (eight times as long: each block's fence writes its XCD's L2 back).
 //
-// Products are 16 x 16 x 32 in binary16, in which int8 codes are exact: 1024 + (code + 128) is a code's byte under the exponent byte 0x64, and one packed
-// addition takes 1152 off again.  S^T = K Q^T: a lane gets four keys of one query, two such tiles are the eight keys that it needs as the operand of
-// O^T += V^T P^T.  V^T is formed on the way: a lane holds head_dim / 16 neighbouring channels of eight keys, and the byte permute that widens codes takes
-// the two halves of a dword from two keys.  The steps of the keys multiply scores (K) and probabilities (V) in binary32.
+// Products are 16 x 16 x 32.  S^T = K Q^T is in binary16, in which int8 codes are exact: 1024 + (code + 128) is a code's byte under the exponent byte 0x64, and
+// one packed addition takes 1152 off again; queries of bfloat16 are scaled by a power of two per row into binary16's range.  A lane gets four keys of one
+// query, two such tiles are the eight keys that it needs as the operand of O^T += V^T P^T.  V^T is formed on the way: a lane holds head_dim / 16 neighbouring channels
+// of eight keys, and the byte permute that packs widened codes takes the two halves of a dword from two keys.  The steps of the keys multiply scores (K) and
+// probabilities (V) in binary32.
 //
-// Softmax in one pass with a running reference m per query that bounds log2(p step_v): exponent(step_v) + score, so that p step_v fits binary16 (at most
-// 2^9) whatever the steps.  m moves (and the sums are scaled) only when a score exceeds it by 2^8, not for every new maximum.  Rounding p step_v to
-// binary16 is off by 2^-11 of each, well below a bfloat16 result's rounding; for an fp16 result, where it would be as much again, what was rounded off is multiplied as
-// well (the matrix cores are idle most of the time).  Queries of bfloat16 are scaled by a power of two per row into binary16's range.
+// O^T += V^T P^T is in bfloat16, in which codes are exact too and whose range is binary32's: p step_v of a key may be any size next to that of another (rows of zeros
+// have step 1, and one large channel makes the step of a row in all of them), so no power of two for all of them would keep binary16 from losing the small
+// ones.  Its 8 bits are made 16 by a second product with what was rounded off, 2^-16 of each p step_v and below (the matrix cores are idle most of the time).
+//
+// Softmax in one pass with a running reference m per query, which is ABOVE the scores (in powers of two), so that p times the largest step (2^121) and the sums stay
+// inside binary32.  m moves (and the sums are scaled) only when a score exceeds what it was set for by 2^8, not for every new maximum.
 #include "decoder.h"
+#include "mfma_tile.h"
 
 namespace samp {
 namespace {
 
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-constexpr float LOWEST = -3.0e38f, SLACK = 8.0f;
+constexpr float LOWEST = -3.0e38f, SLACK = 8.0f, ABOVE = 24.0f;
 constexpr int TILE = 32;                                              // keys of a wave's step
 
 // halves 1024 + 128 + code from the dword whose bytes 0 and 2 are codes and 1 and 3 are zero; codes as binary16
@@ -31,6 +35,13 @@ __device__ __forceinline__ int to_halves(unsigned bytes)
 {
     const v2h biased = __builtin_bit_cast(v2h, bytes ^ 0x64806480u);
     return __builtin_bit_cast(int, biased - v2h{(_Float16)1152.0f, (_Float16)1152.0f});
+}
+
+// byte BYTE of two dwords as two bfloat16 (a code's binary32 has no more than the upper half)
+template <int BYTE> __device__ __forceinline__ int to_bfloats(int lo, int hi)
+{
+    const float a = (float)(int8_t)(lo >> 8 * BYTE), b = (float)(int8_t)(hi >> 8 * BYTE);
+    return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
 template <int D> struct KeyTile {
@@ -176,12 +187,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
                     }
                     kf[h][2 * i + half] = __builtin_bit_cast(v8h, x);
                 }
-        float ev[2][4];                                               // step_v <= 2^ev
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int e = 0; e < 4; e++) ev[h][e] = (float)__builtin_amdgcn_frexp_expf(kt.vs[h][e]);
-        v8h pf[QT], pl[QT];
+        v4i pf[QT], pl[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
             float sc[2][4], top = -INFINITY;
@@ -208,11 +214,11 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) top = __builtin_fmaxf(top, sc[h][e] + ev[h][e]);
-            if (__any(top > m[qt] + SLACK)) {
+                for (int e = 0; e < 4; e++) top = __builtin_fmaxf(top, sc[h][e]);
+            if (__any(top > m[qt] - (ABOVE - SLACK))) {
                 top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
                 top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-                const float to = top > m[qt] + SLACK ? top : m[qt], down = __builtin_amdgcn_exp2f(m[qt] - to);
+                const float to = top > m[qt] - (ABOVE - SLACK) ? top + ABOVE : m[qt], down = __builtin_amdgcn_exp2f(m[qt] - to);
                 m[qt] = to;
                 l[qt] *= down;
 #pragma unroll
@@ -221,26 +227,30 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const float p = __builtin_amdgcn_exp2f(sc[h][e] - m[qt]);
-                    l[qt] += p;
-                    const float pv = masked >> (4 * h + e) & 1u ? 0.0f : p * kt.vs[h][e];
-                    pf[qt][4 * h + e] = to_half(pv);
-                    if (!BF) pl[qt][4 * h + e] = (_Float16)(pv - (float)pf[qt][4 * h + e]);
+                for (int e = 0; e < 4; e += 2) {
+                    float pv[2];
+#pragma unroll
+                    for (int u = 0; u < 2; u++) {
+                        const float p = __builtin_amdgcn_exp2f(sc[h][e + u] - m[qt]);
+                        l[qt] += p;
+                        pv[u] = masked >> (4 * h + e + u) & 1u ? 0.0f : p * kt.vs[h][e + u];
+                    }
+                    const int first_part = narrow2<true>(pv[0], pv[1]);
+                    pf[qt][2 * h + (e >> 1)] = first_part;
+                    pl[qt][2 * h + (e >> 1)] = narrow2<true>(pv[0] - __uint_as_float((unsigned)first_part << 16), pv[1] - __uint_as_float((unsigned)first_part & 0xffff0000u));
                 }
         }
-#pragma unroll
-        for (int j = 0; j < DV; j++) {
-            constexpr unsigned PICK[4] = {0x0c040c00u, 0x0c050c01u, 0x0c060c02u, 0x0c070c03u};
+        each_index([&](auto j_tag) {
+            constexpr int J = decltype(j_tag)::value;
             v4i x;
 #pragma unroll
-            for (int u = 0; u < 4; u++) x[u] = to_halves(__builtin_amdgcn_perm((unsigned)kt.v[2 * u + 1][j >> 2], (unsigned)kt.v[2 * u][j >> 2], PICK[j & 3]));
+            for (int u = 0; u < 4; u++) x[u] = to_bfloats<J & 3>(kt.v[2 * u][J >> 2], kt.v[2 * u + 1][J >> 2]);
 #pragma unroll
             for (int qt = 0; qt < QT; qt++) {
-                o[qt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), pf[qt], o[qt][j], 0, 0, 0);
-                if (!BF) o[qt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, x), pl[qt], o[qt][j], 0, 0, 0);
+                o[qt][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, pf[qt]), o[qt][J], 0, 0, 0);
+                o[qt][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, pl[qt]), o[qt][J], 0, 0, 0);
             }
-        }
+        }, std::make_integer_sequence<int, DV>());
     }
 
     // the waves' parts meet: the lane's channels are DV (4 g + e) + j of query r

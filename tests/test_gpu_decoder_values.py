@@ -1,0 +1,96 @@
+"""Attention over the cache and over whole prompts where values and scores are of very different size: rows of zeros, keys that most of the probability
+falls on but whose value adds nothing, channels that one row alone is large in, contexts that are cut and joined.  Against the definition in binary64,
+with tolerances relative to each result.
+
+Over the cache a probability times a step is held in two bfloat16 numbers (half steps of 2^-8 each: 2^-16 of it, whatever its size); scores, sums and the
+exponential are binary32, of which 2^-20 is allowed for the exponential.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+import torch  # noqa: E402
+
+from test_gpu_decoder import BF16, F16, HALF, TINY, U32, P, Plan, attend, gen, offsets, quantised  # noqa: E402, F401
+
+
+def check_close(got, out, size, big, dtype, m, p_half=2.0 ** -16):
+    """size: sum of p |v|; big: the largest sum of |q k| scale; m keys.  Nothing in it grows with values other than the result's own terms."""
+    D = out.shape[-1]
+    rel = p_half + 2.0 ** -20 + (D + 4) * 2 * U32 * big[..., None] + (m + 8) * 2 * U32
+    tol = HALF[dtype] * out.abs() * 1.01 + size * rel + TINY[dtype]
+    err = (got.double().cpu() - out).abs()
+    worst = (err - tol).max().item()
+    assert worst <= 0, (worst, err.max().item(), (err / tol).max().item())
+
+
+def written(P, k, v, page, n):
+    """A plan of one sequence of n positions with these keys and values, and what the cache holds of them, in binary64."""
+    plan = Plan(P, [n], [n], k.shape[1], k.shape[2], page, seed=n)
+    P.cache_write(plan.cache, k.cuda(), v.cuda(), *plan.args, n)
+    return plan, [c * s[..., None] for c, s in (quantised(k), quantised(v))]
+
+
+def run(P, q, k, v, page, dtype, max_len=None):
+    n, m = k.shape[0], q.shape[0]
+    plan, held = written(P, k, v, page, n)
+    got = P.attention_cache(q.cuda(), plan.cache, plan.args[0], None, plan.args[2], m, max_len=max_len or n)
+    seen = torch.arange(n)[None, :] <= n - m + torch.arange(m)[:, None]
+    out, size, big = attend(q.double(), *held, seen, 1 / math.sqrt(q.shape[2]))
+    check_close(got, out, size, big, dtype, n)
+    return got, out
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D,H,G,n,m", [(128, 4, 1, 32, 1), (64, 6, 2, 300, 1), (128, 8, 2, 70, 5), (64, 4, 4, 3000, 20)])
+@pytest.mark.parametrize("size", [1.0, 1e-3, 1e-5, 1e-6])
+def test_attention_cache_beside_value_rows_of_zeros(P, dtype, D, H, G, n, m, size):
+    q = (torch.randn(m, H, D, generator=gen(1)) * 1.5).to(dtype)
+    k, v = (torch.randn(n, G, D, generator=gen(i)) for i in (2, 3))
+    v *= size
+    v[7 % n], v[n // 2:n // 2 + 9, 0] = 0, 0
+    run(P, q, k.to(dtype), v.to(dtype), 16, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nats", [8, 11, 13, 15, 30])
+@pytest.mark.parametrize("size", [1.0, 0.05])
+def test_attention_cache_of_a_key_that_takes_the_probability_and_gives_nothing(P, dtype, nats, size):
+    """The first key's score lies far above the rest, its value is zero."""
+    D, G, n = 128, 2, 512
+    q = torch.randn(1, G, D, generator=gen(1))
+    k, v = (torch.randn(n, G, D, generator=gen(i)) for i in (2, 3))
+    k[0] = q[0] * (nats * math.sqrt(D) / (q[0] ** 2).sum(-1, keepdim=True))
+    v *= size
+    v[0] = 0
+    q, k, v = q.to(dtype), k.to(dtype), v.to(dtype)
+    # (at 30 nats the rest has 2^-34 of the sum: what is left of it is below fp16)
+    got, out = run(P, q, k, v, 32, dtype)
+    if dtype == BF16 or nats < 30:
+        assert got.any()
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("large,small", [(100.0, 1e-2), (3e4, 1e-2), (1e3, 1e-6)])
+def test_attention_cache_channels_that_one_value_row_is_large_in(P, dtype, large, small):
+    """In the other channels that row's codes are 0, and the result is that of the small rows alone."""
+    D, G, n = 64, 2, 200
+    q = torch.randn(3, 2 * G, D, generator=gen(1)).to(dtype)
+    k, v = (torch.randn(n, G, D, generator=gen(i)) for i in (2, 3))
+    v *= small
+    v[90] = 0
+    v[90, :, 5] = large
+    run(P, q, k.to(dtype), v.to(dtype), 64, dtype)
+
+
+def test_attention_cache_values_of_the_largest_bfloat16(P):
+    """Probabilities that run above their reference times steps of 2^121 fit binary32."""
+    D, n = 64, 100
+    k, v = (torch.randn(n, 1, D, generator=gen(i)) for i in (2, 3))
+    k *= torch.linspace(0.1, 2.5, n)[:, None, None]            # later keys have the higher scores
+    v = torch.where(v > 0, 1.0, -1.0) * torch.finfo(BF16).max * 0.9
+    v[::3] *= 2.0 ** -30
+    q = torch.randn(1, 2, D, generator=gen(1)).to(BF16)
+    run(P, q, k.to(BF16), v.to(BF16), 16, BF16)
