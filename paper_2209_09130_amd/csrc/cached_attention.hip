@@ -8,11 +8,11 @@
 // tile's loads ahead of this one's work (64 contexts +-0, 16 drafts +3 %: other waves hide it, and it costs one of three per SIMD); the last block of a row joining the
 // pieces behind a fence (eight times as long: each block's fence writes its XCD's L2 back).
 //
-// Products are 16 x 16 x 32.  S^T = K Q^T is in binary16, in which int8 codes are exact: 1024 + (code + 128) is a code's byte under the exponent byte 0x64, and
-// one packed addition takes 1152 off again; queries of bfloat16 are scaled by a power of two per row into binary16's range.  A lane gets four keys of one
+// Products are 16 x 16 x 32.  S^T = K Q^T is in the queries' type, in which int8 codes are exact.  In binary16 1024 + (code + 128) is a code's byte under the
+// exponent byte 0x64, and one packed addition takes 1152 off again; in bfloat16 a code is the upper half of its binary32.  A lane gets four keys of one
 // query, two such tiles are the eight keys that it needs as the operand of O^T += V^T P^T.  V^T is formed on the way: a lane holds head_dim / 16 neighbouring channels
-// of eight keys, and the byte permute that packs widened codes takes the two halves of a dword from two keys.  The steps of the keys multiply scores (K) and
-// probabilities (V) in binary32.
+// of eight keys, and the byte permute that packs widened codes takes the two halves of a dword from two keys.  The steps of the keys multiply products (K)
+// and probabilities (V) in binary32.
 //
 // O^T += V^T P^T is in bfloat16, in which codes are exact too and whose range is binary32's: p step_v of a key may be any size next to that of another (rows of zeros
 // have step 1, and one large channel makes the step of a row in all of them), so no power of two for all of them would keep binary16 from losing the small
@@ -37,11 +37,16 @@ __device__ __forceinline__ int to_halves(unsigned bytes)
     return __builtin_bit_cast(int, biased - v2h{(_Float16)1152.0f, (_Float16)1152.0f});
 }
 
-// byte BYTE of two dwords as two bfloat16 (a code's binary32 has no more than the upper half)
-template <int BYTE> __device__ __forceinline__ int to_bfloats(int lo, int hi)
+// bytes LO and HI of two dwords as two bfloat16 (a code's binary32 has no more than the upper half)
+template <int LO, int HI> __device__ __forceinline__ int to_bfloats(int lo, int hi)
 {
-    const float a = (float)(int8_t)(lo >> 8 * BYTE), b = (float)(int8_t)(hi >> 8 * BYTE);
+    const float a = (float)(int8_t)(lo >> 8 * LO), b = (float)(int8_t)(hi >> 8 * HI);
     return (int)__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+template <bool BF> __device__ __forceinline__ v4f mma(const v4i &a, const v4i &b, const v4f &c)
+{
+    if constexpr (BF) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
 }
 
 template <int D> struct KeyTile {
@@ -121,8 +126,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
     look_up();
 
     // queries: operand step (i, half) holds channels 64 i + 16 g + 8 half .. + 7
-    v8h qf[QT][D / 32];
-    float factor[QT];                                                 // of a row's scores, as exponents of two
+    v4i qf[QT][D / 32];
     int limit[QT];                                                    // positions below it are seen; from `first` on the word's bits decide if there are drafts
     uint64_t word[QT];
 #pragma unroll
@@ -131,28 +135,10 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
         const char *from = Q + 2 * ((size_t)(s.first_row + token) * ldq + h * D + 16 * g);
         limit[qt] = min(tree ? len : first + token + 1, len);
         word[qt] = tree ? tree[s.first_row + token] : ~0ull;
-        factor[qt] = scale * 1.44269504088896341f;
-        if constexpr (BF) {
-            float x[D / 32][8], top = 0.0f;
 #pragma unroll
-            for (int i = 0; i < D / 32; i++) {
-                widen8<true>(*reinterpret_cast<const v4i *>(from + 128 * (i >> 1) + 16 * (i & 1)), x[i]);
-#pragma unroll
-                for (int e = 0; e < 8; e++) top = __builtin_fmaxf(top, __builtin_fabsf(x[i][e]));
-            }
-            top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
-            top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-            const int shift = top > 0.0f && top < INFINITY ? min(14 - ilogbf(top), 120) : 0;
-            factor[qt] = ldexpf(factor[qt], -shift);
-#pragma unroll
-            for (int i = 0; i < D / 32; i++)
-#pragma unroll
-                for (int e = 0; e < 8; e++) qf[qt][i][e] = (_Float16)ldexpf(x[i][e], shift);
-        } else {
-#pragma unroll
-            for (int i = 0; i < D / 32; i++) qf[qt][i] = __builtin_bit_cast(v8h, *reinterpret_cast<const v4i *>(from + 128 * (i >> 1) + 16 * (i & 1)));
-        }
+        for (int i = 0; i < D / 32; i++) qf[qt][i] = *reinterpret_cast<const v4i *>(from + 128 * (i >> 1) + 16 * (i & 1));
     }
+    const float factor = scale * 1.44269504088896341f;
     v4f o[QT][DV];
     float m[QT], l[QT];
 #pragma unroll
@@ -171,22 +157,25 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
         }
         const int mine[2] = {__builtin_amdgcn_readlane(entries, 2 * i), __builtin_amdgcn_readlane(entries, 2 * i + 1)};
         const KeyTile<D> kt = load_tile<D>(c, mine, head, t * TILE, last, r, g);
-        v8h kf[2][D / 32];
+        v4i kf[2][D / 32];
 #pragma unroll
         for (int h = 0; h < 2; h++)
 #pragma unroll
             for (int i = 0; i < D / 64; i++)
 #pragma unroll
-                for (int half = 0; half < 2; half++) {
-                    v4i x;
+                for (int half = 0; half < 2; half++)
 #pragma unroll
                     for (int e = 0; e < 2; e++) {
-                        const unsigned four = (unsigned)kt.k[h][i][2 * half + e];
-                        x[2 * e] = to_halves(__builtin_amdgcn_perm(0u, four, 0x0c010c00u));
-                        x[2 * e + 1] = to_halves(__builtin_amdgcn_perm(0u, four, 0x0c030c02u));
+                        const int four = kt.k[h][i][2 * half + e];
+                        v4i &to = kf[h][2 * i + half];
+                        if constexpr (BF) {
+                            to[2 * e] = to_bfloats<0, 1>(four, four);
+                            to[2 * e + 1] = to_bfloats<2, 3>(four, four);
+                        } else {
+                            to[2 * e] = to_halves(__builtin_amdgcn_perm(0u, (unsigned)four, 0x0c010c00u));
+                            to[2 * e + 1] = to_halves(__builtin_amdgcn_perm(0u, (unsigned)four, 0x0c030c02u));
+                        }
                     }
-                    kf[h][2 * i + half] = __builtin_bit_cast(v8h, x);
-                }
         v4i pf[QT], pl[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
@@ -195,9 +184,9 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
             for (int h = 0; h < 2; h++) {
                 v4f acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < D / 32; i++) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[h][i], qf[qt][i], acc, 0, 0, 0);
+                for (int i = 0; i < D / 32; i++) acc = mma<BF>(kf[h][i], qf[qt][i], acc);
 #pragma unroll
-                for (int e = 0; e < 4; e++) sc[h][e] = acc[e] * (kt.ks[h][e] * factor[qt]);
+                for (int e = 0; e < 4; e++) sc[h][e] = acc[e] * kt.ks[h][e];
             }
             unsigned masked = 0;                                      // bit 4 h + e
             if (t >= whole || kt.known != 3u) {
@@ -215,6 +204,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int e = 0; e < 4; e++) top = __builtin_fmaxf(top, sc[h][e]);
+            top *= factor;
             if (__any(top > m[qt] - (ABOVE - SLACK))) {
                 top = __builtin_fmaxf(top, __shfl_xor(top, 16, 64));
                 top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
@@ -231,7 +221,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
                     float pv[2];
 #pragma unroll
                     for (int u = 0; u < 2; u++) {
-                        const float p = __builtin_amdgcn_exp2f(sc[h][e + u] - m[qt]);
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[h][e + u], factor, -m[qt]));
                         l[qt] += p;
                         pv[u] = masked >> (4 * h + e + u) & 1u ? 0.0f : p * kt.vs[h][e + u];
                     }
@@ -244,11 +234,11 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
             constexpr int J = decltype(j_tag)::value;
             v4i x;
 #pragma unroll
-            for (int u = 0; u < 4; u++) x[u] = to_bfloats<J & 3>(kt.v[2 * u][J >> 2], kt.v[2 * u + 1][J >> 2]);
+            for (int u = 0; u < 4; u++) x[u] = to_bfloats<J & 3, J & 3>(kt.v[2 * u][J >> 2], kt.v[2 * u + 1][J >> 2]);
 #pragma unroll
             for (int qt = 0; qt < QT; qt++) {
-                o[qt][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, pf[qt]), o[qt][J], 0, 0, 0);
-                o[qt][J] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, x), __builtin_bit_cast(v8bf, pl[qt]), o[qt][J], 0, 0, 0);
+                o[qt][J] = mma<true>(x, pf[qt], o[qt][J]);
+                o[qt][J] = mma<true>(x, pl[qt], o[qt][J]);
             }
         }, std::make_integer_sequence<int, DV>());
     }

@@ -94,3 +94,15 @@ def test_attention_cache_values_of_the_largest_bfloat16(P):
     v[::3] *= 2.0 ** -30
     q = torch.randn(1, 2, D, generator=gen(1)).to(BF16)
     run(P, q, k.to(BF16), v.to(BF16), 16, BF16)
+
+
+@pytest.mark.parametrize("q_large,k_large", [(2.0 ** 30, 1.0), (2.0 ** 60, 2.0 ** 60), (2.0 ** 100, 2.0 ** 100), (2.0 ** -100, 2.0 ** 90)])
+def test_attention_cache_channels_that_queries_or_keys_are_large_in_alone(P, q_large, k_large):
+    """One channel of the queries is large and no key has anything there; one key is large in a channel that no query has.  The scores are those of the
+    other channels."""
+    D, G, n = 128, 2, 100
+    q = torch.randn(2, 2 * G, D, generator=gen(1))
+    k, v = (torch.randn(n, G, D, generator=gen(i)) for i in (2, 3))
+    q[..., 0], k[..., 0] = q_large, 0
+    q[..., 1], k[40, :, 1] = 0, k_large
+    run(P, q.to(BF16), k.to(BF16), v.to(BF16), 16, BF16)
