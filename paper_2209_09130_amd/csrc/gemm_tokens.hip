@@ -1,6 +1,8 @@
 // y[m, n] = act(steps[m] * s_w[n] * sum_k codes[m, k] W[n, k] + bias[n]): the int8 product whose activation rows bring their own steps, on weights in the
 // order of pack_weight_kernel, with a 16-bit result.  The sum is exact in int32; it becomes binary32 (2^-24), is multiplied by the row's step (2^-24) and, in one
-// fused operation with the bias, by the channel's (2^-24), and is rounded once to 16 bits.
+// fused operation with the bias, by the channel's (2^-24), and is rounded once to 16 bits.  In between the row's step is 2^-24 of itself and the channel's
+// 2^24, so that a sum of 2^31 steps of 2^121 (rows of the largest bfloat16) does not overflow where the channel's step brings it back; no other bit
+// changes (the quantiser's steps are 2^-67 or more).
 #include "decoder.h"
 #include "mfma_tile.h"
 
@@ -9,6 +11,7 @@ namespace {
 
 struct TokensEpi { const float *steps, *s_w, *bias; int gelu; };
 
+constexpr float ROW_SHIFT = 0x1p-24f, CHANNEL_SHIFT = 0x1p24f;
 template <bool BF> __device__ __forceinline__ v2i finish4(const v4i &acc, float step, const v4f &sw, const v4f &b, int gelu)
 {
     float y[4];
@@ -88,9 +91,10 @@ void gemm_tokens_kernel(const char *__restrict__ A, const char *__restrict__ Wp,
 #pragma unroll
     for (int t = 0; t < NTW; t++) {
         if (!epi.bias) bb[t] = v4f{0.f, 0.f, 0.f, 0.f};
+        sw[t] *= CHANNEL_SHIFT;
 #pragma unroll
         for (int i = 0; i < MT; i++)
-            *reinterpret_cast<v2i *>(lds + (16 * i + r) * STRIDE + (16 * (NTW * wave + t) + 4 * q) * 2) = finish4<BF>(acc[t][i], step[i], sw[t], bb[t], epi.gelu);
+            *reinterpret_cast<v2i *>(lds + (16 * i + r) * STRIDE + (16 * (NTW * wave + t) + 4 * q) * 2) = finish4<BF>(acc[t][i], step[i] * ROW_SHIFT, sw[t], bb[t], epi.gelu);
     }
     __syncthreads();
     constexpr int CHUNKS = BN / 8;
@@ -199,7 +203,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_tokens_few_kernel(const c
     if (w || r >= M) return;
 #pragma unroll
     for (int u = 1; u < FEW_WAVES; u++) acc += part[u][lane];
-    *reinterpret_cast<v2i *>(out + 2 * ((size_t)r * N + chan)) = finish4<BF>(acc, step, sw, bb, epi.gelu);
+    *reinterpret_cast<v2i *>(out + 2 * ((size_t)r * N + chan)) = finish4<BF>(acc, step * ROW_SHIFT, sw * CHANNEL_SHIFT, bb, epi.gelu);
 }
 
 // K: sixteen blocks of weights a wave.  The codes of a fused call: what leaves a block below 64 KB of LDS

@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 import torch  # noqa: E402
 
-from test_gpu_decoder import BF16, F16, HALF, TINY, U32, P, Plan, attend, gen, offsets, quantised  # noqa: E402, F401
+from test_gpu_decoder import BF16, F16, HALF, TINY, U32, P, Plan, attend, check_linear, gen, offsets, quantised, weights  # noqa: E402, F401
 
 
 def check_close(got, out, size, big, dtype, m, p_half=2.0 ** -16):
@@ -106,3 +106,17 @@ def test_attention_cache_channels_that_queries_or_keys_are_large_in_alone(P, q_l
     q[..., 0], k[..., 0] = q_large, 0
     q[..., 1], k[40, :, 1] = 0, k_large
     run(P, q.to(BF16), k.to(BF16), v.to(BF16), 16, BF16)
+
+
+@pytest.mark.parametrize("M,K", [(1, 512), (9, 512), (70, 512), (40, 8192)])
+def test_linear_of_the_largest_rows(P, M, K):
+    """The sum times the row's step is past binary32, the channel's step brings it back."""
+    x = torch.randn(M, K, generator=gen(M))
+    x = (x / x.abs().amax(1, keepdim=True) * torch.finfo(BF16).max * 0.9).to(BF16)
+    W, s_w = weights(96, K, 3)
+    W = W.abs() * torch.where(x[:1].float() < 0, -1, 1).to(torch.int8)               # the first row's products add up
+    s_w *= 2.0 ** -30
+    got = P.linear_i8_tokens(x.cuda(), P.pack_weight_i8(W.cuda()), s_w.cuda())
+    codes, steps = quantised(x)
+    assert ((codes @ W.double().T) * steps[:, None]).abs().max() > torch.finfo(torch.float32).max
+    check_linear(got, codes, steps, W, s_w, None, False, BF16)
