@@ -10,7 +10,10 @@
 // of eight waves (long documents -1 to -3 %, eight of 300 to 2048 tokens +12 %), two groups of waves that alternate between products and softmax behind barriers (+12 %
 // at head size 64, spills at 128), half tiles with the next scores' products dealt out between the exponentials (+11 % at 64, spills at 128), wave priorities
 // (+-0), the sum of probabilities by dot products (+2 %).
-// Rounding a probability to 16 bits is off by half a step of each, as the result's own rounding is.
+// Rounding a probability to 16 bits is off by half a step of each, as the result's own rounding is.  The reference lies where the type's range is best used: in binary16
+// 2^7 below the scores, so that probabilities run up to 2^15 and have all their bits down to 2^-21 of the largest (half a step is 2^-32 of it below), for
+// the sake of rows whose largest probability falls on a key with little or no value; in bfloat16, whose range is binary32's, 2^24 above them, so that the sums of the largest
+// values stay inside binary32.
 //
 // A key that a query does not see has no part in its result, whatever it holds.  On the diagonal the product multiplies such keys' V by a probability of 0,
 // which an infinity or NaN survives; so a block with a result that is not finite goes over its tiles again, with V's infinities and NaN left out of the
@@ -22,6 +25,7 @@ namespace samp {
 namespace {
 
 constexpr float LOWEST = -3.0e38f, SLACK = 8.0f;
+template <bool BF> constexpr float ABOVE = BF ? 24.0f : -7.0f;
 constexpr int KEYS = 64;
 
 template <bool BF> __device__ __forceinline__ v16f mma32(const v4i &a, const v4i &b, const v16f &c)
@@ -190,9 +194,10 @@ void causal_attention_kernel(const char *__restrict__ Q, const char *__restrict_
 #pragma unroll
                 for (int e = 0; e < 16; e++) top = __builtin_fmaxf(top, sc[h][e]);
             top *= factor;
-            if (__any(top > m + SLACK)) {
+            constexpr float MOVES = SLACK - ABOVE<BF>;
+            if (__any(top > m + MOVES)) {
                 top = __builtin_fmaxf(top, __shfl_xor(top, 32, 64));
-                const float to = top > m + SLACK ? top : m, down = __builtin_amdgcn_exp2f(m - to);   // (a query's result does not depend on the wave's others)
+                const float to = top > m + MOVES ? top + ABOVE<BF> : m, down = __builtin_amdgcn_exp2f(m - to);   // (a query's result does not depend on the wave's others)
                 m = to;
                 l *= down;
 #pragma unroll

@@ -120,3 +120,41 @@ def test_linear_of_the_largest_rows(P, M, K):
     codes, steps = quantised(x)
     assert ((codes @ W.double().T) * steps[:, None]).abs().max() > torch.finfo(torch.float32).max
     check_linear(got, codes, steps, W, s_w, None, False, BF16)
+
+
+def run_causal(P, q, k, v, dtype):
+    """Probabilities have the type's half step, in binary16 at least 2^-32 of the largest (2^-25, the largest being 2^7 or more)."""
+    n, D = q.shape[0], q.shape[2]
+    got = P.attention_causal(q.cuda(), k.cuda(), v.cuda(), None, n)
+    out, size, big = attend(q.double(), k.double(), v.double(), torch.ones(n, n, dtype=torch.bool).tril(), 1 / math.sqrt(D))
+    if dtype == F16:
+        every = v.double().abs().cumsum(0).repeat_interleave(q.shape[1] // v.shape[1], 1) * 2.0 ** -32
+    else:
+        every = torch.zeros(1)
+    rel = HALF[dtype] + 2.0 ** -20 + (D + 4) * 2 * U32 * big[..., None] + (n + 8) * 2 * U32
+    tol = HALF[dtype] * out.abs() * 1.01 + size * rel + TINY[dtype] + every
+    err = (got.double().cpu() - out).abs()
+    assert (err <= tol).all(), ((err - tol).max().item(), (err / tol).max().item())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nats", [8, 11, 13, 15, 17])
+def test_attention_causal_of_a_key_that_takes_the_probability_and_gives_nothing(P, dtype, nats):
+    """The first key's score lies far above the rest for all queries, its value is zero."""
+    D, G, n = 128, 2, 512
+    q, k, v = (torch.randn(n, G, D, generator=gen(i)) for i in (1, 2, 3))
+    q[..., 0] = 4.0
+    k[..., 0] = 0
+    k[0] = 0
+    k[0, :, 0] = nats * math.sqrt(D) / 4.0
+    v[0] = 0
+    run_causal(P, q.to(dtype), k.to(dtype), v.to(dtype), dtype)
+
+
+def test_attention_causal_values_of_the_largest_bfloat16(P):
+    """Probabilities that run above their reference, and sums over keys, times values near the type's largest."""
+    D, n = 64, 200
+    q, k, v = (torch.randn(n, 1, D, generator=gen(i)) for i in (1, 2, 3))
+    k *= torch.linspace(0.1, 2.5, n)[:, None, None]
+    v = torch.where(v > -1, 1.0, -1.0) * torch.finfo(BF16).max * 0.9
+    run_causal(P, q.to(BF16), k.to(BF16), v.to(BF16), BF16)
