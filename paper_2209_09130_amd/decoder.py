@@ -47,6 +47,15 @@ def _refuse(why: str):
     raise SampError(-1, why)
 
 
+# ctypes passes the low 32 bits of a larger number without a word
+_INT_MAX = 2 ** 31 - 1
+
+
+def _most(n: int) -> int:
+    """A maximum that the host counts with, which may be more than there is: one past int32 counts as that, one below zero is for the entry to refuse."""
+    return max(-1, min(int(n), _INT_MAX))
+
+
 def _device(t: torch.Tensor) -> int:
     if not t.is_cuda:
         _refuse(f"tensors must be on the GPU ({t.device})")
@@ -87,6 +96,8 @@ def _rows2(what: str, x: torch.Tensor) -> Tuple[int, int, int, int]:
     if x.dim() != 2 or x.dtype not in _TYPES or (x.stride(1) != 1 and x.shape[1] > 1):
         _refuse(f"{what}: an fp16 or bfloat16 matrix with dense rows is needed, not {x.dtype} {tuple(x.shape)} {x.stride()}")
     M, K = x.shape
+    if M > _INT_MAX or K > _INT_MAX:
+        _refuse(f"{what}: {M} x {K} is more than int32 counts")
     return x.data_ptr(), x.stride(0) if M > 1 else K, M, K
 
 
@@ -190,6 +201,8 @@ def _places(device: int, table: torch.Tensor, cu: Optional[torch.Tensor], lens: 
     if len(shape) != 2:
         _refuse("the page table is [sequences, pages of a sequence]")
     B, width = shape
+    if B > _INT_MAX or width > _INT_MAX:
+        _refuse(f"the page table: {B} x {width} is more than int32 counts")
     return (_flat("table", table, torch.int32, device), width, _flat("cu", cu, torch.int32, device, B + 1) if cu is not None else 0,
             _flat("lens", lens, torch.int32, device, B), B)
 
@@ -207,7 +220,7 @@ def cache_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, table: torch.T
     t, width, pcu, plens, B = _places(device, table, cu, lens)
     rows = shape[0]
     if rows and B:
-        rc = _fn("samp_cache_write")(cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, int(max_new), rows, _raw_stream(device))
+        rc = _fn("samp_cache_write")(cache.address, pk, ldk, pv, ldv, _TYPES[k.dtype], t, width, pcu, plens, B, _most(max_new), rows, _raw_stream(device))
         if rc:
             _raise(rc)
 
@@ -228,7 +241,7 @@ def cache_read(cache: KVCache, table: torch.Tensor, cu: Optional[torch.Tensor], 
         size = rows * cache.kv_heads * cache.head_dim
         k, v = _flat("out", out[0], dtype, device, size), _flat("out", out[1], dtype, device, size)
     if rows and B:
-        rc = _fn("samp_cache_read")(cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, int(max_rows), rows, _raw_stream(device))
+        rc = _fn("samp_cache_read")(cache.address, k, v, _TYPES[dtype], t, width, pcu, plens, B, _most(max_rows), rows, _raw_stream(device))
         if rc:
             _raise(rc)
     return out
@@ -254,7 +267,7 @@ def attention_cache(q: torch.Tensor, cache: KVCache, table: torch.Tensor, cu: Op
     else:
         to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows and B:
-        max_new, max_len = int(max_new), width * cache.page_len if max_len is None else int(max_len)
+        max_new, max_len = _most(max_new), _most(width * cache.page_len if max_len is None else max_len)
         need = _workspace_bytes("samp_attention_cache_workspace_bytes", rows, B, heads, cache.kv_heads, dim, max_new, max_len)
         ws = q.new_empty((need,), dtype=torch.uint8) if need else None
         rc = _fn("samp_attention_cache")(at, ld, _TYPES[q.dtype], heads, cache.address, t, width, pcu, plens, B, max_new, max_len, rows,
@@ -282,7 +295,7 @@ def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Opti
         to = _flat("out", out, dtype, device, rows * heads * dim)
     if rows == 0:
         return out
-    max_len = int(max_len)
+    max_len = _most(max_len)
     if cu is not None:
         B, pcu = cu.numel() - 1, _flat("cu", cu, torch.int32, device)
     else:

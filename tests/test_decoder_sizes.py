@@ -1,0 +1,59 @@
+"""Sizes past int32 at the decoder's Python entry points: what the C entry cannot count is refused or counts as its largest, never as its low 32 bits."""
+import pytest
+import torch
+
+import paper_2209_09130_amd as P
+from paper_2209_09130_amd import decoder as D
+
+from test_gpu_decoder import BF16, F16, Plan, gen, offsets
+
+
+def meta(*shape, dtype):
+    return torch.empty(shape, dtype=dtype, device="meta")
+
+
+def test_shapes_past_int32_are_refused():
+    for shape in ((2 ** 32 + 5, 8), (2 ** 31, 8), (1, 2 ** 32 + 64)):
+        with pytest.raises(P.SampError, match="int32"):
+            D._rows2("x", meta(*shape, dtype=torch.float16))
+    for shape in ((1, 2 ** 32 + 1), (2 ** 31, 1)):
+        with pytest.raises(P.SampError, match="int32"):
+            D._places(-1, meta(*shape, dtype=torch.int32), None, meta(shape[0], dtype=torch.int32))
+
+
+def test_maxima_past_int32_count_as_its_largest():
+    assert [D._most(n) for n in (1, 2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 0, -3, -(2 ** 32) + 5)] == [1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 0, -1, -1]
+
+
+@pytest.mark.gpu
+def test_calls_with_maxima_past_int32():
+    lens, H, G, dim = [70, 30], 4, 2, 64
+    large = 2 ** 32 + 1
+    plan = Plan(P, lens, lens, G, dim, 16)
+    k, v = (torch.randn(100, G, dim, generator=gen(i)).half().cuda() for i in (1, 2))
+    q = torch.randn(100, H, dim, generator=gen(3)).half().cuda()
+    P.cache_write(plan.cache, k, v, *plan.args, large)
+    want = P.cache_read(plan.cache, *plan.args, 70, 100, F16)
+    assert torch.isfinite(want[0]).all() and torch.isfinite(want[1]).all()
+    got = P.cache_read(plan.cache, *plan.args, large, 100, F16)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert torch.equal(P.attention_causal(q, k, v, plan.args[1], large), P.attention_causal(q, k, v, plan.args[1], 70))
+    assert torch.equal(P.attention_cache(q, plan.cache, *plan.args, large, max_len=70), P.attention_cache(q, plan.cache, *plan.args, 70, max_len=70))
+    assert torch.equal(P.attention_cache(q, plan.cache, *plan.args, 70, max_len=large), P.attention_cache(q, plan.cache, *plan.args, 70, max_len=70))
+    for bad in (0, -3, -(2 ** 32) + 70):
+        with pytest.raises(P.SampError):
+            P.attention_causal(q, k, v, plan.args[1], bad)
+        with pytest.raises(P.SampError):
+            P.cache_write(plan.cache, k, v, *plan.args, bad)
+
+
+@pytest.mark.gpu
+def test_a_page_table_with_room_past_int32():
+    """max_len None is what the table has room for, here 2^31 positions: the same cut, and so the same bytes, as of the largest int32."""
+    plan = Plan(P, [1500], [1], 2, 128, 1024)
+    plan.fill(P, BF16, 4)
+    q = torch.randn(1, 4, 128, generator=gen(3)).bfloat16().cuda()
+    table = torch.full((1, 2 ** 21), -1, dtype=torch.int32, device="cuda")
+    table[:, :2] = plan.args[0]
+    want = P.attention_cache(q, plan.cache, plan.args[0], None, plan.args[2], 1, max_len=2 ** 31 - 1)
+    assert torch.equal(P.attention_cache(q, plan.cache, table, None, plan.args[2], 1), want)
