@@ -348,7 +348,7 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(KvRows rows, int heads
                                                                narrow2<BF>(y[4] * by, y[5] * by), narrow2<BF>(y[6] * by, y[7] * by)};
 }
 
-int row_tiles(int rows) { return rows > 16 ? 2 : 1; }
+int row_tiles(long rows) { return rows > 16 ? 2 : 1; }
 
 template <bool BF, int D>
 hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c, const KvRows &rows, float scale, const uint64_t *tree, Cut cut,
@@ -367,17 +367,22 @@ hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c
 }  // namespace
 
 // Pieces of so many tiles that 512 blocks have them all, but no less than four tiles (a tile for each wave; eight where a block has two row tiles), below which
-// the blocks' own latencies count for more than their number, and no more than 48, so that blocks of contexts of different lengths end together; none at all
-// where a context has at most sixteen tiles more than a piece.  Joining costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
+// the blocks' own latencies count for more than their number, and no more than 48, so that blocks of contexts of different lengths end together: 48 for 512 blocks
+// without a cut, more in proportion where there are more.  None at all where a context has at most sixteen tiles more than a piece, or where blocks of two row
+// tiles (many new tokens) are 512 without and no context has more than a million positions (some 20 ms of one block): their partial results are what costs then (us and MB of them, in pieces of 48 / uncut, 32 query heads on 8 of 128: 512 tokens of a
+// context of 4500 114 and 24 / 93, of 64 contexts up to 4500 4580 and 1560 / 4440, 128 tokens of 16 contexts up to 8192 504 and 195 / 433; one token of 128 contexts up
+// to 8192 223 in pieces of 48 or 96, 231 to 235 uncut).  Joining costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
 // key heads of 128, one context of 4000 8.5 / 9.2 / 11.7 / 16.0 / 23.9 / 36; 64 of 17 to 8192 176 / 139 / 124 / 120 / 121 / 131; 32 of 500 to 1000 21.7 / 19.4 /
 // 18.0 / 15.3 (uncut); 16 drafts on 8 contexts of 300 to 2100, 16 heads of 64, 17.3 / 14.4 / 14.0 / 15.6 / 21.7; one context of 8192, five tokens of 28 heads on 4,
 // 18.1 / 15.3 / 16.6 / 21.6 / 32.0 / 91; 64 contexts of 100 to 300, 12 heads of 64, 15.8 / 13.8 / 10.0 (uncut)
 Cut cached_attention_cut(int batch, int heads, int kv_heads, int max_new, int max_len)
 {
-    const int most = max_new * (heads / kv_heads), qt = row_tiles(most);
+    const long most = (long)max_new * (heads / kv_heads), qt = row_tiles(most);
     const long items = (long)batch * kv_heads * ((most + 16 * qt - 1) / (16 * qt)), tiles = (max_len + (long)TILE - 1) / TILE;
+    if (items >= 512 && qt == 2 && tiles <= 32768) return Cut{1, (int)tiles};
+    const long longest = items > 512 ? 48 * items / 512 : 48;
     long piece = tiles * items / 512;
-    if (piece > 48) piece = 48;
+    if (piece > longest) piece = longest;
     if (piece < 4 * qt) piece = 4 * qt;
     if (tiles <= piece + 16) return Cut{1, (int)tiles};
     long splits = (tiles + piece - 1) / piece;

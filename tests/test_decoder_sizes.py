@@ -1,4 +1,6 @@
 """Sizes past int32 at the decoder's Python entry points: what the C entry cannot count is refused or counts as its largest, never as its low 32 bits."""
+import os
+
 import pytest
 import torch
 
@@ -23,6 +25,23 @@ def test_shapes_past_int32_are_refused():
 
 def test_maxima_past_int32_count_as_its_largest():
     assert [D._most(n) for n in (1, 2 ** 31 - 1, 2 ** 31, 2 ** 32 + 1, 0, -3, -(2 ** 32) + 5)] == [1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 0, -1, -1]
+
+
+def partial_bytes(batch, new, heads, kv_heads, dim, max_len):
+    if not os.path.exists(P.lib_path()):
+        from paper_2209_09130_amd import build as B
+        B.build(force=True)
+    return D._fn("samp_attention_cache_workspace_bytes")(batch * new, batch, heads, kv_heads, dim, new, max_len)
+
+
+def test_calls_that_fill_the_chip_without_a_cut_have_few_partial_results():
+    """Many new tokens have none; one token of many contexts has pieces in proportion; one context is cut as before."""
+    for batch, new, heads, kv_heads, dim, max_len in ((64, 512, 32, 8, 128, 4500), (16, 128, 32, 8, 128, 8192), (1, 512, 32, 8, 128, 4500), (8, 2000, 64, 4, 128, 1 << 20)):
+        assert partial_bytes(batch, new, heads, kv_heads, dim, max_len) == 0
+    assert partial_bytes(4096, 1, 32, 8, 128, 131072) == 4096 * 32 * 2 * 130 * 4      # 4096 tiles in pieces of at most 48 * 64
+    assert partial_bytes(128, 1, 32, 8, 128, 8192) <= 128 * 32 * 3 * 130 * 4 + 256
+    assert partial_bytes(1, 1, 32, 8, 128, 4000) == 32 * 32 * 130 * 4            # 125 tiles, four of them a piece
+    assert partial_bytes(64, 1, 32, 8, 128, 8192) == 64 * 32 * 6 * 130 * 4       # 256 tiles in pieces of at most 48
 
 
 @pytest.mark.gpu
