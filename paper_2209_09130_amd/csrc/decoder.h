@@ -115,8 +115,7 @@ __device__ __forceinline__ SeqRows seq_rows(const KvRows &r, int b, int page_shi
 hipError_t launch_quantize_tokens(const void *x, long ldx, bool bf16, int M, int K, int8_t *codes, float *steps, hipStream_t st);
 hipError_t launch_gemm_i8_tokens(const int8_t *codes, const float *steps, const int8_t *Wp, const float *s_w, const float *bias, bool gelu, void *out,
                                  bool bf16, int M, int N, int K, hipStream_t st);
-// few rows: both in one launch
-bool linear_tokens_is_fused(int M, int K);
+// both in one launch (tokens_fused())
 hipError_t launch_linear_few(const void *x, long ldx, bool bf16, const int8_t *Wp, const float *s_w, const float *bias, bool gelu, void *out, int M, int N, int K,
                              hipStream_t st);
 hipError_t launch_cache_write(const KvCache &cache, const void *k, long ldk, const void *v, long ldv, bool bf16, int head_dim, const KvRows &rows,

@@ -4,6 +4,7 @@
 // 2^24, so that a sum of 2^31 steps of 2^121 (rows of the largest bfloat16) does not overflow where the channel's step brings it back; no other bit
 // changes (the quantiser's steps are 2^-67 or more).
 #include "decoder.h"
+#include "decoder_rules.h"
 #include "mfma_tile.h"
 
 namespace samp {
@@ -123,7 +124,6 @@ hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, 
 // bits and every block quantises them for itself while its weights are on the way, into LDS (rows 16 bytes more than K apart, so that the sixteen rows of an
 // operand read lie in different banks), which saves a launch.  Eight, four, two or one waves share a row, the fewer the more rows there are.  One row, 4096 -> 6144,
 // 25 MB of weights: 6.3 us in the chain of launches (two kernels 1.9 + 7.2); with every lane quantising what it multiplies, sixteen times over, 8.5.
-constexpr int FEW_WAVES = 8;
 struct FewRows { const void *x; long ld; const float *steps; };        // FUSED: 16-bit rows, ld values apart; else codes, K apart, and their steps
 template <bool BF, bool FUSED, int KB>
 __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_tokens_few_kernel(const char *__restrict__ Wp, int K, int N, int M, int sharers, FewRows in, TokensEpi epi,
@@ -206,54 +206,30 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_tokens_few_kernel(const c
     *reinterpret_cast<v2i *>(out + 2 * ((size_t)r * N + chan)) = finish4<BF>(acc, step * ROW_SHIFT, sw * CHANNEL_SHIFT, bb, epi.gelu);
 }
 
-// K: sixteen blocks of weights a wave.  The codes of a fused call: what leaves a block below 64 KB of LDS
-constexpr int FEW_ROWS = 16, FEW_K = 16 * 64 * FEW_WAVES, FEW_CODES = 54 << 10;
 template <bool BF, bool FUSED>
 hipError_t launch_few(const FewRows &in, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, hipStream_t st)
 {
-    const int kb = (K / 64 + FEW_WAVES - 1) / FEW_WAVES, sharers = M == 1 ? 8 : M == 2 ? 4 : M <= 4 ? 2 : 1;
-    auto kern = kb <= 2 ? gemm_tokens_few_kernel<BF, FUSED, 2> : kb <= 4 ? gemm_tokens_few_kernel<BF, FUSED, 4> : kb <= 8 ? gemm_tokens_few_kernel<BF, FUSED, 8>
+    const int kb = tokens_few_blocks(K), sharers = M == 1 ? 8 : M == 2 ? 4 : M <= 4 ? 2 : 1;
+    auto kern = kb == 2 ? gemm_tokens_few_kernel<BF, FUSED, 2> : kb == 4 ? gemm_tokens_few_kernel<BF, FUSED, 4> : kb == 8 ? gemm_tokens_few_kernel<BF, FUSED, 8>
                         : gemm_tokens_few_kernel<BF, FUSED, 16>;
     hipLaunchKernelGGL(kern, dim3(N / 16), dim3(64 * FEW_WAVES), FUSED ? M * (K + 16) : 0, st, (const char *)Wp, K, N, M, sharers, in, epi, (char *)out);
     return hipGetLastError();
 }
 
-// ---- which kernel ------------------------------------------------------------------------------------
-// The tile whose cost is least: its time for K = 4096 where the chip is full of it (small ones: where it is not), times the rounds of blocks (the mean of
-// whole rounds and their fraction).  Over 36 random shapes (17 to 16384 rows, K 256 to 8192, N 256 to 8192) the choice costs 4 % on average against the best
-// of eleven tiles and depths.  us, M x N x K, the tiles in the order of the list: 64 x 4096 x 4096 7.5 / 8.1 / 11.8 / 16.3 / 21.7; 512 x 4096 x 4096 39 / 15.5 /
-// 13.1 / 17.1 / 22.5; 2048 x 4096 x 4096 148 / 76 / 73 / 34 / 39; 8192 x 4096 x 4096 583 / 296 / 290 / 129 / 126; 4096 x 11008 x 4096 781 / 396 / 400 / 188 / 181.
-// What bounds the large ones is how fast a CU gets its operands from L2: a stage of 128 bytes of K is 32 KB (8 x 2) or 40 KB (8 x 3) for 512 and 768 clocks of matrix
-// work, 62 and 52 bytes per clock.
-// Bands: 2048 x 4096 x 4096 on 8 x 2 tiles, one row tile a band / eight 41.6 / 33.8, 8192 x 4096 x 4096 on 8 x 3, one / four / eight 139 / 126 / 136.
-struct TokensTile { int mt, ntw; float us; };
-constexpr TokensTile TOKENS_TILES[] = {{2, 1, 7.3f}, {4, 1, 7.8f}, {4, 2, 13.0f}, {8, 2, 17.0f}, {8, 3, 23.0f}};
-int tokens_tile(int M, int N)
-{
-    int best = 0;
-    float least = 0.0f;
-    for (int i = 0; i < 5; i++) {
-        const long bm = 16 * TOKENS_TILES[i].mt, bn = 64 * TOKENS_TILES[i].ntw, blocks = (M + bm - 1) / bm * ((N + bn - 1) / bn);
-        const float rounds = blocks <= 256 ? 1.0f : 0.5f * ((float)((blocks + 255) / 256) + (float)blocks / 256.0f), cost = rounds * TOKENS_TILES[i].us;
-        if (i == 0 || cost < least) { best = i; least = cost; }
-    }
-    return best;
-}
-
+// ---- which kernel: decoder_rules.h ---------------------------------------------------------------------
 template <bool BF>
 hipError_t gemm_tokens(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, void *out, int M, int N, int K, hipStream_t st)
 {
-    if (M <= FEW_ROWS && K <= FEW_K) return launch_few<BF, false>(FewRows{A, K, epi.steps}, Wp, epi, out, M, N, K, st);
-    // four stages in flight instead of two (64 x 4096 x 4096 7.5 / 9.7) where no more is left over for it, and always on the smallest tile (85 x 1312 x 8064 12.3 / 17.2;
-    // 619 x 2624 x 3328 on 4 x 2 tiles, 256 left over, 14.0 / 12.3)
-    const bool deep = K >= 512 && K % 512 < 256;
-    switch (tokens_tile(M, N)) {
-    case 0: return K >= 512 ? launch_tile<BF, 2, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 2, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
-    case 1: return deep ? launch_tile<BF, 4, 1, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 4, 1, 2>(A, Wp, epi, out, M, N, K, 8, st);
-    case 2: return deep ? launch_tile<BF, 4, 2, 4>(A, Wp, epi, out, M, N, K, 8, st) : launch_tile<BF, 4, 2, 2>(A, Wp, epi, out, M, N, K, 8, st);
-    case 3: return launch_tile<BF, 8, 2, 2>(A, Wp, epi, out, M, N, K, 8, st);
+    if (tokens_few(M, K)) return launch_few<BF, false>(FewRows{A, K, epi.steps}, Wp, epi, out, M, N, K, st);
+    const int tile = tokens_tile(M, N), band = tokens_band(tile);
+    const bool deep = tokens_depth(tile, K) == 4;
+    switch (tile) {
+    case 0: return deep ? launch_tile<BF, 2, 1, 4>(A, Wp, epi, out, M, N, K, band, st) : launch_tile<BF, 2, 1, 2>(A, Wp, epi, out, M, N, K, band, st);
+    case 1: return deep ? launch_tile<BF, 4, 1, 4>(A, Wp, epi, out, M, N, K, band, st) : launch_tile<BF, 4, 1, 2>(A, Wp, epi, out, M, N, K, band, st);
+    case 2: return deep ? launch_tile<BF, 4, 2, 4>(A, Wp, epi, out, M, N, K, band, st) : launch_tile<BF, 4, 2, 2>(A, Wp, epi, out, M, N, K, band, st);
+    case 3: return launch_tile<BF, 8, 2, 2>(A, Wp, epi, out, M, N, K, band, st);
     }
-    return launch_tile<BF, 8, 3, 2>(A, Wp, epi, out, M, N, K, 4, st);
+    return launch_tile<BF, 8, 3, 2>(A, Wp, epi, out, M, N, K, band, st);
 }
 
 }  // namespace
@@ -265,7 +241,6 @@ hipError_t launch_gemm_i8_tokens(const int8_t *codes, const float *steps, const 
     return bf16 ? gemm_tokens<true>(codes, Wp, epi, out, M, N, K, st) : gemm_tokens<false>(codes, Wp, epi, out, M, N, K, st);
 }
 
-bool linear_tokens_is_fused(int M, int K) { return M <= FEW_ROWS && K <= FEW_K && M * (K + 16) <= FEW_CODES; }
 hipError_t launch_linear_few(const void *x, long ldx, bool bf16, const int8_t *Wp, const float *s_w, const float *bias, bool gelu, void *out, int M, int N, int K,
                              hipStream_t st)
 {

@@ -1,6 +1,7 @@
 // Rows that bring their own steps: activation rows quantised as they come, keys and values quantised as they are written to the cache, and the cache
 // read back.  All of them move each byte once; what bounds them is HBM, and for a few rows the launch.
 #include "decoder.h"
+#include "decoder_rules.h"
 
 namespace samp {
 namespace {
@@ -197,14 +198,11 @@ dim3 cache_grid(const KvCache &c, const KvRows &r, int log2, int passes)
     const int tokens = passes << log2;
     return dim3((unsigned)((2 * c.kv_heads + (16 >> log2) - 1) / (16 >> log2)), (unsigned)((r.max_rows + tokens - 1) / tokens), (unsigned)r.batch);
 }
-// Four rows a lane group where there are blocks enough: one / four, 16 prompts of 900 to 2048 tokens written 36.2 / 33.3 us, read 31.0 / 25.3; a chunk of 4 x 512 tokens
-// has 2048 x 8 rows and is better off with one (5.4 us).
-int cache_passes(const KvCache &c, const KvRows &r) { return (long)r.rows * c.kv_heads >= 32768 ? 4 : 1; }
 
 template <bool BF, int D>
 hipError_t cache_write(const KvCache &c, const void *k, long ldk, const void *v, long ldv, const KvRows &r, hipStream_t st)
 {
-    const int n = tokens_log2_for(r.max_rows), passes = cache_passes(c, r);
+    const int n = tokens_log2_for(r.max_rows), passes = cache_passes(r.rows, c.kv_heads);
     auto kern = passes == 4 ? cache_write_kernel<BF, D, 4> : cache_write_kernel<BF, D, 1>;
     hipLaunchKernelGGL(kern, cache_grid(c, r, n, passes), dim3(256), 0, st, c, (const char *)k, ldk, (const char *)v, ldv, r, n);
     return hipGetLastError();
@@ -213,7 +211,7 @@ hipError_t cache_write(const KvCache &c, const void *k, long ldk, const void *v,
 template <bool BF, int D>
 hipError_t cache_read(const KvCache &c, void *k, void *v, const KvRows &r, hipStream_t st)
 {
-    const int n = tokens_log2_for(r.max_rows), passes = cache_passes(c, r);
+    const int n = tokens_log2_for(r.max_rows), passes = cache_passes(r.rows, c.kv_heads);
     auto kern = passes == 4 ? cache_read_kernel<BF, D, 4> : cache_read_kernel<BF, D, 1>;
     hipLaunchKernelGGL(kern, cache_grid(c, r, n, passes), dim3(256), 0, st, c, (char *)k, (char *)v, r, n);
     return hipGetLastError();
