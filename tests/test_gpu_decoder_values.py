@@ -13,13 +13,15 @@ pytestmark = pytest.mark.gpu
 
 import torch  # noqa: E402
 
+import test_gpu_decoder as basic  # noqa: E402
 from test_gpu_decoder import BF16, F16, HALF, TINY, U32, P, Plan, attend, check_linear, gen, offsets, quantised, weights  # noqa: E402, F401
 
 
 def check_close(got, out, size, big, dtype, m, p_half=2.0 ** -16):
-    """size: sum of p |v|; big: the largest sum of |q k| scale; m keys.  Nothing in it grows with values other than the result's own terms."""
+    """size: sum of p |v|; big: the largest sum of |q k| scale; m keys.  Nothing in it grows with values other than the result's own terms.  A lane adds one in 16
+    probabilities; a product adds 32 keys of one tile in four, twice; then two lanes' exchanges, four waves and at most 64 pieces are added."""
     D = out.shape[-1]
-    rel = p_half + 2.0 ** -20 + (D + 4) * 2 * U32 * big[..., None] + (m + 8) * 2 * U32
+    rel = p_half + 2.0 ** -20 + (D + 4) * 2 * U32 * big[..., None] + (m / 16 + 128) * 2 * U32
     tol = HALF[dtype] * out.abs() * 1.01 + size * rel + TINY[dtype]
     err = (got.double().cpu() - out).abs()
     worst = (err - tol).max().item()
@@ -158,3 +160,48 @@ def test_attention_causal_values_of_the_largest_bfloat16(P):
     k *= torch.linspace(0.1, 2.5, n)[:, None, None]
     v = torch.where(v > -1, 1.0, -1.0) * torch.finfo(BF16).max * 0.9
     run_causal(P, q.to(BF16), k.to(BF16), v.to(BF16), BF16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("n,max_len", [(4100, 4100), (5000, 5000), (9000, 9000), (9000, 1), (700, 100000), (2049, 8192)])
+@pytest.mark.parametrize("D,H,G,m", [(128, 8, 1, 1), (64, 4, 4, 40)])
+def test_attention_cache_counts_each_key_once(P, dtype, n, max_len, D, H, G, m):
+    """Queries of zeros: every key a token sees has the same probability, so the result is a count of keys, by tile (a lost or doubled tile is a third of a
+    channel) or by place in the tile (one in some seventy of 32 channels)."""
+    j = torch.arange(n)
+    k = torch.randn(n, G, D, generator=gen(n)).to(dtype)
+    q = torch.zeros(m, H, D, dtype=dtype)
+    for channel in (j // 32 % D, j % D):
+        v = torch.zeros(n, G, D)
+        v[j, :, channel] = 1.0
+        got, out = run(P, q, k, v.to(dtype), 64, dtype, max_len)
+        seen = torch.stack([torch.bincount(channel[:n - m + 1 + i], minlength=D) / (n - m + 1 + i) for i in range(m)]).double()
+        assert (out - seen[:, None]).abs().max() < 1e-6
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("lens,new,H,G,D,page,drafts,max_len", [
+    ([5000, 3, 2049], [1, 2, 1], 8, 2, 128, 64, False, None), ([4100], [40], 4, 4, 64, 16, False, None), ([900, 40], [1, 1], 8, 1, 128, 32, False, 100000),
+    ([9000, 40], [1, 1], 8, 1, 128, 32, False, 1), ([1500], [32], 4, 1, 128, 16, True, None), ([200, 64, 33], [64, 17, 1], 8, 4, 64, 32, True, None),
+    ([700, 300, 12], [600, 290, 12], 16, 8, 64, 32, False, None), ([2500, 1800], [300, 1], 32, 8, 128, 64, False, None)])
+def test_attention_cache_within_its_own_roundings(P, monkeypatch, lens, new, H, G, D, page, drafts, max_len, dtype):
+    """No part of the tolerance grows with values other than a result's own terms, so that a tile left out of a long context shows."""
+    monkeypatch.setattr(basic, "check_attention", lambda got, out, size, big, t, p_type, m, vmax: check_close(got, out, size, big, t, m))
+    basic.run_cached(P, lens, new, H, G, D, page, dtype, basic.tree_words(new, 3) if drafts else None, seed=9, max_len=max_len)
+
+
+def test_the_tolerance_sees_a_tile_left_out():
+    """The check itself, on the CPU: where the keys count alike, the definition without one tile of 32 of them is not within it."""
+    n, D = 9000, 128
+    q, k, v = (torch.randn(m, 1, D, generator=gen(m)).double() for m in (1, n, n + 1))
+    q, v = q * 0.1, v[:n]
+    v[..., 0] *= 30
+    everything = torch.ones(1, n, dtype=torch.bool)
+    out, size, big = attend(q, k, v, everything, 1 / math.sqrt(D))
+    for dtype in (F16, BF16):
+        check_close(out.to(dtype), out, size, big, dtype, n)
+    everything[:, 4000:4032] = False
+    less = attend(q, k, v, everything, 1 / math.sqrt(D))[0]
+    for dtype in (F16, BF16):
+        with pytest.raises(AssertionError):
+            check_close(less.to(dtype), out, size, big, dtype, n)
