@@ -448,8 +448,8 @@ SAMP_API int samp_gemm_i8_tokens_packed(const int8_t *codes, const float *steps,
                                         uint16_t *out, int32_t type, int32_t M, int32_t N, int32_t K, void *stream);
 
 /* The two in one call, x [M,K] -> out [M,N]: the bytes that samp_quantize_tokens and samp_gemm_i8_tokens_packed give.
- * workspace dev, 256-byte aligned; calls that share one must be stream-ordered.  Bytes: 0 where none is needed (NULL will do), and for arguments that the
- * call refuses.                                                                                      */
+ * workspace dev, 256-byte aligned; calls that share one must be stream-ordered.  Bytes: 0 where none is needed for any N (NULL will do), and for arguments that
+ * the call refuses.                                                                                      */
 SAMP_API size_t samp_linear_i8_tokens_workspace_bytes(int32_t M, int32_t K);
 SAMP_API int samp_linear_i8_tokens(const uint16_t *x, int64_t ldx, int32_t type, const int8_t *Wp, const float *s_w, const float *bias, int32_t gelu,
                                    uint16_t *out, int32_t M, int32_t N, int32_t K, void *workspace, size_t workspace_bytes, void *stream);

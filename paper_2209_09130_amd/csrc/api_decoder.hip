@@ -109,7 +109,7 @@ int samp_gemm_i8_tokens_packed(const int8_t *codes, const float *steps, const in
 
 size_t samp_linear_i8_tokens_workspace_bytes(int32_t M, int32_t K)
 {
-    if (check_tokens(M, 16, K) || tokens_fused(M, K)) return 0;
+    if (check_tokens(M, 16, K) || tokens_fused_any(M, K)) return 0;
     return up((size_t)M * K) + up((size_t)M * sizeof(float));
 }
 
@@ -120,7 +120,7 @@ int samp_linear_i8_tokens(const uint16_t *x, int64_t ldx, int32_t type, const in
     if (int rc = check_tokens(M, N, K)) return rc;
     if (int rc = check_product(Wp, s_w, bias, out)) return rc;
     if (int rc = check_rows("x", x, ldx, K)) return rc;
-    if (tokens_fused(M, K)) {
+    if (tokens_fused(M, N, K)) {
         HIP_TRY(launch_linear_few(x, ldx, type == SAMP_TYPE_BF16, Wp, s_w, bias, gelu != 0, out, M, N, K, (hipStream_t)stream));
         return SAMP_OK;
     }

@@ -13,9 +13,18 @@ inline int tokens_few_blocks(int K)
     const int blocks = (K / 64 + FEW_WAVES - 1) / FEW_WAVES;
     return blocks <= 2 ? 2 : blocks <= 4 ? 4 : blocks <= 8 ? 8 : 16;
 }
-// With the quantiser in the same launch: where the codes leave a block below 64 KB of LDS.
+// With the quantiser in the same launch, which saves one, or in front.  Every block (16 channels) reads and quantises all rows: one round of its waves for up to eight rows,
+// two for more, which only pays where rows are short and blocks are no more than one for each CU; and a row of more than 4096 values takes so many registers that a
+// CU holds one block.  us in a chain of launches, weights from memory, K x N, one launch / two: 4096 x 4096 1 row 6.1 / 6.9, 8 7.0 / 7.4, 12 7.9 / 7.7; 4096 x 8192 1 9.0 / 9.4,
+// 8 9.9 / 10.1, 12 11.3 / 10.8; 3328 x 6144 8 8.5 / 8.7, 16 11.3 / 10.1; 2048 x 4096 12 5.4 / 5.9, 16 5.9 / 6.1; 2048 x 8192 12 7.4 / 7.3, 16 8.2 / 7.6;
+// 5120 x 4096 1 7.9 / 7.9, 8 8.6 / 8.6, 9 9.8 / 8.7; 5120 x 5120 1 12.7 / 10.8, 8 14.2 / 12.6; 8192 x 2048 1 7.5 / 7.8, 6 8.9 / 8.6; 8192 x 8192 1 18.4 / 16.3.  (Alone, from
+// the host, the second launch costs another 3 us, so a draw goes to one.)  The codes have to leave a block below 64 KB of LDS.
 constexpr int FEW_CODES = 54 << 10;
-inline bool tokens_fused(int M, int K) { return tokens_few(M, K) && M * (K + 16) <= FEW_CODES; }
+inline bool tokens_fused(int M, int N, int K)
+{
+    return tokens_few(M, K) && M * (K + 16) <= FEW_CODES && (M <= 8 ? K <= 4096 || N <= 4096 : K <= 2048 && N <= 4096);
+}
+inline bool tokens_fused_any(int M, int K) { return tokens_fused(M, 1 << 30, K); }           // for every N
 
 // ---- projection of more rows -------------------------------------------------------------------------
 // The tile (16 mt rows, 64 ntw channels) whose cost is least: its time for K = 4096 where the chip is full of it (small ones: where it is not), times the rounds of blocks

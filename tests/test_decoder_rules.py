@@ -19,7 +19,8 @@ def rules(tmp_path_factory):
                                  'extern "C" {\n'
                                  'int few(int M, int K) { return tokens_few(M, K); }\n'
                                  'int few_blocks(int K) { return tokens_few_blocks(K); }\n'
-                                 'int fused(int M, int K) { return tokens_fused(M, K); }\n'
+                                 'int fused(int M, int N, int K) { return tokens_fused(M, N, K); }\n'
+                                 'int fused_any(int M, int K) { return tokens_fused_any(M, K); }\n'
                                  'int tile(int M, int N) { return tokens_tile(M, N); }\n'
                                  'int rows(int t) { return 16 * TOKENS_TILES[t].mt; }\n'
                                  'int channels(int t) { return 64 * TOKENS_TILES[t].ntw; }\n'
@@ -49,10 +50,19 @@ def test_the_shapes_of_many_rows_reach_every_tile_depth_band_and_remainder(rules
 
 
 def test_the_shapes_of_few_rows_reach_every_kernel(rules):
-    kinds = {(rules.few_blocks(K), bool(rules.fused(M, K))) for M, N, K in FEW if rules.few(M, K)}
-    assert kinds == {(b, f) for b in (2, 4, 8, 16) for f in (True, False)} - {(2, False), (4, False)}
+    kinds = {(rules.few_blocks(K), bool(rules.fused(M, N, K))) for M, N, K in FEW if rules.few(M, K)}
+    assert kinds == {(b, f) for b in (2, 4, 8, 16) for f in (True, False)}
     assert any(not rules.few(M, K) and M <= 16 for M, N, K in FEW)
-    assert {M for M, N, K in FEW if rules.fused(M, K)} >= {1, 2, 3, 4, 5, 8, 9, 16}
+    assert {M for M, N, K in FEW if rules.fused(M, N, K)} >= {1, 2, 3, 4, 5, 8, 9, 16}
+
+
+def test_few_rows_are_quantised_in_the_same_launch_where_that_was_measured_to_be_no_loss(rules):
+    for M, N, K, one in ((1, 4096, 4096, 1), (8, 8192, 4096, 1), (12, 4096, 4096, 0), (12, 8192, 4096, 0), (16, 6144, 3328, 0), (16, 4096, 2048, 1), (16, 8192, 2048, 0),
+                         (1, 5120, 5120, 0), (8, 4096, 5120, 1), (9, 4096, 5120, 0), (1, 8192, 8192, 0), (1, 2048, 8192, 1), (17, 4096, 1024, 0)):
+        assert rules.fused(M, N, K) == one, (M, N, K)
+    for M in range(1, 17):                                       # no workspace is asked for only where no N needs one
+        for K in (64, 2048, 2112, 4096, 4160, 8192):
+            assert rules.fused_any(M, K) == all(rules.fused(M, N, K) for N in (16, 4096, 4112, 8192)), (M, K)
 
 
 def test_the_caches_reach_both_kernels(rules):

@@ -15,7 +15,8 @@ TILED = [(0, 4, 70, 1296, 960), (0, 4, 150, 1552, 576), (0, 4, 300, 144, 704), (
          (3, 2, 1500, 2512, 448), (3, 2, 1000, 2064, 704), (3, 2, 2100, 1296, 320), (3, 2, 700, 4112, 192), (3, 2, 1500, 4112, 1024),
          (4, 2, 1000, 4112, 448), (4, 2, 2100, 2064, 704), (4, 2, 3000, 1552, 320), (4, 2, 2100, 4112, 576), (4, 2, 2100, 2512, 64)]
 # M, N, K
-FEW = [(1, 4112, 8192), (2, 96, 6208), (5, 272, 8192), (6, 2064, 8192), (9, 80, 4672), (13, 2064, 4160), (16, 528, 3328), (8, 1040, 2048), (3, 16, 1024), (4, 144, 576),
+FEW = [(1, 4112, 8192), (1, 4080, 8192), (2, 4112, 1024), (9, 2064, 1984), (16, 4112, 960), (11, 4128, 2048), (8, 4112, 4096), (3, 80, 2112), (5, 272, 3328), (16, 528, 1984),
+       (2, 96, 6208), (5, 272, 8192), (6, 2064, 8192), (9, 80, 4672), (13, 2064, 4160), (16, 528, 3328), (8, 1040, 2048), (3, 16, 1024), (4, 144, 576),
        (16, 272, 4096), (7, 80, 8192), (16, 4112, 8128), (1, 1040, 8256), (12, 80, 14336)]
 # contexts, how many of their positions are new, key heads, head_dim, page_len: more than 32768 rows of a head each, written and read
 CACHES = [([4000, 0, 17, 600], [3900, 0, 17, 600], 8, 128, 64), ([3001, 1, 700, 65], [2800, 1, 33, 65], 12, 64, 16), ([11000, 23000], [10999, 22011], 1, 128, 256)]
