@@ -76,7 +76,8 @@ int check_heads(int32_t heads, int32_t kv_heads, float scale)
 {
     if (kv_heads < 1 || heads < kv_heads || heads % kv_heads || heads > SAMP_MAX_HEADS)
         return fail(SAMP_ERR_SHAPE, "query heads must be a multiple of the key heads, %d at most (%d, %d)", SAMP_MAX_HEADS, heads, kv_heads);
-    if (!std::isfinite(scale) || !(scale > 0.0f)) return fail(SAMP_ERR_SCALE, "the scale is not finite and positive");
+    // (the kernels' exponentials are of base 2)
+    if (!std::isfinite(scale * 1.44269504088896341f) || !(scale > 0.0f)) return fail(SAMP_ERR_SCALE, "the scale is not positive, or log2(e) times it not finite");
     return SAMP_OK;
 }
 

@@ -1,4 +1,5 @@
 """Sizes past int32 at the decoder's Python entry points: what the C entry cannot count is refused or counts as its largest, never as its low 32 bits."""
+import ctypes as C
 import os
 
 import pytest
@@ -42,6 +43,16 @@ def test_calls_that_fill_the_chip_without_a_cut_have_few_partial_results():
     assert partial_bytes(128, 1, 32, 8, 128, 8192) <= 128 * 32 * 3 * 130 * 4 + 256
     assert partial_bytes(1, 1, 32, 8, 128, 4000) == 32 * 32 * 130 * 4            # 125 tiles, four of them a piece
     assert partial_bytes(64, 1, 32, 8, 128, 8192) == 64 * 32 * 6 * 130 * 4       # 256 tiles in pieces of at most 48
+
+
+def test_a_scale_whose_log2_e_fold_overflows_is_refused():
+    """Scores are multiplied by scale log2(e): an infinite factor times a product of 0 would be NaN."""
+    import test_decoder_refusals as refusals
+    fn = {n: D._fn(n) for n in D._SIGNATURES}
+    at, kv = refusals.AT, refusals.cache()
+    for scale in (2.5e38, 3.4e38):
+        assert fn["samp_attention_causal"](at, 256, at, 128, at, 128, 1, 4, 2, 64, at, 2, 3, 5, scale, at, None) == refusals.SCALE
+        assert fn["samp_attention_cache"](at, 256, 0, 4, C.addressof(kv), at, 2, at, at, 2, 3, 32, 5, scale, None, at, None, 0, None) == refusals.SCALE
 
 
 @pytest.mark.gpu
