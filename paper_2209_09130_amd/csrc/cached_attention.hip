@@ -3,10 +3,10 @@
 // What bounds it is HBM: 2 (head_dim + 4) bytes per token and key head, against which the products are small.  So the loop is a stream: every wave
 // takes key tiles of its own (32 keys) straight from the pages into registers, there is no LDS and no barrier before its end, and the
 // query heads of a group (and the new tokens of a sequence) share what was read as the columns of the matrix products.  Long contexts are cut into
-// pieces (splits), each with a partial result, which a second kernel joins.  64 contexts of 17 to 8192 tokens, 32 query heads on 8 key heads of 128 (556 MB): 116 us, 4.8
-// TB/s, of which 5 are the join; one context of 4000: 5.4 + 3.5 us, a chain of dependent loads (offsets, page numbers, keys) and a launch.  Tried and dropped: the next
-// tile's loads ahead of this one's work (64 contexts +-0, 16 drafts +3 %: other waves hide it, and it costs one of three per SIMD); the last block of a row joining the
-// pieces behind a fence (eight times as long: each block's fence writes its XCD's L2 back).
+// pieces (splits), each with a partial result, which a second kernel joins.  Medians, both kernels: 64 contexts of 17 to 8192 tokens, 32 query heads on 8 key heads of 128
+// (556 MB), 112.5 + 5.0 us, 4.7 TB/s; one context of 4000 5.9 + 4.0 us, a chain of dependent loads (offsets, page numbers, keys) and a launch.  Tried and dropped: the
+// next tile's loads ahead of this one's work (64 contexts +-0, 16 drafts +3 %: other waves hide it, and it costs one of three per SIMD).  The last block of a row could join its
+// pieces, stored and read at device scope, if a counter of theirs started at zero: the workspace is the caller's and holds anything.
 //
 // Products are 16 x 16 x 32.  S^T = K Q^T is in the queries' type, in which int8 codes are exact.  In binary16 1024 + (code + 128) is a code's byte under the
 // exponent byte 0x64, and one packed addition takes 1152 off again; in bfloat16 a code is the upper half of its binary32.  A lane gets four keys of one
@@ -369,9 +369,10 @@ hipError_t cached_attention(const void *q, long ldq, int heads, const KvCache &c
 // Pieces of so many tiles that 512 blocks have them all, but no less than four tiles (a tile for each wave; eight where a block has two row tiles), below which
 // the blocks' own latencies count for more than their number, and no more than 48, so that blocks of contexts of different lengths end together: 48 for 512 blocks
 // without a cut, more in proportion where there are more.  None at all where a context has at most sixteen tiles more than a piece, or where blocks of two row
-// tiles (many new tokens) are 512 without and no context has more than a million positions (some 20 ms of one block): their partial results are what costs then (us and MB of them, in pieces of 48 / uncut, 32 query heads on 8 of 128: 512 tokens of a
-// context of 4500 114 and 24 / 93, of 64 contexts up to 4500 4580 and 1560 / 4440, 128 tokens of 16 contexts up to 8192 504 and 195 / 433; one token of 128 contexts up
-// to 8192 223 in pieces of 48 or 96, 231 to 235 uncut).  Joining costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
+// tiles (many new tokens) are 512 without and no context has more than a million positions (some 20 ms of one block): their partial results are what costs
+// then.  us and MB of those, in pieces of 48 / uncut, 32 query heads on 8 of 128: 512 tokens of a context of 4500 114 and 24 / 93, of 64 contexts up to 4500 4580 and
+// 1560 / 4440, 128 tokens of 16 contexts up to 8192 504 and 195 / 433; one token of 128 contexts up to 8192 223 in pieces of 48 or 96, 231 to 235 uncut.  Joining
+// costs a launch.  Both kernels, us, by tiles of a piece (4 / 8 / 16 / 32 / 64 / uncut): 32 query heads on 8
 // key heads of 128, one context of 4000 8.5 / 9.2 / 11.7 / 16.0 / 23.9 / 36; 64 of 17 to 8192 176 / 139 / 124 / 120 / 121 / 131; 32 of 500 to 1000 21.7 / 19.4 /
 // 18.0 / 15.3 (uncut); 16 drafts on 8 contexts of 300 to 2100, 16 heads of 64, 17.3 / 14.4 / 14.0 / 15.6 / 21.7; one context of 8192, five tokens of 28 heads on 4,
 // 18.1 / 15.3 / 16.6 / 21.6 / 32.0 / 91; 64 contexts of 100 to 300, 12 heads of 64, 15.8 / 13.8 / 10.0 (uncut)

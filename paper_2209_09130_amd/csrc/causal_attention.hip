@@ -5,8 +5,9 @@
 // registers: S^T = K Q^T leaves a lane one query and 32 of a tile's 64 keys, and what it makes of them is, as it stands, the operand of
 // O^T += V^T P^T.  The key tiles (64 keys, K and V) are shared by the block's waves: direct loads into one half of LDS while the other is worked on, V
 // transposed by the reads.  One pass, with a reference per query that moves (and rescales) only when a score exceeds it by 2^8.
-// Two documents of 8192 tokens, 32 query heads on 8 key heads of 128: fp16 1.03 ms (1.06 PFLOP/s), bfloat16 0.99 ms; torch's products of 8192 x 8192 x 8192 reach
-// 1.26 and 1.48.  The matrix cores are busy 58 % of the clocks (at 1.67 GHz: the chip is at its power limit), the vector ALUs nearly as long.  Tried and dropped: blocks
+// Two documents of 8192 tokens, 32 query heads on 8 key heads of 128: fp16 1.03 to 1.08 ms between cards (1.01 to 1.06 PFLOP/s), bfloat16 0.99 ms; torch's products of
+// 8192 x 8192 x 8192 reach 1.23 to 1.26 and 1.47.  Eight of 300 to 2048, bfloat16: 142 us, 0.79 PFLOP/s: 6 % more products than needed, and a block holds 21 % more tiles than
+// that for all its waves (long documents 1 % and 3 %): waves wait at the barrier where the diagonal or the sequence's end lies before the block's last.  The matrix cores are busy 58 % of the clocks (at 1.67 GHz: the chip is at its power limit), the vector ALUs nearly as long.  Tried and dropped: blocks
 // of eight waves (long documents -1 to -3 %, eight of 300 to 2048 tokens +12 %), two groups of waves that alternate between products and softmax behind barriers (+12 %
 // at head size 64, spills at 128), half tiles with the next scores' products dealt out between the exponentials (+11 % at 64, spills at 128), wave priorities
 // (+-0), the sum of probabilities by dot products (+2 %).

@@ -58,8 +58,8 @@ __device__ __forceinline__ unsigned max_of_wave(unsigned top)
 }
 
 // The quantiser of a row that brings its own step: step = absmax / 127 and code = 127 x / absmax rounded half to even, decided exactly.  127 x / absmax is
-// a quotient of short integers: where it is no tie it is further than 2^-12 from one, so a product with error 2^-28 that is rounded to binary32
-// lies on the right side, and a tie is a binary32 number, to which it rounds.  The reciprocal therefore comes in two parts, an approximate one and what it
+// a quotient of short integers: where it is no tie it is further than 2^-19 of itself from one (254 x is at least one unit from an odd multiple of absmax, x has 11 bits), so
+// a product with a relative error of 2^-28 that is rounded to binary32 lies on the right side, and a tie is a binary32 number, to which it rounds.  The reciprocal therefore comes in two parts, an approximate one and what it
 // leaves; so does 1 / 127 (quotients by 127 have bits of period seven: none is near a rounding boundary).  True divisions in their place made the cache's
 // writing 30 % longer: every lane of a row forms them.
 // A row without a number of at least 2^-60 is a row of zeros (step 1, as for a weight row of zeros); a row with an infinity or NaN has codes 0 and a step of

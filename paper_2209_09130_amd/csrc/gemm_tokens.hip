@@ -26,7 +26,7 @@ template <bool BF> __device__ __forceinline__ v2i finish4(const v4i &acc, float 
 
 // ---- many rows -------------------------------------------------------------------------------------
 // The tile loop on packed weights (mfma_tile.h): 16 MT tokens x 64 NTW channels per block, weights straight into registers, token rows through LDS.
-// 8192 x 4096 x 4096: 126 us, 2.18 POP/s (torch's int8 product, 8192 x 8192 x 4096: 2.13).
+// 8192 x 4096 x 4096: 133 us in the median, 2.06 POP/s, at least 125 (torch's int8 product, 8192 x 8192 x 4096, on that card: 2.08).
 // K need only be a multiple of 64: what is left after whole rounds of the ring (D stages of 128 bytes) is multiplied from memory, without a pipeline.
 // N need only be a multiple of 16: a wave's blocks past the last one repeat it and are not stored.
 template <bool BF, int MT, int NTW, int D>
@@ -123,7 +123,8 @@ hipError_t launch_tile(const int8_t *A, const int8_t *Wp, const TokensEpi &epi, 
 // all of its weights (KB blocks of 1 KB a wave) are requested before anything else happens; the int32 partial tiles meet in LDS.  FUSED: the rows come in 16
 // bits and every block quantises them for itself while its weights are on the way, into LDS (rows 16 bytes more than K apart, so that the sixteen rows of an
 // operand read lie in different banks), which saves a launch.  Eight, four, two or one waves share a row, the fewer the more rows there are.  One row, 4096 -> 6144,
-// 25 MB of weights: 6.3 us in the chain of launches (two kernels 1.9 + 7.2); with every lane quantising what it multiplies, sixteen times over, 8.5.
+// 25 MB of weights: 8.1 us in a chain of launches with weights from memory (the quantiser in front 8.6), 7.3 with weights in the memory-side cache; with every lane quantising
+// what it multiplies, sixteen times over, some 2 us more.  When it is used: decoder_rules.h.
 struct FewRows { const void *x; long ld; const float *steps; };        // FUSED: 16-bit rows, ld values apart; else codes, K apart, and their steps
 template <bool BF, bool FUSED, int KB>
 __global__ __launch_bounds__(64 * FEW_WAVES) void gemm_tokens_few_kernel(const char *__restrict__ Wp, int K, int N, int M, int sharers, FewRows in, TokensEpi epi,
