@@ -494,6 +494,92 @@ SAMP_API int samp_attention_causal(const uint16_t *q, int64_t ldq, const uint16_
                                    int32_t heads, int32_t kv_heads, int32_t head_dim, const int32_t *cu, int32_t batch, int32_t max_len, int32_t rows,
                                    float scale, uint16_t *out, void *stream);
 
+/* ---- beam search and long contexts over the paged cache ------------------------------------------------
+ * Beside the operators above, on the same cache and page tables: the best continuations of beams, the bookkeeping of pages on the device, bounds of the
+ * keys of a page, and attention over the pages whose bounds promise most.  What is a choice (of candidates, of pages) is decided on numbers that do not
+ * depend on the order of sums or on how the work is cut.                                                     */
+enum { SAMP_TYPE_F32 = 2 };                /* logits only */
+#define SAMP_MAX_BEAMS 64
+#define SAMP_MAX_KEEP 64
+#define SAMP_MAX_VOCAB (1 << 19)
+#define SAMP_MAX_PAGES (1 << 26)           /* of a cache whose pages are counted */
+#define SAMP_MAX_TABLE 32768               /* pages of a sequence that are chosen from */
+
+/* The `keep` best candidates of each of `batch` sequences, best first, with `beams` rows of logits [batch * beams, vocab] each (fp16, bfloat16 or float; rows ld
+ * values apart; aligned to their values).  The candidates of a row r are its tokens v, of
+ *   total = scores[r] + (logits[r,v] - log sum_u exp logits[r,u]),
+ * in binary64 (the exponentials in binary32), scores dev float [batch * beams]; of a row whose finished[r] (dev bytes, or NULL: none) is set there is one, token `end` of total = scores[r], and its
+ * logits are not looked at.  Among equal totals the lower row comes first, in a row the
+ * larger logit, then the lower token.  A total of minus infinity is no candidate; neither are those of a row whose score is
+ * not finite, or whose logits hold NaN or plus infinity.
+ * best dev float [batch, keep]: the totals; parents dev int32: rows; tokens dev int32.  Behind the last candidate: minus infinity, -1, -1.
+ * beams <= SAMP_MAX_BEAMS, keep <= SAMP_MAX_KEEP, vocab <= SAMP_MAX_VOCAB, batch as ever (8192).  workspace as in samp_linear_i8_tokens.        */
+SAMP_API size_t samp_beam_select_workspace_bytes(int32_t type, int32_t batch, int32_t beams, int32_t vocab, int32_t keep);
+SAMP_API int samp_beam_select(const void *logits, int64_t ld, int32_t type, const float *scores, const uint8_t *finished, int32_t end, int32_t batch,
+                              int32_t beams, int32_t vocab, int32_t keep, float *best, int32_t *parents, int32_t *tokens, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Page tables of sequences that go on, from those that are: row i of table_out dev int32 [rows, width] continues row parents[i] (dev int32 [rows]; NULL: row i) of table
+ * [rows_from, width], which holds lens (dev int32 [rows_from]) positions, and has room for its next cu[i+1] - cu[i] positions (cu NULL: max_new each).  refs dev int32 [pages] counts for each
+ * page the table entries that name it (those of other tables too, if there are any; 0: the page is free), refs_out the same of table_out.
+ *   - A row takes its parent's pages up to the last that it needs; its other entries are -1.  A parent that is none of the rows (-1): an empty row.  What no row continues is
+ *     released: pages that nothing names any more are free.
+ *   - The pages that the next positions lie in are the row's own: one that others hold too is replaced, unless all that hold it are about to write it and the row is the
+ *     first of them; and there is one wherever there was none.  New pages are the lowest free ones, in the order of the entries.
+ *   - copies dev int32 [3, rows]: (from, to, positions) of a replaced page that held positions of the row already, (-1, -1, 0) where there is none: for samp_cache_copy,
+ *     which every cache that the table is for has to be given before its next positions are written.
+ *   - lens_out dev int32 [rows]: the next positions counted, as samp_cache_write wants them; 0 for an empty row.
+ *   - lacking dev int32 [1]: pages that were not there, free ones or entries of the table; an entry that lacks one is -1.
+ * page_len a power of two from 16 to 1024, rows and rows_from 1 to 8192, rows * width and rows_from * width < 2^31.  refs that are not what the tables name give tables that nobody can use, but no access outside the
+ * buffers.  workspace as in samp_linear_i8_tokens.                                                            */
+SAMP_API size_t samp_pages_fork_workspace_bytes(int32_t pages, int32_t rows);
+SAMP_API int samp_pages_fork(const int32_t *refs, int32_t pages, const int32_t *table, const int32_t *lens, int32_t rows_from, int32_t width, int32_t page_len,
+                             const int32_t *parents, const int32_t *cu, int32_t max_new, int32_t rows, int32_t *refs_out, int32_t *table_out, int32_t *lens_out,
+                             int32_t *copies, int32_t *lacking, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The pages in use (refs > 0) become the first `used` of the cache (dev int32 [1]): those that lie further back move, in order, to the free ones in front.
+ * refs_out dev int32 [pages], table_out dev int32 [entries]: refs and table with the new numbers, an entry that names no page in use is -1.  copies dev int32
+ * [3, max(1, pages / 2)]: (from, to, page_len) of the pages that move, then (-1, -1, 0).                      */
+SAMP_API size_t samp_pages_compact_workspace_bytes(int32_t pages, int32_t entries);
+SAMP_API int samp_pages_compact(const int32_t *refs, int32_t pages, const int32_t *table, int32_t entries, int32_t page_len, int32_t *refs_out,
+                                int32_t *table_out, int32_t *copies, int32_t *used, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bounds of the keys of whole pages: codes dev int8 [pages, kv_heads, 2, head_dim] and steps dev float [pages, kv_heads].  With x = code * step of each key in binary32,
+ * high and low its largest and smallest value over the page in each channel and top the largest magnitude of both over the channels: step = top * (1 / 127), codes = high / step rounded up
+ * and low / step rounded down, within [-127, 127], 1 / 127, products and quotients in binary32.  Keys of zeros alone have step 1; a page that holds a key that is not finite has codes 0 and a step of NaN.      */
+typedef struct {
+    int8_t *codes;
+    float *steps;
+} samp_key_bounds_t;
+
+/* For every copy (from, to, positions) of copies dev int32 [3, n] the first `positions` (all where more) of page `from` become those of page `to`, keys, values and steps; and their
+ * bounds, if bounds is not NULL.  Page numbers that are none of the cache's are left out.  No page may be written twice, or written and read, or what it holds afterwards is undefined. */
+SAMP_API int samp_cache_copy(const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds, const int32_t *copies, int32_t n, void *stream);
+
+/* Writes the bounds of the pages that the last cu[b+1] - cu[b] of the lens[b] positions of each sequence have filled (arguments as in samp_cache_write, whose keys
+ * they follow).  A page that is not full has none.                                                           */
+SAMP_API int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds, const int32_t *table, int32_t width, const int32_t *cu,
+                               const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows, void *stream);
+
+/* The pages that the new tokens q (as in samp_attention_cache) of each sequence are to read, for each key head: tables dev int32 [batch, kv_heads, keep], their numbers in
+ * the order of their positions, -1 behind the last, and lens_out dev int32 [batch], lens without the positions of the pages that are left out.  A sequence of up to `keep` pages keeps
+ * them all.  Of a longer one the first `sinks` pages and the last `recent` are kept, and of the others those of the highest score, the earlier one among equals:
+ *   score(page) = max over new tokens and query heads of the key head of  (float) sum_d max(c_d high_d, c_d low_d) * (step_q * step_page)
+ * with the codes c of the query's row (the quantiser of a row above), step_q = absmax * (1 / 127) of it (1 and NaN as there) and the page's bounds, the sum a whole number, the products in
+ * binary32; NaN counts as plus infinity, a page number that is none of the cache's as minus infinity.
+ * sinks >= 0, recent at least the pages that max_new positions can lie in ((max_new + page_len - 2) / page_len + 1), sinks + recent <= keep, width <= SAMP_MAX_TABLE.                 */
+SAMP_API int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,
+                               const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows, int32_t keep,
+                               int32_t sinks, int32_t recent, int32_t *tables, int32_t *lens_out, void *stream);
+
+/* samp_attention_cache over the pages that samp_cache_select chooses; where every sequence has up to `keep` pages, what samp_attention_cache computes.  workspace as there. */
+SAMP_API size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t page_len, int32_t max_new,
+                                                      int32_t max_len, int32_t keep);
+SAMP_API int samp_attention_sparse(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,
+                                   const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t max_len,
+                                   int32_t rows, int32_t keep, int32_t sinks, int32_t recent, float scale, const uint64_t *tree, uint16_t *out, void *workspace,
+                                   size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

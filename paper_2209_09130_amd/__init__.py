@@ -12,4 +12,5 @@ from .binding import (  # noqa: F401
 )
 from .decoder import (  # noqa: F401
     KVCache, quantize_tokens, gemm_i8_tokens_packed, linear_i8_tokens, cache_write, cache_read, attention_cache, attention_causal,
+    beam_select, pages_fork, pages_compact, cache_copy, KeyBounds, cache_bounds, cache_select, attention_sparse,
 )

@@ -44,17 +44,26 @@ int check_product(const void *Wp, const float *s_w, const float *bias, const voi
     return SAMP_OK;
 }
 
+int check_page_len(int32_t page_len)
+{
+    if (page_len < 16 || page_len > 1024 || (page_len & (page_len - 1))) return fail(SAMP_ERR_SHAPE, "page_len must be a power of two, 16 to 1024 (%d)", page_len);
+    return SAMP_OK;
+}
+int shift_of(int32_t page_len)
+{
+    int shift = 4;
+    while (1 << shift < page_len) shift++;
+    return shift;
+}
+
 int check_cache(const samp_kv_cache_t *c, KvCache *to)
 {
     if (!c || !c->k || !c->v || !c->k_step || !c->v_step) return fail(SAMP_ERR_ARG, "NULL pointer in the cache");
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_step, 16) || !aligned(c->v_step, 16)) return fail(SAMP_ERR_ARG, "the cache must be 16-byte aligned");
     if (c->head_dim != 64 && c->head_dim != 128) return fail(SAMP_ERR_SHAPE, "head_dim must be 64 or 128 (%d)", c->head_dim);
-    if (c->page_len < 16 || c->page_len > 1024 || (c->page_len & (c->page_len - 1)))
-        return fail(SAMP_ERR_SHAPE, "page_len must be a power of two, 16 to 1024 (%d)", c->page_len);
+    if (int rc = check_page_len(c->page_len)) return rc;
     if (c->pages < 1 || c->kv_heads < 1 || c->kv_heads > SAMP_MAX_HEADS) return fail(SAMP_ERR_SHAPE, "pages >= 1 and 1 to %d key heads needed", SAMP_MAX_HEADS);
-    int shift = 4;
-    while (1 << shift < c->page_len) shift++;
-    *to = KvCache{c->k, c->v, c->k_step, c->v_step, c->pages, c->kv_heads, shift};
+    *to = KvCache{c->k, c->v, c->k_step, c->v_step, c->pages, c->kv_heads, shift_of(c->page_len)};
     return SAMP_OK;
 }
 
@@ -78,6 +87,45 @@ int check_heads(int32_t heads, int32_t kv_heads, float scale)
         return fail(SAMP_ERR_SHAPE, "query heads must be a multiple of the key heads, %d at most (%d, %d)", SAMP_MAX_HEADS, heads, kv_heads);
     // (the kernels' exponentials are of base 2)
     if (!std::isfinite(scale * 1.44269504088896341f) || !(scale > 0.0f)) return fail(SAMP_ERR_SCALE, "the scale is not positive, or log2(e) times it not finite");
+    return SAMP_OK;
+}
+
+int check_bounds(const samp_key_bounds_t *b, KeyBounds *to)
+{
+    if (!b || !b->codes || !b->steps) return fail(SAMP_ERR_ARG, "NULL pointer in the bounds");
+    if (!aligned(b->codes, 16) || !aligned(b->steps, 16)) return fail(SAMP_ERR_ARG, "the bounds must be 16-byte aligned");
+    *to = KeyBounds{b->codes, b->steps};
+    return SAMP_OK;
+}
+
+int check_workspace(const void *workspace, size_t bytes, size_t need)
+{
+    if (need && (!workspace || !aligned(workspace, ALIGN) || bytes < need)) return fail(SAMP_ERR_SPACE, "a 256-byte aligned workspace of %zu bytes is needed", need);
+    return SAMP_OK;
+}
+
+int check_beams(int32_t type, int32_t batch, int32_t beams, int32_t vocab, int32_t keep)
+{
+    if (type != SAMP_TYPE_F16 && type != SAMP_TYPE_BF16 && type != SAMP_TYPE_F32) return fail(SAMP_ERR_ARG, "unknown type %d", (int)type);
+    if (batch < 1 || batch > SAMP_MAX_BATCH || beams < 1 || beams > SAMP_MAX_BEAMS || vocab < 1 || vocab > SAMP_MAX_VOCAB || keep < 1 || keep > SAMP_MAX_KEEP)
+        return fail(SAMP_ERR_SHAPE, "1 to %d sequences, 1 to %d beams, a vocabulary of 1 to %d and keep of 1 to %d are supported (%d, %d, %d, %d)", SAMP_MAX_BATCH,
+                    SAMP_MAX_BEAMS, SAMP_MAX_VOCAB, SAMP_MAX_KEEP, batch, beams, vocab, keep);
+    return SAMP_OK;
+}
+
+int check_pages(int32_t pages)
+{
+    if (pages < 1 || pages > SAMP_MAX_PAGES) return fail(SAMP_ERR_SHAPE, "1 to %d pages are supported (%d)", SAMP_MAX_PAGES, pages);
+    return SAMP_OK;
+}
+
+int check_choice(int32_t width, int32_t page_len, int32_t max_new, int32_t keep, int32_t sinks, int32_t recent)
+{
+    if (width > SAMP_MAX_TABLE) return fail(SAMP_ERR_SHAPE, "pages are chosen from at most %d of a sequence (width %d)", SAMP_MAX_TABLE, width);
+    const long need = ((long)max_new + page_len - 2) / page_len + 1;
+    if (sinks < 0 || recent < need || keep < 1 || (long)sinks + recent > keep)
+        return fail(SAMP_ERR_SHAPE, "sinks >= 0, recent >= %ld for max_new %d, and sinks + recent <= keep are needed (%d, %d, %d)", need, max_new, sinks, recent, keep);
+    if (keep > SAMP_MAX_TABLE) return fail(SAMP_ERR_SHAPE, "keep is at most %d (%d)", SAMP_MAX_TABLE, keep);
     return SAMP_OK;
 }
 
@@ -222,6 +270,160 @@ int samp_attention_causal(const uint16_t *q, int64_t ldq, const uint16_t *k, int
     if ((double)batch * heads * ((max_len + 127) / 128) > 2147483647.0) return fail(SAMP_ERR_SHAPE, "too many strips of queries");
     HIP_TRY(launch_causal_attention(q, ldq, k, ldk, v, ldv, type == SAMP_TYPE_BF16, heads, kv_heads, head_dim, cu, batch, max_len, rows, scale, out,
                                     (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+size_t samp_beam_select_workspace_bytes(int32_t type, int32_t batch, int32_t beams, int32_t vocab, int32_t keep)
+{
+    return check_beams(type, batch, beams, vocab, keep) ? 0 : up(beam_workspace(type, batch, beams, vocab, keep));
+}
+
+int samp_beam_select(const void *logits, int64_t ld, int32_t type, const float *scores, const uint8_t *finished, int32_t end, int32_t batch, int32_t beams,
+                     int32_t vocab, int32_t keep, float *best, int32_t *parents, int32_t *tokens, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_beams(type, batch, beams, vocab, keep)) return rc;
+    if (!logits || !scores || !best || !parents || !tokens) return fail(SAMP_ERR_ARG, "NULL pointer");
+    if (!aligned(logits, type == SAMP_TYPE_F32 ? 4 : 2) || !aligned(scores, 4) || !aligned(best, 4) || !aligned(parents, 4) || !aligned(tokens, 4))
+        return fail(SAMP_ERR_ARG, "logits, scores and results must be aligned to their values");
+    if (ld < vocab || ld > SAMP_MAX_ROW) return fail(SAMP_ERR_SHAPE, "logits: a leading dimension of %d to %d is needed (%lld)", vocab, SAMP_MAX_ROW, (long long)ld);
+    if (int rc = check_workspace(workspace, workspace_bytes, samp_beam_select_workspace_bytes(type, batch, beams, vocab, keep))) return rc;
+    HIP_TRY(launch_beam_select(logits, ld, type, scores, finished, end, batch, beams, vocab, keep, best, parents, tokens, workspace, (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+size_t samp_pages_fork_workspace_bytes(int32_t pages, int32_t rows)
+{
+    return check_pages(pages) || rows < 1 || rows > SAMP_MAX_BATCH ? 0 : pages_fork_workspace(pages, rows);
+}
+
+int samp_pages_fork(const int32_t *refs, int32_t pages, const int32_t *table, const int32_t *lens, int32_t rows_from, int32_t width, int32_t page_len,
+                    const int32_t *parents, const int32_t *cu, int32_t max_new, int32_t rows, int32_t *refs_out, int32_t *table_out, int32_t *lens_out, int32_t *copies,
+                    int32_t *lacking, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_pages(pages)) return rc;
+    if (int rc = check_page_len(page_len)) return rc;
+    if (!refs || !table || !lens || !refs_out || !table_out || !lens_out || !copies || !lacking) return fail(SAMP_ERR_ARG, "NULL pointer");
+    if (rows < 1 || rows > SAMP_MAX_BATCH || rows_from < 1 || rows_from > SAMP_MAX_BATCH || width < 1 || (!cu && max_new < 0))
+        return fail(SAMP_ERR_SHAPE, "1 to %d rows, a table width of at least 1 and max_new >= 0 are needed (%d, %d, %d, %d)", SAMP_MAX_BATCH, rows, rows_from, width, max_new);
+    if ((long long)rows * width > INT32_MAX || (long long)rows_from * width > INT32_MAX) return fail(SAMP_ERR_SHAPE, "a table has less than 2^31 entries");
+    if (refs == refs_out || table == table_out || lens == lens_out) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
+    if (int rc = check_workspace(workspace, workspace_bytes, samp_pages_fork_workspace_bytes(pages, rows))) return rc;
+    const PageFork f{refs, table, lens, parents, cu, pages, rows_from, width, shift_of(page_len), max_new, rows, refs_out, table_out, lens_out, copies, lacking};
+    HIP_TRY(launch_pages_fork(f, workspace, (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+size_t samp_pages_compact_workspace_bytes(int32_t pages, int32_t entries)
+{
+    return check_pages(pages) || entries < 0 ? 0 : pages_compact_workspace(pages, entries);
+}
+
+int samp_pages_compact(const int32_t *refs, int32_t pages, const int32_t *table, int32_t entries, int32_t page_len, int32_t *refs_out, int32_t *table_out,
+                       int32_t *copies, int32_t *used, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (int rc = check_pages(pages)) return rc;
+    if (int rc = check_page_len(page_len)) return rc;
+    if (entries < 0) return fail(SAMP_ERR_SHAPE, "entries >= 0 needed (%d)", entries);
+    if (!refs || !refs_out || !copies || !used || (entries && (!table || !table_out))) return fail(SAMP_ERR_ARG, "NULL pointer");
+    if (refs == refs_out || (entries && table == table_out)) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
+    if (int rc = check_workspace(workspace, workspace_bytes, samp_pages_compact_workspace_bytes(pages, entries))) return rc;
+    HIP_TRY(launch_pages_compact(refs, pages, table, entries, page_len, refs_out, table_out, copies, used, workspace, (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+int samp_cache_copy(const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds, const int32_t *copies, int32_t n, void *stream)
+{
+    KvCache c;
+    KeyBounds kb{nullptr, nullptr};
+    if (int rc = check_cache(cache, &c)) return rc;
+    if (bounds)
+        if (int rc = check_bounds(bounds, &kb)) return rc;
+    if (!copies) return fail(SAMP_ERR_ARG, "copies is NULL");
+    if (n < 1 || n > SAMP_MAX_PAGES) return fail(SAMP_ERR_SHAPE, "1 to %d copies are supported (%d)", SAMP_MAX_PAGES, n);
+    HIP_TRY(launch_cache_copy(c, cache->head_dim, kb, copies, n, (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds, const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens,
+                      int32_t batch, int32_t max_new, int32_t rows, void *stream)
+{
+    KvCache c;
+    KeyBounds kb;
+    KvRows r{table, width, cu, lens, batch, max_new, rows};
+    if (int rc = check_cache(cache, &c)) return rc;
+    if (int rc = check_bounds(bounds, &kb)) return rc;
+    if (int rc = check_kv_rows(r, "max_new")) return rc;
+    HIP_TRY(launch_cache_bounds(c, cache->head_dim, kb, r, (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds, const int32_t *table,
+                      int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows, int32_t keep, int32_t sinks, int32_t recent,
+                      int32_t *tables, int32_t *lens_out, void *stream)
+{
+    KvCache c;
+    KeyBounds kb;
+    KvRows r{table, width, cu, lens, batch, max_new, rows};
+    if (int rc = check_type(type)) return rc;
+    if (int rc = check_cache(cache, &c)) return rc;
+    if (int rc = check_bounds(bounds, &kb)) return rc;
+    if (int rc = check_kv_rows(r, "max_new")) return rc;
+    if (int rc = check_heads(heads, c.kv_heads, 1.0f)) return rc;
+    if (int rc = check_rows("q", q, ldq, (int64_t)heads * cache->head_dim)) return rc;
+    if (int rc = check_choice(width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
+    if (!tables || !lens_out) return fail(SAMP_ERR_ARG, "NULL pointer");
+    if (lens == lens_out) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
+    HIP_TRY(launch_cache_select(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, kb, r, keep, sinks, recent, tables, lens_out, (hipStream_t)stream));
+    return SAMP_OK;
+}
+
+// the tables of the key heads, the lengths, then what the attention over them needs
+static size_t chosen_bytes(int32_t batch, int32_t kv_heads, int32_t keep) { return up(4 * (size_t)batch * kv_heads * keep) + up(4 * (size_t)batch); }
+static int32_t chosen_len(int32_t max_len, int32_t keep, int32_t page_len)
+{
+    const long long most = (long long)keep * page_len;
+    return max_len < most ? max_len : (int32_t)most;
+}
+
+size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t page_len, int32_t max_new,
+                                             int32_t max_len, int32_t keep)
+{
+    Cut cut;
+    if (check_page_len(page_len) || keep < 1 || keep > SAMP_MAX_TABLE) return 0;
+    max_len = chosen_len(max_len, keep, page_len);
+    if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len, &cut)) return 0;
+    return chosen_bytes(batch, kv_heads, keep) + samp_attention_cache_workspace_bytes(rows, batch, heads, kv_heads, head_dim, max_new, max_len);
+}
+
+int samp_attention_sparse(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,
+                          const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t max_len, int32_t rows,
+                          int32_t keep, int32_t sinks, int32_t recent, float scale, const uint64_t *tree, uint16_t *out, void *workspace, size_t workspace_bytes,
+                          void *stream)
+{
+    KvCache c;
+    KeyBounds kb;
+    KvRows r{table, width, cu, lens, batch, max_new, rows};
+    if (int rc = check_type(type)) return rc;
+    if (int rc = check_cache(cache, &c)) return rc;
+    if (int rc = check_bounds(bounds, &kb)) return rc;
+    if (int rc = check_kv_rows(r, "max_new")) return rc;
+    if (int rc = check_heads(heads, c.kv_heads, scale)) return rc;
+    if (int rc = check_choice(width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
+    max_len = chosen_len(max_len, keep, cache->page_len);
+    Cut cut;
+    if (int rc = check_cached(rows, batch, heads, c.kv_heads, cache->head_dim, max_new, max_len, &cut)) return rc;
+    if (int rc = check_rows("q", q, ldq, (int64_t)heads * cache->head_dim)) return rc;
+    if (!out || !aligned(out, 16)) return fail(SAMP_ERR_ARG, "out must be 16-byte aligned and not NULL");
+    if (tree && r.max_rows > 64) return fail(SAMP_ERR_SHAPE, "a tree has at most 64 drafted tokens (max_new %d)", max_new);
+    if (tree && !aligned(tree, 8)) return fail(SAMP_ERR_ARG, "tree must be 8-byte aligned");
+    if (int rc = check_workspace(workspace, workspace_bytes,
+                                 samp_attention_sparse_workspace_bytes(rows, batch, heads, c.kv_heads, cache->head_dim, cache->page_len, max_new, max_len, keep)))
+        return rc;
+    int *const tables = static_cast<int *>(workspace), *const chosen_lens = tables + up(4 * (size_t)batch * c.kv_heads * keep) / 4;
+    float *const partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + chosen_bytes(batch, c.kv_heads, keep));
+    HIP_TRY(launch_cache_select(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, kb, r, keep, sinks, recent, tables, chosen_lens, (hipStream_t)stream));
+    const KvRows chosen{tables, keep, cu, chosen_lens, batch, r.max_rows, rows, c.kv_heads};
+    HIP_TRY(launch_cached_attention(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, chosen, scale, tree, cut, partials, out, (hipStream_t)stream));
     return SAMP_OK;
 }
 

@@ -114,7 +114,7 @@ void cached_attention_kernel(const char *__restrict__ Q, long ldq, KvCache c, Kv
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     const int heads = c.kv_heads * group, len = max(s.len, 0);
     const int first = rows.lens[b] - s.n;                             // position of the first new token (negative: more new tokens than positions)
-    const int *table = rows.table + (size_t)b * rows.width;
+    const int *table = rows.table + ((size_t)b * rows.tables + (rows.tables > 1 ? head : 0)) * rows.width;
 
     // Table entries of the wave's tiles, 32 at a time (lane 2 i + h: group h of its i-th tile): looked up one by one, each would stand in front of its tile's loads
     const int end = split == pieces - 1 ? tiles : (split + 1) * piece, last = (len - 1) & ~15;

@@ -95,7 +95,10 @@ __device__ __forceinline__ v2i quant8(const float (&x)[8], const RowQuant &q)
 struct KvCache { int8_t *k, *v; float *k_step, *v_step; int pages, kv_heads, page_shift; };
 // Which positions of which sequences the packed rows of a call are: rows cu[b] .. cu[b + 1] - 1 (cu null: max_rows each) are the last of the lens[b]
 // positions of sequence b, whose pages are row b of the table
-struct KvRows { const int *table; int width; const int *cu, *lens; int batch, max_rows, rows; };
+// (tables: 1, or kv_heads where each key head has a table of its own, behind each other for a sequence; only the attention reads such)
+struct KvRows { const int *table; int width; const int *cu, *lens; int batch, max_rows, rows, tables = 1; };
+// Bounds of the keys of a page: codes [pages, kv_heads, 2, head_dim] (largest, smallest), steps [pages, kv_heads]
+struct KeyBounds { int8_t *codes; float *steps; };
 
 // n = 0 where cu names rows that the tensors do not have; todo: those of the n that the caller counted with; len: at most what the table has room for
 struct SeqRows { int first_row, n, todo, len; };
@@ -128,5 +131,29 @@ hipError_t launch_cached_attention(const void *q, long ldq, bool bf16, int heads
                                    const uint64_t *tree, Cut cut, float *partials, void *out, hipStream_t st);
 hipError_t launch_causal_attention(const void *q, long ldq, const void *k, long ldk, const void *v, long ldv, bool bf16, int heads, int kv_heads,
                                    int head_dim, const int *cu, int batch, int max_len, int rows, float scale, void *out, hipStream_t st);
+
+// Beam search: type as in samp.h; the bytes of the workspace follow from how a row is cut
+struct BeamCut { int vectors, chunks; };                              // 16-byte vectors of a thread, blocks of a row
+BeamCut beam_cut(int type, int rows, int vocab);
+size_t beam_workspace(int type, int batch, int beams, int vocab, int keep);
+hipError_t launch_beam_select(const void *logits, long ld, int type, const float *scores, const uint8_t *finished, int end, int batch, int beams, int vocab, int keep,
+                              float *best, int *parents, int *tokens, void *ws, hipStream_t st);
+
+// Pages: row i of `to` continues row parents[i] of `from`
+struct PageFork {
+    const int *refs, *table, *lens, *parents, *cu;
+    int pages, rows_from, width, page_shift, max_new, rows;
+    int *refs_out, *table_out, *lens_out, *copies, *lacking;
+};
+size_t pages_fork_workspace(int pages, int rows);
+hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st);
+size_t pages_compact_workspace(int pages, int entries);
+hipError_t launch_pages_compact(const int *refs, int pages, const int *table, int entries, int page_len, int *refs_out, int *table_out, int *copies, int *used, void *ws,
+                                hipStream_t st);
+hipError_t launch_cache_copy(const KvCache &cache, int head_dim, const KeyBounds &bounds, const int *copies, int n, hipStream_t st);
+
+hipError_t launch_cache_bounds(const KvCache &cache, int head_dim, const KeyBounds &bounds, const KvRows &rows, hipStream_t st);
+hipError_t launch_cache_select(const void *q, long ldq, bool bf16, int heads, int head_dim, const KvCache &cache, const KeyBounds &bounds, const KvRows &rows, int keep,
+                               int sinks, int recent, int *tables, int *lens_out, hipStream_t st);
 
 }  // namespace samp

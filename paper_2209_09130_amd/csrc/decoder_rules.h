@@ -57,4 +57,10 @@ inline int tokens_band(int tile) { return tile == 4 ? 4 : 8; }
 // has 2048 x 8 rows and is better off with one (5.4 us).
 inline int cache_passes(long rows, int kv_heads) { return rows * kv_heads >= 32768 ? 4 : 1; }
 
+// ---- bookkeeping of pages ------------------------------------------------------------------------------
+// One block does a whole call where its counters fit the LDS of a CU: two for each page and one for each row, and 64 KB of bits and counts.
+inline long fork_block_lds(long pages, long rows) { return 8 * pages + 4 * rows; }
+inline bool fork_in_block(long pages, long rows) { return fork_block_lds(pages, rows) <= 150 << 10; }
+inline bool compact_in_block(long pages, long entries) { return pages <= 65536 && entries <= 65536; }
+
 }  // namespace samp

@@ -25,6 +25,17 @@ _SIGNATURES = {
     "samp_attention_cache_workspace_bytes": (_I,) * 7,
     "samp_attention_cache": (_P, _L, _I, _I, _P, _P, _I, _P, _P, _I, _I, _I, _I, _F, _P, _P, _P, _Z, _P),
     "samp_attention_causal": (_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _P, _I, _I, _I, _F, _P, _P),
+    "samp_beam_select_workspace_bytes": (_I,) * 5,
+    "samp_beam_select": (_P, _L, _I, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _Z, _P),
+    "samp_pages_fork_workspace_bytes": (_I, _I),
+    "samp_pages_fork": (_P, _I, _P, _P, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _Z, _P),
+    "samp_pages_compact_workspace_bytes": (_I, _I),
+    "samp_pages_compact": (_P, _I, _P, _I, _I, _P, _P, _P, _P, _P, _Z, _P),
+    "samp_cache_copy": (_P, _P, _P, _I, _P),
+    "samp_cache_bounds": (_P, _P, _P, _I, _P, _P, _I, _I, _I, _P),
+    "samp_cache_select": (_P, _L, _I, _I, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P),
+    "samp_attention_sparse_workspace_bytes": (_I,) * 9,
+    "samp_attention_sparse": (_P, _L, _I, _I, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _P, _P, _P, _Z, _P),
 }
 _entry = {}
 
@@ -305,6 +316,233 @@ def attention_causal(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: Opti
     if B:
         rc = _fn("samp_attention_causal")(pq, ldq, pk, ldk, pv, ldv, _TYPES[dtype], heads, shape[1], dim, pcu, B, max_len, rows,
                                           dim ** -0.5 if scale is None else float(scale), to, _raw_stream(device))
+        if rc:
+            _raise(rc)
+    return out
+
+
+# ---- beam search and long contexts ---------------------------------------------------------------------
+_LOGITS = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
+
+def beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, keep: Optional[int] = None, finished: Optional[torch.Tensor] = None,
+                end: int = 0) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """samp_beam_select: (scores float32, parents int32, tokens int32), each [batch, keep], the best first, of logits [batch * beams, vocabulary] (fp16, bfloat16 or
+    float32, dense rows) and scores float32 [batch * beams].  parents are rows of logits, as pages_fork takes them; -1 behind the last candidate.
+    keep: None for beams.  finished: bool or uint8 [batch * beams], rows that go on with `end` alone."""
+    device = _device(logits)
+    if device != _current_device():
+        return _on(device, beam_select, logits, scores, beams, keep, finished, end)
+    if logits.dim() != 2 or logits.dtype not in _LOGITS or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        _refuse(f"logits: a matrix of fp16, bfloat16 or float32 with dense rows is needed, not {logits.dtype} {tuple(logits.shape)} {logits.stride()}")
+    rows, vocab = logits.shape
+    keep = beams if keep is None else keep
+    if not 1 <= beams <= 64 or rows % beams or not 1 <= keep <= 64 or vocab > _INT_MAX:
+        _refuse(f"logits have rows of whole sequences, 1 to 64 beams each, and 1 to 64 candidates are kept ({rows} rows, {beams}, {keep})")
+    if not -_INT_MAX <= end <= _INT_MAX:
+        _refuse(f"end is an int32 ({end})")
+    batch = rows // beams
+    at = _flat("scores", scores, torch.float32, device, rows)
+    done = 0
+    if finished is not None:
+        done = _flat("finished", finished, torch.bool if finished.dtype is torch.bool else torch.uint8, device, rows)
+    best = logits.new_empty((batch, keep), dtype=torch.float32)
+    parents, tokens = logits.new_empty((2, batch, keep), dtype=torch.int32).unbind()
+    if batch:
+        need = _workspace_bytes("samp_beam_select_workspace_bytes", _LOGITS[logits.dtype], batch, beams, vocab, keep)
+        ws = logits.new_empty((need,), dtype=torch.uint8) if need else None
+        rc = _fn("samp_beam_select")(logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, _LOGITS[logits.dtype], at, done, end, batch, beams, vocab, keep,
+                                     best.data_ptr(), parents.data_ptr(), tokens.data_ptr(), ws.data_ptr() if need else 0, need, _raw_stream(device))
+        if rc:
+            _raise(rc)
+    return best, parents, tokens
+
+
+def _table(table: torch.Tensor, device: int) -> Tuple[int, int, int]:
+    if table.dim() != 2 or table.numel() > _INT_MAX:
+        _refuse(f"a page table is [sequences, pages of a sequence], of less than 2^31 entries, not {tuple(table.shape)}")
+    return _flat("table", table, torch.int32, device), table.shape[0], table.shape[1]
+
+
+def pages_fork(refs: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page_len: int, parents: Optional[torch.Tensor] = None,
+               cu: Optional[torch.Tensor] = None, max_new: int = 0) -> Tuple[torch.Tensor, ...]:
+    """samp_pages_fork: (refs, table, lens, copies, lacking) of the sequences that continue rows `parents` (int32; None: each its own) of table int32 [rows, width], with
+    room for their next cu[i + 1] - cu[i] positions (cu None: max_new).  refs int32 [pages]: table entries that name a page, 0 for a free one.  copies int32 [3, rows] is
+    for cache_copy, on every cache that the table is for; lacking int32 [1]: pages that were not there."""
+    device = _device(refs)
+    if device != _current_device():
+        return _on(device, pages_fork, refs, table, lens, page_len, parents, cu, max_new)
+    pages = refs.numel()
+    if pages > _INT_MAX:
+        _refuse(f"{pages} pages are more than int32 counts")
+    pr = _flat("refs", refs, torch.int32, device)
+    pt, rows_from, width = _table(table, device)
+    pl = _flat("lens", lens, torch.int32, device, rows_from)
+    pp, rows = (0, rows_from) if parents is None else (_flat("parents", parents, torch.int32, device), parents.numel())
+    pc = _flat("cu", cu, torch.int32, device, rows + 1) if cu is not None else 0
+    if not 0 < rows <= 8192:
+        _refuse(f"1 to 8192 rows are supported ({rows})")
+    if rows * width > _INT_MAX:
+        _refuse("a page table has less than 2^31 entries")
+    refs_out, table_out, out = torch.empty_like(refs), table.new_empty((rows, width)), table.new_empty((4 * rows + 1,))
+    lens_out, copies, lacking = out[:rows], out[rows:4 * rows].view(3, rows), out[4 * rows:]
+    need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows)
+    ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
+    rc = _fn("samp_pages_fork")(pr, pages, pt, pl, rows_from, width, page_len, pp, pc, _most(max_new), rows, refs_out.data_ptr(), table_out.data_ptr(),
+                                lens_out.data_ptr(), copies.data_ptr(), lacking.data_ptr(), ws.data_ptr() if need else 0, need, _raw_stream(device))
+    if rc:
+        _raise(rc)
+    return refs_out, table_out, lens_out, copies, lacking
+
+
+def pages_compact(refs: torch.Tensor, table: torch.Tensor, page_len: int) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """samp_pages_compact: (refs, table, copies, used) with the pages in use as the first `used` (int32 [1]).  table: int32 of any shape; copies for cache_copy, as from
+    pages_fork."""
+    device = _device(refs)
+    if device != _current_device():
+        return _on(device, pages_compact, refs, table, page_len)
+    pages, entries = refs.numel(), table.numel()
+    if pages > _INT_MAX or entries > _INT_MAX:
+        _refuse(f"{pages} pages or {entries} entries are more than int32 counts")
+    pr, pt = _flat("refs", refs, torch.int32, device), _flat("table", table, torch.int32, device)
+    refs_out, table_out = torch.empty_like(refs), torch.empty_like(table)
+    out = refs.new_empty((3 * max(1, pages // 2) + 1,))
+    copies, used = out[:-1].view(3, -1), out[-1:]
+    need = _workspace_bytes("samp_pages_compact_workspace_bytes", pages, entries)
+    ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
+    rc = _fn("samp_pages_compact")(pr, pages, pt, entries, page_len, refs_out.data_ptr(), table_out.data_ptr(), copies.data_ptr(), used.data_ptr(),
+                                   ws.data_ptr() if need else 0, need, _raw_stream(device))
+    if rc:
+        _raise(rc)
+    return refs_out, table_out, copies, used
+
+
+class _BoundsStruct(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("steps", C.c_void_p)]
+
+
+class KeyBounds:
+    """Bounds of the keys of a cache's pages: codes int8 [pages, kv_heads, 2, head_dim] (largest, smallest) and float32 steps [pages, kv_heads] (contiguous, kept alive by
+    this object), and the samp_key_bounds_t that points at them."""
+
+    def __init__(self, codes: torch.Tensor, steps: torch.Tensor):
+        device = _device(codes)
+        if codes.dim() != 4 or codes.shape[2] != 2 or steps.shape != codes.shape[:2]:
+            _refuse(f"bounds are codes [pages, kv_heads, 2, head_dim] and steps [pages, kv_heads], not {tuple(codes.shape)} {tuple(steps.shape)}")
+        self.codes, self.steps = codes, steps
+        self.device = device
+        self.struct = _BoundsStruct(_flat("codes", codes, torch.int8, device), _flat("steps", steps, torch.float32, device))
+        self.address = C.addressof(self.struct)
+        self.sizes = (codes.shape[0], codes.shape[1], codes.shape[3])
+
+    @classmethod
+    def empty(cls, cache: KVCache) -> "KeyBounds":
+        """Bounds for a cache, none of them written."""
+        return cls(cache.k.new_zeros((cache.pages, cache.kv_heads, 2, cache.head_dim)), cache.k_step.new_zeros((cache.pages, cache.kv_heads)))
+
+    def of(self, cache: KVCache) -> int:
+        if self.device != cache.device or self.sizes != (cache.pages, cache.kv_heads, cache.head_dim):
+            _refuse(f"bounds for {self.sizes} (pages, kv_heads, head_dim) are not those of a cache of {(cache.pages, cache.kv_heads, cache.head_dim)}")
+        return self.address
+
+
+def cache_copy(cache: KVCache, copies: torch.Tensor, bounds: Optional[KeyBounds] = None) -> None:
+    """samp_cache_copy: for every column (from, to, positions) of copies int32 [3, n] the first positions of page `from` become those of page `to`."""
+    device = cache.device
+    if device != _current_device():
+        return _on(device, cache_copy, cache, copies, bounds)
+    if copies.dim() != 2 or copies.shape[0] != 3 or copies.shape[1] > _INT_MAX:
+        _refuse(f"copies are int32 [3, n], not {tuple(copies.shape)}")
+    n = copies.shape[1]
+    at, kb = _flat("copies", copies, torch.int32, device), bounds.of(cache) if bounds is not None else 0
+    if n:
+        rc = _fn("samp_cache_copy")(cache.address, kb, at, n, _raw_stream(device))
+        if rc:
+            _raise(rc)
+
+
+def cache_bounds(cache: KVCache, bounds: KeyBounds, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int,
+                 rows: Optional[int] = None) -> None:
+    """samp_cache_bounds: the bounds of the pages that the last cu[b + 1] - cu[b] of the lens[b] positions of each sequence have filled, after cache_write wrote them.
+    rows: as many as cache_write was given, which an offset may not pass (None: any number)."""
+    device = cache.device
+    if device != _current_device():
+        return _on(device, cache_bounds, cache, bounds, table, cu, lens, max_new, rows)
+    kb = bounds.of(cache)
+    t, width, pcu, plens, B = _places(device, table, cu, lens)
+    max_new = _most(max_new)
+    if rows is None:
+        rows = B * max_new if cu is None else 1 << 24
+    if rows and B:
+        rc = _fn("samp_cache_bounds")(cache.address, kb, t, width, pcu, plens, B, max_new, rows, _raw_stream(device))
+        if rc:
+            _raise(rc)
+
+
+def cache_select(q: torch.Tensor, cache: KVCache, bounds: KeyBounds, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int, keep: int,
+                 sinks: int = 1, recent: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """samp_cache_select: (tables int32 [batch, kv_heads, keep], lens int32 [batch]) of the pages that the new tokens q [rows, heads, head_dim] are to read: the first `sinks`, the
+    last `recent` (None: those that max_new tokens may lie in) and of the others those whose bounds promise most."""
+    device = cache.device
+    if device != _current_device():
+        return _on(device, cache_select, q, cache, bounds, table, cu, lens, max_new, keep, sinks, recent)
+    at, ld = _heads("q", q, device)
+    rows, heads, dim = q.shape
+    if dim != cache.head_dim:
+        _refuse(f"q has heads of {dim}, the cache of {cache.head_dim}")
+    kb = bounds.of(cache)
+    t, width, pcu, plens, B = _places(device, table, cu, lens)
+    tables, lens_out = table.new_empty((B, cache.kv_heads, _choice(keep))), torch.empty_like(lens)
+    max_new = _most(max_new)
+    if rows and B:
+        rc = _fn("samp_cache_select")(at, ld, _TYPES[q.dtype], heads, cache.address, kb, t, width, pcu, plens, B, max_new, rows, keep, *_ends(cache, max_new, rows, sinks, recent),
+                                      tables.data_ptr(), lens_out.data_ptr(), _raw_stream(device))
+        if rc:
+            _raise(rc)
+    else:
+        tables.fill_(-1)
+        lens_out.zero_()
+    return tables, lens_out
+
+
+def _choice(keep: int) -> int:
+    if not 1 <= keep <= 32768:
+        _refuse(f"keep is 1 to 32768 pages ({keep})")
+    return keep
+
+
+def _ends(cache: KVCache, max_new: int, rows: int, sinks: int, recent: Optional[int]) -> Tuple[int, int]:
+    if recent is None:
+        recent = (min(max_new, rows) + cache.page_len - 2) // cache.page_len + 1
+    return _most(sinks), _most(recent)
+
+
+def attention_sparse(q: torch.Tensor, cache: KVCache, bounds: KeyBounds, table: torch.Tensor, cu: Optional[torch.Tensor], lens: torch.Tensor, max_new: int, keep: int,
+                     sinks: int = 1, recent: Optional[int] = None, max_len: Optional[int] = None, scale: Optional[float] = None, tree: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """samp_attention_sparse: attention_cache over the `keep` pages for each sequence and key head that cache_select chooses."""
+    device = cache.device
+    if device != _current_device():
+        return _on(device, attention_sparse, q, cache, bounds, table, cu, lens, max_new, keep, sinks, recent, max_len, scale, tree, out)
+    at, ld = _heads("q", q, device)
+    rows, heads, dim = q.shape
+    if dim != cache.head_dim:
+        _refuse(f"q has heads of {dim}, the cache of {cache.head_dim}")
+    kb = bounds.of(cache)
+    t, width, pcu, plens, B = _places(device, table, cu, lens)
+    words = _flat("tree", tree, torch.int64, device, rows) if tree is not None else 0
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        to = out.data_ptr()
+    else:
+        to = _flat("out", out, q.dtype, device, rows * heads * dim)
+    if rows and B:
+        max_new, max_len = _most(max_new), _most(width * cache.page_len if max_len is None else max_len)
+        need = _workspace_bytes("samp_attention_sparse_workspace_bytes", rows, B, heads, cache.kv_heads, dim, cache.page_len, max_new, max_len, _choice(keep))
+        ws = q.new_empty((need,), dtype=torch.uint8) if need else None
+        rc = _fn("samp_attention_sparse")(at, ld, _TYPES[q.dtype], heads, cache.address, kb, t, width, pcu, plens, B, max_new, max_len, rows, keep,
+                                          *_ends(cache, max_new, rows, sinks, recent), dim ** -0.5 if scale is None else float(scale), words, to,
+                                          ws.data_ptr() if need else 0, need, _raw_stream(device))
         if rc:
             _raise(rc)
     return out

@@ -1,0 +1,191 @@
+"""Beam search's selection against its definition in binary64, on the CPU.
+
+A total is a score plus a logit less the row's log-sum-exp, formed in binary64 from exponentials in binary32.  Those are off by one step (2^-23) each and by their argument's
+rounding, |t| 2^-24 ln 2 for an argument t in powers of two, whose mean under the softmax is at most log2(vocabulary) <= 19; up to 16 are added in binary32 in a row, then 9 sums.  So a
+log-sum-exp is off by less than (2 + 14 + 25) 2^-24 < 48 * 2^-24, and the result is rounded to binary32 once.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+import torch  # noqa: E402
+
+from test_gpu_decoder import F16, BF16, P, gen  # noqa: E402,F401
+
+F32 = torch.float32
+LSE = 48 * 2.0 ** -24
+
+
+def totals(logits, scores, finished, end):
+    """Per row {token: total} as a float64 tensor over the vocabulary (a finished row: its score at place 0), minus infinity for no candidate."""
+    x, s = logits.double(), scores.double()
+    t = s[:, None] + (x - torch.logsumexp(x, 1, keepdim=True))
+    bad = ~torch.isfinite(s) | torch.isnan(x).any(1) | (x == math.inf).any(1)
+    t[bad] = -math.inf
+    t[torch.isnan(t)] = -math.inf                            # (a row of minus infinities)
+    if finished is not None:
+        for r in finished.nonzero().flatten().tolist():
+            t[r] = -math.inf
+            t[r, 0] = s[r] if math.isfinite(s[r]) else -math.inf
+    return t
+
+
+def check(P, logits, scores, beams, keep=None, finished=None, end=7, device=None):
+    """Everything that the definition says: the tokens of a row in the row's order without a gap, the list in order, nothing better left out."""
+    x = (logits if device is None else device)
+    got = P.beam_select(x.cuda(), scores.cuda(), beams, keep, None if finished is None else finished.cuda(), end)
+    best, parents, tokens = (t.cpu() for t in got)
+    keep = keep or beams
+    t = totals(logits, scores, finished, end)
+    B = logits.shape[0] // beams
+    assert best.shape == parents.shape == tokens.shape == (B, keep)
+    for b in range(B):
+        mine = t[b * beams:(b + 1) * beams]
+        n = min(keep, int((mine > -math.inf).sum()))
+        assert (parents[b, n:] == -1).all() and (tokens[b, n:] == -1).all() and (best[b, n:] == -math.inf).all()
+        used = {}
+        for i in range(n):
+            r, v = int(parents[b, i]), int(tokens[b, i])
+            assert b * beams <= r < (b + 1) * beams
+            if finished is not None and finished[r]:
+                assert v == end and best[b, i] == scores[r]
+                v = 0
+            row = used.setdefault(r, [])
+            row.append(v)
+            off = abs(best[b, i].double() - t[r, v]).item()
+            assert off <= LSE + 2.0 ** -24 * abs(t[r, v].item()) * 1.01, (b, i, r, v, off)
+        left = mine.clone()
+        for r, row in used.items():
+            order = torch.sort(logits[r].double(), descending=True, stable=True).indices if finished is None or not finished[r] else torch.tensor([0])
+            assert order[: len(row)].tolist() == row, (b, r)
+            left[r - b * beams, row] = -math.inf
+        if n:
+            assert (best[b, : n - 1] >= best[b, 1:n]).all()
+            assert left.max() <= best[b, n - 1].double() + LSE * 2 + 2.0 ** -24 * abs(best[b, n - 1].item())
+    return best, parents, tokens
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("B,W,V,keep", [(1, 1, 1, 1), (1, 1, 5, 3), (2, 3, 7, 10), (1, 4, 1000, 4), (3, 2, 4095, 64), (2, 5, 4096, 5), (1, 1, 4097, 2), (3, 4, 21128, 8), (40, 4, 32000, 8),
+                                        (2, 64, 300, 64), (130, 3, 17001, 6), (1, 2, 1 << 19, 4)])
+def test_beam_select(P, B, W, V, keep, dtype):
+    g = gen(B + W + V)
+    x = (torch.randn(B * W, V, generator=g) * 3).to(dtype)
+    scores = -10 * torch.rand(B * W, generator=g)
+    check(P, x, scores, W, keep)
+    finished = torch.rand(B * W, generator=g) < 0.3
+    x[torch.rand(B * W, V, generator=g) < 0.1] = -math.inf
+    if W > 1:
+        scores[1::W] = -math.inf
+    check(P, x, scores, W, keep, finished)
+    check(P, x, scores, W, keep, finished.to(torch.uint8), end=-3)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_equal_logits_take_the_lowest_row_then_token(P, dtype):
+    """Rows of one value, in all pieces of a row; and the two zeros, which are equal."""
+    x = torch.zeros(4, 40000, dtype=dtype)
+    best, parents, tokens = check(P, x, torch.zeros(4), 2, 5)
+    assert parents.tolist() == [[0] * 5, [2] * 5] and tokens.tolist() == [[0, 1, 2, 3, 4]] * 2
+    x[:, ::2] = -0.0
+    best, parents, tokens = check(P, x, torch.zeros(4), 2, 5)
+    assert parents.tolist() == [[0] * 5, [2] * 5] and tokens.tolist() == [[0, 1, 2, 3, 4]] * 2
+    x = (torch.randn(1, 30000, generator=gen(3)) * 2).to(dtype).repeat(3, 1)              # beams that are alike
+    best, parents, tokens = check(P, x, torch.tensor([-1.0, -1.0, -1.0]), 3, 9)
+    order = torch.sort(x[0].double(), descending=True, stable=True).indices
+    want, i = [], 0
+    while len(want) < 9:                                     # equal logits of a row count as equal totals: all of the first row, then of the next
+        same = [v for v in order[:64].tolist() if x[0, v] == x[0, order[i]]]
+        want += [(r, v) for r in range(3) for v in same]
+        i += len(same)
+    assert list(zip(parents[0].tolist(), tokens[0].tolist())) == want[:9]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_logits_that_rise_or_fall_all_along(P, dtype):
+    """The best of a row lie next to each other: in one thread's registers, or in one after the other's."""
+    for V in (900, 16384, 33001):
+        x = torch.arange(V).double()
+        x = torch.stack([x, x.flip(0), (x / 8).floor() * 8, x % 97]) * (60.0 / V)
+        check(P, x.to(dtype), torch.tensor([0.0, -0.1, -0.2, -0.3]), 4, 64)
+        check(P, x.to(dtype), torch.tensor([0.0, -0.1, -0.2, -0.3]), 1, 17)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_rows_without_candidates_and_values_at_the_ends(P, dtype):
+    V = 5000
+    low, top = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x = torch.randn(12, V, generator=gen(1)).to(dtype)
+    x[0, 77] = math.nan
+    x[1, 4999] = -math.nan
+    x[2, 0] = math.inf
+    x[3] = -math.inf
+    x[4] = -math.inf
+    x[4, 4321] = 0.5                                         # one token is left
+    x[5] = low                                               # all of them masked by the type's lowest value
+    x[6, 10:] = low
+    x[7] = 2.0 ** -14
+    x[8, 17] = top
+    scores = torch.linspace(-3, -1, 12)
+    scores[9], scores[10] = math.inf, math.nan
+    check(P, x, scores, 1, 3)
+    check(P, x, scores, 4, 8)
+    check(P, x, scores, 12, 16)
+    best, _, tokens = check(P, x[4:6], scores[4:6], 1, 2)
+    assert tokens[0].tolist() == [4321, -1] and best[0, 0] == scores[4] and tokens[1].tolist() == [0, 1]
+    none = P.beam_select(x[:4].cuda(), scores[:4].cuda(), 4)
+    assert (none[0] == -math.inf).all() and (none[1] == -1).all() and (none[2] == -1).all()
+    finished = torch.ones(12, dtype=torch.bool)
+    best, parents, tokens = check(P, x, scores, 4, 3, finished, end=2)       # logits of finished rows are not looked at
+    assert parents[0].tolist() == [3, 2, 1]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_rows_in_place_at_any_alignment(P, dtype):
+    for V, ld, shift in ((1000, 1016, 3), (4001, 4005, 1), (9000, 9011, 7), (16390, 16391, 0)):
+        base = torch.randn(6, ld + shift, generator=gen(V)).to(dtype)
+        base[:, :shift] = 100                                # larger than anything in the rows
+        base[:, shift + V:] = 100
+        view = base.cuda()[:, shift:shift + V]
+        check(P, base[:, shift:shift + V], -torch.rand(6, generator=gen(2)), 3, 6, device=view)
+
+
+def test_beams_of_no_sequences_and_refusals(P):
+    x = torch.zeros(4, 100, dtype=F16, device="cuda")
+    s = torch.zeros(4, device="cuda")
+    best, parents, tokens = P.beam_select(x[:0], s[:0], 4)
+    assert best.shape == parents.shape == tokens.shape == (0, 4)
+    for args, why in (((x, s, 3), "whole sequences"), ((x, s, 0), "beams"), ((x, s, 4, 65), "candidates"), ((x.t(), s, 4), "dense"), ((x.double(), s, 4), "float32"),
+                      ((x, s[:3], 4), "elements"), ((x, s.half(), 4), "float32"), ((x, s, 4, 4, s), "uint8"), ((x, s, 4, 4, None, 1 << 40), "int32")):
+        with pytest.raises(P.SampError, match=why):
+            P.beam_select(*args)
+    with pytest.raises(P.SampError, match="vocabulary"):
+        P.beam_select(torch.zeros(1, (1 << 19) + 1, dtype=F16, device="cuda"), s[:1], 1)
+
+
+def test_selection_in_graphs_and_on_two_streams(P):
+    x = torch.randn(24, 33000, generator=gen(1)).half().cuda()
+    s = -torch.rand(24, generator=gen(2)).cuda()
+    side = [torch.cuda.Stream() for _ in range(2)]
+    graphs = []
+    P.beam_select(x, s, 4, 8)
+    torch.cuda.synchronize()
+    for st in side:
+        with torch.cuda.stream(st):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=st):
+                out = P.beam_select(x, s, 4, 8)
+        graphs.append((g, out))
+    for seed in range(3):
+        x.copy_(torch.randn(24, 33000, generator=gen(seed)).half())
+        torch.cuda.synchronize()
+        for (g, _), st in zip(graphs, side):
+            with torch.cuda.stream(st):
+                g.replay()
+        other = P.beam_select(x, s, 4, 8)
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(out, other))
+    check(P, x.cpu(), s.cpu(), 4, 8)
