@@ -1,11 +1,10 @@
-// Beam search's selection: the best (score, beam, token) of each sequence over the logits of its beams, total = score + logit - log sum exp logits.
+// Beam search's selection: the best (score, beam, token) of each sequence over the logits of its beams, total = score + (logit - log sum exp logits).
 //
 // Two launches.  The first reads every logit once: a block takes a piece of a row into registers, finds its largest value, the sum of exponentials under it and its `keep` best
 // logits: totals of a row are in the order of its logits.  The second joins the pieces of a sequence's rows in binary64 and picks among them.
 //
-// The best of a piece are found by their order as integers: a key holds a logit (as a whole number of the same order) above its index, so keys differ, and the lower
-// index wins among equal logits.  The `keep`-th largest of the threads' own best keys is no more than the `keep`-th largest of all, and no more than `keep` threads have a key that reaches
-// it: only their registers are looked through again.
+// The best of a piece: the `keep`-th largest of the maxima of its groups of threads is no more than the `keep`-th largest value of all.  What reaches it (18 values for keep = 16 and
+// logits in no order) goes to a list in LDS, which is ranked by counting.
 #include "../../include/samp.h"
 #include "decoder.h"
 
@@ -14,62 +13,61 @@
 namespace samp {
 namespace {
 
-constexpr int THREADS = 256;
-// log2(e) in two parts
-constexpr double LOG2E = 1.44269504088896340736;
-constexpr float LOG2E_HI = (float)LOG2E, LOG2E_LO = (float)(LOG2E - (double)LOG2E_HI);
+constexpr int SLOTS = 128, ROOM = 1024;                               // threads of a piece whose values are looked through, and values that are ranked
+constexpr float LOG2E = 1.44269504088896340736f;                      // (1.3e-8 of it off: as much of the mean distance from the largest logit, 2e-7 at most)
 
 enum { F16 = 0, BF16 = 1, F32 = 2 };
 template <int T> struct Logit {
     static constexpr int SIZE = T == F32 ? 4 : 2, VEC = 16 / SIZE;
-    typedef typename std::conditional<T == F32, int64_t, int32_t>::type Key;
-    static constexpr Key NONE = T == F32 ? (Key)INT64_MIN : (Key)INT32_MIN;
-    static constexpr int SHIFT = T == F32 ? 32 : 16;
-    static constexpr int MINUS_INF = T == F16 ? -0x7c00 : T == BF16 ? -0x7f80 : -0x7f800000;
     static constexpr unsigned MINUS_INF_BITS = T == F16 ? 0xfc00u : T == BF16 ? 0xff80u : 0xff800000u;
-    // a value's bits as a whole number of the same order (both zeros are 0), and back
-    static __device__ __forceinline__ int order(unsigned bits)
+    static __device__ __forceinline__ float value(const v4i &raw, int e)
     {
-        if constexpr (T == F32) {
-            const int s = (int)bits >> 31;
-            return ((int)bits ^ (s & 0x7fffffff)) - s;
-        } else {
-            const int v = (int16_t)bits, s = v >> 15;
-            return (v ^ (s & 0x7fff)) - s;
-        }
+        if constexpr (T == F32) return __int_as_float(raw[e]);
+        else if constexpr (T == BF16) return __int_as_float(e & 1 ? raw[e >> 1] & (int)0xffff0000u : raw[e >> 1] << 16);
+        else return (float)__builtin_bit_cast(_Float16, (unsigned short)((unsigned)raw[e >> 1] >> 16 * (e & 1)));
     }
-    static __device__ __forceinline__ float value_of_order(int t)
+    static __device__ __forceinline__ float value(const void *at, int i)
     {
-        const unsigned m = (unsigned)(t < 0 ? -t : t);
-        if constexpr (T == F32) return __uint_as_float(t < 0 ? m | 0x80000000u : m);
-        else return value(t < 0 ? m | 0x8000u : m);
-    }
-    static __device__ __forceinline__ float value(unsigned bits)
-    {
-        if constexpr (T == F32) return __uint_as_float(bits);
-        else if constexpr (T == BF16) return __uint_as_float(bits << 16);
-        else return (float)__builtin_bit_cast(_Float16, (unsigned short)bits);
-    }
-    static __device__ __forceinline__ unsigned bits(const v4i &raw, int e)
-    {
-        if constexpr (T == F32) return (unsigned)raw[e];
-        else return (unsigned)raw[e >> 1] >> 16 * (e & 1) & 0xffffu;
-    }
-    static __device__ __forceinline__ Key key(unsigned bits, int index)
-    {
-        if constexpr (T == F32) return (Key)order(bits) * ((Key)1 << 32) + (Key)(uint32_t)~index;
-        else return (Key)((unsigned)order(bits) << 16 | (0xffffu - (unsigned)index));
-    }
-    static __device__ __forceinline__ int order_of(Key k) { return (int)(k >> SHIFT); }
-    static __device__ __forceinline__ int index_of(Key k)
-    {
-        if constexpr (T == F32) return (int)~(uint32_t)k;
-        else return (int)(0xffffu - ((unsigned)k & 0xffffu));
+        if constexpr (T == F32) return static_cast<const float *>(at)[i];
+        else if constexpr (T == BF16) return __uint_as_float((unsigned)static_cast<const unsigned short *>(at)[i] << 16);
+        else return (float)static_cast<const _Float16 *>(at)[i];
     }
 };
+// (the compiler's own maxima quiet signalling NaN in front: another instruction each)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+template <int CTRL> __device__ __forceinline__ float other_lane(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float max_of_wave(float x)
+{
+    x = max3(x, x, other_lane<0xb1>(x));                              // lanes 1 0 3 2, then 2 3 0 1 of four, eight mirrored, sixteen mirrored
+    x = max3(x, x, other_lane<0x4e>(x));
+    x = max3(x, x, other_lane<0x141>(x));
+    x = max3(x, x, other_lane<0x140>(x));
+    const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 0)), b = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 16));
+    const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 32)), d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 48));
+    return max3(max3(a, b, c), d, d);
+}
+__device__ __forceinline__ float sum_of_wave(float x)
+{
+    x += other_lane<0xb1>(x);
+    x += other_lane<0x4e>(x);
+    x += other_lane<0x141>(x);
+    x += other_lane<0x140>(x);
+    const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 0)), b = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 16));
+    const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 32)), d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 48));
+    return (a + b) + (c + d);
+}
 
 struct Candidate { float logit; int token; };                         // token -1: none
 struct PieceSum { float top, sum; };                                  // sum of exp(x - top)
+struct __attribute__((aligned(8))) Listed { float logit; int place; };
+__device__ __forceinline__ bool before(const Listed &a, const Listed &b) { return a.logit > b.logit || (a.logit == b.logit && a.place < b.place); }
+// The value of a number whose order as an unsigned integer is the values' own (NaN outside the infinities: nothing reaches those)
+__device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t >> 31 ? t & 0x7fffffffu : ~t); }
 
 __device__ __forceinline__ bool row_counts(const float *scores, const uint8_t *finished, int row)
 {
@@ -77,220 +75,372 @@ __device__ __forceinline__ bool row_counts(const float *scores, const uint8_t *f
 }
 
 // One piece of one row.  Vectors of 16 bytes are numbered from the aligned address at or before the row's first value; what of them lies outside the row counts as minus infinity.
-template <int T, int VECTORS>
-__global__ __launch_bounds__(THREADS) void beam_pieces_kernel(const char *__restrict__ logits, long ld, const float *__restrict__ scores,
+template <int T, int THREADS, int VECTORS, int GROUPS>
+__global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__restrict__ logits, long ld, const float *__restrict__ scores,
                                                               const uint8_t *__restrict__ finished, int vocab, int keep, int chunks,
                                                               PieceSum *__restrict__ sums, Candidate *__restrict__ best)
 {
     typedef Logit<T> L;
-    typedef typename L::Key Key;
-    constexpr int PER = VECTORS * L::VEC;                             // values of a thread
-    extern __shared__ __attribute__((aligned(16))) char shared[];
-    v4i *const held = reinterpret_cast<v4i *>(shared);                // [keep][VECTORS]: registers of the threads that are looked through
-    Key *const list = reinterpret_cast<Key *>(shared + (size_t)keep * VECTORS * 16);         // [keep * PER]
-    __shared__ Key tops[THREADS];
-    __shared__ int owner[SAMP_MAX_KEEP];
-    __shared__ Key wave_top[4];
-    __shared__ float wave_part[4];
-    __shared__ Key least;
-    __shared__ int listed;
+    constexpr int VEC = L::VEC, PER = VECTORS * VEC, TEAM = THREADS / GROUPS, WAVES = THREADS / 64;
+    static_assert(GROUPS == 64 || (GROUPS % 64 == 0 && TEAM <= 2), "the same lane of every wave, or one or two neighbours");
+    __shared__ Listed list[ROOM];
+    __shared__ __attribute__((aligned(16))) v4i held[SLOTS][VECTORS];
+    __shared__ int owner[SLOTS];
+    __shared__ __attribute__((aligned(16))) float tops[GROUPS == 64 ? THREADS : GROUPS];
+    __shared__ float wave_top[WAVES], wave_sum[WAVES], least[GROUPS / 64];
+    __shared__ int slots, listed, wave_count[WAVES];
 
     const int row = blockIdx.x / chunks, piece = blockIdx.x - row * chunks;
-    if (!row_counts(scores, finished, row)) return;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    if (VECTORS > 2 && !row_counts(scores, finished, row)) return;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const char *from = logits + (size_t)row * ld * L::SIZE;
     const int phase = (int)(reinterpret_cast<uintptr_t>(from) & 15) / L::SIZE;
     const int first = piece * THREADS * PER - phase;                  // token of the piece's first place
 
     v4i raw[VECTORS];
+    if (first >= 0 && first + THREADS * PER <= vocab) {
+        const v4i *const all = reinterpret_cast<const v4i *>(from + (long)first * L::SIZE) + tid;
 #pragma unroll
-    for (int i = 0; i < VECTORS; i++) {
-        const int at = first + (i * THREADS + tid) * L::VEC;
-        if (at >= 0 && at + L::VEC <= vocab) raw[i] = *reinterpret_cast<const v4i *>(from + (long)at * L::SIZE);
-        else {
-            unsigned x[L::VEC];
+        for (int i = 0; i < VECTORS; i++) raw[i] = all[i * THREADS];
+    } else {
 #pragma unroll
-            for (int e = 0; e < L::VEC; e++) {
-                x[e] = L::MINUS_INF_BITS;
-                if (at + e >= 0 && at + e < vocab) {
-                    if constexpr (T == F32) x[e] = *reinterpret_cast<const unsigned *>(from + (long)(at + e) * 4);
-                    else x[e] = *reinterpret_cast<const unsigned short *>(from + (long)(at + e) * 2);
+        for (int i = 0; i < VECTORS; i++) {
+            const int at = first + (i * THREADS + tid) * VEC;
+            if (at >= 0 && at + VEC <= vocab) raw[i] = *reinterpret_cast<const v4i *>(from + (long)at * L::SIZE);
+            else {
+                unsigned x[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; e++) {
+                    x[e] = L::MINUS_INF_BITS;
+                    if (at + e >= 0 && at + e < vocab) {
+                        if constexpr (T == F32) x[e] = *reinterpret_cast<const unsigned *>(from + (long)(at + e) * 4);
+                        else x[e] = *reinterpret_cast<const unsigned short *>(from + (long)(at + e) * 2);
+                    }
                 }
+#pragma unroll
+                for (int e = 0; e < 4; e++) raw[i][e] = T == F32 ? (int)x[e] : (int)(x[(2 * e) % VEC] | x[(2 * e + 1) % VEC] << 16);
+            }
+        }
+    }
+    // (a short piece waits for its logits and for the row's flags at the same time)
+    if (VECTORS <= 2 && !row_counts(scores, finished, row)) return;
+    if (tid == 0) slots = listed = 0;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < VECTORS; i++)
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) top = max3(top, L::value(raw[i], e), L::value(raw[i], e + 1));
+    if constexpr (GROUPS == 64) tops[tid] = top;
+    else {
+        const float pair = TEAM == 2 ? max3(top, top, other_lane<0xb1>(top)) : top;
+        if (tid % TEAM == 0) tops[tid / TEAM] = pair;
+    }
+    float m = max_of_wave(top);
+    if (m == -INFINITY) m = 0.0f;
+    // (converted again for each use: 32 registers, and waves enough to wait for memory.  With the values kept, 178 registers, 64 x 8 x 128256 took 84 us)
+    auto again = [&]() {
+#pragma unroll
+        for (int i = 0; i < VECTORS; i++) asm("" : "+v"(raw[i]));
+    };
+    again();
+    // exp(x - m) as 2^(x log2(e) - reference), one multiply-add in front of each; the reference is m log2(e) but for its rounding, which the sum makes up for.  Where
+    // that product is past binary32 (logits of the type's lowest value alone) the difference comes first.
+    float part[4] = {}, sum;
+    if (__builtin_fabsf(m) < 0x1p126f) {
+        const float reference = m * LOG2E;
+#pragma unroll
+        for (int i = 0; i < VECTORS; i++)
+#pragma unroll
+            for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(L::value(raw[i], e), LOG2E, -reference));
+        sum = ((part[0] + part[1]) + (part[2] + part[3])) * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, LOG2E, -reference));
+    } else {
+#pragma unroll
+        for (int i = 0; i < VECTORS; i++)
+#pragma unroll
+            for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f((L::value(raw[i], e) - m) * LOG2E);
+        sum = (part[0] + part[1]) + (part[2] + part[3]);
+    }
+    again();
+    sum = sum_of_wave(sum);
+    if (lane == 0) {
+        wave_top[w] = m;
+        wave_sum[w] = sum;
+    }
+    __syncthreads();
+    if (tid < GROUPS) {
+        // the `keep`-th largest of the groups' maxima: the smallest of those that fewer than `keep` are above
+        float mine = tops[tid];
+        int above = 0;
+        if constexpr (GROUPS == 64) {
+#pragma unroll
+            for (int i = 1; i < WAVES; i++) mine = max3(mine, mine, tops[64 * i + tid]);
+#pragma unroll
+            for (int i = 0; i < 64; i++) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), i)) > mine;
+        } else {
+            const v4f *const all = reinterpret_cast<const v4f *>(tops);
+#pragma unroll 16
+            for (int i = 0; i < GROUPS / 4; i++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) above += all[i][e] > mine;
+        }
+        const float t = -max_of_wave(above < keep ? -mine : -INFINITY);
+        if (lane == 0) least[w] = t;
+    }
+    if (w == WAVES - 1) {
+        const float u = lane < WAVES ? wave_top[lane] : -INFINITY, all = max_of_wave(lane < WAVES && wave_sum[lane] != 0.0f ? u : -INFINITY);
+        const float s = lane < WAVES && wave_sum[lane] != 0.0f ? wave_sum[lane] * __builtin_amdgcn_exp2f((u - all) * LOG2E) : 0.0f;
+        const float total = sum_of_wave(s);
+        if (lane == 0) sums[blockIdx.x] = PieceSum{all, total};
+    }
+    __syncthreads();
+    float limit = least[0];
+#pragma unroll
+    for (int i = 1; i < GROUPS / 64; i++) limit = __builtin_fminf(limit, least[i]);
+    limit = __builtin_fmaxf(limit, -3.40282347e38f);                  // (minus infinity is no candidate)
+
+    // threads that have a value that reaches `limit` leave all of theirs in LDS, where the block looks through them
+    if (top >= limit) {
+        int *count = &slots;
+        asm("" : "+v"(count));                                        // (few lanes: an addition of theirs each, not one of the wave's)
+        const int slot = atomicAdd(count, 1);
+        if (slot < SLOTS) {
+            owner[slot] = tid;
+#pragma unroll
+            for (int i = 0; i < VECTORS; i++) held[slot][i] = raw[i];
+        }
+    }
+    __syncthreads();
+    int n = slots;                                                    // (this and what follows from it: the same for the whole block)
+    if (n <= SLOTS) {
+        for (int at = tid; at < n * PER; at += THREADS) {
+            const int slot = at / PER, e = at % PER;
+            const float x = L::value(&held[slot][0], e);
+            if (x >= limit) {
+                int *count = &listed;
+                asm("" : "+v"(count));
+                const int to = atomicAdd(count, 1);                   // (in any order: they are ranked)
+                if (to < ROOM) list[to] = Listed{x, (e / VEC * THREADS + owner[slot]) * VEC + e % VEC};
+            }
+        }
+        __syncthreads();
+        n = listed;
+    } else n = ROOM + 1;
+    if (n > ROOM) {
+        // Many reach the limit, as in rows of one value.  The `keep`-th largest value itself, bit by bit from the top; what is above it, less than `keep` values; and those that
+        // equal it, in the order of their places.
+        unsigned t = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 0; bit--) {
+            again();
+            const float v = value_of_order(t | 1u << bit);
+            int reach = 0;
+#pragma unroll
+            for (int i = 0; i < VECTORS; i++)
+#pragma unroll
+                for (int e = 0; e < VEC; e++) reach += L::value(raw[i], e) >= v;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) reach += __shfl_xor(reach, o, 64);
+            __syncthreads();
+            if (lane == 0) wave_count[w] = reach;
+            __syncthreads();
+            reach = 0;
+#pragma unroll
+            for (int i = 0; i < WAVES; i++) reach += wave_count[i];
+            if (reach >= keep) t |= 1u << bit;
+        }
+        limit = __builtin_fmaxf(value_of_order(t), -3.40282347e38f);
+        again();
+        __syncthreads();
+        if (tid == 0) listed = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < VECTORS; i++)
+#pragma unroll
+            for (int e = 0; e < VEC; e++)
+                if (L::value(raw[i], e) > limit) {
+                    const int to = atomicAdd(&listed, 1);
+                    if (to < ROOM) list[to] = Listed{L::value(raw[i], e), (i * THREADS + tid) * VEC + e};
+                }
+        __syncthreads();
+        n = listed;
+        again();
+#pragma unroll
+        for (int i = 0; i < VECTORS; i++) {
+            int at = tid;
+            asm("" : "+v"(at));
+            unsigned equal = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) equal |= (unsigned)(L::value(raw[i], e) == limit) << e;
+            int before = __popc(equal);
+            const int mine = before;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int other = __shfl_up(before, o, 64);
+                if (lane >= o) before += other;
+            }
+            __syncthreads();
+            if (lane == 63) wave_count[w] = before;
+            __syncthreads();
+            int to = n + before - mine;
+#pragma unroll
+            for (int u = 0; u < WAVES; u++) {
+                to += u < w ? wave_count[u] : 0;
+                n += wave_count[u];
             }
 #pragma unroll
-            for (int e = 0; e < 4; e++) raw[i][e] = T == F32 ? (int)x[e] : (int)(x[(2 * e) % L::VEC] | x[(2 * e + 1) % L::VEC] << 16);
+            for (int e = 0; e < VEC; e++) {
+                if ((equal >> e & 1) && to < ROOM) list[to] = Listed{limit, (i * THREADS + at) * VEC + e};
+                to += equal >> e & 1;
+            }
         }
+        __syncthreads();
+        n = min(n, keep);                                             // (those above come first in the list)
     }
-    Key top = L::NONE;
-#pragma unroll
-    for (int i = 0; i < VECTORS; i++)
-#pragma unroll
-        for (int e = 0; e < L::VEC; e++) top = max(top, L::key(L::bits(raw[i], e), (i * THREADS + tid) * L::VEC + e));
-    tops[tid] = top;
-    Key most = top;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) most = max(most, (Key)__shfl_xor(most, o, 64));
-    if (lane == 0) wave_top[w] = most;
-    if (tid == 0) {
-        least = L::NONE;
-        listed = 0;
-    }
-    if (tid < keep) owner[tid] = -1;
-    __syncthreads();
-    most = max(max(wave_top[0], wave_top[1]), max(wave_top[2], wave_top[3]));
-    // (NaN of negative sign lie below, of positive sign above all numbers)
-    const float m = L::order_of(most) > L::MINUS_INF ? L::value_of_order(L::order_of(most)) : 0.0f;
-
-    // how many threads have a better key: the first `keep` of them are looked through
-    if (L::order_of(top) > L::MINUS_INF) {
-        int better = 0;
-        for (int i = 0; i < THREADS; i++) better += tops[i] > top;
-        if (better < keep) {
-            owner[better] = tid;
-#pragma unroll
-            for (int i = 0; i < VECTORS; i++) held[better * VECTORS + i] = raw[i];
-            if (better == keep - 1) least = top;
-        }
-    }
-    float part[4] = {};
-#pragma unroll
-    for (int i = 0; i < VECTORS; i++)
-#pragma unroll
-        for (int e = 0; e < L::VEC; e++) {
-            const float d = L::value(L::bits(raw[i], e)) - m;          // (logits of the type's lowest value alone: zeros)
-            part[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(d, LOG2E_HI, d * LOG2E_LO));
-        }
-    float sum = (part[0] + part[1]) + (part[2] + part[3]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (lane == 0) wave_part[w] = sum;
-    __syncthreads();
-    if (tid == 0) sums[blockIdx.x] = PieceSum{m, (wave_part[0] + wave_part[1]) + (wave_part[2] + wave_part[3])};
-
-    for (int at = tid; at < keep * PER; at += THREADS) {
-        const int slot = at / PER, who = owner[slot];
-        if (who < 0) continue;
-        const int i = at % PER / L::VEC, e = at % L::VEC;
-        unsigned b;
-        if constexpr (T == F32) b = (unsigned)reinterpret_cast<const int *>(held)[(slot * VECTORS + i) * 4 + e];
-        else b = reinterpret_cast<const unsigned short *>(held)[(slot * VECTORS + i) * 8 + e];
-        const Key k = L::key(b, (i * THREADS + who) * L::VEC + e);
-        if (k >= least && L::order_of(k) > L::MINUS_INF) list[atomicAdd(&listed, 1)] = k;     // (in any order: they are ranked)
-    }
-    __syncthreads();
-    const int n = listed;
     Candidate *const to = best + (size_t)blockIdx.x * keep;
     for (int at = tid; at < n; at += THREADS) {
-        const Key k = list[at];
+        const Listed k = list[at];
         int better = 0;
-        for (int i = 0; i < n; i++) better += list[i] > k;
-        if (better < keep) to[better] = Candidate{L::value_of_order(L::order_of(k)), first + L::index_of(k)};
+#pragma unroll 4
+        for (int i = 0; i < n; i++) better += before(list[i], k);
+        if (better < keep) to[better] = Candidate{k.logit, first + k.place};
     }
     if (tid < keep && tid >= n) to[tid] = Candidate{-INFINITY, -1};
 }
 
-// One sequence.  The pieces' lists are sorted: entry p of the list whose first entry is the r-th best of all first entries can be among the `keep` best only where r + p < keep, and those
-// keep (keep + 1) / 2 are ranked by counting.  place = beam << 20 | token.
-struct __attribute__((aligned(16))) Entry { double total; float logit; int place; };
-constexpr Entry NONE{-INFINITY, 0.0f, INT32_MAX};
-__device__ __forceinline__ bool before(const Entry &a, const Entry &b)
+// One sequence.  The pieces' lists are sorted: entry p of the list whose first entry is the r-th best of all first entries can be among the `keep` best only where r + p < keep; of those
+// keep (keep + 1) / 2 the ones that reach a total that `keep` entries reach are ranked by counting, several lanes to an entry.  Entries are a total as a whole number of the same order, then row, logit and token.
+constexpr int JOIN = 1024;
+struct __attribute__((aligned(16))) Entry { unsigned long long total, then; };
+constexpr Entry NO_ENTRY{0, ~0ull};
+__device__ __forceinline__ bool before(const Entry &a, const Entry &b) { return a.total > b.total || (a.total == b.total && a.then < b.then); }
+__device__ __forceinline__ Entry entry_of(double total, int r, float logit, int token)
 {
-    if (a.total != b.total) return a.total > b.total;
-    const bool one_row = (a.place ^ b.place) >> 20 == 0;
-    return one_row && a.logit != b.logit ? a.logit > b.logit : a.place < b.place;
+    if (!(total > -INFINITY)) return NO_ENTRY;
+    const unsigned long long t = (unsigned long long)__double_as_longlong(total + 0.0);
+    const unsigned l = __float_as_uint(logit + 0.0f), high_first = l >> 31 ? l : ~(l | 0x80000000u);
+    return Entry{t >> 63 ? ~t : t | 1ull << 63, (unsigned long long)r << 52 | (unsigned long long)high_first << 20 | (unsigned)token};
+}
+__device__ __forceinline__ double total_of(const Entry &e)
+{
+    return __longlong_as_double((long long)(e.total >> 63 ? e.total & ~(1ull << 63) : ~e.total));
+}
+// f(entry, how many of the n come before it) for every one of them that is there
+template <class F> __device__ __forceinline__ void rank_entries(const Entry *all, int n, F &&f)
+{
+    int share = 1;
+    while (share < 64 && n * share * 2 <= JOIN) share *= 2;
+    const int mine = threadIdx.x & (share - 1);
+    for (int i = (int)threadIdx.x / share; i < n; i += JOIN / share) {
+        const Entry e = all[i];
+        int better = 0;
+#pragma unroll 4
+        for (int j = mine; j < n; j += share) better += before(all[j], e);
+        for (int o = 1; o < share; o <<= 1) better += __shfl_xor(better, o, 64);
+        if (mine == 0 && e.total) f(i, e, better);
+    }
 }
 
-__global__ __launch_bounds__(THREADS) void beam_join_kernel(const PieceSum *__restrict__ sums, const Candidate *__restrict__ best, const float *__restrict__ scores,
-                                                            const uint8_t *__restrict__ finished, int end, int beams, int keep, int chunks,
-                                                            float *__restrict__ out, int *__restrict__ parents, int *__restrict__ tokens)
+__global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restrict__ sums, const Candidate *__restrict__ best, const float *__restrict__ scores,
+                                                         const uint8_t *__restrict__ finished, int end, int beams, int keep, int chunks, float *__restrict__ out,
+                                                         int *__restrict__ parents, int *__restrict__ tokens)
 {
-    extern __shared__ __attribute__((aligned(16))) char shared[];
-    const int lists = beams * chunks, pairs = keep * (keep + 1) / 2;
-    Entry *const first = reinterpret_cast<Entry *>(shared), *const pair = first + lists;
+    extern __shared__ __attribute__((aligned(16))) Entry first[];
+    const int lists = beams * chunks;
+    Entry *const pair = first + lists;
     __shared__ double lse[SAMP_MAX_BEAMS];                            // log sum exp; NaN where a row's logits have no candidates
-    __shared__ int list_of[SAMP_MAX_KEEP];
+    __shared__ float score[SAMP_MAX_BEAMS];                           // NaN where a row has none
+    __shared__ bool done[SAMP_MAX_BEAMS];
+    __shared__ int list_of[SAMP_MAX_KEEP], there;
+    __shared__ unsigned long long enough;                             // a total that at least `keep` entries reach, or 0
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    for (int r = w; r < beams; r += THREADS / 64) {
-        const int row = b * beams + r;
-        double o = __builtin_nan("");
-        if (row_counts(scores, finished, row)) {
-            float top = -INFINITY;
-            for (int c = lane; c < chunks; c += 64) {
-                const PieceSum p = sums[(size_t)row * chunks + c];
-                if (!(p.sum == 0.0f)) top = __builtin_fmaxf(top, p.top);
-            }
-            top = wave_max(top);
-            double sum = 0.0;
-            for (int c = lane; c < chunks; c += 64) {
-                const PieceSum p = sums[(size_t)row * chunks + c];
-                if (!(p.sum == 0.0f)) sum += (double)p.sum * exp((double)p.top - (double)top);
-            }
-            sum = wave_sum(sum);
-            // (no finite logit: a sum of 0; NaN or plus infinity: a sum of NaN)
-            if (sum > 0.0) o = (double)top + log(sum);
-        }
-        if (lane == 0) lse[r] = o;
+    const size_t row0 = (size_t)b * beams;
+    // (of rows that do not count nothing was written: what is read of them is not used)
+    const Candidate head = tid < lists ? best[(row0 * chunks + tid) * keep] : Candidate{0.0f, -1};
+    if (tid < beams) {
+        const float s = scores[row0 + tid];
+        score[tid] = __builtin_isfinite(s) ? s : __builtin_nanf("");
+        done[tid] = finished && finished[row0 + tid];
     }
     if (tid < keep) list_of[tid] = -1;
+    if (tid == 0) there = 0, enough = 0;
+    for (int r = w; r < beams; r += JOIN / 64) {
+        const PieceSum *const of = sums + (row0 + r) * chunks;
+        const PieceSum mine = lane < chunks ? of[lane] : PieceSum{0.0f, 0.0f};
+        float top = mine.sum == 0.0f ? -INFINITY : mine.top;          // (a sum of 0: nothing finite there)
+        for (int c = lane + 64; c < chunks; c += 64)
+            if (!(of[c].sum == 0.0f)) top = __builtin_fmaxf(top, of[c].top);
+        top = wave_max(top);
+        double sum = mine.sum == 0.0f ? 0.0 : (double)mine.sum * exp((double)mine.top - (double)top);
+        for (int c = lane + 64; c < chunks; c += 64)
+            if (!(of[c].sum == 0.0f)) sum += (double)of[c].sum * exp((double)of[c].top - (double)top);
+        sum = wave_sum(sum);
+        // (no finite logit: a sum of 0; NaN or plus infinity: a sum of NaN)
+        if (lane == 0) lse[r] = sum > 0.0 ? (double)top + log(sum) : __builtin_nan("");
+    }
     __syncthreads();
-    auto entry = [&](int list, int p) {
-        const int r = list / chunks, c = list - r * chunks, row = b * beams + r;
-        Entry e = NONE;
-        if (finished && finished[row]) {
-            const float s = scores[row];
-            if (c == 0 && p == 0 && __builtin_isfinite(s)) e = Entry{(double)s, 0.0f, r << 20};
-        } else if (__builtin_isfinite(lse[r])) {
-            const Candidate x = best[((size_t)row * chunks + c) * keep + p];
-            if (x.token >= 0) e = Entry{(double)scores[row] + ((double)x.logit - lse[r]), x.logit, r << 20 | x.token};
-        }
-        return e;
+    auto entry = [&](int list, int p, const Candidate &x) {
+        const int r = list / chunks;
+        if (done[r]) return list == r * chunks && p == 0 ? entry_of((double)score[r], r, 0.0f, 0) : NO_ENTRY;
+        return x.token >= 0 ? entry_of((double)score[r] + ((double)x.logit - lse[r]), r, x.logit, x.token) : NO_ENTRY;
     };
-    for (int i = tid; i < lists; i += THREADS) first[i] = entry(i, 0);
+    if (tid < lists) first[tid] = entry(tid, 0, head);
+    for (int i = tid + JOIN; i < lists; i += JOIN) first[i] = entry(i, 0, best[(row0 * chunks + i) * keep]);
     __syncthreads();
-    for (int i = tid; i < lists; i += THREADS) {
-        const Entry e = first[i];
-        if (e.place == INT32_MAX) continue;
-        int better = 0;
-        for (int j = 0; j < lists; j++) better += before(first[j], e);
+    rank_entries(first, lists, [&](int i, const Entry &e, int better) {
         if (better < keep) list_of[better] = i;
-    }
+        if (better == keep - 1) enough = e.total;
+    });
     __syncthreads();
-    for (int at = tid; at < keep * keep; at += THREADS) {
-        const int r = at / keep, p = at - r * keep;
+    if (lists < keep) {
+        // of few lists entry `deep` - 1 of the `deep`-th part of `keep` lists
+        const int deep = (keep + lists - 1) / lists, part = (keep + deep - 1) / deep;
+        if (tid < lists) pair[tid] = entry(tid, deep - 1, best[(row0 * chunks + tid) * keep + deep - 1]);
+        __syncthreads();
+        rank_entries(pair, lists, [&](int, const Entry &e, int better) {
+            if (better == part - 1) enough = e.total;
+        });
+        __syncthreads();
+    }
+    for (int at = tid; at < keep * keep; at += JOIN) {
+        const int r = at / keep, p = at - r * keep, list = list_of[r];
         if (r + p >= keep) continue;
-        pair[r * keep - r * (r - 1) / 2 + p] = list_of[r] >= 0 ? entry(list_of[r], p) : NONE;
+        const Entry e = list >= 0 ? entry(list, p, best[(row0 * chunks + list) * keep + p]) : NO_ENTRY;
+        if (e.total && e.total >= enough) pair[atomicAdd(&there, 1)] = e;              // (in any order: they are ranked)
     }
     __syncthreads();
-    int there = 0;
-    for (int i = 0; i < pairs; i++) there += pair[i].place != INT32_MAX;
-    for (int i = tid; i < pairs; i += THREADS) {
-        const Entry e = pair[i];
-        if (e.place == INT32_MAX) continue;
-        int better = 0;
-        for (int j = 0; j < pairs; j++) better += before(pair[j], e);
-        if (better < keep) {
-            const int r = e.place >> 20, row = b * beams + r;
-            out[(size_t)b * keep + better] = (float)e.total;
-            parents[(size_t)b * keep + better] = row;
-            tokens[(size_t)b * keep + better] = finished && finished[row] ? end : e.place & 0xfffff;
-        }
+    const size_t to = (size_t)b * keep;
+    rank_entries(pair, there, [&](int, const Entry &e, int better) {
+        if (better >= keep) return;
+        const int r = (int)(e.then >> 52);
+        out[to + better] = (float)total_of(e);
+        parents[to + better] = (int)row0 + r;
+        tokens[to + better] = done[r] ? end : (int)(e.then & 0xfffff);
+    });
+    if (tid < keep && tid >= there) {
+        out[to + tid] = -INFINITY;
+        parents[to + tid] = tokens[to + tid] = -1;
     }
-    for (int i = tid; i < keep; i += THREADS)
-        if (i >= there) {
-            out[(size_t)b * keep + i] = -INFINITY;
-            parents[(size_t)b * keep + i] = tokens[(size_t)b * keep + i] = -1;
-        }
 }
 
-int values_of(int type, int vectors) { return THREADS * vectors * (type == F32 ? 4 : 8); }
+// pieces of 512 threads with eight vectors each, or of 256 with two
+struct Piece { int threads, vectors; };
+constexpr Piece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
+int values_of(int type, Piece p) { return p.threads * p.vectors * (type == F32 ? 4 : 8); }
 
+template <int T, int THREADS, int VECTORS>
+void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, int chunks, PieceSum *sums, Candidate *best,
+            hipStream_t st)
+{
+    auto kern = keep <= 16 ? beam_pieces_kernel<T, THREADS, VECTORS, 64> : beam_pieces_kernel<T, THREADS, VECTORS, 256>;
+    hipLaunchKernelGGL(kern, dim3((unsigned)(rows * chunks)), dim3(THREADS), 0, st, (const char *)logits, ld, scores, finished,
+                       vocab, keep, chunks, sums, best);
+}
 template <int T>
 void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, BeamCut cut, PieceSum *sums, Candidate *best,
             hipStream_t st)
 {
-    auto kern = cut.vectors == 8 ? beam_pieces_kernel<T, 8> : beam_pieces_kernel<T, 2>;
-    const size_t lds = (size_t)keep * cut.vectors * (16 + Logit<T>::VEC * sizeof(typename Logit<T>::Key));
-    hipLaunchKernelGGL(kern, dim3((unsigned)(rows * cut.chunks)), dim3(THREADS), lds, st, (const char *)logits, ld, scores, finished, vocab, keep, cut.chunks, sums, best);
+    if (cut.large) pieces<T, LONG_PIECE.threads, LONG_PIECE.vectors>(logits, ld, scores, finished, rows, vocab, keep, cut.chunks, sums, best, st);
+    else pieces<T, SHORT_PIECE.threads, SHORT_PIECE.vectors>(logits, ld, scores, finished, rows, vocab, keep, cut.chunks, sums, best, st);
 }
 
 }  // namespace
@@ -298,9 +448,9 @@ void pieces(const void *logits, long ld, const float *scores, const uint8_t *fin
 BeamCut beam_cut(int type, int rows, int vocab)
 {
     const int phase = (type == F32 ? 4 : 8) - 1;                      // places that a row may begin behind an aligned address
-    auto chunks = [&](int vectors) { return (vocab + phase + values_of(type, vectors) - 1) / values_of(type, vectors); };
-    const int vectors = (long)rows * chunks(8) >= 512 ? 8 : 2;
-    return BeamCut{vectors, chunks(vectors)};
+    auto chunks = [&](Piece p) { return (vocab + phase + values_of(type, p) - 1) / values_of(type, p); };
+    const bool large = (long)rows * chunks(LONG_PIECE) >= 512;
+    return BeamCut{large, chunks(large ? LONG_PIECE : SHORT_PIECE)};
 }
 
 size_t beam_workspace(int type, int batch, int beams, int vocab, int keep)
@@ -313,15 +463,16 @@ hipError_t launch_beam_select(const void *logits, long ld, int type, const float
                               float *best, int *parents, int *tokens, void *ws, hipStream_t st)
 {
     const BeamCut cut = beam_cut(type, batch * beams, vocab);
+    const int rows = batch * beams;
     Candidate *const candidates = static_cast<Candidate *>(ws);
-    PieceSum *const sums = reinterpret_cast<PieceSum *>(candidates + (size_t)batch * beams * cut.chunks * keep);
-    if (type == F16) pieces<F16>(logits, ld, scores, finished, batch * beams, vocab, keep, cut, sums, candidates, st);
-    else if (type == BF16) pieces<BF16>(logits, ld, scores, finished, batch * beams, vocab, keep, cut, sums, candidates, st);
-    else pieces<F32>(logits, ld, scores, finished, batch * beams, vocab, keep, cut, sums, candidates, st);
+    PieceSum *const sums = reinterpret_cast<PieceSum *>(candidates + (size_t)rows * cut.chunks * keep);
+    if (type == F16) pieces<F16>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
+    else if (type == BF16) pieces<BF16>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
+    else pieces<F32>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
     const size_t lds = sizeof(Entry) * ((size_t)beams * cut.chunks + (size_t)keep * (keep + 1) / 2);
-    if (lds > 64 << 10)
-        if (hipError_t e = hipFuncSetAttribute((const void *)beam_join_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)batch), dim3(THREADS), lds, st, sums, candidates, scores, finished, end, beams, keep, cut.chunks, best, parents,
+    if (lds > 60 << 10)
+        if (hipError_t err = hipFuncSetAttribute((const void *)beam_join_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return err;
+    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)batch), dim3(JOIN), lds, st, sums, candidates, scores, finished, end, beams, keep, cut.chunks, best, parents,
                        tokens);
     return hipGetLastError();
 }

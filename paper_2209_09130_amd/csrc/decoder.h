@@ -133,7 +133,7 @@ hipError_t launch_causal_attention(const void *q, long ldq, const void *k, long 
                                    int head_dim, const int *cu, int batch, int max_len, int rows, float scale, void *out, hipStream_t st);
 
 // Beam search: type as in samp.h; the bytes of the workspace follow from how a row is cut
-struct BeamCut { int vectors, chunks; };                              // 16-byte vectors of a thread, blocks of a row
+struct BeamCut { bool large; int chunks; };                           // kind and number of a row's pieces
 BeamCut beam_cut(int type, int rows, int vocab);
 size_t beam_workspace(int type, int batch, int beams, int vocab, int keep);
 hipError_t launch_beam_select(const void *logits, long ld, int type, const float *scores, const uint8_t *finished, int end, int batch, int beams, int vocab, int keep,
