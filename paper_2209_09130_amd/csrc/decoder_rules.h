@@ -58,9 +58,11 @@ inline int tokens_band(int tile) { return tile == 4 ? 4 : 8; }
 inline int cache_passes(long rows, int kv_heads) { return rows * kv_heads >= 32768 ? 4 : 1; }
 
 // ---- bookkeeping of pages ------------------------------------------------------------------------------
-// One block does a whole call where its counters fit the LDS of a CU: two for each page and one for each row, and 64 KB of bits and counts.
-inline long fork_block_lds(long pages, long rows) { return 8 * pages + 4 * rows; }
-inline bool fork_in_block(long pages, long rows) { return fork_block_lds(pages, rows) <= 150 << 10; }
-inline bool compact_in_block(long pages, long entries) { return pages <= 65536 && entries <= 65536; }
+// One block does a whole call where its counters fit the LDS of a CU: two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 for each old
+// one; 6 bytes for each page.
+inline long fork_block_lds(long pages, long rows_from, long rows) { return 10 * pages + 16 * rows_from + (32 + 4) * rows; }
+inline bool fork_in_block(long pages, long rows_from, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10; }
+inline long compact_block_lds(long pages) { return 4 * pages + 2 * (pages / 2 + 1); }
+inline bool compact_in_block(long pages, long entries) { return pages <= 24 * 1024 && entries <= 65536; }
 
 }  // namespace samp

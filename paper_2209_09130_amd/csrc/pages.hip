@@ -12,32 +12,59 @@ namespace {
 
 constexpr int BLOCK = 1024, NONE = 0x7fffffff;
 
-// the sum of the values of the threads before this one, and of all; `parts` holds a value for each wave
-__device__ __forceinline__ int block_scan(int v, int *parts, int &all)
+// A barrier for what the threads hand each other in LDS: stores to memory need not have arrived
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+template <bool LDS> __device__ __forceinline__ void barrier()
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    int sum = v;
+    if constexpr (LDS) lds_barrier();
+    else __syncthreads();
+}
+
+// the sum of the lanes up to this one (row shifts, then the last lanes of rows 0 and 2, then of row 1)
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+// the sums of the values of the threads before this one, and of all, N of them at a time; `parts` holds a value for each wave
+template <int WAVES, int N>
+__device__ __forceinline__ void block_scan(const int (&v)[N], int (*parts)[WAVES], int (&before)[N], int (&all)[N])
+{
+    static_assert(WAVES <= 16, "a wave's first lanes hold the waves' sums");
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int sum[N];
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int other = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += other;
+    for (int n = 0; n < N; n++) sum[n] = wave_scan(v[n]);
+    lds_barrier();                                                    // (parts may still be read from a scan before)
+#pragma unroll
+    for (int n = 0; n < N; n++)
+        if (lane == 63) parts[n][w] = sum[n];
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+        const int waves = wave_scan(lane < WAVES ? parts[n][lane] : 0);
+        all[n] = __builtin_amdgcn_readlane(waves, WAVES - 1);
+        before[n] = sum[n] - v[n] + (w ? __builtin_amdgcn_readlane(waves, max(w - 1, 0)) : 0);
     }
-    __syncthreads();
-    if (lane == 63) parts[w] = sum;
-    __syncthreads();
-    int before = 0;
-    all = 0;
-    for (int i = 0; i < (int)blockDim.x >> 6; i++) {
-        const int p = parts[i];
-        before += i < w ? p : 0;
-        all += p;
-    }
-    return before + sum - v;
+}
+template <int WAVES> __device__ __forceinline__ int block_scan(int v, int (&parts)[WAVES], int &all)
+{
+    const int one[1] = {v};
+    int before[1], sum[1];
+    block_scan<WAVES, 1>(one, &parts, before, sum);
+    all = sum[0];
+    return before[0];
 }
 
 // ---- fork --------------------------------------------------------------------------------------------
-// Entries first .. end - 1 of a row are those that its next positions lie in; wide: how many of them the table has no room for
-struct RowPlan { int parent, held, first, end; long len; int wide; };
+// Entries first .. end - 1 of a row are those that its next positions lie in, page what its parent has in the first of them; len: its next length; wide: how many entries the
+// table has no room for
+struct __attribute__((aligned(16))) RowPlan { int parent, held, first, end, page, len, wide, pad; };
 __device__ __forceinline__ RowPlan row_plan(const PageFork &f, int i)
 {
     RowPlan r{};
@@ -48,8 +75,9 @@ __device__ __forceinline__ RowPlan row_plan(const PageFork &f, int i)
     }
     const int held = f.lens[r.parent], next = f.cu ? f.cu[i + 1] - f.cu[i] : f.max_new;
     r.held = held > 0 ? held : 0;
-    r.len = (long)r.held + (next > 0 ? next : 0);
-    const long end = (r.len + (1 << f.page_shift) - 1) >> f.page_shift, first = next > 0 ? r.held >> f.page_shift : end;
+    const long len = (long)r.held + (next > 0 ? next : 0);
+    r.len = len > NONE ? NONE : (int)len;
+    const long end = (len + (1 << f.page_shift) - 1) >> f.page_shift, first = next > 0 ? r.held >> f.page_shift : end;
     r.end = (int)(end < f.width ? end : f.width);
     r.first = (int)(first < f.width ? first : f.width);
     r.wide = (int)(end - (first > f.width ? first : f.width));
@@ -60,146 +88,231 @@ __device__ __forceinline__ bool in_cache(const PageFork &f, int page) { return (
 
 // Counters of pages: `rest` is what names a page in the new tables and does not write it, `first` the place of the first entry that does
 struct Counters { int *rest, *first; };
-
-// The old tables' names leave, the new ones' come; entries that nothing is written to are done with.  Threads `at`, at + step .. of all
-__device__ __forceinline__ void count_names(const PageFork &f, const Counters &c, long at, long step)
-{
-    const long old = (long)f.rows_from * f.width;
-    for (long i = at; i < old; i += step) {
-        const int page = f.table[i];
-        if (in_cache(f, page)) atomicAdd(&c.rest[page], -1);
-    }
-    const long all = (long)f.rows * f.width;
-    for (long i = at; i < all; i += step) {
-        const int row = (int)(i / f.width), j = (int)(i - (long)row * f.width);
-        const RowPlan r = row_plan(f, row);
-        int page = j < r.end && r.parent >= 0 ? f.table[(long)r.parent * f.width + j] : -1;
-        if (!in_cache(f, page)) page = -1;
-        if (j < r.first || j >= r.end) {
-            if (page >= 0) atomicAdd(&c.rest[page], 1);
-            f.table_out[i] = page;
-        }
-    }
-}
-
-// Eight lanes a row: which of its entries first + lane, + 8 .. are written
 __device__ __forceinline__ int child_page(const PageFork &f, const RowPlan &r, int j)
 {
     const int page = j < r.end ? f.table[(long)r.parent * f.width + j] : -1;
     return in_cache(f, page) ? page : -1;
 }
-__device__ __forceinline__ void count_writers(const PageFork &f, const Counters &c, int row, int lane)
-{
-    const RowPlan r = row_plan(f, row);
-    for (int j = r.first + lane; j < r.end; j += 8) {
-        const int page = child_page(f, r, j);
-        if (page >= 0) atomicMin(&c.first[page], row * f.width + j);
-    }
-}
 // the entry's page stays where nothing else names the page but entries that write it too, later ones
 __device__ __forceinline__ bool stays(const Counters &c, int page, int place) { return page >= 0 && c.rest[page] == 0 && c.first[page] == place; }
-__device__ __forceinline__ unsigned of_eight(bool b) { return (unsigned)(__ballot(b) >> (threadIdx.x & 56)) & 0xffu; }
 
-__device__ __forceinline__ int count_needs(const PageFork &f, const Counters &c, int row, int lane)
+// One block.  A thread has every BLOCK-th row (neighbours in different waves) and its first written entry, which is all there is to a row that goes on by a token;
+// f(its number or -1, its plan) for each round of them.
+template <class Plan, class F> __device__ __forceinline__ void each_row(const PageFork &f, Plan &&plan, F &&do_row)
 {
-    const RowPlan r = row_plan(f, row);
-    int needs = 0;
-    for (int j0 = r.first; j0 < r.end; j0 += 8) {
-        const int j = j0 + lane;
-        needs += __popc(of_eight(j < r.end && !stays(c, child_page(f, r, j), row * f.width + j)));
+    constexpr int WAVES = BLOCK / 64;
+    for (int i0 = 0; i0 < f.rows; i0 += BLOCK) {
+        const int row = i0 + (int)(threadIdx.x & 63) * WAVES + (int)(threadIdx.x >> 6);
+        RowPlan r{};
+        if (row < f.rows) r = plan(row);
+        do_row(row < f.rows ? row : -1, r);
     }
-    return needs;
 }
-// list: the free pages in order, as many as were asked for or as there are
-__device__ __forceinline__ void give_pages(const PageFork &f, const Counters &c, const int *list, int free_pages, int row, int lane, int rank)
+// The written entries behind the first of the wave's rows that have any, 64 lanes to a row: entry(lane of the row, whether there is one, its place, its page).
+// All lanes of a wave call it together
+template <class Entry> __device__ __forceinline__ void later_entries(const PageFork &f, int row, const RowPlan &r, Entry &&entry)
 {
-    const RowPlan r = row_plan(f, row);
-    int from = -1, to = -1;
-    for (int j0 = r.first; j0 < r.end; j0 += 8) {
-        const int j = j0 + lane, page = child_page(f, r, j);
-        const bool need = j < r.end && !stays(c, page, row * f.width + j);
-        const unsigned mask = of_eight(need);
-        const int at = rank + __popc(mask & ((1u << lane) - 1));
-        const int fresh = need && at < free_pages ? list[at] : -1;
-        if (j < r.end) f.table_out[(long)row * f.width + j] = need ? fresh : page;
-        if (j == r.first && fresh >= 0 && page >= 0 && (r.held & ((1 << f.page_shift) - 1))) {
-            from = page;
-            to = fresh;
+    const int lane = threadIdx.x & 63;
+    for (unsigned long long many = __ballot(row >= 0 && r.end - r.first > 1); many; many &= many - 1) {
+        const int owner = __builtin_ctzll(many), first = __builtin_amdgcn_readlane(r.first, owner), end = __builtin_amdgcn_readlane(r.end, owner);
+        const int at = __builtin_amdgcn_readlane(row, owner) * f.width;
+        const int *const from = f.table + (long)__builtin_amdgcn_readlane(r.parent, owner) * f.width;
+        for (int j0 = first + 1; j0 < end; j0 += 256) {
+            int page[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) page[u] = from[min(j0 + 64 * u + lane, end - 1)];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int j = j0 + 64 * u + lane;
+                if (j0 + 64 * u < end) entry(owner, j < end, at + j, in_cache(f, page[u]) ? page[u] : -1);
+            }
         }
-        rank += __popc(mask);
-    }
-    if (lane == 0) {
-        f.copies[row] = from;
-        f.copies[f.rows + row] = to;
-        f.copies[2 * f.rows + row] = from >= 0 ? r.held & ((1 << f.page_shift) - 1) : 0;
-        f.lens_out[row] = r.len > NONE ? NONE : (int)r.len;
     }
 }
 
-// One block: needs of the rows (in `needs`, which becomes their ranks), free pages in order, counts, entries
-__device__ __forceinline__ void assign(const PageFork &f, const Counters &c, int *needs, int *list, int *parts)
+__device__ __forceinline__ void count_writers(const PageFork &f, const Counters &c, int row, const RowPlan &r)
 {
-    const int tid = threadIdx.x, eighth = tid >> 3, lane = tid & 7;
+    if (row >= 0 && r.first < r.end && r.page >= 0) atomicMin(&c.first[r.page], row * f.width + r.first);
+    later_entries(f, row, r, [&](int, bool there, int place, int page) {
+        if (there && page >= 0) atomicMin(&c.first[page], place);
+    });
+}
+
+// Needs of the rows (in `needs`, which becomes their ranks), free pages in order, counts, entries.  plan(row): its RowPlan; list: the free pages, as many as were asked for or as
+// there are.  LDS: needs and list lie there.
+template <bool LDS, class List, class Plan>
+__device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Plan &&plan, int *needs, List *list, int (*parts)[BLOCK / 64])
+{
+    const int tid = threadIdx.x, lane = tid & 63;
     int wide = 0;
-    for (int row = eighth; row < f.rows; row += BLOCK / 8) {
-        const int n = count_needs(f, c, row, lane);
-        if (lane == 0) {
+    each_row(f, plan, [&](int row, const RowPlan &r) {
+        int n = row >= 0 && r.first < r.end && !stays(c, r.page, row * f.width + r.first);
+        later_entries(f, row, r, [&](int owner, bool there, int place, int page) {
+            const int more = __popcll(__ballot(there && !stays(c, page, place)));
+            n += lane == owner ? more : 0;
+        });
+        if (row >= 0) {
             needs[row] = n;
-            wide += row_plan(f, row).wide;
+            wide += r.wide;
         }
+    });
+    // (a thread has some neighbouring pages, and some neighbouring rows)
+    const int per = (f.pages + BLOCK - 1) / BLOCK;
+    const long at = (long)tid * per, end = min(at + per, (long)f.pages);
+    int mine = 0;
+#pragma unroll 4
+    for (long i = at; i < end; i++) mine += c.rest[i] == 0 && c.first[i] == NONE;
+    barrier<LDS>();
+    const int rows_per = (f.rows + BLOCK - 1) / BLOCK, row0 = tid * rows_per, row1 = min(row0 + rows_per, f.rows);
+    int sum = 0;
+    for (int i = row0; i < row1; i++) sum += needs[i];
+    const int v[3] = {sum, mine, wide};
+    int before[3], all[3];
+    block_scan<BLOCK / 64, 3>(v, parts, before, all);
+    const int wanted = all[0], free_pages = all[1];
+    int rank = before[0];
+    for (int i = row0; i < row1; i++) {
+        const int n = needs[i];
+        needs[i] = rank;
+        rank += n;
     }
-    __syncthreads();
-    int wanted, free_pages, all_wide;
-    {
-        const int per = (f.rows + BLOCK - 1) / BLOCK, at = tid * per;
-        int sum = 0;
-        for (int i = at; i < min(at + per, f.rows); i++) sum += needs[i];
-        int rank = block_scan(sum, parts, wanted);
-        for (int i = at; i < min(at + per, f.rows); i++) {
-            const int n = needs[i];
-            needs[i] = rank;
-            rank += n;
-        }
+    rank = before[1];
+#pragma unroll 4
+    for (long i = at; i < end; i++) {
+        int n = c.rest[i];
+        const bool unwritten = c.first[i] == NONE;
+        if (n == 0 && unwritten) {
+            if (rank < wanted) {
+                list[rank] = (List)i;
+                n = 1;
+            }
+            rank++;
+        } else if (n == 0) n = 1;                                     // the first of its writers
+        f.refs_out[i] = n;
     }
-    block_scan(wide, parts, all_wide);
-    {
-        const int per = (f.pages + BLOCK - 1) / BLOCK;
-        const long at = (long)tid * per, end = min(at + per, (long)f.pages);
-        int sum = 0;
-        for (long i = at; i < end; i++) sum += c.rest[i] == 0 && c.first[i] == NONE;
-        int rank = block_scan(sum, parts, free_pages);
-        for (long i = at; i < end; i++) {
-            int n = c.rest[i];
-            if (n == 0 && c.first[i] == NONE) {
-                if (rank < wanted) {
-                    list[rank] = (int)i;
-                    n = 1;
+    if (tid == 0) f.lacking[0] = max(wanted - free_pages, 0) + all[2];
+    barrier<LDS>();
+    each_row(f, plan, [&](int row, const RowPlan &r) {
+        int rank = row >= 0 ? needs[row] : 0;
+        if (row >= 0) {
+            int from = -1, to = -1;
+            const int part = r.held & ((1 << f.page_shift) - 1), place = row * f.width + r.first;
+            if (r.first < r.end) {
+                const bool need = !stays(c, r.page, place);
+                const int fresh = need && rank < free_pages ? (int)list[rank] : -1;
+                f.table_out[place] = need ? fresh : r.page;
+                rank += need;
+                if (fresh >= 0 && r.page >= 0 && part) {
+                    from = r.page;
+                    to = fresh;
                 }
-                rank++;
-            } else if (n == 0) n = 1;                                 // the first of its writers
-            f.refs_out[i] = n;
+            }
+            f.copies[row] = from;
+            f.copies[f.rows + row] = to;
+            f.copies[2 * f.rows + row] = from >= 0 ? part : 0;
+            f.lens_out[row] = r.len;
         }
-    }
-    if (tid == 0) f.lacking[0] = max(wanted - free_pages, 0) + all_wide;
-    __syncthreads();
-    for (int row = eighth; row < f.rows; row += BLOCK / 8) give_pages(f, c, list, free_pages, row, lane, needs[row]);
+        later_entries(f, row, r, [&](int owner, bool there, int place, int page) {
+            const bool need = there && !stays(c, page, place);
+            const unsigned long long mask = __ballot(need);
+            const int at = __builtin_amdgcn_readlane(rank, owner) + __popcll(mask & ((1ull << lane) - 1));
+            if (there) f.table_out[place] = !need ? page : at < free_pages ? (int)list[at] : -1;
+            rank += lane == owner ? __popcll(mask) : 0;
+        });
+    });
 }
 
-__global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f, int *__restrict__ list)
+// What a row of the old tables becomes: how many rows continue it, and how many of those have no next position; pages that it fills, and whether it has begun another
+struct __attribute__((aligned(16))) Children { int all, idle, whole, part; };
+
+// the entries of a new row that nothing is written to, by a wave
+__device__ __forceinline__ void copy_row(const PageFork &f, int row, int lane)
 {
-    extern __shared__ __attribute__((aligned(16))) int shared[];
-    __shared__ int parts[BLOCK / 64];
-    const Counters c{shared, shared + f.pages};
-    int *const needs = shared + 2 * f.pages;
-    for (int i = threadIdx.x; i < f.pages; i += BLOCK) {
-        c.rest[i] = f.refs[i];
-        c.first[i] = NONE;
+    const RowPlan r = row_plan(f, row);
+    const int *const from = f.table + (long)max(r.parent, 0) * f.width;
+    int *const to = f.table_out + (long)row * f.width;
+    for (int j0 = 0; j0 < f.width; j0 += 256) {
+        int page[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) page[u] = from[min(j0 + 64 * u + lane, f.width - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int j = j0 + 64 * u + lane;
+            if (j < f.width && (j < r.first || j >= r.end)) to[j] = j < r.end && in_cache(f, page[u]) ? page[u] : -1;
+        }
     }
-    __syncthreads();
-    count_names(f, c, threadIdx.x, BLOCK);
-    for (int row = threadIdx.x >> 3; row < f.rows; row += BLOCK / 8) count_writers(f, c, row, threadIdx.x & 7);
-    __syncthreads();
-    assign(f, c, needs, list, parts);
+}
+
+// The first block does the bookkeeping, the others copy what does not depend on it, sixteen rows each.
+__global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f)
+{
+    extern __shared__ __attribute__((aligned(16))) char shared[];
+    __shared__ int parts[3][BLOCK / 64];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int WAVES = BLOCK / 64;
+    if (blockIdx.x) {
+        const int row = ((int)blockIdx.x - 1) * WAVES + w;
+        if (row < f.rows) copy_row(f, row, lane);
+        return;
+    }
+    RowPlan *const plans = reinterpret_cast<RowPlan *>(shared);
+    Children *const children = reinterpret_cast<Children *>(plans + f.rows);
+    int *const counters = reinterpret_cast<int *>(children + f.rows_from), *const needs = counters + 2 * f.pages;
+    unsigned short *const list = reinterpret_cast<unsigned short *>(needs + f.rows);
+    const Counters c{counters, counters + f.pages};
+    for (int i = tid; i < f.rows_from; i += BLOCK) {
+        const int held = max(f.lens[i], 0);
+        children[i] = Children{0, 0, held >> f.page_shift, held & ((1 << f.page_shift) - 1)};
+    }
+    for (int i0 = 0; i0 < f.pages; i0 += 4 * BLOCK) {
+        int n[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) n[u] = f.refs[min(i0 + u * BLOCK + tid, f.pages - 1)];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int i = i0 + u * BLOCK + tid;
+            if (i < f.pages) {
+                c.rest[i] = n[u];
+                c.first[i] = NONE;
+            }
+        }
+    }
+    lds_barrier();
+    auto plan = [&](int row) {
+        RowPlan r = row_plan(f, row);
+        r.page = r.first < r.end ? child_page(f, r, r.first) : -1;
+        return r;
+    };
+    each_row(f, plan, [&](int row, const RowPlan &r) {
+        if (row >= 0) plans[row] = r;
+        if (row >= 0 && r.parent >= 0) {
+            atomicAdd(&children[r.parent].all, 1);
+            if (r.len == r.held) atomicAdd(&children[r.parent].idle, 1);
+        }
+        count_writers(f, c, row, r);
+    });
+    lds_barrier();
+    // A wave a row of the old tables: its names leave as often as no row takes them on (rows that go on write from the page that their next position lies in), several rows' entries requested at a time
+    constexpr int AT_ONCE = 8;
+    for (int row0 = w; row0 < f.rows_from; row0 += AT_ONCE * WAVES)
+        for (int j0 = 0; j0 < f.width; j0 += 64) {
+            const int j = j0 + lane, at = min(j, f.width - 1);
+            int old[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; u++) old[u] = f.table[(long)min(row0 + u * WAVES, f.rows_from - 1) * f.width + at];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; u++) {
+                const int row = row0 + u * WAVES;
+                if (row >= f.rows_from) break;
+                const Children n = children[row];
+                const int all = __builtin_amdgcn_readfirstlane(n.all) - 1, whole = __builtin_amdgcn_readfirstlane(n.whole);
+                const int then = __builtin_amdgcn_readfirstlane(n.part) ? __builtin_amdgcn_readfirstlane(n.idle) - 1 : -1;
+                const int more = j < whole ? all : j == whole ? then : -1;
+                if (more && j < f.width && in_cache(f, old[u])) atomicAdd(&c.rest[old[u]], more);
+            }
+        }
+    lds_barrier();
+    assign<true>(f, c, [&](int row) { return plans[row]; }, needs, list, parts);
 }
 
 __global__ __launch_bounds__(256) void fork_clear_kernel(PageFork f, Counters c)
@@ -210,16 +323,31 @@ __global__ __launch_bounds__(256) void fork_clear_kernel(PageFork f, Counters c)
         c.first[i] = NONE;
     }
 }
+// a wave a row
 __global__ __launch_bounds__(256) void fork_count_kernel(PageFork f, Counters c)
 {
-    const long at = (long)blockIdx.x * 256 + threadIdx.x, step = (long)gridDim.x * 256;
-    count_names(f, c, at, step);
-    for (long row = at >> 3; row < f.rows; row += step >> 3) count_writers(f, c, (int)row, threadIdx.x & 7);
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    RowPlan r{};
+    if (row < f.rows) r = row_plan(f, row);
+    for (int j = blockIdx.y * 64 + lane; j < f.width; j += 64 * gridDim.y) {
+        const int old = row < f.rows_from ? f.table[(long)row * f.width + j] : -1, child = row < f.rows ? child_page(f, r, j) : -1;
+        if (in_cache(f, old)) atomicAdd(&c.rest[old], -1);
+        if (row >= f.rows) continue;
+        if (j < r.first || j >= r.end) {
+            if (child >= 0) atomicAdd(&c.rest[child], 1);
+            f.table_out[(long)row * f.width + j] = child;
+        } else if (child >= 0) atomicMin(&c.first[child], row * f.width + j);
+    }
 }
 __global__ __launch_bounds__(BLOCK) void fork_assign_kernel(PageFork f, Counters c, int *needs, int *list)
 {
-    __shared__ int parts[BLOCK / 64];
-    assign(f, c, needs, list, parts);
+    __shared__ int parts[3][BLOCK / 64];
+    auto plan = [&](int row) {
+        RowPlan r = row_plan(f, row);
+        r.page = r.first < r.end ? child_page(f, r, r.first) : -1;
+        return r;
+    };
+    assign<false>(f, c, plan, needs, list, parts);
 }
 
 // ---- compact -----------------------------------------------------------------------------------------
@@ -262,30 +390,71 @@ __device__ __forceinline__ void finish_moves(const Compact &a, const UsedPages &
     if (at == 0) a.used[0] = used;
 }
 
+// One block: the new number of every page in LDS (`where`), and the free ones in front of `used`.  A thread has PER neighbouring pages.
+template <int PER>
 __global__ __launch_bounds__(BLOCK) void compact_block_kernel(Compact a)
 {
-    extern __shared__ __attribute__((aligned(16))) unsigned long long words[];
-    __shared__ int parts[BLOCK / 64];
-    const int tid = threadIdx.x, count = (a.pages + 63) >> 6;
-    int *const before = reinterpret_cast<int *>(words + count);
-    for (int i = tid; i < count << 6; i += BLOCK) {
-        const unsigned long long bits = __ballot(i < a.pages && a.refs[min(i, a.pages - 1)] > 0);
-        if ((i & 63) == 0) words[i >> 6] = bits;
+    extern __shared__ __attribute__((aligned(16))) int where[];       // [pages]
+    __shared__ int parts[BLOCK / 64], in_front;
+    unsigned short *const holes = reinterpret_cast<unsigned short *>(where + a.pages);         // [pages / 2]
+    const int tid = threadIdx.x, n = max(1, a.pages / 2), first = tid * PER;
+    constexpr int AT_ONCE = 4;
+    int entry[AT_ONCE], refs[PER];
+#pragma unroll
+    for (int i = 0; i < PER; i++) refs[i] = first + i < a.pages ? a.refs[first + i] : 0;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; u++) entry[u] = tid + u * BLOCK < a.entries ? a.table[tid + u * BLOCK] : -1;
+    int count = 0, used;
+#pragma unroll
+    for (int i = 0; i < PER; i++) count += refs[i] > 0;
+    const int before = block_scan(count, parts, used);
+    int rank = before;
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+        const int page = first + i;
+        if (page == used) in_front = rank;                            // pages in use that stay
+        if (page < used && refs[i] <= 0) holes[page - rank] = (unsigned short)page;
+        rank += refs[i] > 0;
     }
+    if (used >= a.pages && tid == 0) in_front = used;
     __syncthreads();
-    int used, base = 0;
-    for (int i0 = 0; i0 < count; i0 += BLOCK) {
-        const int i = i0 + tid;
-        const int in_front = block_scan(i < count ? __popcll(words[i]) : 0, parts, used);
-        if (i < count) before[i] = base + in_front;
-        base += used;
+    const int stay = in_front, moved = used - stay;
+    rank = before;
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+        const int page = first + i;
+        if (page >= a.pages) continue;
+        int to = -1;
+        if (refs[i] > 0) {
+            to = page < used ? page : holes[rank - stay];
+            a.refs_out[to] = refs[i];
+            if (page >= used) {
+                a.copies[rank - stay] = page;
+                a.copies[n + rank - stay] = to;
+            }
+        }
+        if (page >= used) a.refs_out[page] = 0;
+        where[page] = to;
+        rank += refs[i] > 0;
     }
-    used = base;
+    for (int i = tid; i < n; i += BLOCK) {
+        if (i >= moved) a.copies[i] = a.copies[n + i] = -1;
+        a.copies[2 * n + i] = i < moved ? a.page_len : 0;
+    }
+    if (tid == 0) a.used[0] = used;
     __syncthreads();
-    const UsedPages u{words, before};
-    for (int i = tid; i < a.pages; i += BLOCK) list_moves(a, u, used, i);
-    __syncthreads();
-    finish_moves(a, u, used, tid, BLOCK);
+    for (int i0 = 0; i0 < a.entries; i0 += AT_ONCE * BLOCK) {
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) {
+            const int i = i0 + u * BLOCK + tid;
+            if (i0) entry[u] = i < a.entries ? a.table[i] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) {
+            const int i = i0 + u * BLOCK + tid;
+            if (i < a.entries) a.table_out[i] = (unsigned)entry[u] < (unsigned)a.pages ? where[entry[u]] : -1;
+        }
+    }
 }
 
 constexpr int CHUNK = 64 * 256;                                       // pages of a block
@@ -379,30 +548,29 @@ size_t room(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t pages_fork_workspace(int pages, int rows)
+size_t pages_fork_workspace(int pages, int rows_from, int rows)
 {
-    const size_t list = room(4 * (size_t)pages);
-    return fork_in_block(pages, rows) ? list : 3 * list + room(4 * (size_t)rows);
+    return fork_in_block(pages, rows_from, rows) ? 0 : 3 * room(4 * (size_t)pages) + room(4 * (size_t)rows);
 }
 
 hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st)
 {
-    char *at = static_cast<char *>(ws);
-    int *const list = take<int>(at, f.pages);
-    if (fork_in_block(f.pages, f.rows)) {
-        const size_t lds = fork_block_lds(f.pages, f.rows);
-        if (lds > 64 << 10)
+    if (fork_in_block(f.pages, f.rows_from, f.rows)) {
+        const size_t lds = fork_block_lds(f.pages, f.rows_from, f.rows);
+        if (lds > 60 << 10)
             if (hipError_t e = hipFuncSetAttribute((const void *)fork_block_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-        hipLaunchKernelGGL(fork_block_kernel, dim3(1), dim3(BLOCK), lds, st, f, list);
+        hipLaunchKernelGGL(fork_block_kernel, dim3((unsigned)(1 + (f.rows + BLOCK / 64 - 1) / (BLOCK / 64))), dim3(BLOCK), lds, st, f);
         return hipGetLastError();
     }
+    char *at = static_cast<char *>(ws);
+    int *const list = take<int>(at, f.pages);
     Counters c;
     c.rest = take<int>(at, f.pages);
     c.first = take<int>(at, f.pages);
     int *const needs = take<int>(at, f.rows);
-    const long entries = (long)f.width * (f.rows > f.rows_from ? f.rows : f.rows_from);
+    const int most = f.rows > f.rows_from ? f.rows : f.rows_from;
     hipLaunchKernelGGL(fork_clear_kernel, dim3((unsigned)((f.pages + 255) / 256)), dim3(256), 0, st, f, c);
-    hipLaunchKernelGGL(fork_count_kernel, dim3(blocks_for((entries + 255) / 256, 4096)), dim3(256), 0, st, f, c);
+    hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)((most + 3) / 4), blocks_for((f.width + 63) / 64, 64)), dim3(256), 0, st, f, c);
     hipLaunchKernelGGL(fork_assign_kernel, dim3(1), dim3(BLOCK), 0, st, f, c, needs, list);
     return hipGetLastError();
 }
@@ -420,7 +588,11 @@ hipError_t launch_pages_compact(const int *refs, int pages, const int *table, in
     const Compact a{refs, table, pages, entries, page_len, refs_out, table_out, copies, used};
     const size_t count = ((size_t)pages + 63) / 64;
     if (compact_in_block(pages, entries)) {
-        hipLaunchKernelGGL(compact_block_kernel, dim3(1), dim3(BLOCK), 12 * count, st, a);
+        const size_t lds = compact_block_lds(pages);
+        auto kern = pages <= 4 * BLOCK ? compact_block_kernel<4> : pages <= 8 * BLOCK ? compact_block_kernel<8> : compact_block_kernel<24>;
+        if (lds > 60 << 10)
+            if (hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
+        hipLaunchKernelGGL(kern, dim3(1), dim3(BLOCK), lds, st, a);
         return hipGetLastError();
     }
     const int chunks = (int)(((size_t)pages + CHUNK - 1) / CHUNK);

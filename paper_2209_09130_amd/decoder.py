@@ -27,7 +27,7 @@ _SIGNATURES = {
     "samp_attention_causal": (_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _P, _I, _I, _I, _F, _P, _P),
     "samp_beam_select_workspace_bytes": (_I,) * 5,
     "samp_beam_select": (_P, _L, _I, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _Z, _P),
-    "samp_pages_fork_workspace_bytes": (_I, _I),
+    "samp_pages_fork_workspace_bytes": (_I, _I, _I),
     "samp_pages_fork": (_P, _I, _P, _P, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _Z, _P),
     "samp_pages_compact_workspace_bytes": (_I, _I),
     "samp_pages_compact": (_P, _I, _P, _I, _I, _P, _P, _P, _P, _P, _Z, _P),
@@ -386,7 +386,7 @@ def pages_fork(refs: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page
         _refuse("a page table has less than 2^31 entries")
     refs_out, table_out, out = torch.empty_like(refs), table.new_empty((rows, width)), table.new_empty((4 * rows + 1,))
     lens_out, copies, lacking = out[:rows], out[rows:4 * rows].view(3, rows), out[4 * rows:]
-    need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows)
+    need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows_from, rows)
     ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
     rc = _fn("samp_pages_fork")(pr, pages, pt, pl, rows_from, width, page_len, pp, pc, _most(max_new), rows, refs_out.data_ptr(), table_out.data_ptr(),
                                 lens_out.data_ptr(), copies.data_ptr(), lacking.data_ptr(), ws.data_ptr() if need else 0, need, _raw_stream(device))
