@@ -567,14 +567,16 @@ SAMP_API int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_boun
  *   score(page) = max over new tokens and query heads of the key head of  (float) sum_d max(c_d high_d, c_d low_d) * (step_q * step_page)
  * with the codes c of the query's row (the quantiser of a row above), step_q = absmax * (1 / 127) of it (1 and NaN as there) and the page's bounds, the sum a whole number, the products in
  * binary32; NaN counts as plus infinity, a page number that is none of the cache's as minus infinity.
- * sinks >= 0, recent at least the pages that max_new positions can lie in ((max_new + page_len - 2) / page_len + 1), sinks + recent <= keep, width <= SAMP_MAX_TABLE.                 */
+ * sinks >= 0, recent at least the pages that max_new positions can lie in ((max_new + page_len - 2) / page_len + 1), sinks + recent <= keep, width <= SAMP_MAX_TABLE.
+ * workspace as in samp_linear_i8_tokens.                                                                     */
+SAMP_API size_t samp_cache_select_workspace_bytes(int32_t batch, int32_t kv_heads, int32_t width);
 SAMP_API int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,
                                const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows, int32_t keep,
-                               int32_t sinks, int32_t recent, int32_t *tables, int32_t *lens_out, void *stream);
+                               int32_t sinks, int32_t recent, int32_t *tables, int32_t *lens_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* samp_attention_cache over the pages that samp_cache_select chooses; where every sequence has up to `keep` pages, what samp_attention_cache computes.  workspace as there. */
-SAMP_API size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t page_len, int32_t max_new,
-                                                      int32_t max_len, int32_t keep);
+SAMP_API size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t page_len, int32_t width,
+                                                      int32_t max_new, int32_t max_len, int32_t keep);
 SAMP_API int samp_attention_sparse(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,
                                    const int32_t *table, int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t max_len,
                                    int32_t rows, int32_t keep, int32_t sinks, int32_t recent, float scale, const uint64_t *tree, uint16_t *out, void *workspace,

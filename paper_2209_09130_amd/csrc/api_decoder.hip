@@ -358,9 +358,15 @@ int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_bounds_t *bou
     return SAMP_OK;
 }
 
+size_t samp_cache_select_workspace_bytes(int32_t batch, int32_t kv_heads, int32_t width)
+{
+    if (batch < 1 || batch > SAMP_MAX_BATCH || kv_heads < 1 || kv_heads > SAMP_MAX_HEADS || width < 1 || width > SAMP_MAX_TABLE) return 0;
+    return up(cache_select_workspace(batch, kv_heads, width));
+}
+
 int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds, const int32_t *table,
                       int32_t width, const int32_t *cu, const int32_t *lens, int32_t batch, int32_t max_new, int32_t rows, int32_t keep, int32_t sinks, int32_t recent,
-                      int32_t *tables, int32_t *lens_out, void *stream)
+                      int32_t *tables, int32_t *lens_out, void *workspace, size_t workspace_bytes, void *stream)
 {
     KvCache c;
     KeyBounds kb;
@@ -374,11 +380,12 @@ int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t head
     if (int rc = check_choice(width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
     if (!tables || !lens_out) return fail(SAMP_ERR_ARG, "NULL pointer");
     if (lens == lens_out) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
-    HIP_TRY(launch_cache_select(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, kb, r, keep, sinks, recent, tables, lens_out, (hipStream_t)stream));
+    if (int rc = check_workspace(workspace, workspace_bytes, samp_cache_select_workspace_bytes(batch, c.kv_heads, width))) return rc;
+    HIP_TRY(launch_cache_select(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, kb, r, keep, sinks, recent, tables, lens_out, workspace, (hipStream_t)stream));
     return SAMP_OK;
 }
 
-// the tables of the key heads, the lengths, then what the attention over them needs
+// The tables of the key heads and the lengths; then what the choice needs, and after it, in the same place, the attention
 static size_t chosen_bytes(int32_t batch, int32_t kv_heads, int32_t keep) { return up(4 * (size_t)batch * kv_heads * keep) + up(4 * (size_t)batch); }
 static int32_t chosen_len(int32_t max_len, int32_t keep, int32_t page_len)
 {
@@ -386,14 +393,15 @@ static int32_t chosen_len(int32_t max_len, int32_t keep, int32_t page_len)
     return max_len < most ? max_len : (int32_t)most;
 }
 
-size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t page_len, int32_t max_new,
-                                             int32_t max_len, int32_t keep)
+size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t page_len, int32_t width,
+                                             int32_t max_new, int32_t max_len, int32_t keep)
 {
     Cut cut;
-    if (check_page_len(page_len) || keep < 1 || keep > SAMP_MAX_TABLE) return 0;
+    if (check_page_len(page_len) || keep < 1 || keep > SAMP_MAX_TABLE || width < 1 || width > SAMP_MAX_TABLE) return 0;
     max_len = chosen_len(max_len, keep, page_len);
     if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len, &cut)) return 0;
-    return chosen_bytes(batch, kv_heads, keep) + samp_attention_cache_workspace_bytes(rows, batch, heads, kv_heads, head_dim, max_new, max_len);
+    const size_t choice = samp_cache_select_workspace_bytes(batch, kv_heads, width), attention = samp_attention_cache_workspace_bytes(rows, batch, heads, kv_heads, head_dim, max_new, max_len);
+    return chosen_bytes(batch, kv_heads, keep) + (choice > attention ? choice : attention);
 }
 
 int samp_attention_sparse(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,
@@ -418,11 +426,11 @@ int samp_attention_sparse(const uint16_t *q, int64_t ldq, int32_t type, int32_t 
     if (tree && r.max_rows > 64) return fail(SAMP_ERR_SHAPE, "a tree has at most 64 drafted tokens (max_new %d)", max_new);
     if (tree && !aligned(tree, 8)) return fail(SAMP_ERR_ARG, "tree must be 8-byte aligned");
     if (int rc = check_workspace(workspace, workspace_bytes,
-                                 samp_attention_sparse_workspace_bytes(rows, batch, heads, c.kv_heads, cache->head_dim, cache->page_len, max_new, max_len, keep)))
+                                 samp_attention_sparse_workspace_bytes(rows, batch, heads, c.kv_heads, cache->head_dim, cache->page_len, width, max_new, max_len, keep)))
         return rc;
     int *const tables = static_cast<int *>(workspace), *const chosen_lens = tables + up(4 * (size_t)batch * c.kv_heads * keep) / 4;
     float *const partials = reinterpret_cast<float *>(static_cast<char *>(workspace) + chosen_bytes(batch, c.kv_heads, keep));
-    HIP_TRY(launch_cache_select(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, kb, r, keep, sinks, recent, tables, chosen_lens, (hipStream_t)stream));
+    HIP_TRY(launch_cache_select(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, kb, r, keep, sinks, recent, tables, chosen_lens, partials, (hipStream_t)stream));
     const KvRows chosen{tables, keep, cu, chosen_lens, batch, r.max_rows, rows, c.kv_heads};
     HIP_TRY(launch_cached_attention(q, ldq, type == SAMP_TYPE_BF16, heads, cache->head_dim, c, chosen, scale, tree, cut, partials, out, (hipStream_t)stream));
     return SAMP_OK;

@@ -32,6 +32,20 @@ template <bool BF> __device__ __forceinline__ int narrow2(float lo, float hi)
     return __builtin_bit_cast(int, __builtin_convertvector((v2f{lo, hi}), half2));          // one instruction
 }
 
+// A barrier for what the threads of a block hand each other in LDS: loads from memory and stores to it stay on their way
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// the sum of the lanes up to this one (row shifts, then the last lanes of rows 0 and 2, then of row 1)
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
 // The largest magnitude of 16-bit values, by their bits (two running maxima, in the halves of a dword): infinities come above every number and NaN above them
 typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned max_halves(unsigned a, unsigned b)
@@ -153,7 +167,8 @@ hipError_t launch_pages_compact(const int *refs, int pages, const int *table, in
 hipError_t launch_cache_copy(const KvCache &cache, int head_dim, const KeyBounds &bounds, const int *copies, int n, hipStream_t st);
 
 hipError_t launch_cache_bounds(const KvCache &cache, int head_dim, const KeyBounds &bounds, const KvRows &rows, hipStream_t st);
+size_t cache_select_workspace(int batch, int kv_heads, int width);
 hipError_t launch_cache_select(const void *q, long ldq, bool bf16, int heads, int head_dim, const KvCache &cache, const KeyBounds &bounds, const KvRows &rows, int keep,
-                               int sinks, int recent, int *tables, int *lens_out, hipStream_t st);
+                               int sinks, int recent, int *tables, int *lens_out, void *ws, hipStream_t st);
 
 }  // namespace samp

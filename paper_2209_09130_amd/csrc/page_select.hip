@@ -99,166 +99,331 @@ template <bool BF> __device__ __forceinline__ float largest(unsigned bits)
 }
 constexpr unsigned ALWAYS = 0xffffffffu;                              // above the order of every number
 
-// One block: a sequence and a key head.  The pages' scores go to LDS as whole numbers, then the `keep`-th largest of them is found eight bits at a time, and the pages that
-// are chosen are written in order.
-template <bool BF, int D>
-__global__ __launch_bounds__(1024) void select_pages_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks, int recent,
-                                    int *__restrict__ tables, int *__restrict__ lens_out)
+__device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t & 0x80000000u ? t & 0x7fffffffu : ~t); }
+constexpr int BINS = 1024, LIST = 512, WORDS = SAMP_MAX_TABLE / 64;
+struct Scored { unsigned score; int page; };
+
+// What scores are made with: a sequence, a key head, its table and the queries that see it
+struct Seen { SeqRows s; int b, head, group, pages, sinks, recent; const int *table; };
+
+// The scores of the pages first .. first + 63 of a sequence, a page a lane of the wave: f(page of the lane, whether it is the first time, score), again for every sixteen rows of queries.  All waves
+// of the block, four, call it together.  entry: the table's of the lane's page.  A wave requests the bounds of its pages together: 16 of them are the columns of a product, 16 rows of queries its rows.
+template <bool BF, int D, class F>
+__device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq, const KvCache &c, const KeyBounds &bounds, const Seen &seen, int first, int entry, F &&f)
 {
-    extern __shared__ __attribute__((aligned(16))) unsigned score[];  // [width]
+    constexpr int STEPS = 2 * D / 64;                                 // products of 64 codes
     __shared__ __attribute__((aligned(16))) int8_t codes[16][2 * D];  // positive parts, negative parts of sixteen rows of queries
     __shared__ float steps[16];
-    __shared__ int count[256], parts[16];
-    __shared__ int found[2];                                          // a digit, and how many are above it
-    const int b = blockIdx.x / c.kv_heads, head = blockIdx.x - b * c.kv_heads, tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
-    const SeqRows s = seq_rows(rows, b, c.page_shift);
-    const int pages = (max(s.len, 0) + (1 << c.page_shift) - 1) >> c.page_shift, chosen = min(pages, keep);
-    const int *const table = rows.table + (size_t)b * rows.width;
-    int *const to = tables + (size_t)blockIdx.x * keep;
-    if (head == 0 && tid == 0) lens_out[b] = rows.lens[b] - ((pages - chosen) << c.page_shift);
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4, all = seen.s.todo * seen.group, pages = seen.pages;
+    for (int r0 = 0; r0 < all || r0 == 0; r0 += 16) {
+        if (r0) lds_barrier();
+        // sixteen lanes a row of queries, requested in front of the bounds: loads arrive in their order
+        constexpr int PER = D / 16;
+        const int row = tid >> 4, token = (r0 + row) / seen.group, h = seen.head * seen.group + (r0 + row) - token * seen.group;
+        v4i raw = {0, 0, 0, 0};
+        if (r0 + row < all) {
+            const char *from = Q + 2 * ((size_t)(seen.s.first_row + token) * ldq + h * D + r * PER);
+            if constexpr (PER == 8) raw = *reinterpret_cast<const v4i *>(from);
+            else {
+                const v2i half = *reinterpret_cast<const v2i *>(from);
+                raw[0] = half[0];
+                raw[1] = half[1];
+            }
+        }
+        const bool ok = (unsigned)entry < (unsigned)c.pages;
+        const float page_step = bounds.steps[(size_t)(ok ? entry : 0) * c.kv_heads + seen.head];
+        v4i bf[4][STEPS];
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            const int e = __shfl(ok ? entry : 0, 16 * t + r, 64);
+            const int8_t *from = bounds.codes + ((size_t)e * c.kv_heads + seen.head) * (2 * D) + 16 * g;
+#pragma unroll
+            for (int i = 0; i < STEPS; i++) bf[t][i] = *reinterpret_cast<const v4i *>(from + 64 * i);
+        }
+        const unsigned top = max_of_16_lanes(bits_max16(raw));
+        const RowQuant q = row_quant<BF>(top);
+        float x[8];
+        widen8<BF>(raw, x);
+        const v2i code = quant8(x, q);
+#pragma unroll
+        for (int i = 0; i < PER / 4; i++) {
+            int pos = 0, neg = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int v = (int8_t)(code[i] >> 8 * e);
+                pos |= (max(v, 0) & 0xff) << 8 * e;
+                neg |= (min(v, 0) & 0xff) << 8 * e;
+            }
+            *reinterpret_cast<int *>(&codes[row][r * PER + 4 * i]) = pos;
+            *reinterpret_cast<int *>(&codes[row][D + r * PER + 4 * i]) = neg;
+        }
+        // (the product is the definition's step; the quantiser's own is the quotient)
+        if (r == 0) steps[row] = !q.finite || q.hi == 0.0f ? q.step : largest<BF>(top) * INV_127;
+        lds_barrier();
+        v4i qf[STEPS];
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) qf[i] = *reinterpret_cast<const v4i *>(&codes[r][64 * i + 16 * g]);
+        const v4f qs = *reinterpret_cast<const v4f *>(&steps[4 * g]);
+        unsigned mine = 0;
+#pragma unroll
+        for (int t = 0; t < 4; t++) {
+            v4i sum = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < STEPS; i++) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[i], bf[t][i], sum, 0, 0, 0);
+            const float s = __shfl(page_step, 16 * t + r, 64);
+            unsigned best = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (r0 + 4 * g + e < all) best = max(best, order_of((float)sum[e] * (qs[e] * s)));
+            best = max(best, (unsigned)__shfl_xor((int)best, 16, 64));
+            best = max(best, (unsigned)__shfl_xor((int)best, 32, 64));
+            if (g == t) mine = best;
+        }
+        const int p = first + lane;
+        if (!ok) mine = order_of(-INFINITY);
+        if (p < seen.sinks || p >= pages - seen.recent) mine = ALWAYS;
+        if (p < pages) f(p, r0 == 0, mine);
+    }
+}
+
+__device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &rows, int b, int head, int group, int sinks, int recent)
+{
+    Seen seen{seq_rows(rows, b, c.page_shift), b, head, group, 0, sinks, recent, rows.table + (size_t)b * rows.width};
+    seen.pages = (max(seen.s.len, 0) + (1 << c.page_shift) - 1) >> c.page_shift;
+    return seen;
+}
+
+// scores [batch, kv_heads, width]; a block has 256 pages of a sequence and a key head.  Blocks go to the eight XCDs in turn: the key heads of the same pages have blocks of the same XCD, so
+// that a page's steps, which lie next to each other, come to one L2.
+template <bool BF, int D>
+__global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
+                                                          int recent, unsigned *__restrict__ scores)
+{
+    const int of_xcd = blockIdx.x >> 3, head = of_xcd % c.kv_heads, item = of_xcd / c.kv_heads * 8 + (blockIdx.x & 7), chunks = (rows.width + 255) >> 8;
+    const int chunk = item / rows.batch, b = item - chunk * rows.batch;
+    if (chunk >= chunks) return;
+    const int page = chunk * 256 + threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];          // (on its way with the lengths)
+    const Seen seen = what_is_seen(c, rows, b, head, group, sinks, recent);
+    if (seen.pages <= keep || chunk * 256 >= seen.pages) return;
+    unsigned *const to = scores + ((size_t)b * c.kv_heads + head) * rows.width;
+    score_pages<BF, D>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
+                       [&](int p, bool new_page, unsigned x) { to[p] = new_page ? x : max(to[p], x); });
+}
+
+// One block: a sequence and a key head.  The scores are counted in BINS steps between the smallest and the largest; the pages of the step in which the `keep`-th largest lies are
+// ranked by counting, and where they are too many (equal scores), that score is found eight bits at a time.  prepare(score): leaves the scores of the thread's pages in LDS.
+template <class F>
+__device__ __forceinline__ void choose_pages(const KvCache &c, const KvRows &rows, const Seen &seen, int keep, int *__restrict__ to, int *__restrict__ lens_out, F &&prepare)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned score[];  // [width]
+    __shared__ __attribute__((aligned(16))) int count[BINS];
+    __shared__ Scored list[LIST];
+    __shared__ unsigned long long bits[WORDS];
+    __shared__ float lows[16], highs[16];
+    __shared__ int found[2], listed;                                  // a digit, and how many are above it
+    const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int pages = seen.pages, chosen = min(pages, keep), groups = (pages + 63) >> 6, sinks = seen.sinks, recent = seen.recent;
+    const int *const table = seen.table;
+    if (seen.head == 0 && tid == 0) lens_out[seen.b] = rows.lens[seen.b] - ((pages - chosen) << c.page_shift);
     if (pages <= keep) {
         for (int i = tid; i < keep; i += blockDim.x) to[i] = i < pages ? table[i] : -1;
         return;
     }
+    for (int i = tid; i < BINS; i += blockDim.x) count[i] = 0;
+    for (int i = tid; i < groups; i += blockDim.x) bits[i] = 0;
+    if (tid == 0) listed = 0;
+    prepare(score);
 
-    const int all = s.todo * group;
-    for (int r0 = 0; r0 < all || r0 == 0; r0 += 16) {
-        // sixteen lanes a row of queries
-        for (int row = tid >> 4; row < 16; row += blockDim.x >> 4) {
-            constexpr int PER = D / 16;
-            const int token = (r0 + row) / group, h = head * group + (r0 + row) - token * group;
-            v4i raw = {0, 0, 0, 0};
-            if (r0 + row < all) {
-                const char *from = Q + 2 * ((size_t)(s.first_row + token) * ldq + h * D + r * PER);
-                if constexpr (PER == 8) raw = *reinterpret_cast<const v4i *>(from);
-                else {
-                    const v2i half = *reinterpret_cast<const v2i *>(from);
-                    raw[0] = half[0];
-                    raw[1] = half[1];
-                }
-            }
-            const unsigned top = max_of_16_lanes(bits_max16(raw));
-            const RowQuant q = row_quant<BF>(top);
-            float x[8];
-            widen8<BF>(raw, x);
-            const v2i code = quant8(x, q);
-#pragma unroll
-            for (int i = 0; i < PER / 4; i++) {
-                int pos = 0, neg = 0;
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const int v = (int8_t)(code[i] >> 8 * e);
-                    pos |= (max(v, 0) & 0xff) << 8 * e;
-                    neg |= (min(v, 0) & 0xff) << 8 * e;
-                }
-                *reinterpret_cast<int *>(&codes[row][r * PER + 4 * i]) = pos;
-                *reinterpret_cast<int *>(&codes[row][D + r * PER + 4 * i]) = neg;
-            }
-            // (the product is the definition's step; the quantiser's own is the quotient)
-            if (r == 0) steps[row] = !q.finite || q.hi == 0.0f ? q.step : largest<BF>(top) * INV_127;
+    // steps of the scores that are finite (a thread has the pages whose scores it wrote)
+    float low = INFINITY, high = -INFINITY;
+    for (int p = 64 * w + lane; p < pages; p += 64 * waves) {
+        const float x = value_of_order(score[p]);
+        if (score[p] != ALWAYS && __builtin_isfinite(x)) {
+            low = __builtin_fminf(low, x);
+            high = __builtin_fmaxf(high, x);
         }
-        __syncthreads();
-        v4i qf[2 * D / 64];
-#pragma unroll
-        for (int i = 0; i < 2 * D / 64; i++) qf[i] = *reinterpret_cast<const v4i *>(&codes[r][64 * i + 16 * g]);
-        const v4f qs = *reinterpret_cast<const v4f *>(&steps[4 * g]);
-        for (int p0 = 16 * w; p0 < pages; p0 += 16 * waves) {
-            const int p = p0 + r, entry = p < pages ? table[p] : -1;
-            const bool ok = (unsigned)entry < (unsigned)c.pages;
-            const size_t at = (size_t)(ok ? entry : 0) * c.kv_heads + head;
-            const int8_t *from = bounds.codes + at * 2 * D + 16 * g;
-            v4i sum = {0, 0, 0, 0}, bf[2 * D / 64];
-#pragma unroll
-            for (int i = 0; i < 2 * D / 64; i++) bf[i] = *reinterpret_cast<const v4i *>(from + 64 * i);
-            const float step = bounds.steps[at];
-#pragma unroll
-            for (int i = 0; i < 2 * D / 64; i++) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[i], bf[i], sum, 0, 0, 0);
-            unsigned best = 0;
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (r0 + 4 * g + e < all) best = max(best, order_of((float)sum[e] * (qs[e] * step)));
-            best = max(best, (unsigned)__shfl_xor((int)best, 16, 64));
-            best = max(best, (unsigned)__shfl_xor((int)best, 32, 64));
-            if (!ok) best = order_of(-INFINITY);
-            if (p < sinks || p >= pages - recent) best = ALWAYS;
-            if (g == 0 && p < pages) score[p] = r0 ? max(score[p], best) : best;
-        }
-        __syncthreads();
     }
-
-    // the `keep`-th largest, and how many pages of just that score are kept
-    unsigned known = 0;
-    int left = keep;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < 256; i += blockDim.x) count[i] = 0;
-        __syncthreads();
-        for (int p = tid; p < pages; p += blockDim.x) {
-            const unsigned x = score[p];
-            if (shift == 24 || (x ^ known) >> (shift + 8) == 0) atomicAdd(&count[x >> shift & 255], 1);
-        }
-        __syncthreads();
-        if (tid < 64) {                                               // digits 4 lane .. 4 lane + 3, from above
-            int n[4], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 4; i++) sum += n[i] = count[255 - 4 * tid - i];
-            int before = sum;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int other = __shfl_up(before, o, 64);
-                if (tid >= o) before += other;
-            }
-            before -= sum;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                if (before < left && before + n[i] >= left) {
-                    found[0] = 255 - 4 * tid - i;
-                    found[1] = before;
-                }
-                before += n[i];
-            }
-        }
-        __syncthreads();
-        known |= (unsigned)found[0] << shift;
-        left -= found[1];
+    low = -wave_max(-low);
+    high = wave_max(high);
+    if (lane == 0) {
+        lows[w] = low;
+        highs[w] = high;
     }
-
-    int written = 0, equal = 0;
-    for (int p0 = 0; p0 < pages; p0 += blockDim.x) {
-        const int p = p0 + tid;
-        const unsigned x = p < pages ? score[p] : 0;
-        const bool above = p < pages && x > known, same = p < pages && x == known;
-        const unsigned long long below = (1ull << lane) - 1, m_above = __ballot(above), m_same = __ballot(same);
-        __syncthreads();
-        if (lane == 0) parts[w] = __popcll(m_above) | __popcll(m_same) << 16;
-        __syncthreads();
-        int n_above = 0, n_same = 0, all_above = 0, all_same = 0;
-        for (int i = 0; i < waves; i++) {
-            const int v = parts[i];
-            n_above += i < w ? v & 0xffff : 0;
-            n_same += i < w ? v >> 16 : 0;
-            all_above += v & 0xffff;
-            all_same += v >> 16;
+    lds_barrier();
+    for (int i = 0; i < waves; i++) {
+        low = __builtin_fminf(low, lows[i]);
+        high = __builtin_fmaxf(high, highs[i]);
+    }
+    const float rate = high > low ? (float)(BINS - 1) / (high - low) : 0.0f;
+    // (rising with the score whatever the roundings: differences, products and whole parts do)
+    auto bin_of = [&](unsigned x) {
+        const float v = value_of_order(x), f = (v - low) * rate;
+        return v <= low ? 0 : v >= high ? BINS - 1 : f < (float)(BINS - 1) ? (int)f : BINS - 1;
+    };
+    for (int p = 64 * w + lane; p < pages; p += 64 * waves)
+        if (score[p] != ALWAYS) atomicAdd(&count[bin_of(score[p])], 1);
+    lds_barrier();
+    const int want = keep - min(sinks, pages) - min(recent, pages);   // of the pages that are not kept anyway
+    if (w == 0) {
+        // lane l has the steps 16 l .. 16 l + 15 from above; then sixteen lanes have one each of those of the lane in which the `want`-th lies
+        int sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const v4i four = *reinterpret_cast<const v4i *>(&count[BINS - 16 * lane - 4 * i - 4]);
+            sum += (four[0] + four[1]) + (four[2] + four[3]);
         }
-        n_above += __popcll(m_above & below);
-        n_same += equal + __popcll(m_same & below);
-        if (above || (same && n_same < left)) to[written + n_above + min(n_same, left) - min(equal, left)] = table[p];
-        written += all_above + min(equal + all_same, left) - min(equal, left);
-        equal += all_same;
+        const int upto = wave_scan(sum), owner = min((int)__popcll(__ballot(upto < want)), 63);
+        const int in_front = owner ? __builtin_amdgcn_readlane(upto, owner - 1) : 0;
+        const int one = lane < 16 ? count[BINS - 1 - 16 * owner - lane] : 0, then = in_front + wave_scan(one);
+        if (lane < 16 && then >= want && then - one < want) {
+            found[0] = BINS - 1 - 16 * owner - lane;
+            found[1] = then - one;
+        }
+        if (want <= 0 && lane == 0) {
+            found[0] = BINS;
+            found[1] = 0;
+        }
+    }
+    lds_barrier();
+    const int step_of_last = found[0], left = want - found[1];
+    for (int p = 64 * w + lane; p < pages; p += 64 * waves) {
+        if (score[p] == ALWAYS || bin_of(score[p]) != step_of_last) continue;
+        const int at = atomicAdd(&listed, 1);                         // (in any order: they are ranked)
+        if (at < LIST) list[at] = Scored{score[p], p};
+    }
+    lds_barrier();
+    const int n = listed;
+    unsigned least = 0;                                               // scores above it are kept too, of pages of that step
+    if (n <= LIST) {
+        for (int i = tid; i < n; i += blockDim.x) {
+            const Scored mine = list[i];
+            int better = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; j++) better += list[j].score > mine.score || (list[j].score == mine.score && list[j].page < mine.page);
+            if (better < left) atomicOr(&bits[mine.page >> 6], 1ull << (mine.page & 63));
+        }
+        least = ALWAYS;
+    } else {
+        int rest = left;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            lds_barrier();
+            for (int i = tid; i < 256; i += blockDim.x) count[i] = 0;
+            lds_barrier();
+            for (int p = 64 * w + lane; p < pages; p += 64 * waves) {
+                const unsigned x = score[p];
+                if (x != ALWAYS && bin_of(x) == step_of_last && (shift == 24 || (x ^ least) >> (shift + 8) == 0)) atomicAdd(&count[x >> shift & 255], 1);
+            }
+            lds_barrier();
+            if (w == 0) {
+                int m[4], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 4; i++) sum += m[i] = count[255 - 4 * lane - i];
+                int before = wave_scan(sum) - sum;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    if (before < rest && before + m[i] >= rest) {
+                        found[0] = 255 - 4 * lane - i;
+                        found[1] = before;
+                    }
+                    before += m[i];
+                }
+            }
+            lds_barrier();
+            least |= (unsigned)found[0] << shift;
+            rest -= found[1];
+        }
+        // of the pages of just that score the first `rest`
+        for (int p0 = 64 * w; p0 < pages; p0 += 64 * waves) {
+            const unsigned long long word = __ballot(p0 + lane < pages && score[p0 + lane] == least);
+            if (lane == 0) bits[p0 >> 6] = word;
+        }
+        lds_barrier();
+        if (w == 0) {
+            int before = 0;
+            for (int i0 = 0; i0 < groups; i0 += 64) {
+                unsigned long long word = i0 + lane < groups ? bits[i0 + lane] : 0;
+                const int m = __popcll(word), upto = wave_scan(m);
+                int drop = before + upto - rest;                      // of this word the last `drop` go
+                for (; drop > 0 && word; drop--) word &= ~(1ull << (63 - __builtin_clzll(word)));
+                if (i0 + lane < groups) bits[i0 + lane] = word;
+                before += __shfl(upto, 63, 64);
+            }
+        }
+    }
+    lds_barrier();
+    for (int p0 = 64 * w; p0 < pages; p0 += 64 * waves) {
+        const unsigned x = p0 + lane < pages ? score[p0 + lane] : 0;
+        const int bin = x == ALWAYS ? BINS : bin_of(x);
+        const unsigned long long word = __ballot(p0 + lane < pages && (x == ALWAYS || bin > step_of_last || (bin == step_of_last && x > least)));
+        if (lane == 0) bits[p0 >> 6] |= word;
+    }
+    lds_barrier();
+    int before = 0;
+    for (int i0 = 0; i0 < groups; i0 += 64) {
+        const int upto = wave_scan(i0 + lane < groups ? __popcll(bits[i0 + lane]) : 0);
+        for (int i = (i0 + waves - 1 - w) / waves * waves + w; i < min(i0 + 64, groups); i += waves) {
+            const unsigned long long word = bits[i];
+            const int at = before + (i > i0 ? __builtin_amdgcn_readlane(upto, max(i - i0 - 1, 0)) : 0);
+            if (word >> lane & 1) to[at + __popcll(word & ((1ull << lane) - 1))] = table[64 * i + lane];
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
 }
 
+// The scores formed by the same block, or read
+template <bool BF, int D>
+__global__ __launch_bounds__(256, 4) void select_pages_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
+                                                           int recent, int *__restrict__ tables, int *__restrict__ lens_out)
+{
+    const int b = blockIdx.x / c.kv_heads, page = threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];
+    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, group, sinks, recent);
+    choose_pages(c, rows, seen, keep, tables + (size_t)blockIdx.x * keep, lens_out, [&](unsigned *score) {
+        score_pages<BF, D>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
+                           [&](int p, bool new_page, unsigned x) { score[p] = new_page ? x : max(score[p], x); });
+    });
+}
+__global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows rows, int keep, int sinks, int recent, const unsigned *__restrict__ scores,
+                                                             int *__restrict__ tables, int *__restrict__ lens_out)
+{
+    const int b = blockIdx.x / c.kv_heads, step = blockDim.x;
+    const unsigned *const from = scores + (size_t)blockIdx.x * rows.width;
+    unsigned x[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++) x[u] = from[min((int)threadIdx.x + u * step, rows.width - 1)];         // (on their way with the lengths; what nobody wrote is not used)
+    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, 1, sinks, recent);
+    choose_pages(c, rows, seen, keep, tables + (size_t)blockIdx.x * keep, lens_out, [&](unsigned *score) {
+        for (int p0 = threadIdx.x; p0 < seen.pages; p0 += 4 * step) {
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                if (p0 >= 4 * step) x[u] = from[min(p0 + u * step, seen.pages - 1)];
+                if (p0 + u * step < seen.pages) score[p0 + u * step] = x[u];
+            }
+        }
+    });
+}
+
+// Scores in a launch of their own where a sequence may have more pages than one block should wait for
+constexpr int OF_BLOCK = 256;                                         // pages of a block, 64 of a wave
+bool scores_apart(int width) { return width > OF_BLOCK; }
+
 template <bool BF, int D>
 hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, const KeyBounds &bounds, const KvRows &rows, int keep, int sinks, int recent, int *tables,
-                        int *lens_out, hipStream_t st)
+                        int *lens_out, unsigned *scores, hipStream_t st)
 {
-    auto kern = select_pages_kernel<BF, D>;
     const size_t lds = 4 * (size_t)rows.width;
-    if (lds > 48 << 10)
-        if (hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-    const int threads = rows.width <= 64 ? 256 : rows.width <= 512 ? 512 : 1024;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(rows.batch * c.kv_heads)), dim3(threads), lds, st, (const char *)q, ldq, c, bounds, rows, heads / c.kv_heads, keep, sinks,
-                       recent, tables, lens_out);
+    const int group = heads / c.kv_heads;
+    const dim3 grid((unsigned)(rows.batch * c.kv_heads));
+    if (!scores_apart(rows.width)) {
+        hipLaunchKernelGGL((select_pages_kernel<BF, D>), grid, dim3(256), lds, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent, tables, lens_out);
+        return hipGetLastError();
+    }
+    if (lds > 40 << 10)
+        if (hipError_t e = hipFuncSetAttribute((const void *)select_scored_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
+    const unsigned items = (unsigned)((rows.width + 255) / 256) * rows.batch;
+    hipLaunchKernelGGL((page_scores_kernel<BF, D>), dim3((items + 7) / 8 * 8 * c.kv_heads), dim3(256), 0, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent,
+                       scores);
+    const int threads = rows.width <= 512 ? 256 : rows.width <= 1024 ? 512 : 1024;
+    hipLaunchKernelGGL(select_scored_kernel, grid, dim3(threads), lds, st, c, rows, keep, sinks, recent, scores, tables, lens_out);
     return hipGetLastError();
 }
 
@@ -273,13 +438,16 @@ hipError_t launch_cache_bounds(const KvCache &c, int D, const KeyBounds &bounds,
     return hipGetLastError();
 }
 
+size_t cache_select_workspace(int batch, int kv_heads, int width) { return scores_apart(width) ? 4 * (size_t)batch * kv_heads * width : 0; }
+
 hipError_t launch_cache_select(const void *q, long ldq, bool bf16, int heads, int D, const KvCache &c, const KeyBounds &bounds, const KvRows &rows, int keep, int sinks,
-                               int recent, int *tables, int *lens_out, hipStream_t st)
+                               int recent, int *tables, int *lens_out, void *ws, hipStream_t st)
 {
-    if (D == 128) return bf16 ? select_pages<true, 128>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, st)
-                              : select_pages<false, 128>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, st);
-    return bf16 ? select_pages<true, 64>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, st)
-                : select_pages<false, 64>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, st);
+    unsigned *const scores = static_cast<unsigned *>(ws);
+    if (D == 128) return bf16 ? select_pages<true, 128>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, scores, st)
+                              : select_pages<false, 128>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, scores, st);
+    return bf16 ? select_pages<true, 64>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, scores, st)
+                : select_pages<false, 64>(q, ldq, heads, c, bounds, rows, keep, sinks, recent, tables, lens_out, scores, st);
 }
 
 }  // namespace samp

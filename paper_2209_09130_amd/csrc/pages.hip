@@ -12,25 +12,12 @@ namespace {
 
 constexpr int BLOCK = 1024, NONE = 0x7fffffff;
 
-// A barrier for what the threads hand each other in LDS: stores to memory need not have arrived
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 template <bool LDS> __device__ __forceinline__ void barrier()
 {
     if constexpr (LDS) lds_barrier();
     else __syncthreads();
 }
 
-// the sum of the lanes up to this one (row shifts, then the last lanes of rows 0 and 2, then of row 1)
-__device__ __forceinline__ int wave_scan(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-    return x;
-}
 // the sums of the values of the threads before this one, and of all, N of them at a time; `parts` holds a value for each wave
 template <int WAVES, int N>
 __device__ __forceinline__ void block_scan(const int (&v)[N], int (*parts)[WAVES], int (&before)[N], int (&all)[N])

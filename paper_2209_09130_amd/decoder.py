@@ -33,8 +33,9 @@ _SIGNATURES = {
     "samp_pages_compact": (_P, _I, _P, _I, _I, _P, _P, _P, _P, _P, _Z, _P),
     "samp_cache_copy": (_P, _P, _P, _I, _P),
     "samp_cache_bounds": (_P, _P, _P, _I, _P, _P, _I, _I, _I, _P),
-    "samp_cache_select": (_P, _L, _I, _I, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P),
-    "samp_attention_sparse_workspace_bytes": (_I,) * 9,
+    "samp_cache_select_workspace_bytes": (_I,) * 3,
+    "samp_cache_select": (_P, _L, _I, _I, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _Z, _P),
+    "samp_attention_sparse_workspace_bytes": (_I,) * 10,
     "samp_attention_sparse": (_P, _L, _I, _I, _P, _P, _P, _I, _P, _P, _I, _I, _I, _I, _I, _I, _I, _F, _P, _P, _P, _Z, _P),
 }
 _entry = {}
@@ -495,8 +496,10 @@ def cache_select(q: torch.Tensor, cache: KVCache, bounds: KeyBounds, table: torc
     tables, lens_out = table.new_empty((B, cache.kv_heads, _choice(keep))), torch.empty_like(lens)
     max_new = _most(max_new)
     if rows and B:
+        need = _workspace_bytes("samp_cache_select_workspace_bytes", B, cache.kv_heads, width)
+        ws = q.new_empty((need,), dtype=torch.uint8) if need else None
         rc = _fn("samp_cache_select")(at, ld, _TYPES[q.dtype], heads, cache.address, kb, t, width, pcu, plens, B, max_new, rows, keep, *_ends(cache, max_new, rows, sinks, recent),
-                                      tables.data_ptr(), lens_out.data_ptr(), _raw_stream(device))
+                                      tables.data_ptr(), lens_out.data_ptr(), ws.data_ptr() if need else 0, need, _raw_stream(device))
         if rc:
             _raise(rc)
     else:
@@ -538,7 +541,7 @@ def attention_sparse(q: torch.Tensor, cache: KVCache, bounds: KeyBounds, table: 
         to = _flat("out", out, q.dtype, device, rows * heads * dim)
     if rows and B:
         max_new, max_len = _most(max_new), _most(width * cache.page_len if max_len is None else max_len)
-        need = _workspace_bytes("samp_attention_sparse_workspace_bytes", rows, B, heads, cache.kv_heads, dim, cache.page_len, max_new, max_len, _choice(keep))
+        need = _workspace_bytes("samp_attention_sparse_workspace_bytes", rows, B, heads, cache.kv_heads, dim, cache.page_len, width, max_new, max_len, _choice(keep))
         ws = q.new_empty((need,), dtype=torch.uint8) if need else None
         rc = _fn("samp_attention_sparse")(at, ld, _TYPES[q.dtype], heads, cache.address, kb, t, width, pcu, plens, B, max_new, max_len, rows, keep,
                                           *_ends(cache, max_new, rows, sinks, recent), dim ** -0.5 if scale is None else float(scale), words, to,
