@@ -12,75 +12,121 @@ namespace {
 constexpr float INV_127 = 1.0f / 127.0f;
 
 // ---- bounds ------------------------------------------------------------------------------------------
-// A wave takes a page of a key head: D / 16 lanes hold 16 channels each of 1024 / D keys at a time; then the lanes of the same channels meet.  What bounds it is HBM for whole prompts, and
-// the launch for a decode step, in which few pages become full and the other waves end at once.
+// A wave takes a page of a key head: D / 16 lanes hold 16 channels each of 1024 / D keys at a time; then the lanes of the same channels meet and share them out, D / 64 of them a lane.
+// What bounds it is HBM for whole prompts, and the launch for a decode step, in which few pages become full and the other waves end at once.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+// Of two channels the lower half of the lanes (or of each 32, 16, 8) gets the first, the upper the second, each from both halves
+template <int HALF, bool MAX> __device__ __forceinline__ float share(float a, float b, int lane)
+{
+    float x, y;
+    if constexpr (HALF == 32) {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        x = __uint_as_float(both[0]), y = __uint_as_float(both[1]);
+    } else if constexpr (HALF == 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        x = __uint_as_float(both[0]), y = __uint_as_float(both[1]);
+    } else {
+        const bool upper = lane & HALF;
+        const int give = __float_as_int(upper ? a : b);
+        x = upper ? b : a;
+        y = __int_as_float(HALF == 8 ? __builtin_amdgcn_update_dpp(0, give, 0x128, 0xf, 0xf, true) : __builtin_amdgcn_ds_swizzle(give, HALF << 10 | 0x1f));
+    }
+    return MAX ? max3(x, x, y) : min3(x, x, y);
+}
+
 template <int D>
 __global__ __launch_bounds__(256) void cache_bounds_kernel(KvCache c, KeyBounds bounds, KvRows rows)
 {
-    constexpr int LANES = D / 16, KEYS = 64 / LANES;
+    constexpr int LANES = D / 16, KEYS = 64 / LANES, TURN = 32 / KEYS;
     const SeqRows s = seq_rows(rows, blockIdx.z, c.page_shift);
     const int lane = threadIdx.x & 63, from = max(rows.lens[blockIdx.z] - s.n, 0), to = min(rows.lens[blockIdx.z] - s.n + s.todo, s.len);
     const int index = (from >> c.page_shift) + blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.x;
     if (s.todo <= 0 || to <= 0 || index >= to >> c.page_shift) return;
     const int page = rows.table[(size_t)blockIdx.z * rows.width + index];
     if ((unsigned)page >= (unsigned)c.pages) return;
-    const size_t row = ((size_t)page * c.kv_heads + head) << c.page_shift;
-    const int8_t *const k = c.k + row * D + 16 * lane;
-    const float *const steps = c.k_step + row + lane / LANES;
+    const size_t at = (size_t)page * c.kv_heads + head, row = at << c.page_shift;
+    const int8_t *const k = c.k + row * D + 16 * (lane % LANES);
+    const float *const steps = c.k_step + row;
+    const int len = 1 << c.page_shift;
     float high[16], low[16];
 #pragma unroll
     for (int e = 0; e < 16; e++) {
         high[e] = -INFINITY;
         low[e] = INFINITY;
     }
-    bool odd = false;                                                 // a step that is not finite: that of a key that is not
-    for (int i0 = 0; i0 < 1 << c.page_shift; i0 += 16) {              // sixteen keys a turn: page_len is a multiple
-        v4i raw[16 / KEYS];
-        float step[16 / KEYS];
+    float odd = 0.0f;                                                 // NaN with a step that is not finite, that of a key that is not
+    for (int i0 = 0; i0 < len; i0 += 32) {                            // (of a page of sixteen each key twice)
+        v4i raw[TURN];
+        float step[TURN];
 #pragma unroll
-        for (int i = 0; i < 16 / KEYS; i++) {
-            raw[i] = *reinterpret_cast<const v4i *>(k + (size_t)(i0 + i * KEYS) * D);
-            step[i] = steps[i0 + i * KEYS];
+        for (int i = 0; i < TURN; i++) {
+            const int key = (i0 + i * KEYS + lane / LANES) & (len - 1);
+            raw[i] = *reinterpret_cast<const v4i *>(k + key * D);
+            step[i] = steps[key];
         }
 #pragma unroll
-        for (int i = 0; i < 16 / KEYS; i++) {
-            odd |= !__builtin_isfinite(step[i]);
+        for (int i = 0; i < TURN; i += 2) {
+            odd += step[i] * 0.0f + step[i + 1] * 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; e++) {
-                const float x = (float)(int8_t)(raw[i][e >> 2] >> 8 * (e & 3)) * step[i];
-                high[e] = __builtin_fmaxf(high[e], x);
-                low[e] = __builtin_fminf(low[e], x);
+                const float x = (float)(int8_t)(raw[i][e >> 2] >> 8 * (e & 3)) * step[i], y = (float)(int8_t)(raw[i + 1][e >> 2] >> 8 * (e & 3)) * step[i + 1];
+                high[e] = max3(high[e], x, y);
+                low[e] = min3(low[e], x, y);
             }
         }
     }
+    const bool bad = __any(!(odd == 0.0f));
 #pragma unroll
-    for (int o = LANES; o < 64; o <<= 1)
+    for (int e = 0; e < 8; e++) {
+        high[e] = share<32, true>(high[e], high[e + 8], lane);
+        low[e] = share<32, false>(low[e], low[e + 8], lane);
+    }
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            high[e] = __builtin_fmaxf(high[e], __shfl_xor(high[e], o, 64));
-            low[e] = __builtin_fminf(low[e], __shfl_xor(low[e], o, 64));
-        }
-    odd = __any(odd);
+    for (int e = 0; e < 4; e++) {
+        high[e] = share<16, true>(high[e], high[e + 4], lane);
+        low[e] = share<16, false>(low[e], low[e + 4], lane);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+        high[e] = share<8, true>(high[e], high[e + 2], lane);
+        low[e] = share<8, false>(low[e], low[e + 2], lane);
+    }
+    constexpr int MINE = D / 64;                                      // channels of a lane
+    int channel = 16 * (lane % LANES) + (lane >> 5 & 1) * 8 + (lane >> 4 & 1) * 4 + (lane >> 3 & 1) * 2;
+    if constexpr (MINE == 1) {
+        high[0] = share<4, true>(high[0], high[1], lane);
+        low[0] = share<4, false>(low[0], low[1], lane);
+        channel += lane >> 2 & 1;
+    }
     float top = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 16; e++) top = __builtin_fmaxf(top, __builtin_fmaxf(__builtin_fabsf(high[e]), __builtin_fabsf(low[e])));
+    for (int e = 0; e < MINE; e++) top = max3(top, __builtin_fabsf(high[e]), __builtin_fabsf(low[e]));
+    top = wave_max(top);
+    const bool some = top > 0.0f && !bad;
+    const float step = bad ? __builtin_nanf("") : some ? top * INV_127 : 1.0f;
+    int codes[2] = {0, 0};
 #pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o, 64));
-    const bool some = top > 0.0f && !odd;
-    const float step = odd ? __builtin_nanf("") : some ? top * INV_127 : 1.0f;
-    const size_t at = (size_t)page * c.kv_heads + head;
-    if (lane < 2 * LANES) {                                           // the first lanes write the high codes, the next ones the low codes
-        const bool is_low = lane >= LANES;
-        int code[16];
+    for (int e = 0; e < MINE; e++) {
+        const float up = __builtin_fminf(__builtin_ceilf(__fdiv_rn(high[e], step)), 127.0f), down = __builtin_fmaxf(__builtin_floorf(__fdiv_rn(low[e], step)), -127.0f);
+        codes[0] |= (some ? (int)up & 0xff : 0) << 8 * e;
+        codes[1] |= (some ? (int)down & 0xff : 0) << 8 * e;
+    }
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            const float q = __fdiv_rn(is_low ? low[e] : high[e], step), r = is_low ? __builtin_fmaxf(__builtin_floorf(q), -127.0f) : __builtin_fminf(__builtin_ceilf(q), 127.0f);
-            code[e] = some ? (int)r : 0;
-        }
-        v4i packed;
-#pragma unroll
-        for (int i = 0; i < 4; i++) packed[i] = pack4(code[4 * i], code[4 * i + 1], code[4 * i + 2], code[4 * i + 3]);
-        *reinterpret_cast<v4i *>(bounds.codes + at * 2 * D + 16 * lane) = packed;
+    for (int i = 0; i < 2; i++) {
+        int8_t *const to_codes = bounds.codes + (2 * at + i) * D + channel;
+        if constexpr (MINE == 2) *reinterpret_cast<short *>(to_codes) = (short)codes[i];
+        else *to_codes = (int8_t)codes[i];
     }
     if (lane == 0) bounds.steps[at] = step;
 }
