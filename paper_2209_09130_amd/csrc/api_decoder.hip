@@ -291,10 +291,10 @@ int samp_beam_select(const void *logits, int64_t ld, int32_t type, const float *
     return SAMP_OK;
 }
 
-size_t samp_pages_fork_workspace_bytes(int32_t pages, int32_t rows_from, int32_t rows)
+size_t samp_pages_fork_workspace_bytes(int32_t pages, int32_t rows_from, int32_t width, int32_t rows)
 {
-    if (check_pages(pages) || rows < 1 || rows > SAMP_MAX_BATCH || rows_from < 1 || rows_from > SAMP_MAX_BATCH) return 0;
-    return pages_fork_workspace(pages, rows_from, rows);
+    if (check_pages(pages) || rows < 1 || rows > SAMP_MAX_BATCH || rows_from < 1 || rows_from > SAMP_MAX_BATCH || width < 1) return 0;
+    return pages_fork_workspace(pages, rows_from, width, rows);
 }
 
 int samp_pages_fork(const int32_t *refs, int32_t pages, const int32_t *table, const int32_t *lens, int32_t rows_from, int32_t width, int32_t page_len,
@@ -308,7 +308,7 @@ int samp_pages_fork(const int32_t *refs, int32_t pages, const int32_t *table, co
         return fail(SAMP_ERR_SHAPE, "1 to %d rows, a table width of at least 1 and max_new >= 0 are needed (%d, %d, %d, %d)", SAMP_MAX_BATCH, rows, rows_from, width, max_new);
     if ((long long)rows * width > INT32_MAX || (long long)rows_from * width > INT32_MAX) return fail(SAMP_ERR_SHAPE, "a table has less than 2^31 entries");
     if (refs == refs_out || table == table_out || lens == lens_out) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
-    if (int rc = check_workspace(workspace, workspace_bytes, samp_pages_fork_workspace_bytes(pages, rows_from, rows))) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, samp_pages_fork_workspace_bytes(pages, rows_from, width, rows))) return rc;
     const PageFork f{refs, table, lens, parents, cu, pages, rows_from, width, shift_of(page_len), max_new, rows, refs_out, table_out, lens_out, copies, lacking};
     HIP_TRY(launch_pages_fork(f, workspace, (hipStream_t)stream));
     return SAMP_OK;

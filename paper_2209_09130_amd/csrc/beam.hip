@@ -7,6 +7,7 @@
 // logits in no order) goes to a list in LDS, which is ranked by counting.
 #include "../../include/samp.h"
 #include "decoder.h"
+#include "decoder_rules.h"
 
 #include <type_traits>
 
@@ -422,11 +423,6 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
     }
 }
 
-// pieces of 512 threads with eight vectors each, or of 256 with two
-struct Piece { int threads, vectors; };
-constexpr Piece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
-int values_of(int type, Piece p) { return p.threads * p.vectors * (type == F32 ? 4 : 8); }
-
 template <int T, int THREADS, int VECTORS>
 void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, int chunks, PieceSum *sums, Candidate *best,
             hipStream_t st)
@@ -447,10 +443,8 @@ void pieces(const void *logits, long ld, const float *scores, const uint8_t *fin
 
 BeamCut beam_cut(int type, int rows, int vocab)
 {
-    const int phase = (type == F32 ? 4 : 8) - 1;                      // places that a row may begin behind an aligned address
-    auto chunks = [&](Piece p) { return (vocab + phase + values_of(type, p) - 1) / values_of(type, p); };
-    const bool large = (long)rows * chunks(LONG_PIECE) >= 512;
-    return BeamCut{large, chunks(large ? LONG_PIECE : SHORT_PIECE)};
+    const bool wide = type == F32, large = long_pieces(wide, rows, vocab);
+    return BeamCut{large, piece_chunks(large ? LONG_PIECE : SHORT_PIECE, wide, vocab)};
 }
 
 size_t beam_workspace(int type, int batch, int beams, int vocab, int keep)

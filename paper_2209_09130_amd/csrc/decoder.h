@@ -159,7 +159,7 @@ struct PageFork {
     int pages, rows_from, width, page_shift, max_new, rows;
     int *refs_out, *table_out, *lens_out, *copies, *lacking;
 };
-size_t pages_fork_workspace(int pages, int rows_from, int rows);
+size_t pages_fork_workspace(int pages, int rows_from, int width, int rows);
 hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st);
 size_t pages_compact_workspace(int pages, int entries);
 hipError_t launch_pages_compact(const int *refs, int pages, const int *table, int entries, int page_len, int *refs_out, int *table_out, int *copies, int *used, void *ws,

@@ -57,12 +57,34 @@ inline int tokens_band(int tile) { return tile == 4 ? 4 : 8; }
 // has 2048 x 8 rows and is better off with one (5.4 us).
 inline int cache_passes(long rows, int kv_heads) { return rows * kv_heads >= 32768 ? 4 : 1; }
 
+// ---- beam search's selection -----------------------------------------------------------------------------
+// A row is cut into pieces of 512 threads with eight vectors of 16 bytes each where that makes enough of them, else of 256 with two.  us, both kernels, long / short pieces, rows x vocabulary:
+// 16 bits 64 x 32000 13.9 / 11.4, 256 x 32000 15.6 / 14.4, 512 x 32000 18.1 / 18.8, 64 x 128256 14.7 / 14.7, 128 x 128256 17.1 / 18.9; binary32, whose short pieces are half as many
+// values, 4 x 21128 11.3 / 9.7, 64 x 32000 12.4 / 12.0, 16 x 128256 12.2 / 14.7, 32 x 128256 13.3 / 16.1, 512 x 32000 20.8 / 25.0, 128 x 128256 20.8 / 27.4.
+struct BeamPiece { int threads, vectors; };
+constexpr BeamPiece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
+inline int piece_chunks(BeamPiece p, bool wide, int vocab)
+{
+    const int vector = wide ? 4 : 8, values = p.threads * p.vectors * vector;
+    return (vocab + vector - 1 + values - 1) / values;                // (a row may begin `vector` - 1 places behind an aligned address)
+}
+inline bool long_pieces(bool wide, int rows, int vocab) { return (long)rows * piece_chunks(LONG_PIECE, wide, vocab) >= (wide ? 128 : 512); }
+
 // ---- bookkeeping of pages ------------------------------------------------------------------------------
-// One block does a whole call where its counters fit the LDS of a CU: two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 for each old
-// one; 6 bytes for each page.
+// One block does a whole call where its counters fit the LDS of a CU (two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 bytes for each
+// old one; 6 bytes for each page) and its 16 waves are no slower than the launches of several.  us in a chain of calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 4.8 / 8.4,
+// 4000 x 256 x 40 10.6 / 13.4, 13000 x 256 x 64 15.6 / 27.3, 12000 x 64 x 512 16.9 / 25.8, 8000 x 1800 x 16 34.2 / 34.2, 9000 x 1024 x 64 28.4 / 23.8; compacted, pages, 300 3.0 / 12.0,
+// 4096 4.9 / 15.2, 8192 10.9 / 16.9, 16384 24.8 / 19.9.
 inline long fork_block_lds(long pages, long rows_from, long rows) { return 10 * pages + 16 * rows_from + (32 + 4) * rows; }
-inline bool fork_in_block(long pages, long rows_from, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10; }
+inline bool fork_in_block(long pages, long rows_from, long width, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10 && rows_from * width <= 49152; }
 inline long compact_block_lds(long pages) { return 4 * pages + 2 * (pages / 2 + 1); }
-inline bool compact_in_block(long pages, long entries) { return pages <= 24 * 1024 && entries <= 65536; }
+inline bool compact_in_block(long pages, long entries) { return pages <= 8192 && entries <= 65536; }
+
+// ---- pages that are read -------------------------------------------------------------------------------
+// The scores of up to 256 pages of a sequence (64 a wave) are formed by the block that chooses among them, those of more in a launch of their own: one CU gets 35 to 50 GB/s of bounds from
+// pages all over memory.  us, one launch / two: sequences x key heads x pages 1 x 8 x 256 7.1 / 9.0, 8 x 8 x 100 6.7 / 8.5, 64 x 8 x 128 8.3 / 10.6, 64 x 8 x 256 11.3 / 12.8; a
+// block of sixteen waves for 1 x 8 x 1563 21 / 11.
+constexpr int SCORED_TOGETHER = 256;
+inline bool scores_apart(int width) { return width > SCORED_TOGETHER; }
 
 }  // namespace samp

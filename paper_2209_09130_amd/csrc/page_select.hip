@@ -5,6 +5,7 @@
 // so that the choice is the same however it is computed.
 #include "../../include/samp.h"
 #include "decoder.h"
+#include "decoder_rules.h"
 
 namespace samp {
 namespace {
@@ -239,18 +240,18 @@ __device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &row
     return seen;
 }
 
-// scores [batch, kv_heads, width]; a block has 256 pages of a sequence and a key head.  Blocks go to the eight XCDs in turn: the key heads of the same pages have blocks of the same XCD, so
+// scores [batch, kv_heads, width]; a block has SCORED_TOGETHER pages of a sequence and a key head.  Blocks go to the eight XCDs in turn: the key heads of the same pages have blocks of the same XCD, so
 // that a page's steps, which lie next to each other, come to one L2.
 template <bool BF, int D>
 __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
                                                           int recent, unsigned *__restrict__ scores)
 {
-    const int of_xcd = blockIdx.x >> 3, head = of_xcd % c.kv_heads, item = of_xcd / c.kv_heads * 8 + (blockIdx.x & 7), chunks = (rows.width + 255) >> 8;
+    const int of_xcd = blockIdx.x >> 3, head = of_xcd % c.kv_heads, item = of_xcd / c.kv_heads * 8 + (blockIdx.x & 7), chunks = (rows.width + SCORED_TOGETHER - 1) / SCORED_TOGETHER;
     const int chunk = item / rows.batch, b = item - chunk * rows.batch;
     if (chunk >= chunks) return;
-    const int page = chunk * 256 + threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];          // (on its way with the lengths)
+    const int page = chunk * SCORED_TOGETHER + threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];          // (on its way with the lengths)
     const Seen seen = what_is_seen(c, rows, b, head, group, sinks, recent);
-    if (seen.pages <= keep || chunk * 256 >= seen.pages) return;
+    if (seen.pages <= keep || chunk * SCORED_TOGETHER >= seen.pages) return;
     unsigned *const to = scores + ((size_t)b * c.kv_heads + head) * rows.width;
     score_pages<BF, D>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
                        [&](int p, bool new_page, unsigned x) { to[p] = new_page ? x : max(to[p], x); });
@@ -448,10 +449,6 @@ __global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows r
     });
 }
 
-// Scores in a launch of their own where a sequence may have more pages than one block should wait for
-constexpr int OF_BLOCK = 256;                                         // pages of a block, 64 of a wave
-bool scores_apart(int width) { return width > OF_BLOCK; }
-
 template <bool BF, int D>
 hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, const KeyBounds &bounds, const KvRows &rows, int keep, int sinks, int recent, int *tables,
                         int *lens_out, unsigned *scores, hipStream_t st)
@@ -465,7 +462,7 @@ hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, co
     }
     if (lds > 40 << 10)
         if (hipError_t e = hipFuncSetAttribute((const void *)select_scored_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-    const unsigned items = (unsigned)((rows.width + 255) / 256) * rows.batch;
+    const unsigned items = (unsigned)((rows.width + SCORED_TOGETHER - 1) / SCORED_TOGETHER) * rows.batch;
     hipLaunchKernelGGL((page_scores_kernel<BF, D>), dim3((items + 7) / 8 * 8 * c.kv_heads), dim3(256), 0, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent,
                        scores);
     const int threads = rows.width <= 512 ? 256 : rows.width <= 1024 ? 512 : 1024;

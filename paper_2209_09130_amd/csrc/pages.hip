@@ -535,14 +535,14 @@ size_t room(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t pages_fork_workspace(int pages, int rows_from, int rows)
+size_t pages_fork_workspace(int pages, int rows_from, int width, int rows)
 {
-    return fork_in_block(pages, rows_from, rows) ? 0 : 3 * room(4 * (size_t)pages) + room(4 * (size_t)rows);
+    return fork_in_block(pages, rows_from, width, rows) ? 0 : 3 * room(4 * (size_t)pages) + room(4 * (size_t)rows);
 }
 
 hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st)
 {
-    if (fork_in_block(f.pages, f.rows_from, f.rows)) {
+    if (fork_in_block(f.pages, f.rows_from, f.width, f.rows)) {
         const size_t lds = fork_block_lds(f.pages, f.rows_from, f.rows);
         if (lds > 60 << 10)
             if (hipError_t e = hipFuncSetAttribute((const void *)fork_block_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
@@ -576,9 +576,7 @@ hipError_t launch_pages_compact(const int *refs, int pages, const int *table, in
     const size_t count = ((size_t)pages + 63) / 64;
     if (compact_in_block(pages, entries)) {
         const size_t lds = compact_block_lds(pages);
-        auto kern = pages <= 4 * BLOCK ? compact_block_kernel<4> : pages <= 8 * BLOCK ? compact_block_kernel<8> : compact_block_kernel<24>;
-        if (lds > 60 << 10)
-            if (hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
+        auto kern = pages <= 4 * BLOCK ? compact_block_kernel<4> : compact_block_kernel<8>;
         hipLaunchKernelGGL(kern, dim3(1), dim3(BLOCK), lds, st, a);
         return hipGetLastError();
     }

@@ -27,7 +27,7 @@ _SIGNATURES = {
     "samp_attention_causal": (_P, _L, _P, _L, _P, _L, _I, _I, _I, _I, _P, _I, _I, _I, _F, _P, _P),
     "samp_beam_select_workspace_bytes": (_I,) * 5,
     "samp_beam_select": (_P, _L, _I, _P, _P, _I, _I, _I, _I, _I, _P, _P, _P, _P, _Z, _P),
-    "samp_pages_fork_workspace_bytes": (_I, _I, _I),
+    "samp_pages_fork_workspace_bytes": (_I,) * 4,
     "samp_pages_fork": (_P, _I, _P, _P, _I, _I, _I, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _Z, _P),
     "samp_pages_compact_workspace_bytes": (_I, _I),
     "samp_pages_compact": (_P, _I, _P, _I, _I, _P, _P, _P, _P, _P, _Z, _P),
@@ -347,8 +347,8 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, keep: Op
     done = 0
     if finished is not None:
         done = _flat("finished", finished, torch.bool if finished.dtype is torch.bool else torch.uint8, device, rows)
-    best = logits.new_empty((batch, keep), dtype=torch.float32)
-    parents, tokens = logits.new_empty((2, batch, keep), dtype=torch.int32).unbind()
+    best, parents, tokens = scores.new_empty((3, batch, keep)).unbind()
+    parents, tokens = parents.view(torch.int32), tokens.view(torch.int32)
     if batch:
         need = _workspace_bytes("samp_beam_select_workspace_bytes", _LOGITS[logits.dtype], batch, beams, vocab, keep)
         ws = logits.new_empty((need,), dtype=torch.uint8) if need else None
@@ -357,6 +357,11 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, keep: Op
         if rc:
             _raise(rc)
     return best, parents, tokens
+
+
+def _parts(like: torch.Tensor, sizes: Tuple[int, ...]) -> Tuple[torch.Tensor, ...]:
+    """Flat results in one allocation (an allocation and a view take about as long as a call's checks)."""
+    return torch.split_with_sizes(like.new_empty(sum(sizes)), sizes)
 
 
 def _table(table: torch.Tensor, device: int) -> Tuple[int, int, int]:
@@ -385,15 +390,14 @@ def pages_fork(refs: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page
         _refuse(f"1 to 8192 rows are supported ({rows})")
     if rows * width > _INT_MAX:
         _refuse("a page table has less than 2^31 entries")
-    refs_out, table_out, out = torch.empty_like(refs), table.new_empty((rows, width)), table.new_empty((4 * rows + 1,))
-    lens_out, copies, lacking = out[:rows], out[rows:4 * rows].view(3, rows), out[4 * rows:]
-    need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows_from, rows)
+    refs_out, table_out, lens_out, copies, lacking = _parts(refs, (pages, rows * width, rows, 3 * rows, 1))
+    need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows_from, width, rows)
     ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
     rc = _fn("samp_pages_fork")(pr, pages, pt, pl, rows_from, width, page_len, pp, pc, _most(max_new), rows, refs_out.data_ptr(), table_out.data_ptr(),
                                 lens_out.data_ptr(), copies.data_ptr(), lacking.data_ptr(), ws.data_ptr() if need else 0, need, _raw_stream(device))
     if rc:
         _raise(rc)
-    return refs_out, table_out, lens_out, copies, lacking
+    return refs_out, table_out.view(rows, width), lens_out, copies.view(3, rows), lacking
 
 
 def pages_compact(refs: torch.Tensor, table: torch.Tensor, page_len: int) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
@@ -406,16 +410,15 @@ def pages_compact(refs: torch.Tensor, table: torch.Tensor, page_len: int) -> Tup
     if pages > _INT_MAX or entries > _INT_MAX:
         _refuse(f"{pages} pages or {entries} entries are more than int32 counts")
     pr, pt = _flat("refs", refs, torch.int32, device), _flat("table", table, torch.int32, device)
-    refs_out, table_out = torch.empty_like(refs), torch.empty_like(table)
-    out = refs.new_empty((3 * max(1, pages // 2) + 1,))
-    copies, used = out[:-1].view(3, -1), out[-1:]
+    n = max(1, pages // 2)
+    refs_out, table_out, copies, used = _parts(refs, (pages, entries, 3 * n, 1))
     need = _workspace_bytes("samp_pages_compact_workspace_bytes", pages, entries)
     ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
     rc = _fn("samp_pages_compact")(pr, pages, pt, entries, page_len, refs_out.data_ptr(), table_out.data_ptr(), copies.data_ptr(), used.data_ptr(),
                                    ws.data_ptr() if need else 0, need, _raw_stream(device))
     if rc:
         _raise(rc)
-    return refs_out, table_out, copies, used
+    return refs_out, table_out.view(table.shape), copies.view(3, n), used
 
 
 class _BoundsStruct(C.Structure):

@@ -1,8 +1,9 @@
 """Beam search's selection against its definition in binary64, on the CPU.
 
-A total is a score plus a logit less the row's log-sum-exp, formed in binary64 from exponentials in binary32.  Those are off by one step (2^-23) each and by their argument's
-rounding, |t| 2^-24 ln 2 for an argument t in powers of two, whose mean under the softmax is at most log2(vocabulary) <= 19; up to 16 are added in binary32 in a row, then 9 sums.  So a
-log-sum-exp is off by less than (2 + 14 + 25) 2^-24 < 48 * 2^-24, and the result is rounded to binary32 once.
+A total is a score plus a logit less the row's log-sum-exp, formed in binary64 from sums of exponentials in binary32.  In units of 2^-24, relative to a sum: an exponential has a step (2); its argument
+t, in powers of two, is rounded, |t| ln 2 with a mean under the softmax of at most log2(vocabulary) <= 19 (13.2), and log2(e) in it is 1.34e-8 off (3); a thread adds 16 in a row (15), then
+there are two additions, six over the wave and three over the waves (11), and a wave's sum is scaled by a power with a step of its own (3).  So a log-sum-exp is off by less than 48 * 2^-24, and the result
+is rounded to binary32 once.
 """
 import math
 
@@ -69,7 +70,7 @@ def check(P, logits, scores, beams, keep=None, finished=None, end=7, device=None
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("B,W,V,keep", [(1, 1, 1, 1), (1, 1, 5, 3), (2, 3, 7, 10), (1, 4, 1000, 4), (3, 2, 4095, 64), (2, 5, 4096, 5), (1, 1, 4097, 2), (3, 4, 21128, 8), (40, 4, 32000, 8),
-                                        (2, 64, 300, 64), (130, 3, 17001, 6), (1, 2, 1 << 19, 4)])
+                                        (2, 64, 300, 64), (130, 3, 17001, 6), (1, 2, 1 << 19, 4), (65, 8, 33001, 16)])
 def test_beam_select(P, B, W, V, keep, dtype):
     g = gen(B + W + V)
     x = (torch.randn(B * W, V, generator=g) * 3).to(dtype)
@@ -150,6 +151,26 @@ def test_rows_in_place_at_any_alignment(P, dtype):
         base[:, shift + V:] = 100
         view = base.cuda()[:, shift:shift + V]
         check(P, base[:, shift:shift + V], -torch.rand(6, generator=gen(2)), 3, 6, device=view)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("keep", [16, 64])
+def test_long_pieces_of_every_kind_of_row(P, dtype, keep):
+    """A batch whose rows are cut into long pieces: rows in no order, of one value, rising, falling, of few values, masked by minus infinity or the type's lowest value."""
+    B, W, V = 66, 8, 40003
+    x = torch.randn(B * W, V, generator=gen(keep))
+    at = torch.arange(V)
+    x[0::9] = 1.5
+    x[1::9] = (at * (40.0 / V)).repeat(len(x[1::9]), 1)
+    x[2::9] = (-at * (40.0 / V)).repeat(len(x[2::9]), 1)
+    x[3::9] = (at % 7).float().repeat(len(x[3::9]), 1)
+    x[4::9, torch.randperm(V, generator=gen(1))[: V - 9]] = -math.inf
+    x = x.to(dtype)
+    x[5::9, 20:] = torch.finfo(dtype).min
+    x[6, 39999], x[7, 3] = math.nan, math.inf
+    scores = -20 * torch.rand(B * W, generator=gen(2))
+    scores[100::37] = -math.inf
+    check(P, x, scores, W, keep)
 
 
 def test_beams_of_no_sequences_and_refusals(P):

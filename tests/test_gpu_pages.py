@@ -101,7 +101,7 @@ def state(rows, width, page_len, pages, seed, shared=0.5, spare=0):
 
 
 SIZES = [(1, 1, 16, 1), (4, 3, 16, 9), (7, 5, 32, 40), (33, 9, 16, 300), (130, 17, 64, 2000), (300, 6, 16, 1000)]
-LARGE = [(5, 4, 16, 40000), (150, 40, 16, 30000), (8192, 2, 16, 17000)]
+LARGE = [(5, 4, 16, 40000), (150, 40, 16, 30000), (8192, 2, 16, 17000), (1000, 70, 16, 9000)]
 
 
 @pytest.mark.parametrize("rows,width,page_len,pages", SIZES + LARGE)
@@ -302,7 +302,7 @@ def test_beam_search_over_a_paged_cache(P, D, G, H, page):
 def test_bookkeeping_in_graphs(P):
     """Captured once, replayed on new inputs: counts and tables come out as from the calls."""
     refs, table, lens = state(60, 8, 16, 700, 3)
-    for pages in (700, 30000):                               # one block, several kernels
+    for pages in (700, 8000, 30000):                         # one block, with more LDS than a launch has by itself, several kernels
         dev = [ints(refs + [0] * (pages - 700)).cuda(), ints(table).cuda(), ints(lens).cuda(), torch.zeros(60, dtype=torch.int32, device="cuda")]
 
         def step():
