@@ -75,7 +75,7 @@ inline bool long_pieces(bool wide, int rows, int vocab) { return (long)rows * pi
 // old one; 6 bytes for each page) and its 16 waves are no slower than the launches of several.  us in a chain of calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 4.8 / 8.4,
 // 4000 x 256 x 40 10.6 / 13.4, 13000 x 256 x 64 15.6 / 27.3, 12000 x 64 x 512 16.9 / 25.8, 8000 x 1800 x 16 34.2 / 34.2, 9000 x 1024 x 64 28.4 / 23.8; compacted, pages, 300 3.0 / 12.0,
 // 4096 4.9 / 15.2, 8192 10.9 / 16.9, 16384 24.8 / 19.9.
-inline long fork_block_lds(long pages, long rows_from, long rows) { return 10 * pages + 16 * rows_from + (32 + 4) * rows; }
+inline long fork_block_lds(long pages, long rows_from, long rows) { return 10 * ((pages + 3) & ~3l) + 16 * rows_from + (32 + 4) * rows; }
 inline bool fork_in_block(long pages, long rows_from, long width, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10 && rows_from * width <= 49152; }
 inline long compact_block_lds(long pages) { return 4 * pages + 2 * (pages / 2 + 1); }
 inline bool compact_in_block(long pages, long entries) { return pages <= 8192 && entries <= 65536; }

@@ -6,6 +6,7 @@
 #include "../../include/samp.h"
 #include "decoder.h"
 #include "decoder_rules.h"
+#include "divisor.h"
 
 namespace samp {
 namespace {
@@ -143,12 +144,29 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
             wide += r.wide;
         }
     });
-    // (a thread has some neighbouring pages, and some neighbouring rows)
-    const int per = (f.pages + BLOCK - 1) / BLOCK;
+    // (a thread has some neighbouring pages, and some neighbouring rows; of counters in LDS at most PAGES, which it keeps)
+    constexpr int PAGES = 16;
+    const int per = LDS ? ((f.pages + BLOCK - 1) / BLOCK + 3) & ~3 : (f.pages + BLOCK - 1) / BLOCK;
     const long at = (long)tid * per, end = min(at + per, (long)f.pages);
-    int mine = 0;
+    int mine = 0, rest[PAGES];
+    unsigned is_free = 0, written = 0;                                // bits of the pages that are kept
+    if constexpr (LDS) {
+#pragma unroll
+        for (int q = 0; q < PAGES; q += 4)
+            if (q < per && at + q < end) {                            // (the counters of four pages at a time, some of them behind the last page's)
+                const v4i r = *reinterpret_cast<const v4i *>(&c.rest[at + q]), w = *reinterpret_cast<const v4i *>(&c.first[at + q]);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    rest[q + e] = r[e];
+                    written |= (unsigned)(w[e] != NONE) << (q + e);
+                    is_free |= (unsigned)(r[e] == 0 && w[e] == NONE && at + q + e < end) << (q + e);
+                }
+            }
+        mine = __popc(is_free);
+    } else {
 #pragma unroll 4
-    for (long i = at; i < end; i++) mine += c.rest[i] == 0 && c.first[i] == NONE;
+        for (long i = at; i < end; i++) mine += c.rest[i] == 0 && c.first[i] == NONE;
+    }
     barrier<LDS>();
     const int rows_per = (f.rows + BLOCK - 1) / BLOCK, row0 = tid * rows_per, row1 = min(row0 + rows_per, f.rows);
     int sum = 0;
@@ -164,18 +182,30 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
         rank += n;
     }
     rank = before[1];
-#pragma unroll 4
-    for (long i = at; i < end; i++) {
-        int n = c.rest[i];
-        const bool unwritten = c.first[i] == NONE;
-        if (n == 0 && unwritten) {
+    auto count_of = [&](long page, int n, bool free_page, bool is_written) {
+        if (free_page) {
             if (rank < wanted) {
-                list[rank] = (List)i;
+                list[rank] = (List)page;
                 n = 1;
             }
             rank++;
-        } else if (n == 0) n = 1;                                     // the first of its writers
-        f.refs_out[i] = n;
+        } else if (n == 0 && is_written) n = 1;                       // the first of its writers
+        f.refs_out[page] = n;
+    };
+    if constexpr (LDS) {
+#pragma unroll
+        for (int q = 0; q < PAGES; q += 4) {
+            if (q >= per) break;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (at + q + e < end) count_of(at + q + e, rest[q + e], is_free >> (q + e) & 1, written >> (q + e) & 1);
+        }
+    } else {
+#pragma unroll 4
+        for (long i = at; i < end; i++) {
+            const bool is_written = c.first[i] != NONE;
+            count_of(i, c.rest[i], c.rest[i] == 0 && !is_written, is_written);
+        }
     }
     if (tid == 0) f.lacking[0] = max(wanted - free_pages, 0) + all[2];
     barrier<LDS>();
@@ -230,8 +260,8 @@ __device__ __forceinline__ void copy_row(const PageFork &f, int row, int lane)
     }
 }
 
-// The first block does the bookkeeping, the others copy what does not depend on it, sixteen rows each.
-__global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f)
+// The first block does the bookkeeping, the others copy what does not depend on it, sixteen rows each.  by: divisor() of the width
+__global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f, unsigned by)
 {
     extern __shared__ __attribute__((aligned(16))) char shared[];
     __shared__ int parts[3][BLOCK / 64];
@@ -244,9 +274,10 @@ __global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f)
     }
     RowPlan *const plans = reinterpret_cast<RowPlan *>(shared);
     Children *const children = reinterpret_cast<Children *>(plans + f.rows);
-    int *const counters = reinterpret_cast<int *>(children + f.rows_from), *const needs = counters + 2 * f.pages;
+    const int padded = (f.pages + 3) & ~3;
+    int *const counters = reinterpret_cast<int *>(children + f.rows_from), *const needs = counters + 2 * padded;
     unsigned short *const list = reinterpret_cast<unsigned short *>(needs + f.rows);
-    const Counters c{counters, counters + f.pages};
+    const Counters c{counters, counters + padded};
     for (int i = tid; i < f.rows_from; i += BLOCK) {
         const int held = max(f.lens[i], 0);
         children[i] = Children{0, 0, held >> f.page_shift, held & ((1 << f.page_shift) - 1)};
@@ -279,25 +310,22 @@ __global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f)
         count_writers(f, c, row, r);
     });
     lds_barrier();
-    // A wave a row of the old tables: its names leave as often as no row takes them on (rows that go on write from the page that their next position lies in), several rows' entries requested at a time
+    // The old tables' names leave as often as no row takes them on (rows that go on write from the page that their next position lies in), eight entries of a thread requested at a time
     constexpr int AT_ONCE = 8;
-    for (int row0 = w; row0 < f.rows_from; row0 += AT_ONCE * WAVES)
-        for (int j0 = 0; j0 < f.width; j0 += 64) {
-            const int j = j0 + lane, at = min(j, f.width - 1);
-            int old[AT_ONCE];
+    const int entries = f.rows_from * f.width;
+    for (int i0 = 0; i0 < entries; i0 += AT_ONCE * BLOCK) {
+        int old[AT_ONCE];
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; u++) old[u] = f.table[(long)min(row0 + u * WAVES, f.rows_from - 1) * f.width + at];
+        for (int u = 0; u < AT_ONCE; u++) old[u] = f.table[min(i0 + u * BLOCK + tid, entries - 1)];
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; u++) {
-                const int row = row0 + u * WAVES;
-                if (row >= f.rows_from) break;
-                const Children n = children[row];
-                const int all = __builtin_amdgcn_readfirstlane(n.all) - 1, whole = __builtin_amdgcn_readfirstlane(n.whole);
-                const int then = __builtin_amdgcn_readfirstlane(n.part) ? __builtin_amdgcn_readfirstlane(n.idle) - 1 : -1;
-                const int more = j < whole ? all : j == whole ? then : -1;
-                if (more && j < f.width && in_cache(f, old[u])) atomicAdd(&c.rest[old[u]], more);
-            }
+        for (int u = 0; u < AT_ONCE; u++) {
+            if (i0 + u * BLOCK >= entries) break;
+            const int i = min(i0 + u * BLOCK + tid, entries - 1), row = (int)over((unsigned)i, by, (unsigned)f.width), j = i - row * f.width;
+            const Children n = children[row];
+            const int more = (j < n.whole ? n.all : j == n.whole && n.part ? n.idle : 0) - 1;
+            if (more && i0 + u * BLOCK + tid < entries && in_cache(f, old[u])) atomicAdd(&c.rest[old[u]], more);
         }
+    }
     lds_barrier();
     assign<true>(f, c, [&](int row) { return plans[row]; }, needs, list, parts);
 }
@@ -546,7 +574,8 @@ hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st)
         const size_t lds = fork_block_lds(f.pages, f.rows_from, f.rows);
         if (lds > 60 << 10)
             if (hipError_t e = hipFuncSetAttribute((const void *)fork_block_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-        hipLaunchKernelGGL(fork_block_kernel, dim3((unsigned)(1 + (f.rows + BLOCK / 64 - 1) / (BLOCK / 64))), dim3(BLOCK), lds, st, f);
+        hipLaunchKernelGGL(fork_block_kernel, dim3((unsigned)(1 + (f.rows + BLOCK / 64 - 1) / (BLOCK / 64))), dim3(BLOCK), lds, st, f,
+                           divisor((unsigned long long)f.rows_from * f.width, f.width));
         return hipGetLastError();
     }
     char *at = static_cast<char *>(ws);
