@@ -119,13 +119,14 @@ int check_pages(int32_t pages)
     return SAMP_OK;
 }
 
-int check_choice(int32_t width, int32_t page_len, int32_t max_new, int32_t keep, int32_t sinks, int32_t recent)
+int check_choice(int32_t batch, int32_t kv_heads, int32_t width, int32_t page_len, int32_t max_new, int32_t keep, int32_t sinks, int32_t recent)
 {
     if (width > SAMP_MAX_TABLE) return fail(SAMP_ERR_SHAPE, "pages are chosen from at most %d of a sequence (width %d)", SAMP_MAX_TABLE, width);
     const long need = ((long)max_new + page_len - 2) / page_len + 1;
     if (sinks < 0 || recent < need || keep < 1 || (long)sinks + recent > keep)
         return fail(SAMP_ERR_SHAPE, "sinks >= 0, recent >= %ld for max_new %d, and sinks + recent <= keep are needed (%d, %d, %d)", need, max_new, sinks, recent, keep);
     if (keep > SAMP_MAX_TABLE) return fail(SAMP_ERR_SHAPE, "keep is at most %d (%d)", SAMP_MAX_TABLE, keep);
+    if ((double)batch * kv_heads * (width / 64 + 1) > 2147483647.0) return fail(SAMP_ERR_SHAPE, "batch x key heads x pages is past 2^37");
     return SAMP_OK;
 }
 
@@ -377,7 +378,7 @@ int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t head
     if (int rc = check_kv_rows(r, "max_new")) return rc;
     if (int rc = check_heads(heads, c.kv_heads, 1.0f)) return rc;
     if (int rc = check_rows("q", q, ldq, (int64_t)heads * cache->head_dim)) return rc;
-    if (int rc = check_choice(width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
+    if (int rc = check_choice(batch, c.kv_heads, width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
     if (!tables || !lens_out) return fail(SAMP_ERR_ARG, "NULL pointer");
     if (lens == lens_out) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
     if (int rc = check_workspace(workspace, workspace_bytes, samp_cache_select_workspace_bytes(batch, c.kv_heads, width))) return rc;
@@ -417,7 +418,7 @@ int samp_attention_sparse(const uint16_t *q, int64_t ldq, int32_t type, int32_t 
     if (int rc = check_bounds(bounds, &kb)) return rc;
     if (int rc = check_kv_rows(r, "max_new")) return rc;
     if (int rc = check_heads(heads, c.kv_heads, scale)) return rc;
-    if (int rc = check_choice(width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
+    if (int rc = check_choice(batch, c.kv_heads, width, cache->page_len, r.max_rows, keep, sinks, recent)) return rc;
     max_len = chosen_len(max_len, keep, cache->page_len);
     Cut cut;
     if (int rc = check_cached(rows, batch, heads, c.kv_heads, cache->head_dim, max_new, max_len, &cut)) return rc;

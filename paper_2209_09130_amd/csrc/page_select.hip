@@ -153,9 +153,10 @@ struct Scored { unsigned score; int page; };
 // What scores are made with: a sequence, a key head, its table and the queries that see it
 struct Seen { SeqRows s; int b, head, group, pages, sinks, recent; const int *table; };
 
-// The scores of the pages first .. first + 63 of a sequence, a page a lane of the wave: f(page of the lane, whether it is the first time, score), again for every sixteen rows of queries.  All waves
-// of the block, four, call it together.  entry: the table's of the lane's page.  A wave requests the bounds of its pages together: 16 of them are the columns of a product, 16 rows of queries its rows.
-template <bool BF, int D, class F>
+// The scores of the pages first .. first + 16 TILES - 1 of a sequence, a page a lane of the wave: f(page of the lane, whether it is the first time, score), again for every sixteen rows of queries.  All
+// waves of the block, four, call it together.  entry: the table's of the lane's page.  A wave requests the bounds of its pages together: 16 of them are the columns of a product, 16 rows of
+// queries its rows.
+template <bool BF, int D, int TILES, class F>
 __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq, const KvCache &c, const KeyBounds &bounds, const Seen &seen, int first, int entry, F &&f)
 {
     constexpr int STEPS = 2 * D / 64;                                 // products of 64 codes
@@ -179,9 +180,9 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
         }
         const bool ok = (unsigned)entry < (unsigned)c.pages;
         const float page_step = bounds.steps[(size_t)(ok ? entry : 0) * c.kv_heads + seen.head];
-        v4i bf[4][STEPS];
+        v4i bf[TILES][STEPS];
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
+        for (int t = 0; t < TILES; t++) {
             const int e = __shfl(ok ? entry : 0, 16 * t + r, 64);
             const int8_t *from = bounds.codes + ((size_t)e * c.kv_heads + seen.head) * (2 * D) + 16 * g;
 #pragma unroll
@@ -213,7 +214,7 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
         const v4f qs = *reinterpret_cast<const v4f *>(&steps[4 * g]);
         unsigned mine = 0;
 #pragma unroll
-        for (int t = 0; t < 4; t++) {
+        for (int t = 0; t < TILES; t++) {
             v4i sum = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < STEPS; i++) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[i], bf[t][i], sum, 0, 0, 0);
@@ -229,7 +230,7 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
         const int p = first + lane;
         if (!ok) mine = order_of(-INFINITY);
         if (p < seen.sinks || p >= pages - seen.recent) mine = ALWAYS;
-        if (p < pages) f(p, r0 == 0, mine);
+        if (lane < 16 * TILES && p < pages) f(p, r0 == 0, mine);
     }
 }
 
@@ -240,20 +241,20 @@ __device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &row
     return seen;
 }
 
-// scores [batch, kv_heads, width]; a block has SCORED_TOGETHER pages of a sequence and a key head.  Blocks go to the eight XCDs in turn: the key heads of the same pages have blocks of the same XCD, so
-// that a page's steps, which lie next to each other, come to one L2.
+// scores [batch, kv_heads, width]; a wave has 32 pages of a sequence and a key head.  What bounds it is a chain of dependent loads (lengths and page numbers, bounds) and then HBM: 64 contexts of 900 to 32768 tokens in
+// pages of 64, 8 key heads of 128 (35 MB) 13.2 us, one of 100000 4.3.  (64 pages a wave: 13.5 and 5.4; blocks of the key heads of a page on one XCD, which shares their steps: no difference.)
+constexpr int OF_WAVE = 32;
 template <bool BF, int D>
 __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
                                                           int recent, unsigned *__restrict__ scores)
 {
-    const int of_xcd = blockIdx.x >> 3, head = of_xcd % c.kv_heads, item = of_xcd / c.kv_heads * 8 + (blockIdx.x & 7), chunks = (rows.width + SCORED_TOGETHER - 1) / SCORED_TOGETHER;
-    const int chunk = item / rows.batch, b = item - chunk * rows.batch;
-    if (chunk >= chunks) return;
-    const int page = chunk * SCORED_TOGETHER + threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];          // (on its way with the lengths)
+    const int head = blockIdx.x % c.kv_heads, item = blockIdx.x / c.kv_heads, chunk = item / rows.batch, b = item - chunk * rows.batch;
+    const int first = chunk * 4 * OF_WAVE + __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * OF_WAVE), page = first + (threadIdx.x & 63);
+    const int entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];              // (on its way with the lengths)
     const Seen seen = what_is_seen(c, rows, b, head, group, sinks, recent);
-    if (seen.pages <= keep || chunk * SCORED_TOGETHER >= seen.pages) return;
+    if (seen.pages <= keep || chunk * 4 * OF_WAVE >= seen.pages) return;
     unsigned *const to = scores + ((size_t)b * c.kv_heads + head) * rows.width;
-    score_pages<BF, D>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
+    score_pages<BF, D, OF_WAVE / 16>(Q, ldq, c, bounds, seen, first, page < seen.pages ? entry : -1,
                        [&](int p, bool new_page, unsigned x) { to[p] = new_page ? x : max(to[p], x); });
 }
 
@@ -425,7 +426,7 @@ __global__ __launch_bounds__(256, 4) void select_pages_kernel(const char *__rest
     const int b = blockIdx.x / c.kv_heads, page = threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];
     const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, group, sinks, recent);
     choose_pages(c, rows, seen, keep, tables + (size_t)blockIdx.x * keep, lens_out, [&](unsigned *score) {
-        score_pages<BF, D>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
+        score_pages<BF, D, 4>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
                            [&](int p, bool new_page, unsigned x) { score[p] = new_page ? x : max(score[p], x); });
     });
 }
@@ -462,8 +463,8 @@ hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, co
     }
     if (lds > 40 << 10)
         if (hipError_t e = hipFuncSetAttribute((const void *)select_scored_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-    const unsigned items = (unsigned)((rows.width + SCORED_TOGETHER - 1) / SCORED_TOGETHER) * rows.batch;
-    hipLaunchKernelGGL((page_scores_kernel<BF, D>), dim3((items + 7) / 8 * 8 * c.kv_heads), dim3(256), 0, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent,
+    const unsigned items = (unsigned)((rows.width + 4 * OF_WAVE - 1) / (4 * OF_WAVE)) * rows.batch;
+    hipLaunchKernelGGL((page_scores_kernel<BF, D>), dim3(items * c.kv_heads), dim3(256), 0, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent,
                        scores);
     const int threads = rows.width <= 512 ? 256 : rows.width <= 1024 ? 512 : 1024;
     hipLaunchKernelGGL(select_scored_kernel, grid, dim3(threads), lds, st, c, rows, keep, sinks, recent, scores, tables, lens_out);
