@@ -82,7 +82,7 @@ inline bool compact_in_block(long pages, long entries) { return pages <= 8192 &&
 
 // ---- pages that are read -------------------------------------------------------------------------------
 // The scores of up to 256 pages of a sequence (64 a wave) are formed by the block that chooses among them, those of more in a launch of their own: one CU gets 35 to 50 GB/s of bounds from
-// pages all over memory.  us, one launch / two: sequences x key heads x pages 1 x 8 x 256 7.1 / 9.0, 8 x 8 x 100 6.7 / 8.5, 64 x 8 x 128 8.3 / 10.6, 64 x 8 x 256 11.3 / 12.8; a
+// pages all over memory.  us, one launch / two: sequences x key heads x pages 1 x 8 x 256 7.4 / 9.0, 8 x 8 x 100 5.8 / 8.5, 64 x 8 x 128 7.7 / 10.6, 64 x 8 x 256 11.7 / 12.8; a
 // block of sixteen waves for 1 x 8 x 1563 21 / 11.
 constexpr int SCORED_TOGETHER = 256;
 inline bool scores_apart(int width) { return width > SCORED_TOGETHER; }

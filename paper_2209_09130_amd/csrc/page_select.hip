@@ -144,7 +144,7 @@ template <bool BF> __device__ __forceinline__ float largest(unsigned bits)
 {
     return BF ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)bits);
 }
-constexpr unsigned ALWAYS = 0xffffffffu;                              // above the order of every number
+constexpr unsigned ALWAYS = 0xfffffffeu;                              // above the order of every number, and a number above it
 
 __device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t & 0x80000000u ? t & 0x7fffffffu : ~t); }
 constexpr int BINS = 1024, LIST = 512, WORDS = SAMP_MAX_TABLE / 64;
@@ -258,10 +258,59 @@ __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restr
                        [&](int p, bool new_page, unsigned x) { to[p] = new_page ? x : max(to[p], x); });
 }
 
-// One block: a sequence and a key head.  The scores are counted in BINS steps between the smallest and the largest; the pages of the step in which the `keep`-th largest lies are
-// ranked by counting, and where they are too many (equal scores), that score is found eight bits at a time.  prepare(score): leaves the scores of the thread's pages in LDS.
-template <class F>
-__device__ __forceinline__ void choose_pages(const KvCache &c, const KvRows &rows, const Seen &seen, int keep, int *__restrict__ to, int *__restrict__ lens_out, F &&prepare)
+// Whether a sequence keeps all its pages, which are its table then; and its length without those that it does not keep
+__device__ __forceinline__ bool keeps_all(const KvCache &c, const KvRows &rows, const Seen &seen, int keep, int *__restrict__ to, int *__restrict__ lens_out)
+{
+    if (seen.head == 0 && threadIdx.x == 0) lens_out[seen.b] = rows.lens[seen.b] - ((seen.pages - min(seen.pages, keep)) << c.page_shift);
+    if (seen.pages > keep) return false;
+    for (int i = threadIdx.x; i < keep; i += blockDim.x) to[i] = i < seen.pages ? seen.table[i] : -1;
+    return true;
+}
+
+// Scores formed by the block that chooses, a page a thread: a page is kept if fewer than `keep` come before it.  72 blocks of up to 157 pages 6.5 us; counting steps instead, as below, 7.0.
+template <bool BF, int D>
+__global__ __launch_bounds__(SCORED_TOGETHER, 4) void select_pages_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep,
+                                                                          int sinks, int recent, int *__restrict__ tables, int *__restrict__ lens_out)
+{
+    constexpr int WAVES = SCORED_TOGETHER / 64;
+    __shared__ __attribute__((aligned(16))) unsigned score[SCORED_TOGETHER];
+    __shared__ unsigned long long bits[WAVES];
+    const int b = blockIdx.x / c.kv_heads, page = threadIdx.x, lane = page & 63, w = __builtin_amdgcn_readfirstlane(page >> 6);
+    const int entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];
+    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, group, sinks, recent);
+    int *const to = tables + (size_t)blockIdx.x * keep;
+    if (keeps_all(c, rows, seen, keep, to, lens_out)) return;
+    if (page >= seen.pages) score[page] = 0;
+    score_pages<BF, D, 4>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
+                          [&](int p, bool new_page, unsigned x) { score[p] = new_page ? x : max(score[p], x); });
+    lds_barrier();
+    const unsigned mine = score[page];
+    int better = 0;
+    for (int v = 0; v < WAVES && 64 * v < seen.pages; v++) {
+        const int others = (int)score[64 * v + lane];                 // of 64 pages, each to all lanes in turn
+        // an equal score counts where its page is an earlier one
+        if (v == w) {
+#pragma unroll
+            for (int i = 0; i < 64; i++) better += (unsigned)__builtin_amdgcn_readlane(others, i) >= mine + (i >= lane);
+        } else {
+            const unsigned least = mine + (v > w);
+#pragma unroll
+            for (int i = 0; i < 64; i++) better += (unsigned)__builtin_amdgcn_readlane(others, i) >= least;
+        }
+    }
+    const bool kept = page < seen.pages && better < keep;
+    const unsigned long long word = __ballot(kept);
+    if (lane == 0) bits[w] = word;
+    lds_barrier();
+    int at = __popcll(word & ((1ull << lane) - 1));
+    for (int v = 0; v < w; v++) at += __popcll(bits[v]);
+    if (kept) to[at] = entry;
+}
+
+// Scores that are there already.  They are counted in BINS steps between the smallest and the largest; the pages of the step in which the `keep`-th largest lies are ranked by counting, and
+// where they are too many (equal scores), that score is found eight bits at a time.
+__global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows rows, int keep, int sinks, int recent, const unsigned *__restrict__ scores,
+                                                             int *__restrict__ tables, int *__restrict__ lens_out)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned score[];  // [width]
     __shared__ __attribute__((aligned(16))) int count[BINS];
@@ -269,18 +318,26 @@ __device__ __forceinline__ void choose_pages(const KvCache &c, const KvRows &row
     __shared__ unsigned long long bits[WORDS];
     __shared__ float lows[16], highs[16];
     __shared__ int found[2], listed;                                  // a digit, and how many are above it
-    const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int pages = seen.pages, chosen = min(pages, keep), groups = (pages + 63) >> 6, sinks = seen.sinks, recent = seen.recent;
+    const int b = blockIdx.x / c.kv_heads, step = blockDim.x, tid = threadIdx.x, lane = tid & 63, waves = step >> 6, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned *const from = scores + (size_t)blockIdx.x * rows.width;
+    unsigned x[4];
+#pragma unroll
+    for (int u = 0; u < 4; u++) x[u] = from[min(tid + u * step, rows.width - 1)];              // (on their way with the lengths; what nobody wrote is not used)
+    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, 1, sinks, recent);
+    const int pages = seen.pages, groups = (pages + 63) >> 6;
     const int *const table = seen.table;
-    if (seen.head == 0 && tid == 0) lens_out[seen.b] = rows.lens[seen.b] - ((pages - chosen) << c.page_shift);
-    if (pages <= keep) {
-        for (int i = tid; i < keep; i += blockDim.x) to[i] = i < pages ? table[i] : -1;
-        return;
-    }
-    for (int i = tid; i < BINS; i += blockDim.x) count[i] = 0;
-    for (int i = tid; i < groups; i += blockDim.x) bits[i] = 0;
+    int *const to = tables + (size_t)blockIdx.x * keep;
+    if (keeps_all(c, rows, seen, keep, to, lens_out)) return;
+    for (int i = tid; i < BINS; i += step) count[i] = 0;
+    for (int i = tid; i < groups; i += step) bits[i] = 0;
     if (tid == 0) listed = 0;
-    prepare(score);
+    for (int p0 = tid; p0 < pages; p0 += 4 * step) {
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            if (p0 >= 4 * step) x[u] = from[min(p0 + u * step, pages - 1)];
+            if (p0 + u * step < pages) score[p0 + u * step] = x[u];
+        }
+    }
 
     // steps of the scores that are finite (a thread has the pages whose scores it wrote)
     float low = INFINITY, high = -INFINITY;
@@ -418,38 +475,6 @@ __device__ __forceinline__ void choose_pages(const KvCache &c, const KvRows &row
     }
 }
 
-// The scores formed by the same block, or read
-template <bool BF, int D>
-__global__ __launch_bounds__(256, 4) void select_pages_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
-                                                           int recent, int *__restrict__ tables, int *__restrict__ lens_out)
-{
-    const int b = blockIdx.x / c.kv_heads, page = threadIdx.x, entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];
-    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, group, sinks, recent);
-    choose_pages(c, rows, seen, keep, tables + (size_t)blockIdx.x * keep, lens_out, [&](unsigned *score) {
-        score_pages<BF, D, 4>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
-                           [&](int p, bool new_page, unsigned x) { score[p] = new_page ? x : max(score[p], x); });
-    });
-}
-__global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows rows, int keep, int sinks, int recent, const unsigned *__restrict__ scores,
-                                                             int *__restrict__ tables, int *__restrict__ lens_out)
-{
-    const int b = blockIdx.x / c.kv_heads, step = blockDim.x;
-    const unsigned *const from = scores + (size_t)blockIdx.x * rows.width;
-    unsigned x[4];
-#pragma unroll
-    for (int u = 0; u < 4; u++) x[u] = from[min((int)threadIdx.x + u * step, rows.width - 1)];         // (on their way with the lengths; what nobody wrote is not used)
-    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, 1, sinks, recent);
-    choose_pages(c, rows, seen, keep, tables + (size_t)blockIdx.x * keep, lens_out, [&](unsigned *score) {
-        for (int p0 = threadIdx.x; p0 < seen.pages; p0 += 4 * step) {
-#pragma unroll
-            for (int u = 0; u < 4; u++) {
-                if (p0 >= 4 * step) x[u] = from[min(p0 + u * step, seen.pages - 1)];
-                if (p0 + u * step < seen.pages) score[p0 + u * step] = x[u];
-            }
-        }
-    });
-}
-
 template <bool BF, int D>
 hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, const KeyBounds &bounds, const KvRows &rows, int keep, int sinks, int recent, int *tables,
                         int *lens_out, unsigned *scores, hipStream_t st)
@@ -458,7 +483,7 @@ hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, co
     const int group = heads / c.kv_heads;
     const dim3 grid((unsigned)(rows.batch * c.kv_heads));
     if (!scores_apart(rows.width)) {
-        hipLaunchKernelGGL((select_pages_kernel<BF, D>), grid, dim3(256), lds, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent, tables, lens_out);
+        hipLaunchKernelGGL((select_pages_kernel<BF, D>), grid, dim3(SCORED_TOGETHER), 0, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent, tables, lens_out);
         return hipGetLastError();
     }
     if (lds > 40 << 10)
