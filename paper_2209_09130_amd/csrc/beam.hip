@@ -144,10 +144,10 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
         for (int i = 0; i < VECTORS; i++) asm("" : "+v"(raw[i]));
     };
     again();
-    // exp(x - m) as 2^(x log2(e) - reference), one multiply-add in front of each; the reference is m log2(e) but for its rounding, which the sum makes up for.  Where
-    // that product is past binary32 (logits of the type's lowest value alone) the difference comes first.
+    // exp(x - m) as 2^(x log2(e) - reference), one multiply-add in front of each; the reference is m log2(e) but for its rounding, at most 1, which the sum makes
+    // up for.  Of larger logits (a row of the type's lowest value) the difference comes first.
     float part[4] = {}, sum;
-    if (__builtin_fabsf(m) < 0x1p126f) {
+    if (__builtin_fabsf(m) < 0x1p24f) {
         const float reference = m * LOG2E;
 #pragma unroll
         for (int i = 0; i < VECTORS; i++)

@@ -143,6 +143,29 @@ def test_rows_without_candidates_and_values_at_the_ends(P, dtype):
     assert parents[0].tolist() == [3, 2, 1]
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_logits_of_any_size(P, dtype):
+    """Logits whose product with log2(e) has no fraction left, up to the type's largest: differences decide."""
+    V = 9000
+    x = torch.randn(10, V, generator=gen(1))
+    for r, e in enumerate((20, 23, 24, 25, 30, 40, 80, 120, 125, 126)):
+        x[r] = x[r] * 3 + 2.0 ** e if e < 25 else (x[r].abs().clamp(max=1.9)) * 2.0 ** e
+        x[r, 5:9] = x[r].max()
+    scores = torch.linspace(-3, -1, 10)
+    for sign in (1, -1):
+        check(P, (sign * x).to(dtype), scores, 1, 7)
+        check(P, (sign * x).to(dtype), scores, 5, 9)
+
+
+def test_signalling_nan_spoils_only_its_row(P):
+    for dtype, ints, bits in ((BF16, torch.int16, 0x7f81), (F16, torch.int16, 0x7c01), (F32, torch.int32, 0x7f800001)):
+        x = torch.randn(6, 5000, generator=gen(1)).to(dtype)
+        clean = check(P, x, torch.zeros(6), 1, 4)
+        x.view(ints)[2, 4000] = bits
+        best, parents, tokens = check(P, x, torch.zeros(6), 1, 4)
+        assert (tokens[2] == -1).all() and all(torch.equal(a[[0, 1, 3, 4, 5]], b[[0, 1, 3, 4, 5]]) for a, b in zip(clean, (best, parents, tokens)))
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 def test_rows_in_place_at_any_alignment(P, dtype):
     for V, ld, shift in ((1000, 1016, 3), (4001, 4005, 1), (9000, 9011, 7), (16390, 16391, 0)):
