@@ -139,6 +139,24 @@ def test_fork_of_tables_with_holes_and_pages_behind_the_end(P, pages):
     check_fork(P, refs, table, [40, 33, 40, 0], 16, [0, 0, 0, -1], 20)
 
 
+@pytest.mark.parametrize("pages", [4000, 30000])
+@pytest.mark.parametrize("rows", [1, 17, 70, 1100])
+def test_fork_of_rows_that_write_few_and_many_entries(P, rows, pages):
+    """Rows of one wave go on by nothing, one token, a few pages and most of a table, over pages that others name too."""
+    width, page_len = 40, 16
+    held = [(13 * i) % 90 for i in range(rows)]
+    table, refs = [], [0] * pages
+    for i in range(rows):
+        table.append([(7 * (i // 3) + j) % pages if j < 8 and (i + j) % 11 else -1 for j in range(width)])
+        for p in table[-1]:
+            if p >= 0:
+                refs[p] += 1
+    parents = [min(rows - 1, i // 8 * 8 + (5 * i) % 8) for i in range(rows)]
+    for new in (20, 100, [(0, 1, 20, 70, 500, 3)[(i + i // 16) % 6] for i in range(rows)], [500 if i % 64 == 5 else i % 2 for i in range(rows)]):
+        check_fork(P, refs, table, held, page_len, parents, new)
+        check_fork(P, refs, table, held, page_len, None, new)
+
+
 @pytest.mark.parametrize("pages,rows", [(50, 6), (20000, 6)])
 def test_fork_says_how_many_pages_are_lacking(P, pages, rows):
     refs, table, lens = state(rows, 4, 16, pages, 1)
