@@ -153,23 +153,20 @@ struct Scored { unsigned score; int page; };
 // What scores are made with: a sequence, a key head, its table and the queries that see it
 struct Seen { SeqRows s; int b, head, group, pages, sinks, recent; const int *table; };
 
-// The scores of the pages first .. first + 16 TILES - 1 of a sequence, a page a lane of the wave: f(page of the lane, whether it is the first time, score), again for every sixteen rows of queries.  All
-// waves of the block, four, call it together.  entry: the table's of the lane's page.  A wave requests the bounds of its pages together: 16 of them are the columns of a product, 16 rows of
-// queries its rows.
+// The scores of the pages first .. first + 16 TILES - 1 of a sequence, a page a lane of the wave: f(page of the lane, score).  All waves of the block, four, call it together.  entry: the
+// table's of the lane's page.  A wave requests the bounds of its pages together and keeps them for all rows of queries: 16 of them are the columns of a product, 16 rows of queries, which the
+// block quantises while the bounds or the last product's operands are on their way, its rows.
 template <bool BF, int D, int TILES, class F>
 __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq, const KvCache &c, const KeyBounds &bounds, const Seen &seen, int first, int entry, F &&f)
 {
-    constexpr int STEPS = 2 * D / 64;                                 // products of 64 codes
+    constexpr int STEPS = 2 * D / 64, PER = D / 16;                   // products of 64 codes; values of a lane, sixteen lanes a row of queries
     __shared__ __attribute__((aligned(16))) int8_t codes[16][2 * D];  // positive parts, negative parts of sixteen rows of queries
     __shared__ float steps[16];
-    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4, all = seen.s.todo * seen.group, pages = seen.pages;
-    for (int r0 = 0; r0 < all || r0 == 0; r0 += 16) {
-        if (r0) lds_barrier();
-        // sixteen lanes a row of queries, requested in front of the bounds: loads arrive in their order
-        constexpr int PER = D / 16;
-        const int row = tid >> 4, token = (r0 + row) / seen.group, h = seen.head * seen.group + (r0 + row) - token * seen.group;
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4, all = seen.s.todo * seen.group, pages = seen.pages, row = tid >> 4;
+    auto request = [&](int r0) __attribute__((always_inline)) {
         v4i raw = {0, 0, 0, 0};
         if (r0 + row < all) {
+            const int token = (r0 + row) / seen.group, h = seen.head * seen.group + (r0 + row) - token * seen.group;
             const char *from = Q + 2 * ((size_t)(seen.s.first_row + token) * ldq + h * D + r * PER);
             if constexpr (PER == 8) raw = *reinterpret_cast<const v4i *>(from);
             else {
@@ -178,21 +175,29 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
                 raw[1] = half[1];
             }
         }
-        const bool ok = (unsigned)entry < (unsigned)c.pages;
-        const float page_step = bounds.steps[(size_t)(ok ? entry : 0) * c.kv_heads + seen.head];
-        v4i bf[TILES][STEPS];
+        return raw;
+    };
+    v4i raw = request(0);                                             // in front of the bounds: loads arrive in their order
+    const bool ok = (unsigned)entry < (unsigned)c.pages;
+    const float page_step = bounds.steps[(size_t)(ok ? entry : 0) * c.kv_heads + seen.head];
+    v4i bf[TILES][STEPS];
 #pragma unroll
-        for (int t = 0; t < TILES; t++) {
-            const int e = __shfl(ok ? entry : 0, 16 * t + r, 64);
-            const int8_t *from = bounds.codes + ((size_t)e * c.kv_heads + seen.head) * (2 * D) + 16 * g;
+    for (int t = 0; t < TILES; t++) {
+        const int e = __shfl(ok ? entry : 0, 16 * t + r, 64);
+        const int8_t *from = bounds.codes + ((size_t)e * c.kv_heads + seen.head) * (2 * D) + 16 * g;
 #pragma unroll
-            for (int i = 0; i < STEPS; i++) bf[t][i] = *reinterpret_cast<const v4i *>(from + 64 * i);
-        }
+        for (int i = 0; i < STEPS; i++) bf[t][i] = *reinterpret_cast<const v4i *>(from + 64 * i);
+    }
+    unsigned best[TILES];                                             // of the lane's rows of queries
+#pragma unroll
+    for (int t = 0; t < TILES; t++) best[t] = 0;
+    for (int r0 = 0; r0 < all; r0 += 16) {
         const unsigned top = max_of_16_lanes(bits_max16(raw));
         const RowQuant q = row_quant<BF>(top);
         float x[8];
         widen8<BF>(raw, x);
         const v2i code = quant8(x, q);
+        if (r0) lds_barrier();
 #pragma unroll
         for (int i = 0; i < PER / 4; i++) {
             int pos = 0, neg = 0;
@@ -207,31 +212,34 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
         }
         // (the product is the definition's step; the quantiser's own is the quotient)
         if (r == 0) steps[row] = !q.finite || q.hi == 0.0f ? q.step : largest<BF>(top) * INV_127;
+        raw = request(r0 + 16);
         lds_barrier();
         v4i qf[STEPS];
 #pragma unroll
         for (int i = 0; i < STEPS; i++) qf[i] = *reinterpret_cast<const v4i *>(&codes[r][64 * i + 16 * g]);
         const v4f qs = *reinterpret_cast<const v4f *>(&steps[4 * g]);
-        unsigned mine = 0;
 #pragma unroll
         for (int t = 0; t < TILES; t++) {
             v4i sum = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < STEPS; i++) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(qf[i], bf[t][i], sum, 0, 0, 0);
             const float s = __shfl(page_step, 16 * t + r, 64);
-            unsigned best = 0;
 #pragma unroll
             for (int e = 0; e < 4; e++)
-                if (r0 + 4 * g + e < all) best = max(best, order_of((float)sum[e] * (qs[e] * s)));
-            best = max(best, (unsigned)__shfl_xor((int)best, 16, 64));
-            best = max(best, (unsigned)__shfl_xor((int)best, 32, 64));
-            if (g == t) mine = best;
+                if (r0 + 4 * g + e < all) best[t] = max(best[t], order_of((float)sum[e] * (qs[e] * s)));
         }
-        const int p = first + lane;
-        if (!ok) mine = order_of(-INFINITY);
-        if (p < seen.sinks || p >= pages - seen.recent) mine = ALWAYS;
-        if (lane < 16 * TILES && p < pages) f(p, r0 == 0, mine);
     }
+    unsigned mine = 0;
+#pragma unroll
+    for (int t = 0; t < TILES; t++) {
+        best[t] = max(best[t], (unsigned)__shfl_xor((int)best[t], 16, 64));
+        best[t] = max(best[t], (unsigned)__shfl_xor((int)best[t], 32, 64));
+        if (g == t) mine = best[t];
+    }
+    const int p = first + lane;
+    if (!ok) mine = order_of(-INFINITY);
+    if (p < seen.sinks || p >= pages - seen.recent) mine = ALWAYS;
+    if (lane < 16 * TILES && p < pages) f(p, mine);
 }
 
 __device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &rows, int b, int head, int group, int sinks, int recent)
@@ -242,7 +250,8 @@ __device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &row
 }
 
 // scores [batch, kv_heads, width]; a wave has 32 pages of a sequence and a key head.  What bounds it is a chain of dependent loads (lengths and page numbers, bounds) and then HBM: 64 contexts of 900 to 32768 tokens in
-// pages of 64, 8 key heads of 128 (35 MB) 13.2 us, one of 100000 4.3.  (64 pages a wave: 13.5 and 5.4; blocks of the key heads of a page on one XCD, which shares their steps: no difference.)
+// pages of 64, 8 key heads of 128 (35 MB) 13.0 us, one of 100000 4.3; 25 of 85000 in pages of 32, 4 key heads, 35 rows of queries each (69 MB) 21 us, 37 where the bounds were read
+// again for every sixteen rows.  (64 pages a wave: 13.5 and 5.4; blocks of the key heads of a page on one XCD, which shares their steps: no difference.)
 constexpr int OF_WAVE = 32;
 template <bool BF, int D>
 __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
@@ -255,7 +264,7 @@ __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restr
     if (seen.pages <= keep || chunk * 4 * OF_WAVE >= seen.pages) return;
     unsigned *const to = scores + ((size_t)b * c.kv_heads + head) * rows.width;
     score_pages<BF, D, OF_WAVE / 16>(Q, ldq, c, bounds, seen, first, page < seen.pages ? entry : -1,
-                       [&](int p, bool new_page, unsigned x) { to[p] = new_page ? x : max(to[p], x); });
+                       [&](int p, unsigned x) { to[p] = x; });
 }
 
 // Whether a sequence keeps all its pages, which are its table then; and its length without those that it does not keep
@@ -282,7 +291,7 @@ __global__ __launch_bounds__(SCORED_TOGETHER, 4) void select_pages_kernel(const 
     if (keeps_all(c, rows, seen, keep, to, lens_out)) return;
     if (page >= seen.pages) score[page] = 0;
     score_pages<BF, D, 4>(Q, ldq, c, bounds, seen, __builtin_amdgcn_readfirstlane(page & ~63), page < seen.pages ? entry : -1,
-                          [&](int p, bool new_page, unsigned x) { score[p] = new_page ? x : max(score[p], x); });
+                          [&](int p, unsigned x) { score[p] = x; });
     lds_barrier();
     const unsigned mine = score[page];
     int better = 0;
