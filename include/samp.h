@@ -12,7 +12,8 @@
  * is int8; dequantise + bias + residual + LayerNorm + quantise are one kernel;
  * the softmax output is quantised (Section 4.2, Appendix B); the last kernel of
  * a layer emits floating point when its consumer is not quantised.
- * The last section holds the operators of an 8-bit decoder's attention block.
+ * The last two sections hold the operators of an 8-bit decoder's attention block, and those of
+ * beam search and long contexts over its paged cache.
  *
  * Conventions
  *   - All `dev` pointers are device memory of the current HIP device, owned by
@@ -497,7 +498,7 @@ SAMP_API int samp_attention_causal(const uint16_t *q, int64_t ldq, const uint16_
 /* ---- beam search and long contexts over the paged cache ------------------------------------------------
  * Beside the operators above, on the same cache and page tables: the best continuations of beams, the bookkeeping of pages on the device, bounds of the
  * keys of a page, and attention over the pages whose bounds promise most.  What is a choice (of candidates, of pages) is decided on numbers that do not
- * depend on the order of sums or on how the work is cut.                                                     */
+ * depend on the order of sums or on how the work is cut.  Results overlap neither arguments nor each other, except the caches and bounds that a call is to change.  */
 enum { SAMP_TYPE_F32 = 2 };                /* logits only */
 #define SAMP_MAX_BEAMS 64
 #define SAMP_MAX_KEEP 64
@@ -513,7 +514,7 @@ enum { SAMP_TYPE_F32 = 2 };                /* logits only */
  * larger logit, then the lower token.  A total of minus infinity is no candidate; neither are those of a row whose score is
  * not finite, or whose logits hold NaN or plus infinity.
  * best dev float [batch, keep]: the totals; parents dev int32: rows; tokens dev int32.  Behind the last candidate: minus infinity, -1, -1.
- * beams <= SAMP_MAX_BEAMS, keep <= SAMP_MAX_KEEP, vocab <= SAMP_MAX_VOCAB, batch as ever (8192).  workspace as in samp_linear_i8_tokens.        */
+ * beams <= SAMP_MAX_BEAMS, keep <= SAMP_MAX_KEEP, vocab <= SAMP_MAX_VOCAB, 1 to 8192 sequences.  workspace as in samp_linear_i8_tokens.        */
 SAMP_API size_t samp_beam_select_workspace_bytes(int32_t type, int32_t batch, int32_t beams, int32_t vocab, int32_t keep);
 SAMP_API int samp_beam_select(const void *logits, int64_t ld, int32_t type, const float *scores, const uint8_t *finished, int32_t end, int32_t batch,
                               int32_t beams, int32_t vocab, int32_t keep, float *best, int32_t *parents, int32_t *tokens, void *workspace,

@@ -1,7 +1,8 @@
 """ctypes binding of the decoder's entry points in include/samp.h (same names, argument marshalling only).
 
 Every call runs on the current stream of its tensors' device, allocates its output (and workspace, where the C entry takes one) from
-torch's allocator, and raises SampError for what the library refuses.  Activations are fp16 or bfloat16 tensors on the GPU.
+torch's allocator, and raises SampError for what the library refuses.  Activations are fp16 or bfloat16 tensors on the GPU (logits float32 too).  Results of one
+call may be parts of one allocation.
 """
 from __future__ import annotations
 
