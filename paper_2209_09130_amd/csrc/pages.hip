@@ -146,7 +146,7 @@ template <bool LDS, class List, class Plan>
 __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Plan &&plan, int *needs, List *list, int (*parts)[BLOCK / 64])
 {
     const int tid = threadIdx.x, lane = tid & 63;
-    int wide = 0;
+    int wide = 0, wide_high = 0;                                      // (8192 rows lack up to 2^28 each)
     each_row(f, plan, [&](int row, const RowPlan &r) {
         int n = row >= 0 && r.first < r.end && !stays(c, r.page, row * f.width + r.first);
         later_entries(f, row, r, [&](int owner, bool there, int place, int page) __attribute__((always_inline)) {
@@ -156,7 +156,8 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
         });
         if (row >= 0) {
             needs[row] = n;
-            wide += r.wide;
+            wide += r.wide & 0xffff;
+            wide_high += r.wide >> 16;
         }
     });
     // (a thread has some neighbouring pages, and some neighbouring rows; of counters in LDS at most PAGES, which it keeps)
@@ -186,9 +187,9 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
     const int rows_per = (f.rows + BLOCK - 1) / BLOCK, row0 = tid * rows_per, row1 = min(row0 + rows_per, f.rows);
     int sum = 0;
     for (int i = row0; i < row1; i++) sum += needs[i];
-    const int v[3] = {sum, mine, wide};
-    int before[3], all[3];
-    block_scan<BLOCK / 64, 3>(v, parts, before, all);
+    const int v[4] = {sum, mine, wide, wide_high};
+    int before[4], all[4];
+    block_scan<BLOCK / 64, 4>(v, parts, before, all);
     const int wanted = all[0], free_pages = all[1];
     int rank = before[0];
     for (int i = row0; i < row1; i++) {
@@ -222,7 +223,7 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
             count_of(i, c.rest[i], c.rest[i] == 0 && !is_written, is_written);
         }
     }
-    if (tid == 0) f.lacking[0] = max(wanted - free_pages, 0) + all[2];
+    if (tid == 0) f.lacking[0] = (int)min(max(wanted - free_pages, 0) + all[2] + ((long)all[3] << 16), (long)NONE);
     barrier<LDS>();
     each_row(f, plan, [&](int row, const RowPlan &r) {
         int rank = row >= 0 ? needs[row] : 0;
@@ -280,7 +281,7 @@ __device__ __forceinline__ void copy_row(const PageFork &f, int row, int lane)
 __global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f, unsigned by)
 {
     extern __shared__ __attribute__((aligned(16))) char shared[];
-    __shared__ int parts[3][BLOCK / 64];
+    __shared__ int parts[4][BLOCK / 64];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     constexpr int WAVES = BLOCK / 64;
     if (blockIdx.x) {
@@ -372,7 +373,7 @@ __global__ __launch_bounds__(256) void fork_count_kernel(PageFork f, Counters c)
 }
 __global__ __launch_bounds__(BLOCK) void fork_assign_kernel(PageFork f, Counters c, int *needs, int *list)
 {
-    __shared__ int parts[3][BLOCK / 64];
+    __shared__ int parts[4][BLOCK / 64];
     auto plan = [&](int row) {
         RowPlan r = row_plan(f, row);
         r.page = r.first < r.end ? child_page(f, r, r.first) : -1;

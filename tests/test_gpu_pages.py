@@ -168,6 +168,11 @@ def test_fork_says_how_many_pages_are_lacking(P, pages, rows):
     # the largest numbers that an int32 holds
     got = P.pages_fork(ints(refs).cuda(), ints(table).cuda(), ints([2 ** 31 - 1] * rows).cuda(), 16, None, offsets([2 ** 31 - 1] + [0] * (rows - 1)).cuda())
     assert got[2].tolist() == [2 ** 31 - 1] * rows and int(got[4]) > 0
+    # sums of such numbers, and one past an int32
+    width = 5
+    for n in (1, 15, 16, 40):
+        got = P.pages_fork(ints([0] * pages).cuda(), torch.full((n, width), -1, dtype=torch.int32, device="cuda"), ints([0] * n).cuda(), 16, None, None, 2 ** 31 - 1)
+        assert int(got[4]) == min(2 ** 31 - 1, max(n * width - pages, 0) + n * (2 ** 27 - width)) and got[2].tolist() == [2 ** 31 - 1] * n
     # counts that are not the tables': no access outside the buffers, every entry a page or -1
     got = P.pages_fork(ints([0] * pages).cuda(), ints(table).cuda(), ints(lens).cuda(), 16, ints([0] * rows).cuda(), None, 33)
     assert ((got[1] >= -1) & (got[1] < pages)).all()
