@@ -362,7 +362,7 @@ def beam_select(logits: torch.Tensor, scores: torch.Tensor, beams: int, keep: Op
 
 def _parts(like: torch.Tensor, sizes: Tuple[int, ...]) -> Tuple[torch.Tensor, ...]:
     """Flat results in one allocation (an allocation and a view take about as long as a call's checks)."""
-    return torch.split_with_sizes(like.new_empty(sum(sizes)), sizes)
+    return torch.unsafe_split_with_sizes(like.new_empty(sum(sizes)), sizes)          # (views that autograd does not follow: 1.3 us for 1.7)
 
 
 def _table(table: torch.Tensor, device: int) -> Tuple[int, int, int]:
