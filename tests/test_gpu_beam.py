@@ -176,6 +176,16 @@ def test_rows_in_place_at_any_alignment(P, dtype):
         check(P, base[:, shift:shift + V], -torch.rand(6, generator=gen(2)), 3, 6, device=view)
 
 
+def test_rows_further_apart_than_32_bits(P):
+    rows, V, ld = 600, 5000, 1 << 22                         # 2^22 values between rows is the most: 4.7 GiB
+    base = torch.empty(rows * ld, dtype=F16, device="cuda").view(rows, ld)
+    x = torch.randn(rows, V, generator=gen(3)).half()
+    base[:, :V] = x.cuda()
+    scores = -torch.rand(rows, generator=gen(4))
+    got, want = (P.beam_select(t, scores.cuda(), 2, 5) for t in (base[:, :V], x.cuda()))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("keep", [16, 64])
 def test_long_pieces_of_every_kind_of_row(P, dtype, keep):

@@ -211,6 +211,26 @@ def test_pages_compact(P, pages):
         assert torch.equal(a.cpu().flatten(), ints(b).flatten())
 
 
+def test_bookkeeping_of_the_most_pages(P):
+    pages = 1 << 26
+    refs = (torch.rand(pages, device="cuda") < 0.3).int() * torch.randint(1, 5, (pages,), dtype=torch.int32, device="cuda")
+    used = refs.nonzero().flatten().int()
+    n = used.numel()
+    refs_out, table_out, copies, count = P.pages_compact(refs, used, 16)
+    stay = int((used < n).sum())
+    assert int(count) == n and not refs_out[n:].any() and torch.equal(refs_out[table_out.long()], refs[used.long()])
+    assert torch.equal(table_out[:stay], used[:stay]) and torch.equal(copies[0, : n - stay], used[stay:]) and torch.equal(copies[1, : n - stay], table_out[stay:])
+    assert torch.equal(copies[1, : n - stay], (refs[:n] == 0).nonzero().flatten().int()) and (copies[:2, n - stay:] == -1).all() and not copies[2, n - stay:].any()
+    # two rows of 3 million entries, which go on into as many free pages
+    width = 3_000_000
+    table = torch.full((2, width), -1, dtype=torch.int32, device="cuda")
+    fresh, out, lens, _, lacking = P.pages_fork(refs, table, ints([0, 0]).cuda(), 16, None, None, 16 * width)
+    assert torch.equal(out.flatten(), (refs == 0).nonzero().flatten()[: 2 * width].int()) and lens.tolist() == [16 * width] * 2 and int(lacking) == 0
+    want = refs.clone()
+    want[out.flatten().long()] = 1
+    assert torch.equal(fresh, want)
+
+
 @pytest.mark.parametrize("G,D,page", [(1, 64, 16), (12, 64, 32), (8, 128, 64), (3, 128, 1024), (2, 64, 256)])
 def test_cache_copy(P, G, D, page):
     pages, g = 21, gen(D + page)

@@ -213,6 +213,26 @@ def test_pages_of_one_score_and_scores_that_are_not_numbers(P):
         assert want[1] == [0, 1, 2, 3, 48, 49] if bad else 20 in want[1]               # (all of them the highest: the first ones)
 
 
+def test_caches_and_bounds_past_32_bits(P):
+    """The same pages at the two ends of a cache whose bounds are past 2^31 bytes: what is written there, chosen and read is the same."""
+    G, H, D, page, pages = 8, 16, 128, 16, (1 << 20) + 600
+    cache = P.KVCache.empty(pages, G, page, D)
+    bounds = P.KeyBounds.empty(cache)
+    assert bounds.codes.numel() > 1 << 31
+    for n in (20, 290):                                      # pages of a sequence: scores formed by the block that chooses, and apart
+        low = torch.arange(n, dtype=torch.int32, device="cuda")
+        table, lens = torch.stack([low, pages - 1 - low]), torch.tensor([16 * n, 16 * n], dtype=torch.int32, device="cuda")
+        k, v = (torch.randn(16 * n, G, D, generator=gen(n + i)).half().cuda().repeat(2, 1, 1) for i in (0, 1))
+        P.cache_write(cache, k, v, table, None, lens, 16 * n)
+        P.cache_bounds(cache, bounds, table, None, lens, 16 * n)
+        assert torch.equal(bounds.codes[table[0]], bounds.codes[table[1]]) and torch.equal(bounds.steps[table[0]], bounds.steps[table[1]]) and bounds.codes[pages - n].any()
+        q = torch.randn(1, H, D, generator=gen(n)).half().cuda().repeat(2, 1, 1)
+        chosen, _ = P.cache_select(q, cache, bounds, table, None, lens, 1, 7)
+        assert torch.equal(chosen[0], pages - 1 - chosen[1]) and (chosen[0].sort().values == chosen[0]).all()
+        o = P.attention_sparse(q, cache, bounds, table, None, lens, 1, 7)
+        assert torch.equal(o[0], o[1]) and o.abs().sum() > 0
+
+
 def test_sequences_without_positions_or_new_tokens(P):
     plan = Plan(P, [0, 700, 3], [0, 0, 3], 2, 64, 16)
     plan.fill(P, F16, 3)
