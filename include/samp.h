@@ -531,7 +531,7 @@ SAMP_API int samp_beam_select(const void *logits, int64_t ld, int32_t type, cons
  *     which every cache that the table is for has to be given before its next positions are written.
  *   - lens_out dev int32 [rows]: the next positions counted, as samp_cache_write wants them; 0 for an empty row.
  *   - lacking dev int32 [1]: pages that were not there, free ones or entries of the table (2^31 - 1 where more); an entry that lacks one is -1.
- * page_len a power of two from 16 to 1024, rows and rows_from 1 to 8192, rows * width and rows_from * width < 2^31.  refs that are not what the tables name give tables that nobody can use, but no access outside the
+ * page_len a power of two from 16 to 1024, rows and rows_from 1 to 8192, rows * width and rows_from * width <= 2^30.  refs that are not what the tables name give tables that nobody can use, but no access outside the
  * buffers.  workspace as in samp_linear_i8_tokens.                                                            */
 SAMP_API size_t samp_pages_fork_workspace_bytes(int32_t pages, int32_t rows_from, int32_t width, int32_t rows);
 SAMP_API int samp_pages_fork(const int32_t *refs, int32_t pages, const int32_t *table, const int32_t *lens, int32_t rows_from, int32_t width, int32_t page_len,

@@ -307,7 +307,7 @@ int samp_pages_fork(const int32_t *refs, int32_t pages, const int32_t *table, co
     if (!refs || !table || !lens || !refs_out || !table_out || !lens_out || !copies || !lacking) return fail(SAMP_ERR_ARG, "NULL pointer");
     if (rows < 1 || rows > SAMP_MAX_BATCH || rows_from < 1 || rows_from > SAMP_MAX_BATCH || width < 1 || (!cu && max_new < 0))
         return fail(SAMP_ERR_SHAPE, "1 to %d rows, a table width of at least 1 and max_new >= 0 are needed (%d, %d, %d, %d)", SAMP_MAX_BATCH, rows, rows_from, width, max_new);
-    if ((long long)rows * width > INT32_MAX || (long long)rows_from * width > INT32_MAX) return fail(SAMP_ERR_SHAPE, "a table has less than 2^31 entries");
+    if ((long long)rows * width > 1 << 30 || (long long)rows_from * width > 1 << 30) return fail(SAMP_ERR_SHAPE, "a table has at most 2^30 entries");
     if (refs == refs_out || table == table_out || lens == lens_out) return fail(SAMP_ERR_ARG, "results must not overlap inputs");
     if (int rc = check_workspace(workspace, workspace_bytes, samp_pages_fork_workspace_bytes(pages, rows_from, width, rows))) return rc;
     const PageFork f{refs, table, lens, parents, cu, pages, rows_from, width, shift_of(page_len), max_new, rows, refs_out, table_out, lens_out, copies, lacking};

@@ -72,11 +72,12 @@ inline bool long_pieces(bool wide, int rows, int vocab) { return (long)rows * pi
 
 // ---- bookkeeping of pages ------------------------------------------------------------------------------
 // One block does a whole call where its counters fit the LDS of a CU (two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 bytes for each
-// old one; 6 bytes for each page) and its 16 waves are no slower than the launches of several.  us in a chain of calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 5.3 / 8.6,
-// 4000 x 256 x 40 9.6 / 13.6, 13000 x 256 x 64 16.7 / 27.5, 12000 x 64 x 512 17.4 / 26.1, 8000 x 1800 x 16 34.2 / 34.2, 9000 x 1024 x 64 28.4 / 23.8; compacted, pages, 300 2.9 / 8.2,
+// old one; 6 bytes for each page) and its 16 waves are no slower than the launches of several.  us in a chain of calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 5.4 / 13.6,
+// 4000 x 256 x 40 9.6 / 15.6, 14000 x 64 x 64 13.8 / 15.7, 13000 x 256 x 64 16.7 / 15.6, 12000 x 64 x 512 17.3 / 15.4, 6000 x 1024 x 32 21.1 / 16.8, 9000 x 1024 x 64 28.4 / 17.3
+// (from the host four more launches cost another 10 us, so draws go to one block); compacted, pages, 300 2.9 / 8.2,
 // 4096 4.9 / 10.2, 8192 10.9 / 11.3, 16384 24.8 / 13.9.
 inline long fork_block_lds(long pages, long rows_from, long rows) { return 10 * ((pages + 3) & ~3l) + 16 * rows_from + (32 + 4) * rows; }
-inline bool fork_in_block(long pages, long rows_from, long width, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10 && rows_from * width <= 49152; }
+inline bool fork_in_block(long pages, long rows_from, long width, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10 && rows_from * width <= 32768; }
 inline long compact_block_lds(long pages) { return 4 * pages + 2 * (pages / 2 + 1); }
 inline bool compact_in_block(long pages, long entries) { return pages <= 8192 && entries <= 65536; }
 

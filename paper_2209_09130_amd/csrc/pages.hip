@@ -13,12 +13,6 @@ namespace {
 
 constexpr int BLOCK = 1024, NONE = 0x7fffffff;
 
-template <bool LDS> __device__ __forceinline__ void barrier()
-{
-    if constexpr (LDS) lds_barrier();
-    else __syncthreads();
-}
-
 // the sums of the values of the threads before this one, and of all, N of them at a time; `parts` holds a value for each wave
 template <int WAVES, int N>
 __device__ __forceinline__ void block_scan(const int (&v)[N], int (*parts)[WAVES], int (&before)[N], int (&all)[N])
@@ -140,10 +134,10 @@ __device__ __forceinline__ void count_writers(const PageFork &f, const Counters 
     });
 }
 
-// Needs of the rows (in `needs`, which becomes their ranks), free pages in order, counts, entries.  plan(row): its RowPlan; list: the free pages, as many as were asked for or as
-// there are.  LDS: needs and list lie there.
-template <bool LDS, class List, class Plan>
-__device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Plan &&plan, int *needs, List *list, int (*parts)[BLOCK / 64])
+// One block, everything in LDS.  Needs of the rows (in `needs`, which becomes their ranks), free pages in order, counts, entries.  plan(row): its RowPlan; list: the free pages, as many as
+// were asked for or as there are.
+template <class Plan>
+__device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Plan &&plan, int *needs, unsigned short *list, int (*parts)[BLOCK / 64])
 {
     const int tid = threadIdx.x, lane = tid & 63;
     int wide = 0, wide_high = 0;                                      // (8192 rows lack up to 2^28 each)
@@ -160,34 +154,28 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
             wide_high += r.wide >> 16;
         }
     });
-    // (a thread has some neighbouring pages, and some neighbouring rows; of counters in LDS at most PAGES, which it keeps)
+    // (a thread has some neighbouring pages, at most PAGES, whose counters it keeps, and some neighbouring rows)
     constexpr int PAGES = 16;
-    const int per = LDS ? ((f.pages + BLOCK - 1) / BLOCK + 3) & ~3 : (f.pages + BLOCK - 1) / BLOCK;
-    const long at = (long)tid * per, end = min(at + per, (long)f.pages);
-    int mine = 0, rest[PAGES];
-    unsigned is_free = 0, written = 0;                                // bits of the pages that are kept
-    if constexpr (LDS) {
+    const int per = ((f.pages + BLOCK - 1) / BLOCK + 3) & ~3;
+    const int at = tid * per, end = min(at + per, f.pages);
+    int rest[PAGES];
+    unsigned is_free = 0, written = 0;                                // bits of the pages
 #pragma unroll
-        for (int q = 0; q < PAGES; q += 4)
-            if (q < per && at + q < end) {                            // (the counters of four pages at a time, some of them behind the last page's)
-                const v4i r = *reinterpret_cast<const v4i *>(&c.rest[at + q]), w = *reinterpret_cast<const v4i *>(&c.first[at + q]);
+    for (int q = 0; q < PAGES; q += 4)
+        if (q < per && at + q < end) {                                // (the counters of four pages at a time, some of them behind the last page's)
+            const v4i r = *reinterpret_cast<const v4i *>(&c.rest[at + q]), w = *reinterpret_cast<const v4i *>(&c.first[at + q]);
 #pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    rest[q + e] = r[e];
-                    written |= (unsigned)(w[e] != NONE) << (q + e);
-                    is_free |= (unsigned)(r[e] == 0 && w[e] == NONE && at + q + e < end) << (q + e);
-                }
+            for (int e = 0; e < 4; e++) {
+                rest[q + e] = r[e];
+                written |= (unsigned)(w[e] != NONE) << (q + e);
+                is_free |= (unsigned)(r[e] == 0 && w[e] == NONE && at + q + e < end) << (q + e);
             }
-        mine = __popc(is_free);
-    } else {
-#pragma unroll 4
-        for (long i = at; i < end; i++) mine += c.rest[i] == 0 && c.first[i] == NONE;
-    }
-    barrier<LDS>();
+        }
+    lds_barrier();
     const int rows_per = (f.rows + BLOCK - 1) / BLOCK, row0 = tid * rows_per, row1 = min(row0 + rows_per, f.rows);
     int sum = 0;
     for (int i = row0; i < row1; i++) sum += needs[i];
-    const int v[4] = {sum, mine, wide, wide_high};
+    const int v[4] = {sum, (int)__popc(is_free), wide, wide_high};
     int before[4], all[4];
     block_scan<BLOCK / 64, 4>(v, parts, before, all);
     const int wanted = all[0], free_pages = all[1];
@@ -198,33 +186,25 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
         rank += n;
     }
     rank = before[1];
-    auto count_of = [&](long page, int n, bool free_page, bool is_written) {
-        if (free_page) {
-            if (rank < wanted) {
-                list[rank] = (List)page;
-                n = 1;
-            }
-            rank++;
-        } else if (n == 0 && is_written) n = 1;                       // the first of its writers
-        f.refs_out[page] = n;
-    };
-    if constexpr (LDS) {
 #pragma unroll
-        for (int q = 0; q < PAGES; q += 4) {
-            if (q >= per) break;
+    for (int q = 0; q < PAGES; q += 4) {
+        if (q >= per) break;
 #pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (at + q + e < end) count_of(at + q + e, rest[q + e], is_free >> (q + e) & 1, written >> (q + e) & 1);
-        }
-    } else {
-#pragma unroll 4
-        for (long i = at; i < end; i++) {
-            const bool is_written = c.first[i] != NONE;
-            count_of(i, c.rest[i], c.rest[i] == 0 && !is_written, is_written);
+        for (int e = q; e < q + 4; e++) {
+            if (at + e >= end) continue;
+            int n = rest[e];
+            if (is_free >> e & 1) {
+                if (rank < wanted) {
+                    list[rank] = (unsigned short)(at + e);
+                    n = 1;
+                }
+                rank++;
+            } else if (n == 0 && (written >> e & 1)) n = 1;           // the first of its writers
+            f.refs_out[at + e] = n;
         }
     }
     if (tid == 0) f.lacking[0] = (int)min(max(wanted - free_pages, 0) + all[2] + ((long)all[3] << 16), (long)NONE);
-    barrier<LDS>();
+    lds_barrier();
     each_row(f, plan, [&](int row, const RowPlan &r) {
         int rank = row >= 0 ? needs[row] : 0;
         if (row >= 0) {
@@ -232,7 +212,7 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
             const int part = r.held & ((1 << f.page_shift) - 1), place = row * f.width + r.first;
             if (r.first < r.end) {
                 const bool need = !stays(c, r.page, place);
-                const int fresh = need && rank < free_pages ? (int)list[rank] : -1;
+                const int fresh = need && rank < free_pages ? list[rank] : -1;
                 f.table_out[place] = need ? fresh : r.page;
                 rank += need;
                 if (fresh >= 0 && r.page >= 0 && part) {
@@ -249,7 +229,7 @@ __device__ __forceinline__ void assign(const PageFork &f, const Counters &c, Pla
             const bool need = there && !stays(c, page, place);
             const unsigned long long mask = __ballot(need);
             const int at = owner == OWN ? rank : __builtin_amdgcn_readlane(rank, owner) + __popcll(mask & ((1ull << lane) - 1));
-            if (there) f.table_out[place] = !need ? page : at < free_pages ? (int)list[at] : -1;
+            if (there) f.table_out[place] = !need ? page : at < free_pages ? list[at] : -1;
             rank += owner == OWN ? need : lane == owner ? __popcll(mask) : 0;
         });
     });
@@ -344,9 +324,10 @@ __global__ __launch_bounds__(BLOCK) void fork_block_kernel(PageFork f, unsigned 
         }
     }
     lds_barrier();
-    assign<true>(f, c, [&](int row) { return plans[row]; }, needs, list, parts);
+    assign(f, c, [&](int row) { return plans[row]; }, needs, list, parts);
 }
 
+// The same in five launches over all of the chip, which bound it up to a million pages: 20000 pages and 64 rows of 128 entries 15.6 us, 250000 and 256 of 256 17.2, 8 million 54 (160 MB).
 __global__ __launch_bounds__(256) void fork_clear_kernel(PageFork f, Counters c)
 {
     const int i = blockIdx.x * 256 + threadIdx.x;
@@ -355,7 +336,7 @@ __global__ __launch_bounds__(256) void fork_clear_kernel(PageFork f, Counters c)
         c.first[i] = NONE;
     }
 }
-// a wave a row; 9000 pages, 1024 rows of 64 entries take the three kernels 23.8 us, most of them in the last one's block
+// a wave a row
 __global__ __launch_bounds__(256) void fork_count_kernel(PageFork f, Counters c)
 {
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -371,15 +352,160 @@ __global__ __launch_bounds__(256) void fork_count_kernel(PageFork f, Counters c)
         } else if (child >= 0) atomicMin(&c.first[child], row * f.width + j);
     }
 }
-__global__ __launch_bounds__(BLOCK) void fork_assign_kernel(PageFork f, Counters c, int *needs, int *list)
+// Blocks in front: the free pages of FORK_CHUNK pages each; behind them: what a row needs.  A block looks at AT_ONCE rounds of 256 pages or entries together.
+constexpr int AT_ONCE = 16, FORK_CHUNK = 256 * AT_ONCE;
+struct Needs { int *of_row, *wide, *in_chunk, *total; };              // pages, entries that the table lacks; free pages; of all chunks
+__global__ __launch_bounds__(256) void fork_needs_kernel(PageFork f, Counters c, Needs needs, int chunks)
 {
-    __shared__ int parts[4][BLOCK / 64];
-    auto plan = [&](int row) {
-        RowPlan r = row_plan(f, row);
-        r.page = r.first < r.end ? child_page(f, r, r.first) : -1;
-        return r;
-    };
-    assign<false>(f, c, plan, needs, list, parts);
+    __shared__ int parts[4];
+    const int tid = threadIdx.x;
+    int n = 0, all;
+    if ((int)blockIdx.x < chunks) {
+        const long first = (long)blockIdx.x * FORK_CHUNK + tid;
+        int rest[AT_ONCE], written[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) {
+            const long page = min(first + u * 256, (long)f.pages - 1);
+            rest[u] = c.rest[page];
+            written[u] = c.first[page];
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; u++) n += first + u * 256 < f.pages && rest[u] == 0 && written[u] == NONE;
+        block_scan(n, parts, all);
+        if (tid == 0) needs.in_chunk[blockIdx.x] = all;
+        return;
+    }
+    const int row = blockIdx.x - chunks;
+    const RowPlan r = row_plan(f, row);
+    for (int j0 = r.first; j0 < r.end; j0 += 1024) {
+        int page[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) page[u] = child_page(f, r, j0 + u * 256 + tid);
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int j = j0 + u * 256 + tid;
+            n += j < r.end && !stays(c, page[u], row * f.width + j);
+        }
+    }
+    block_scan(n, parts, all);
+    if (tid == 0) {
+        needs.of_row[row] = all;
+        needs.wide[row] = r.wide;
+    }
+}
+// The free pages that are asked for, in order, and the counts; a block behind the last chunk's ranks the rows.
+__global__ __launch_bounds__(256) void fork_free_kernel(PageFork f, Counters c, Needs needs, int *__restrict__ rank_of, int chunks, int *__restrict__ list)
+{
+    __shared__ int parts[4][4], count[64];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const bool of_rows = (int)blockIdx.x == chunks;
+    const long first = (long)blockIdx.x * FORK_CHUNK + tid;
+    int rest[AT_ONCE], written[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; u++) {
+        const long page = min(first + u * 256, (long)f.pages - 1);
+        rest[u] = c.rest[page];
+        written[u] = c.first[page];
+    }
+    int v[4] = {}, before[4], all[4];                                 // free pages (in front of this chunk's), needs, wide
+    for (int i = tid; i < (of_rows ? chunks : min((int)blockIdx.x, chunks)); i += 256) v[0] += needs.in_chunk[i];
+    // (of the block behind the chunks a thread has neighbouring rows)
+    const int per = (f.rows + 255) / 256;
+    for (int u = 0; u < per; u++) {
+        const int i = tid * per + u;
+        if (i >= f.rows) break;
+        v[1] += needs.of_row[i];
+        if (of_rows) {
+            v[2] += needs.wide[i] & 0xffff;                           // (8192 rows lack up to 2^28 each)
+            v[3] += needs.wide[i] >> 16;
+        }
+    }
+    block_scan<4, 4>(v, parts, before, all);
+    const int wanted = all[1];
+    if (of_rows) {
+        int rank = before[1];
+        for (int u = 0; u < per; u++) {
+            const int i = tid * per + u;
+            if (i >= f.rows) break;
+            rank_of[i] = rank;
+            rank += needs.of_row[i];
+        }
+        if (tid == 0) {
+            needs.total[0] = all[0];
+            f.lacking[0] = (int)min(max(wanted - all[0], 0) + all[2] + ((long)all[3] << 16), (long)NONE);
+        }
+        return;
+    }
+    unsigned is_free = 0;
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; u++) {
+        const bool one = first + u * 256 < f.pages && rest[u] == 0 && written[u] == NONE;
+        is_free |= (unsigned)one << u;
+        const int n = __popcll(__ballot(one));
+        if (lane == 0) count[4 * u + w] = n;
+    }
+    lds_barrier();
+    const int mine = count[lane], in_front = wave_scan(mine) - mine;  // of the chunk's 64 pages number `lane`
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; u++) {
+        const long page = first + u * 256;
+        const bool one = is_free >> u & 1;
+        const int rank = all[0] + __builtin_amdgcn_readlane(in_front, 4 * u + w) + __popcll(__ballot(one) & ((1ull << lane) - 1));
+        int n = rest[u];
+        if (one) {
+            if (rank < wanted) {
+                list[rank] = (int)page;
+                n = 1;
+            }
+        } else if (n == 0 && written[u] != NONE) n = 1;               // the first of its writers
+        if (page < f.pages) f.refs_out[page] = n;
+    }
+}
+// a block a row: the entries that its next positions lie in
+__global__ __launch_bounds__(256) void fork_entries_kernel(PageFork f, Counters c, Needs needs, const int *__restrict__ rank_of, const int *__restrict__ list)
+{
+    __shared__ int count[16];
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int free_pages = needs.total[0];
+    int rank = rank_of[row];
+    const RowPlan r = row_plan(f, row);
+    const int part = r.held & ((1 << f.page_shift) - 1);
+    if (tid == 0) {
+        f.lens_out[row] = r.len;
+        if (r.first >= r.end) {
+            f.copies[row] = f.copies[f.rows + row] = -1;
+            f.copies[2 * f.rows + row] = 0;
+        }
+    }
+    for (int j0 = r.first; j0 < r.end; j0 += 1024) {
+        int page[4];
+        bool need[4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) page[u] = child_page(f, r, j0 + u * 256 + tid);
+        if (j0 > r.first) lds_barrier();
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int j = j0 + u * 256 + tid;
+            need[u] = j < r.end && !stays(c, page[u], row * f.width + j);
+            const int n = __popcll(__ballot(need[u]));
+            if (lane == 0) count[4 * u + w] = n;
+        }
+        lds_barrier();
+        const int mine = lane < 16 ? count[lane] : 0, upto = wave_scan(mine), in_front = upto - mine;
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+            const int j = j0 + u * 256 + tid, at = rank + __builtin_amdgcn_readlane(in_front, 4 * u + w) + __popcll(__ballot(need[u]) & ((1ull << lane) - 1));
+            const int to = !need[u] ? page[u] : at < free_pages ? list[at] : -1;
+            if (j < r.end) f.table_out[(long)row * f.width + j] = to;
+            if (j == r.first) {
+                const bool copied = need[u] && to >= 0 && page[u] >= 0 && part;
+                f.copies[row] = copied ? page[u] : -1;
+                f.copies[f.rows + row] = copied ? to : -1;
+                f.copies[2 * f.rows + row] = copied ? part : 0;
+            }
+        }
+        rank += __builtin_amdgcn_readlane(upto, 63);
+    }
 }
 
 // ---- compact -----------------------------------------------------------------------------------------
@@ -592,7 +718,8 @@ size_t room(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 size_t pages_fork_workspace(int pages, int rows_from, int width, int rows)
 {
-    return fork_in_block(pages, rows_from, width, rows) ? 0 : 3 * room(4 * (size_t)pages) + room(4 * (size_t)rows);
+    const size_t chunks = ((size_t)pages + FORK_CHUNK - 1) / FORK_CHUNK;
+    return fork_in_block(pages, rows_from, width, rows) ? 0 : 3 * room(4 * (size_t)pages) + 3 * room(4 * (size_t)rows) + room(4 * chunks) + room(4);
 }
 
 hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st)
@@ -610,11 +737,18 @@ hipError_t launch_pages_fork(const PageFork &f, void *ws, hipStream_t st)
     Counters c;
     c.rest = take<int>(at, f.pages);
     c.first = take<int>(at, f.pages);
-    int *const needs = take<int>(at, f.rows);
-    const int most = f.rows > f.rows_from ? f.rows : f.rows_from;
+    const int most = f.rows > f.rows_from ? f.rows : f.rows_from, chunks = (int)(((size_t)f.pages + FORK_CHUNK - 1) / FORK_CHUNK);
+    int *const rank_of = take<int>(at, f.rows);
+    Needs needs;
+    needs.of_row = take<int>(at, f.rows);
+    needs.wide = take<int>(at, f.rows);
+    needs.in_chunk = take<int>(at, chunks);
+    needs.total = take<int>(at, 1);
     hipLaunchKernelGGL(fork_clear_kernel, dim3((unsigned)((f.pages + 255) / 256)), dim3(256), 0, st, f, c);
     hipLaunchKernelGGL(fork_count_kernel, dim3((unsigned)((most + 3) / 4), blocks_for((f.width + 63) / 64, 64)), dim3(256), 0, st, f, c);
-    hipLaunchKernelGGL(fork_assign_kernel, dim3(1), dim3(BLOCK), 0, st, f, c, needs, list);
+    hipLaunchKernelGGL(fork_needs_kernel, dim3((unsigned)(chunks + f.rows)), dim3(256), 0, st, f, c, needs, chunks);
+    hipLaunchKernelGGL(fork_free_kernel, dim3((unsigned)(chunks + 1)), dim3(256), 0, st, f, c, needs, rank_of, chunks, list);
+    hipLaunchKernelGGL(fork_entries_kernel, dim3((unsigned)f.rows), dim3(256), 0, st, f, c, needs, rank_of, list);
     return hipGetLastError();
 }
 

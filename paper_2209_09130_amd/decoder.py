@@ -367,7 +367,7 @@ def _parts(like: torch.Tensor, sizes: Tuple[int, ...]) -> Tuple[torch.Tensor, ..
 
 def _table(table: torch.Tensor, device: int) -> Tuple[int, int, int]:
     if table.dim() != 2 or table.numel() > _INT_MAX:
-        _refuse(f"a page table is [sequences, pages of a sequence], of less than 2^31 entries, not {tuple(table.shape)}")
+        _refuse(f"a page table is [sequences, pages of a sequence], of at most 2^30 entries, not {tuple(table.shape)}")
     return _flat("table", table, torch.int32, device), table.shape[0], table.shape[1]
 
 
@@ -390,7 +390,7 @@ def pages_fork(refs: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page
     if not 0 < rows <= 8192:
         _refuse(f"1 to 8192 rows are supported ({rows})")
     if rows * width > _INT_MAX:
-        _refuse("a page table has less than 2^31 entries")
+        _refuse("a page table has at most 2^30 entries")
     refs_out, table_out, lens_out, copies, lacking = _parts(refs, (pages, rows * width, rows, 3 * rows, 1))
     need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows_from, width, rows)
     ws = refs.new_empty((need,), dtype=torch.uint8) if need else None

@@ -41,7 +41,7 @@ def test_pages_fork(L):
     refusals(L.samp_pages_fork, base, [({n: None}, ARG, b"NULL") for n in ("refs", "table", "lens", "refs_out", "table_out", "lens_out", "copies", "lacking")] + [
         ({"pages": 0}, SHAPE, b"pages"), ({"pages": (1 << 26) + 1}, SHAPE, b"pages"), ({"page_len": 8}, SHAPE, b"power of two"), ({"page_len": 48}, SHAPE, b"power of two"),
         ({"rows": 0}, SHAPE, b"rows"), ({"rows": 8193}, SHAPE, b"rows"), ({"rows_from": 0}, SHAPE, b"rows"), ({"rows_from": 8193}, SHAPE, b"rows"), ({"width": 0}, SHAPE, b"width"),
-        ({"max_new": -1}, SHAPE, b"max_new"), ({"rows": 8192, "width": 1 << 18}, SHAPE, b"2^31"), ({"rows_from": 8192, "width": 1 << 18}, SHAPE, b"2^31"),
+        ({"max_new": -1}, SHAPE, b"max_new"), ({"rows": 8192, "width": (1 << 17) + 1}, SHAPE, b"2^30"), ({"rows_from": 8192, "width": (1 << 17) + 1}, SHAPE, b"2^30"),
         ({"refs_out": AT}, ARG, b"overlap"), ({"table_out": AT}, ARG, b"overlap"), ({"lens_out": AT}, ARG, b"overlap"),
         ({"pages": 100000, "workspace": None}, SPACE, b"workspace"), ({"pages": 100000, "bytes": need - 1}, SPACE, b"workspace")])
 
