@@ -14,7 +14,8 @@
 namespace samp {
 namespace {
 
-constexpr int SLOTS = 128, ROOM = 1024;                               // threads of a piece whose values are looked through, and values that are ranked
+constexpr int SLOTS = 128, ROOM = 512;                                // threads of a piece whose values are looked through, and values that are ranked (1000 take longer than the way round: 4096 rows of 1000 equal
+                                                                      // logits 413 us, 39)
 constexpr float LOG2E = 1.44269504088896340736f;                      // (1.3e-8 of it off: as much of the mean distance from the largest logit, 2e-7 at most)
 
 enum { F16 = 0, BF16 = 1, F32 = 2 };
@@ -65,19 +66,54 @@ __device__ __forceinline__ float sum_of_wave(float x)
 
 struct Candidate { float logit; int token; };                         // token -1: none
 struct PieceSum { float top, sum; };                                  // sum of exp(x - top)
-struct __attribute__((aligned(8))) Listed { float logit; int place; };
-__device__ __forceinline__ bool before(const Listed &a, const Listed &b) { return a.logit > b.logit || (a.logit == b.logit && a.place < b.place); }
+// A number of the order of the value (one zero; not for NaN); with the place behind it, the lower one first
+__device__ __forceinline__ unsigned order_of(float x)
+{
+    const unsigned u = __float_as_uint(x + 0.0f);
+    return u >> 31 ? ~u : u | 1u << 31;
+}
+__device__ __forceinline__ unsigned long long listed_of(float x, int place) { return (unsigned long long)order_of(x) << 32 | (unsigned)~place; }
+__device__ __forceinline__ bool before(unsigned long long a, unsigned long long b) { return a > b; }
 // The value of a number whose order as an unsigned integer is the values' own (NaN outside the infinities: nothing reaches those)
 __device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t >> 31 ? t & 0x7fffffffu : ~t); }
+
+// How many of `all` come before `mine`, counted by 2^n lanes `step` that have each every step-th; and f(entry, how many come before it) for each of n entries, by THREADS threads.
+// Eight (numbers of 16 bytes: four) are read together; one at a time took 110 clocks each.
+template <class T> __device__ __forceinline__ int count_before(const T *all, int n, int first, int step, const T &mine)
+{
+    constexpr int BATCH = 64 / sizeof(T);
+    int better = 0, j = first;
+    for (; j + (BATCH - 1) * step < n; j += BATCH * step) {
+        T x[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; u++) x[u] = all[j + u * step];
+#pragma unroll
+        for (int u = 0; u < BATCH; u++) better += before(x[u], mine);
+    }
+    for (; j < n; j += step) better += before(all[j], mine);
+    return better;
+}
+template <int THREADS, class T, class F> __device__ __forceinline__ void rank_entries(const T *all, int n, F &&f)
+{
+    int share = 1;
+    while (share < 64 && n * share * 2 <= THREADS) share *= 2;
+    const int mine = threadIdx.x & (share - 1);
+    for (int i = (int)threadIdx.x / share; i < n; i += THREADS / share) {
+        const T e = all[i];
+        int better = count_before(all, n, mine, share, e);
+        for (int o = 1; o < share; o <<= 1) better += __shfl_xor(better, o, 64);
+        if (mine == 0) f(i, e, better);
+    }
+}
 
 __device__ __forceinline__ bool row_counts(const float *scores, const uint8_t *finished, int row)
 {
     return __builtin_isfinite(scores[row]) && !(finished && finished[row]);
 }
 
-// One piece of one row: what bounds it is HBM where there are rows enough (512 rows of 128256, of which a quarter are finished or have no score and are not read: 97 MB, 25.6 us, 3.8 TB/s;
+// One piece of one row: what bounds it is HBM where there are rows enough (512 rows of 128256, of which a quarter are finished or have no score and are not read: 97 MB, 24.2 us, 4.0 TB/s;
 // the vector ALUs issue half of that time, nine instructions a logit), else its chain of one trip to memory, two reductions and the list: 35 rows of 50265
-// binary32 7.0 us, 4 rows of 21128 4.4.  Vectors of 16 bytes are numbered from the aligned address at or before the row's first value; what of them lies outside the row counts as minus infinity.
+// binary32 6.4 us, 4 rows of 21128 4.6.  Vectors of 16 bytes are numbered from the aligned address at or before the row's first value; what of them lies outside the row counts as minus infinity.
 template <int T, int THREADS, int VECTORS, int GROUPS>
 __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__restrict__ logits, long ld, const float *__restrict__ scores,
                                                               const uint8_t *__restrict__ finished, int vocab, int keep, int chunks,
@@ -86,7 +122,7 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
     typedef Logit<T> L;
     constexpr int VEC = L::VEC, PER = VECTORS * VEC, TEAM = THREADS / GROUPS, WAVES = THREADS / 64;
     static_assert(GROUPS == 64 || (GROUPS % 64 == 0 && TEAM <= 2), "the same lane of every wave, or one or two neighbours");
-    __shared__ Listed list[ROOM];
+    __shared__ __attribute__((aligned(16))) unsigned long long list[ROOM];
     __shared__ __attribute__((aligned(16))) v4i held[SLOTS][VECTORS];
     __shared__ int owner[SLOTS];
     __shared__ __attribute__((aligned(16))) float tops[GROUPS == 64 ? THREADS : GROUPS];
@@ -157,6 +193,7 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
             for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(L::value(raw[i], e), LOG2E, -reference));
         sum = ((part[0] + part[1]) + (part[2] + part[3])) * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, LOG2E, -reference));
     } else {
+        again();
 #pragma unroll
         for (int i = 0; i < VECTORS; i++)
 #pragma unroll
@@ -222,20 +259,21 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
                 int *count = &listed;
                 asm("" : "+v"(count));
                 const int to = atomicAdd(count, 1);                   // (in any order: they are ranked)
-                if (to < ROOM) list[to] = Listed{x, (e / VEC * THREADS + owner[slot]) * VEC + e % VEC};
+                if (to < ROOM) list[to] = listed_of(x, (e / VEC * THREADS + owner[slot]) * VEC + e % VEC);
             }
         }
         __syncthreads();
         n = listed;
     } else n = ROOM + 1;
     if (n > ROOM) {
-        // Many reach the limit, as in rows of one value.  The `keep`-th largest value itself, bit by bit from the top; what is above it, less than `keep` values; and those that
-        // equal it, in the order of their places.
+        // Many reach the limit, as in rows whose tokens have one value but for a few.  The `keep`-th largest value itself: the limit, which `keep` values reach, if fewer are above it, and
+        // else bit by bit from the top; what is above it, less than `keep` values; and those that equal it, in the order of their places, as far as they are wanted.
         unsigned t = 0;
+        bool is_limit = false;
 #pragma unroll 1
-        for (int bit = 31; bit >= 0; bit--) {
+        for (int bit = 32; bit >= 0 && !is_limit; bit--) {
             again();
-            const float v = value_of_order(t | 1u << bit);
+            const float v = value_of_order(bit < 32 ? t | 1u << bit : order_of(limit) + 1);
             int reach = 0;
 #pragma unroll
             for (int i = 0; i < VECTORS; i++)
@@ -249,9 +287,10 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
             reach = 0;
 #pragma unroll
             for (int i = 0; i < WAVES; i++) reach += wave_count[i];
-            if (reach >= keep) t |= 1u << bit;
+            if (bit == 32) is_limit = reach < keep;
+            else if (reach >= keep) t |= 1u << bit;
         }
-        limit = __builtin_fmaxf(value_of_order(t), -3.40282347e38f);
+        if (!is_limit) limit = __builtin_fmaxf(value_of_order(t), -3.40282347e38f);
         again();
         __syncthreads();
         if (tid == 0) listed = 0;
@@ -262,51 +301,49 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
             for (int e = 0; e < VEC; e++)
                 if (L::value(raw[i], e) > limit) {
                     const int to = atomicAdd(&listed, 1);
-                    if (to < ROOM) list[to] = Listed{L::value(raw[i], e), (i * THREADS + tid) * VEC + e};
+                    if (to < ROOM) list[to] = listed_of(L::value(raw[i], e), (i * THREADS + tid) * VEC + e);
                 }
         __syncthreads();
         n = listed;
         again();
 #pragma unroll
         for (int i = 0; i < VECTORS; i++) {
-            int at = tid;
-            asm("" : "+v"(at));
-            unsigned equal = 0;
+            if (n < keep) {                                           // (the same for the whole block)
+                int at = tid;
+                asm("" : "+v"(at));
+                unsigned equal = 0;
 #pragma unroll
-            for (int e = 0; e < VEC; e++) equal |= (unsigned)(L::value(raw[i], e) == limit) << e;
-            int before = __popc(equal);
-            const int mine = before;
+                for (int e = 0; e < VEC; e++) equal |= (unsigned)(L::value(raw[i], e) == limit) << e;
+                int before = __popc(equal);
+                const int mine = before;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int other = __shfl_up(before, o, 64);
-                if (lane >= o) before += other;
-            }
-            __syncthreads();
-            if (lane == 63) wave_count[w] = before;
-            __syncthreads();
-            int to = n + before - mine;
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int other = __shfl_up(before, o, 64);
+                    if (lane >= o) before += other;
+                }
+                __syncthreads();
+                if (lane == 63) wave_count[w] = before;
+                __syncthreads();
+                int to = n + before - mine;
 #pragma unroll
-            for (int u = 0; u < WAVES; u++) {
-                to += u < w ? wave_count[u] : 0;
-                n += wave_count[u];
-            }
+                for (int u = 0; u < WAVES; u++) {
+                    to += u < w ? wave_count[u] : 0;
+                    n += wave_count[u];
+                }
 #pragma unroll
-            for (int e = 0; e < VEC; e++) {
-                if ((equal >> e & 1) && to < ROOM) list[to] = Listed{limit, (i * THREADS + at) * VEC + e};
-                to += equal >> e & 1;
+                for (int e = 0; e < VEC; e++) {
+                    if ((equal >> e & 1) && to < ROOM) list[to] = listed_of(limit, (i * THREADS + at) * VEC + e);
+                    to += equal >> e & 1;
+                }
             }
         }
         __syncthreads();
         n = min(n, keep);                                             // (those above come first in the list)
     }
     Candidate *const to = best + (size_t)blockIdx.x * keep;
-    for (int at = tid; at < n; at += THREADS) {
-        const Listed k = list[at];
-        int better = 0;
-#pragma unroll 4
-        for (int i = 0; i < n; i++) better += before(list[i], k);
-        if (better < keep) to[better] = Candidate{k.logit, first + k.place};
-    }
+    rank_entries<THREADS>(list, n, [&](int, unsigned long long e, int better) {
+        if (better < keep) to[better] = Candidate{value_of_order((unsigned)(e >> 32)), first + (int)~(unsigned)e};
+    });
     if (tid < keep && tid >= n) to[tid] = Candidate{-INFINITY, -1};
 }
 
@@ -315,7 +352,7 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
 constexpr int JOIN = 1024;
 struct __attribute__((aligned(16))) Entry { unsigned long long total, then; };
 constexpr Entry NO_ENTRY{0, ~0ull};
-__device__ __forceinline__ bool before(const Entry &a, const Entry &b) { return a.total > b.total || (a.total == b.total && a.then < b.then); }
+__device__ __forceinline__ bool before(const Entry &a, const Entry &b) { return (a.total > b.total) | ((a.total == b.total) & (a.then < b.then)); }
 __device__ __forceinline__ Entry entry_of(double total, int r, float logit, int token)
 {
     if (!(total > -INFINITY)) return NO_ENTRY;
@@ -327,23 +364,63 @@ __device__ __forceinline__ double total_of(const Entry &e)
 {
     return __longlong_as_double((long long)(e.total >> 63 ? e.total & ~(1ull << 63) : ~e.total));
 }
-// f(entry, how many of the n come before it) for every one of them that is there
-template <class F> __device__ __forceinline__ void rank_entries(const Entry *all, int n, F &&f)
+// f(entry's place, entry, how many of the n come before it) for the `keep` best that are there, and perhaps for more.  Of many, only those are ranked that reach the `keep`-th largest of the
+// maxima of TOPS groups, by the upper half of their totals: `keep` entries do.  1088 lists, keep = 64, 18 us, all ranked against all 85; 512, keep = 32, 9.0
+// and 19.8; up to FEW entries that is as fast (136 of 64 sequences 6.9, this way 8.5).
+constexpr int FEW = 192, TOPS = 128, RANKED = 512;
+struct Best { __attribute__((aligned(16))) unsigned top[TOPS]; unsigned bound; int n, at[RANKED]; };
+template <class F> __device__ __forceinline__ void rank_best(const Entry *all, int n, int keep, Best &best, F &&f)
 {
-    int share = 1;
-    while (share < 64 && n * share * 2 <= JOIN) share *= 2;
-    const int mine = threadIdx.x & (share - 1);
-    for (int i = (int)threadIdx.x / share; i < n; i += JOIN / share) {
-        const Entry e = all[i];
-        int better = 0;
-#pragma unroll 4
-        for (int j = mine; j < n; j += share) better += before(all[j], e);
-        for (int o = 1; o < share; o <<= 1) better += __shfl_xor(better, o, 64);
-        if (mine == 0 && e.total) f(i, e, better);
+    const int tid = threadIdx.x;
+    int some = n;
+    if (n > FEW) {
+        if (tid < TOPS) best.top[tid] = 0;
+        if (tid == 0) best.bound = ~0u, best.n = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += JOIN) atomicMax(&best.top[i % TOPS], (unsigned)(all[i].total >> 32));
+        __syncthreads();
+        if (tid < TOPS) {
+            const unsigned mine = best.top[tid];
+            const v4i *const tops = reinterpret_cast<const v4i *>(best.top);
+            int above = 0;
+#pragma unroll 8
+            for (int j = 0; j < TOPS / 4; j++) {
+                const v4i t = tops[j];
+#pragma unroll
+                for (int e = 0; e < 4; e++) above += (unsigned)t[e] > mine;
+            }
+            if (above < keep) atomicMin(&best.bound, mine);
+        }
+        __syncthreads();
+        const unsigned bound = best.bound;
+        for (int i = tid; i < n; i += JOIN) {
+            const unsigned long long total = all[i].total;
+            if (!total || (unsigned)(total >> 32) < bound) continue;
+            const int to = atomicAdd(&best.n, 1);                     // (in any order: they are ranked)
+            if (to < RANKED) best.at[to] = i;
+        }
+        __syncthreads();
+        some = best.n;
     }
+    if (n <= FEW || some > RANKED) {
+        rank_entries<JOIN>(all, n, [&](int i, const Entry &e, int better) {
+            if (e.total) f(i, e, better);
+        });
+        return;
+    }
+    int share = 1;
+    while (share < 64 && some * share * 2 <= JOIN) share *= 2;
+    const int mine = tid & (share - 1), i = tid / share;
+    if (i >= some) return;                                            // (all lanes of an entry: no more than RANKED of them, JOIN threads)
+    const Entry e = all[best.at[i]];
+    int better = 0;
+#pragma unroll 4
+    for (int j = mine; j < some; j += share) better += before(all[best.at[j]], e);
+    for (int o = 1; o < share; o <<= 1) better += __shfl_xor(better, o, 64);
+    if (mine == 0) f(best.at[i], e, better);
 }
 
-// A block a sequence.  A few dependent steps over some thousand numbers: 7.2 us for 64 sequences of 8 rows in 32 pieces, keep = 16; 5.4 for one of 4 rows in 6 pieces.
+// A block a sequence.  A few dependent steps over some thousand numbers: 7.3 us for 64 sequences of 8 rows in 4 pieces each, keep = 16; 5.6 for one of 4 rows in 6.
 __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restrict__ sums, const Candidate *__restrict__ best, const float *__restrict__ scores,
                                                          const uint8_t *__restrict__ finished, int end, int beams, int keep, int chunks, float *__restrict__ out,
                                                          int *__restrict__ parents, int *__restrict__ tokens)
@@ -355,6 +432,7 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
     __shared__ float score[SAMP_MAX_BEAMS];                           // NaN where a row has none
     __shared__ bool done[SAMP_MAX_BEAMS];
     __shared__ int list_of[SAMP_MAX_KEEP], there;
+    __shared__ Best ranked;
     __shared__ unsigned long long enough;                             // a total that at least `keep` entries reach, or 0
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const size_t row0 = (size_t)b * beams;
@@ -390,7 +468,7 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
     if (tid < lists) first[tid] = entry(tid, 0, head);
     for (int i = tid + JOIN; i < lists; i += JOIN) first[i] = entry(i, 0, best[(row0 * chunks + i) * keep]);
     __syncthreads();
-    rank_entries(first, lists, [&](int i, const Entry &e, int better) {
+    rank_best(first, lists, keep, ranked, [&](int i, const Entry &e, int better) {
         if (better < keep) list_of[better] = i;
         if (better == keep - 1) enough = e.total;
     });
@@ -400,8 +478,8 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
         const int deep = (keep + lists - 1) / lists, part = (keep + deep - 1) / deep;
         if (tid < lists) pair[tid] = entry(tid, deep - 1, best[(row0 * chunks + tid) * keep + deep - 1]);
         __syncthreads();
-        rank_entries(pair, lists, [&](int, const Entry &e, int better) {
-            if (better == part - 1) enough = e.total;
+        rank_entries<JOIN>(pair, lists, [&](int, const Entry &e, int better) {
+            if (e.total && better == part - 1) enough = e.total;
         });
         __syncthreads();
     }
@@ -413,7 +491,7 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
     }
     __syncthreads();
     const size_t to = (size_t)b * keep;
-    rank_entries(pair, there, [&](int, const Entry &e, int better) {
+    rank_best(pair, there, keep, ranked, [&](int, const Entry &e, int better) {
         if (better >= keep) return;
         const int r = (int)(e.then >> 52);
         out[to + better] = (float)total_of(e);

@@ -61,6 +61,8 @@ inline int cache_passes(long rows, int kv_heads) { return rows * kv_heads >= 327
 // A row is cut into pieces of 512 threads with eight vectors of 16 bytes each where that makes enough of them, else of 256 with two.  us, both kernels, long / short pieces, rows x vocabulary:
 // 16 bits 64 x 32000 13.9 / 11.4, 256 x 32000 15.6 / 14.4, 512 x 32000 18.1 / 18.8, 64 x 128256 14.7 / 14.7, 128 x 128256 17.1 / 18.9; binary32, whose short pieces are half as many
 // values, 4 x 21128 11.3 / 9.7, 64 x 32000 12.4 / 12.0, 16 x 128256 12.2 / 14.7, 32 x 128256 13.3 / 16.1, 512 x 32000 20.8 / 25.0, 128 x 128256 20.8 / 27.4.
+// A long piece takes as long as five or six short ones, full or not: 16 bits 1024 x 1000 22.3 / 13.6, 1024 x 16000 21.7 / 19.7, 1024 x 21000 21.7 / 22.3, 1024 x 36000 30.3 / 27.7, 1024 x 50304
+// 29.4 / 36.5; binary32 1024 x 8000 19.0 / 18.3, 1024 x 12000 20.0 / 20.8, 512 x 12000 16.7 / 15.5, 512 x 21000 17.9 / 19.3.
 struct BeamPiece { int threads, vectors; };
 constexpr BeamPiece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
 inline int piece_chunks(BeamPiece p, bool wide, int vocab)
@@ -68,7 +70,11 @@ inline int piece_chunks(BeamPiece p, bool wide, int vocab)
     const int vector = wide ? 4 : 8, values = p.threads * p.vectors * vector;
     return (vocab + vector - 1 + values - 1) / values;                // (a row may begin `vector` - 1 places behind an aligned address)
 }
-inline bool long_pieces(bool wide, int rows, int vocab) { return (long)rows * piece_chunks(LONG_PIECE, wide, vocab) >= (wide ? 128 : 512); }
+inline bool long_pieces(bool wide, int rows, int vocab)
+{
+    const int chunks = piece_chunks(LONG_PIECE, wide, vocab);
+    return (long)rows * chunks >= (wide ? 128 : 512) && 2 * piece_chunks(SHORT_PIECE, wide, vocab) >= 11 * chunks;
+}
 
 // ---- bookkeeping of pages ------------------------------------------------------------------------------
 // One block does a whole call where its counters fit the LDS of a CU (two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 bytes for each

@@ -669,38 +669,51 @@ __global__ __launch_bounds__(256) void compact_finish_kernel(Compact a, UsedPage
 }
 
 // ---- copies ------------------------------------------------------------------------------------------
+template <int D> __device__ __forceinline__ void copy_part(const KvCache &c, const KeyBounds &bounds, int from, int to, int rows, int head, bool is_v, int lane)
+{
+    const size_t src = ((size_t)from * c.kv_heads + head) << c.page_shift, dst = ((size_t)to * c.kv_heads + head) << c.page_shift;
+    int8_t *const codes = is_v ? c.v : c.k;
+    float *const steps = is_v ? c.v_step : c.k_step;
+    const v4i *const read = reinterpret_cast<const v4i *>(codes + src * D);
+    v4i *const write = reinterpret_cast<v4i *>(codes + dst * D);
+    const int chunks = rows * (D / 16);
+    for (int at = lane; at < rows; at += 64) steps[dst + at] = steps[src + at];
+    constexpr int BATCH = 8;
+    for (int at = lane; at < chunks; at += 64 * BATCH) {
+        v4i held[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; i++) held[i] = read[min(at + 64 * i, chunks - 1)];
+#pragma unroll
+        for (int i = 0; i < BATCH; i++)
+            if (at + 64 * i < chunks) write[at + 64 * i] = held[i];
+    }
+    if (bounds.codes && !is_v) {
+        const size_t a = (size_t)from * c.kv_heads + head, b = (size_t)to * c.kv_heads + head;
+        if (lane < 2 * D / 16) reinterpret_cast<v4i *>(bounds.codes + b * 2 * D)[lane] = reinterpret_cast<const v4i *>(bounds.codes + a * 2 * D)[lane];
+        if (lane == 0) bounds.steps[b] = bounds.steps[a];
+    }
+}
+
 // A wave copies the keys or the values of one key head of one page at a time, all of what it reads requested before the first of it is written (up to 8 KB; in turns, more).
-// Bound by HBM: 980 pages of 64 positions, 8 key heads of 128 (265 MB read and written) 53.9 us, 4.9 TB/s, near a large copy's 5.0; the begun pages of 256 beams (11 MB) 5.3 us.
+// It has every so-manieth entry of the list, looked up 64 at a time, as a list may be long and hold few copies (20 among 50000 of 8 key heads 6.6 us, each looked up by itself 41).
+// Bound by HBM: 980 pages of 64 positions, 8 key heads of 128 (265 MB read and written) 53.9 us, 4.9 TB/s, near a large copy's 5.0; the begun pages of 256 beams (11 MB) 4.3 us.
 template <int D>
 __global__ __launch_bounds__(256) void cache_copy_kernel(KvCache c, KeyBounds bounds, const int *__restrict__ copies, int n)
 {
-    const int lane = threadIdx.x & 63;
-    const long step = (long)gridDim.x * 4, units = 2l * n * c.kv_heads;
-    for (long u = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); u < units; u += step) {
-        const int entry = (int)(u / (2 * c.kv_heads)), part = (int)(u - (long)entry * 2 * c.kv_heads), head = part >> 1;
-        const bool is_v = part & 1;
-        const int from = copies[entry], to = copies[n + entry], rows = min(copies[2 * (long)n + entry], 1 << c.page_shift);
-        if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages || rows <= 0 || from == to) continue;
-        const size_t src = ((size_t)from * c.kv_heads + head) << c.page_shift, dst = ((size_t)to * c.kv_heads + head) << c.page_shift;
-        int8_t *const codes = is_v ? c.v : c.k;
-        float *const steps = is_v ? c.v_step : c.k_step;
-        const v4i *const read = reinterpret_cast<const v4i *>(codes + src * D);
-        v4i *const write = reinterpret_cast<v4i *>(codes + dst * D);
-        const int chunks = rows * (D / 16);
-        for (int at = lane; at < rows; at += 64) steps[dst + at] = steps[src + at];
-        constexpr int BATCH = 8;
-        for (int at = lane; at < chunks; at += 64 * BATCH) {
-            v4i held[BATCH];
-#pragma unroll
-            for (int i = 0; i < BATCH; i++) held[i] = read[min(at + 64 * i, chunks - 1)];
-#pragma unroll
-            for (int i = 0; i < BATCH; i++)
-                if (at + 64 * i < chunks) write[at + 64 * i] = held[i];
+    const int lane = threadIdx.x & 63, parts = 2 * c.kv_heads, group = blockIdx.x / parts, part = blockIdx.x - group * parts, head = part >> 1, waves = gridDim.x / parts * 4;
+    const bool is_v = part & 1;
+    for (int e0 = 4 * group + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); e0 < n; e0 += 64 * waves) {
+        const int mine = e0 + lane * waves;
+        int from_of = -1, to_of = -1, rows_of = 0;
+        if (mine < n) {
+            from_of = copies[mine];
+            to_of = copies[n + mine];
+            rows_of = min(copies[2 * (long)n + mine], 1 << c.page_shift);
         }
-        if (bounds.codes && !is_v) {
-            const size_t a = (size_t)from * c.kv_heads + head, b = (size_t)to * c.kv_heads + head;
-            if (lane < 2 * D / 16) reinterpret_cast<v4i *>(bounds.codes + b * 2 * D)[lane] = reinterpret_cast<const v4i *>(bounds.codes + a * 2 * D)[lane];
-            if (lane == 0) bounds.steps[b] = bounds.steps[a];
+        const bool copied = (unsigned)from_of < (unsigned)c.pages && (unsigned)to_of < (unsigned)c.pages && rows_of > 0 && from_of != to_of;
+        for (unsigned long long left = __ballot(copied); left; left &= left - 1) {
+            const int owner = __builtin_ctzll(left);
+            copy_part<D>(c, bounds, __builtin_amdgcn_readlane(from_of, owner), __builtin_amdgcn_readlane(to_of, owner), __builtin_amdgcn_readlane(rows_of, owner), head, is_v, lane);
         }
     }
 }
@@ -785,7 +798,8 @@ hipError_t launch_pages_compact(const int *refs, int pages, const int *table, in
 
 hipError_t launch_cache_copy(const KvCache &c, int D, const KeyBounds &bounds, const int *copies, int n, hipStream_t st)
 {
-    const unsigned blocks = blocks_for((2l * n * c.kv_heads + 3) / 4, 8192);
+    const int parts = 2 * c.kv_heads;
+    const unsigned blocks = parts * blocks_for((n + 3l) / 4, max(1, 8192 / parts));
     auto kern = D == 128 ? cache_copy_kernel<128> : cache_copy_kernel<64>;
     hipLaunchKernelGGL(kern, dim3(blocks), dim3(256), 0, st, c, bounds, copies, n);
     return hipGetLastError();

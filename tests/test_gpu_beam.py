@@ -105,6 +105,21 @@ def test_equal_logits_take_the_lowest_row_then_token(P, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
+@pytest.mark.parametrize("rows,V", [(4, 1000), (4, 33001), (260, 45003)])
+def test_few_tokens_above_many_of_one_value(P, dtype, rows, V):
+    """Masks that leave some tokens and set the others to one finite value: those behind the best are the first of the masked ones.  And few values in all."""
+    g = gen(V)
+    mask = {F16: torch.finfo(F16).min, BF16: -1e4, F32: torch.finfo(F32).min}[dtype]
+    x = torch.full((rows, V), mask, dtype=dtype)
+    for r in range(rows):
+        allowed = torch.randint(0, V, (r % 12,), generator=g)
+        x[r, allowed] = torch.randn(len(allowed), generator=g).to(dtype)
+    check(P, x, -torch.rand(rows, generator=g), 4, 8)
+    check(P, x, -torch.rand(rows, generator=g), 2, 64)
+    check(P, torch.randint(-2, 3, (rows, V), generator=g).to(dtype), -torch.rand(rows, generator=g), 4, 16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
 def test_logits_that_rise_or_fall_all_along(P, dtype):
     """The best of a row lie next to each other: in one thread's registers, or in one after the other's."""
     for V in (900, 16384, 33001):
@@ -190,7 +205,7 @@ def test_rows_further_apart_than_32_bits(P):
 @pytest.mark.parametrize("keep", [16, 64])
 def test_long_pieces_of_every_kind_of_row(P, dtype, keep):
     """A batch whose rows are cut into long pieces: rows in no order, of one value, rising, falling, of few values, masked by minus infinity or the type's lowest value."""
-    B, W, V = 66, 8, 40003
+    B, W, V = 66, 8, 45003
     x = torch.randn(B * W, V, generator=gen(keep))
     at = torch.arange(V)
     x[0::9] = 1.5

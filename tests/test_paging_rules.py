@@ -53,7 +53,7 @@ def test_pieces_cover_a_row_that_begins_anywhere(rules):
 
 
 def test_both_pieces_are_tested(rules):
-    assert rules.large(0, 65 * 8, 33001) and rules.large(1, 65 * 8, 33001) and rules.large(0, 66 * 8, 40003) and rules.large(1, 66 * 8, 40003)
+    assert not rules.large(0, 65 * 8, 33001) and rules.large(1, 65 * 8, 33001) and rules.large(0, 66 * 8, 45003) and rules.large(1, 66 * 8, 45003)
     assert rules.large(1, 2, 1 << 19) == 0 and rules.large(0, 160, 32000) == 0 and rules.large(1, 160, 32000)
 
 
