@@ -318,8 +318,8 @@ __global__ __launch_bounds__(SCORED_TOGETHER, 4) void select_pages_kernel(const 
 }
 
 // Scores that are there already.  They are counted in BINS steps between the smallest and the largest; the pages of the step in which the `keep`-th largest lies are ranked by counting, and
-// where they are too many (equal scores), that score is found eight bits at a time.  A chain of steps on one CU a key head: 8 blocks of 1563 pages 6.2 us, 512 of up to 512 5.9, 64 of
-// 4688 9.4.
+// where they are too many (equal scores), that score is found eight bits at a time.  A chain of steps on one CU a key head: 8 blocks of 1563 pages 5.5 us, 512 of up to 512 5.1, 8 of
+// 32768 28.
 __global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows rows, int keep, int sinks, int recent, const unsigned *__restrict__ scores,
                                                              int *__restrict__ tables, int *__restrict__ lens_out)
 {
@@ -340,24 +340,26 @@ __global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows r
     int *const to = tables + (size_t)blockIdx.x * keep;
     if (keeps_all(c, rows, seen, keep, to, lens_out)) return;
     for (int i = tid; i < BINS; i += step) count[i] = 0;
-    for (int i = tid; i < groups; i += step) bits[i] = 0;
     if (tid == 0) listed = 0;
-    for (int p0 = tid; p0 < pages; p0 += 4 * step) {
-#pragma unroll
-        for (int u = 0; u < 4; u++) {
-            if (p0 >= 4 * step) x[u] = from[min(p0 + u * step, pages - 1)];
-            if (p0 + u * step < pages) score[p0 + u * step] = x[u];
-        }
-    }
-
-    // steps of the scores that are finite (a thread has the pages whose scores it wrote)
+    // steps of the scores that are finite
     float low = INFINITY, high = -INFINITY;
-    for (int p = 64 * w + lane; p < pages; p += 64 * waves) {
-        const float x = value_of_order(score[p]);
-        if (score[p] != ALWAYS && __builtin_isfinite(x)) {
-            low = __builtin_fminf(low, x);
-            high = __builtin_fmaxf(high, x);
+    auto have = [&](int p, unsigned x) __attribute__((always_inline)) {
+        if (p >= pages) return;
+        score[p] = x;
+        const float value = value_of_order(x);
+        if (x != ALWAYS && __builtin_isfinite(value)) {
+            low = __builtin_fminf(low, value);
+            high = __builtin_fmaxf(high, value);
         }
+    };
+#pragma unroll
+    for (int u = 0; u < 4; u++) have(tid + u * step, x[u]);
+    for (int p0 = tid + 4 * step; p0 < pages; p0 += 8 * step) {
+        unsigned more[8];
+#pragma unroll
+        for (int u = 0; u < 8; u++) more[u] = from[min(p0 + u * step, pages - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; u++) have(p0 + u * step, more[u]);
     }
     low = -wave_max(-low);
     high = wave_max(high);
@@ -402,24 +404,29 @@ __global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows r
     }
     lds_barrier();
     const int step_of_last = found[0], left = want - found[1];
-    for (int p = 64 * w + lane; p < pages; p += 64 * waves) {
-        if (score[p] == ALWAYS || bin_of(score[p]) != step_of_last) continue;
-        const int at = atomicAdd(&listed, 1);                         // (in any order: they are ranked)
-        if (at < LIST) list[at] = Scored{score[p], p};
+    for (int p0 = 64 * w; p0 < pages; p0 += 64 * waves) {
+        const int p = p0 + lane;
+        const unsigned x = score[min(p, pages - 1)];
+        const int bin = p >= pages ? -1 : x == ALWAYS ? BINS + 1 : bin_of(x);      // (found[0] is BINS where only those that are always kept are)
+        const unsigned long long word = __ballot(bin > step_of_last);
+        if (lane == 0) bits[p0 >> 6] = word;
+        if (bin == step_of_last && x != ALWAYS) {
+            const int at = atomicAdd(&listed, 1);                     // (in any order: they are ranked)
+            if (at < LIST) list[at] = Scored{x, p};
+        }
     }
     lds_barrier();
     const int n = listed;
-    unsigned least = 0;                                               // scores above it are kept too, of pages of that step
     if (n <= LIST) {
         for (int i = tid; i < n; i += blockDim.x) {
             const Scored mine = list[i];
             int better = 0;
 #pragma unroll 4
-            for (int j = 0; j < n; j++) better += list[j].score > mine.score || (list[j].score == mine.score && list[j].page < mine.page);
+            for (int j = 0; j < n; j++) better += (list[j].score > mine.score) | ((list[j].score == mine.score) & (list[j].page < mine.page));
             if (better < left) atomicOr(&bits[mine.page >> 6], 1ull << (mine.page & 63));
         }
-        least = ALWAYS;
     } else {
+        unsigned least = 0;                                           // scores above it are kept too, of pages of that step
         int rest = left;
         for (int shift = 24; shift >= 0; shift -= 8) {
             lds_barrier();
@@ -465,25 +472,28 @@ __global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows r
                 before += __shfl(upto, 63, 64);
             }
         }
+        lds_barrier();
+        for (int p0 = 64 * w; p0 < pages; p0 += 64 * waves) {
+            const unsigned x = p0 + lane < pages ? score[p0 + lane] : 0;
+            const int bin = x == ALWAYS ? BINS : bin_of(x);
+            const unsigned long long word = __ballot(p0 + lane < pages && (x == ALWAYS || bin > step_of_last || (bin == step_of_last && x > least)));
+            if (lane == 0) bits[p0 >> 6] |= word;
+        }
     }
     lds_barrier();
-    for (int p0 = 64 * w; p0 < pages; p0 += 64 * waves) {
-        const unsigned x = p0 + lane < pages ? score[p0 + lane] : 0;
-        const int bin = x == ALWAYS ? BINS : bin_of(x);
-        const unsigned long long word = __ballot(p0 + lane < pages && (x == ALWAYS || bin > step_of_last || (bin == step_of_last && x > least)));
-        if (lane == 0) bits[p0 >> 6] |= word;
-    }
-    lds_barrier();
+    // the pages that are kept, in order, where the scores were; then their numbers
     int before = 0;
     for (int i0 = 0; i0 < groups; i0 += 64) {
         const int upto = wave_scan(i0 + lane < groups ? __popcll(bits[i0 + lane]) : 0);
         for (int i = (i0 + waves - 1 - w) / waves * waves + w; i < min(i0 + 64, groups); i += waves) {
             const unsigned long long word = bits[i];
             const int at = before + (i > i0 ? __builtin_amdgcn_readlane(upto, max(i - i0 - 1, 0)) : 0);
-            if (word >> lane & 1) to[at + __popcll(word & ((1ull << lane) - 1))] = table[64 * i + lane];
+            if (word >> lane & 1) score[at + __popcll(word & ((1ull << lane) - 1))] = 64 * i + lane;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
+    lds_barrier();
+    for (int i = tid; i < keep; i += step) to[i] = table[score[i]];
 }
 
 template <bool BF, int D>

@@ -168,6 +168,8 @@ def test_attention_sparse_of_long_contexts(P, dtype):
     run_sparse(P, [9000, 70, 20000], [1, 1, 1], 8, 2, 128, 16, 300, 1, 1, dtype, seed=1)
     run_sparse(P, [16 * 1500 + 3], [2], 4, 1, 64, 16, 40, 1, 2, dtype, seed=2, topic=0.0)
     run_sparse(P, [5000, 4000], [40, 1], 8, 2, 64, 32, 20, 2, 3, dtype, seed=3)        # more rows than one product has columns
+    run_sparse(P, [16 * 300, 16 * 299 + 1, 30], [1, 1, 1], 4, 2, 64, 16, 3, 1, 2, dtype, seed=4)              # none but those that are always kept
+    run_sparse(P, [16 * 600], [1], 4, 2, 64, 16, 599, 0, 1, dtype, seed=5)             # all but one
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
