@@ -47,10 +47,11 @@ template <int HALF, bool MAX> __device__ __forceinline__ float share(float a, fl
     return MAX ? max3(x, x, y) : min3(x, x, y);
 }
 
-template <int D>
+// AT: keys at a time, 32, or 16 for pages of no more (138 MB in pages of 64 24.8 us; of 16 38.5, bound by the vector ALUs, and 49.0 by the kernel of 32, each key twice)
+template <int D, int AT>
 __global__ __launch_bounds__(256) void cache_bounds_kernel(KvCache c, KeyBounds bounds, KvRows rows)
 {
-    constexpr int LANES = D / 16, KEYS = 64 / LANES, TURN = 32 / KEYS;
+    constexpr int LANES = D / 16, KEYS = 64 / LANES, TURN = AT / KEYS;
     const SeqRows s = seq_rows(rows, blockIdx.z, c.page_shift);
     const int lane = threadIdx.x & 63, from = max(rows.lens[blockIdx.z] - s.n, 0), to = min(rows.lens[blockIdx.z] - s.n + s.todo, s.len);
     const int index = (from >> c.page_shift) + blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), head = blockIdx.x;
@@ -68,21 +69,22 @@ __global__ __launch_bounds__(256) void cache_bounds_kernel(KvCache c, KeyBounds 
         low[e] = INFINITY;
     }
     float odd = 0.0f;                                                 // NaN with a step that is not finite, that of a key that is not
-    for (int i0 = 0; i0 < len; i0 += 32) {                            // (of a page of sixteen each key twice)
+    for (int i0 = 0; i0 < len; i0 += AT) {
         v4i raw[TURN];
         float step[TURN];
 #pragma unroll
         for (int i = 0; i < TURN; i++) {
-            const int key = (i0 + i * KEYS + lane / LANES) & (len - 1);
+            const int key = i0 + i * KEYS + lane / LANES;
             raw[i] = *reinterpret_cast<const v4i *>(k + key * D);
             step[i] = steps[key];
         }
 #pragma unroll
         for (int i = 0; i < TURN; i += 2) {
-            odd += step[i] * 0.0f + step[i + 1] * 0.0f;
+            constexpr int NEXT = TURN > 1;
+            odd += step[i] * 0.0f + step[i + NEXT] * 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; e++) {
-                const float x = (float)(int8_t)(raw[i][e >> 2] >> 8 * (e & 3)) * step[i], y = (float)(int8_t)(raw[i + 1][e >> 2] >> 8 * (e & 3)) * step[i + 1];
+                const float x = (float)(int8_t)(raw[i][e >> 2] >> 8 * (e & 3)) * step[i], y = (float)(int8_t)(raw[i + NEXT][e >> 2] >> 8 * (e & 3)) * step[i + NEXT];
                 high[e] = max3(high[e], x, y);
                 low[e] = min3(low[e], x, y);
             }
@@ -523,7 +525,7 @@ hipError_t launch_cache_bounds(const KvCache &c, int D, const KeyBounds &bounds,
 {
     const int most = min(r.width, ((r.max_rows - 1) >> c.page_shift) + 1);             // pages that max_rows positions in a row can fill
     const dim3 grid((unsigned)c.kv_heads, (unsigned)((most + 3) / 4), (unsigned)r.batch);
-    auto kern = D == 128 ? cache_bounds_kernel<128> : cache_bounds_kernel<64>;
+    auto kern = c.page_shift == 4 ? (D == 128 ? cache_bounds_kernel<128, 16> : cache_bounds_kernel<64, 16>) : D == 128 ? cache_bounds_kernel<128, 32> : cache_bounds_kernel<64, 32>;
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, c, bounds, r);
     return hipGetLastError();
 }
