@@ -70,7 +70,8 @@ def check(P, logits, scores, beams, keep=None, finished=None, end=7, device=None
 
 @pytest.mark.parametrize("dtype", [F16, BF16, F32])
 @pytest.mark.parametrize("B,W,V,keep", [(1, 1, 1, 1), (1, 1, 5, 3), (2, 3, 7, 10), (1, 4, 1000, 4), (3, 2, 4095, 64), (2, 5, 4096, 5), (1, 1, 4097, 2), (3, 4, 21128, 8), (40, 4, 32000, 8),
-                                        (2, 64, 300, 64), (130, 3, 17001, 6), (1, 2, 1 << 19, 4), (65, 8, 33001, 16)])
+                                        (2, 64, 300, 64), (130, 3, 17001, 6), (1, 2, 1 << 19, 4), (65, 8, 33001, 16),
+                                        (1, 13, 1 << 19, 64), (1, 30, 1 << 19, 64), (2, 16, 128256, 32)])                   # long lists in the join, of more LDS than a launch has by itself
 def test_beam_select(P, B, W, V, keep, dtype):
     g = gen(B + W + V)
     x = (torch.randn(B * W, V, generator=g) * 3).to(dtype)
