@@ -62,7 +62,8 @@ inline int cache_passes(long rows, int kv_heads) { return rows * kv_heads >= 327
 // 16 bits 64 x 32000 13.9 / 11.4, 256 x 32000 15.6 / 14.4, 512 x 32000 18.1 / 18.8, 64 x 128256 14.7 / 14.7, 128 x 128256 17.1 / 18.9; binary32, whose short pieces are half as many
 // values, 4 x 21128 11.3 / 9.7, 64 x 32000 12.4 / 12.0, 16 x 128256 12.2 / 14.7, 32 x 128256 13.3 / 16.1, 512 x 32000 20.8 / 25.0, 128 x 128256 20.8 / 27.4.
 // A long piece takes as long as five or six short ones, full or not: 16 bits 1024 x 1000 22.3 / 13.6, 1024 x 16000 21.7 / 19.7, 1024 x 21000 21.7 / 22.3, 1024 x 36000 30.3 / 27.7, 1024 x 50304
-// 29.4 / 36.5; binary32 1024 x 8000 19.0 / 18.3, 1024 x 12000 20.0 / 20.8, 512 x 12000 16.7 / 15.5, 512 x 21000 17.9 / 19.3.
+// 29.4 / 36.5; binary32 1024 x 8000 19.0 / 18.3, 1024 x 12000 20.0 / 20.8, 512 x 12000 16.7 / 15.5, 512 x 21000 17.9 / 19.3.  (Long pieces of 256 threads take as long, with four
+// vectors of 512 up to 2 us longer: 512 x 128256 29.7 and 31.8.)
 struct BeamPiece { int threads, vectors; };
 constexpr BeamPiece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
 inline int piece_chunks(BeamPiece p, bool wide, int vocab)
