@@ -568,6 +568,8 @@ SAMP_API int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_boun
  *   score(page) = max over new tokens and query heads of the key head of  (float) sum_d max(c_d high_d, c_d low_d) * (step_q * step_page)
  * with the codes c of the query's row (the quantiser of a row above), step_q = absmax * (1 / 127) of it (1 and NaN as there) and the page's bounds, the sum a whole number, the products in
  * binary32; NaN counts as plus infinity, a page number that is none of the cache's as minus infinity.
+ * Of a sequence with more new tokens than max_new, and more than `keep` pages, the pages are those up to the last row that is computed (no computed row sees a later position, except that a tree's word
+ * may name a later draft: it is seen only if its page is kept), `recent` the last of them.
  * sinks >= 0, recent at least the pages that max_new positions can lie in ((max_new + page_len - 2) / page_len + 1), sinks + recent <= keep, width <= SAMP_MAX_TABLE.
  * workspace as in samp_linear_i8_tokens.                                                                     */
 SAMP_API size_t samp_cache_select_workspace_bytes(int32_t batch, int32_t kv_heads, int32_t width);

@@ -245,10 +245,16 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
     if (lane < 16 * TILES && p < pages) f(p, mine);
 }
 
-__device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &rows, int b, int head, int group, int sinks, int recent)
+// Of a sequence that keeps only some of its pages and has more new tokens than max_rows, those behind the last row that is computed are none: what follows that row it does not see
+__device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &rows, int b, int head, int group, int keep, int sinks, int recent)
 {
     Seen seen{seq_rows(rows, b, c.page_shift), b, head, group, 0, sinks, recent, rows.table + (size_t)b * rows.width};
-    seen.pages = (max(seen.s.len, 0) + (1 << c.page_shift) - 1) >> c.page_shift;
+    const int last = (1 << c.page_shift) - 1;
+    seen.pages = (max(seen.s.len, 0) + last) >> c.page_shift;
+    if (seen.pages > keep && seen.s.n > seen.s.todo) {
+        const long upto = (long)rows.lens[b] - (seen.s.n - seen.s.todo);
+        if (upto < seen.s.len) seen.pages = (int)(max(upto, 0l) + last) >> c.page_shift;
+    }
     return seen;
 }
 
@@ -263,7 +269,7 @@ __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restr
     const int head = blockIdx.x % c.kv_heads, item = blockIdx.x / c.kv_heads, chunk = item / rows.batch, b = item - chunk * rows.batch;
     const int first = chunk * 4 * OF_WAVE + __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * OF_WAVE), page = first + (threadIdx.x & 63);
     const int entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];              // (on its way with the lengths)
-    const Seen seen = what_is_seen(c, rows, b, head, group, sinks, recent);
+    const Seen seen = what_is_seen(c, rows, b, head, group, keep, sinks, recent);
     if (seen.pages <= keep || chunk * 4 * OF_WAVE >= seen.pages) return;
     unsigned *const to = scores + ((size_t)b * c.kv_heads + head) * rows.width;
     score_pages<BF, D, OF_WAVE / 16>(Q, ldq, c, bounds, seen, first, page < seen.pages ? entry : -1,
@@ -289,7 +295,7 @@ __global__ __launch_bounds__(SCORED_TOGETHER, 4) void select_pages_kernel(const 
     __shared__ unsigned long long bits[WAVES];
     const int b = blockIdx.x / c.kv_heads, page = threadIdx.x, lane = page & 63, w = __builtin_amdgcn_readfirstlane(page >> 6);
     const int entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];
-    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, group, sinks, recent);
+    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, group, keep, sinks, recent);
     int *const to = tables + (size_t)blockIdx.x * keep;
     if (keeps_all(c, rows, seen, keep, to, lens_out)) return;
     if (page >= seen.pages) score[page] = 0;
@@ -336,7 +342,7 @@ __global__ __launch_bounds__(1024) void select_scored_kernel(KvCache c, KvRows r
     unsigned x[4];
 #pragma unroll
     for (int u = 0; u < 4; u++) x[u] = from[min(tid + u * step, rows.width - 1)];              // (on their way with the lengths; what nobody wrote is not used)
-    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, 1, sinks, recent);
+    const Seen seen = what_is_seen(c, rows, b, blockIdx.x - b * c.kv_heads, 1, keep, sinks, recent);
     const int pages = seen.pages, groups = (pages + 63) >> 6;
     const int *const table = seen.table;
     int *const to = tables + (size_t)blockIdx.x * keep;

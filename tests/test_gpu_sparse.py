@@ -352,3 +352,44 @@ def test_sparse_calls_in_graphs_and_on_streams(P):
         want = call()
         for _, out in graphs:
             assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("H,G,D,page", [(8, 2, 64, 16), (4, 4, 128, 32), (7, 1, 64, 16)])
+@pytest.mark.parametrize("lens,new,most,keep", [([700, 900, 40, 330], [100, 7, 3, 300], 4, 5), ([300], [100], 1, 2), ([9000, 500], [200, 1], 3, 20), ([16 * 400, 600], [16 * 390, 2], 2, 14)])
+def test_more_new_tokens_than_the_maximum(P, lens, new, most, keep, H, G, D, page, dtype):
+    """Of a sequence with more new tokens than max_new the first max_new rows are computed: they choose among the pages up to their own and see what attention_cache's rows see of them."""
+    plan = Plan(P, lens, new, G, D, page, seed=H)
+    k, v = (torch.randn(sum(lens), G, D, generator=gen(i)).to(dtype) for i in (1, 2))
+    q = (torch.randn(plan.total, H, D, generator=gen(3)) * 1.5).to(dtype)
+    start = offsets(lens)
+    P.cache_write(plan.cache, k.cuda(), v.cuda(), plan.args[0], start.cuda(), plan.args[2], max(lens))
+    bounds = P.KeyBounds.empty(plan.cache)
+    P.cache_bounds(plan.cache, bounds, plan.args[0], start.cuda(), plan.args[2], max(lens))
+    sinks, recent = 0 if keep == 2 else 1, (most + page - 2) // page + 1
+    tables, short = P.cache_select(q.cuda(), plan.cache, bounds, *plan.args, most, keep, sinks, recent)
+    out = torch.full((plan.total, H, D), 7.0, dtype=dtype, device="cuda")
+    P.attention_sparse(q.cuda(), plan.cache, bounds, *plan.args, most, keep, sinks, recent, out=out)
+    whole = P.attention_cache(q.cuda(), plan.cache, *plan.args, most)
+    codes, steps = bounds.codes.cpu(), bounds.steps.cpu()
+    for b, (n, m) in enumerate(zip(lens, new)):
+        at, todo, pages = int(plan.cu[b]), min(m, most), -(-n // page)
+        if pages > keep:
+            pages = -(-(n - m + todo) // page)
+        chosen = choose_definition(q[at:at + todo], codes, steps, plan.table[b], pages, keep, sinks, recent, H, G)
+        assert int(short[b]) == n - (pages - min(pages, keep)) * page
+        for g in range(G):
+            want = [int(plan.table[b, j]) for j in chosen[g]]
+            assert tables[b, g].tolist() == want + [-1] * (keep - len(want)), (b, g)
+        assert (out[at + todo:at + m] == 7).all()
+        held = [(lambda c, s: c * s[..., None])(*quantised(x[int(start[b]):int(start[b]) + n])) for x in (k, v)]
+        seen = torch.arange(n)[None, :] <= n - m + torch.arange(todo)[:, None]
+        for g in range(G):
+            of = torch.zeros(n, dtype=torch.bool)
+            for j in chosen[g]:
+                of[j * page:(j + 1) * page] = True
+            heads = slice(g * H // G, (g + 1) * H // G)
+            want = attend(q[at:at + todo, heads].double(), held[0][:, g:g + 1], held[1][:, g:g + 1], seen & of, D ** -0.5)
+            check_attention(out[at:at + todo, heads], *want, dtype, F16, n, held[1].abs().max().item())
+            if pages <= keep:
+                check_attention(whole[at:at + todo, heads], *want, dtype, F16, n, held[1].abs().max().item())
