@@ -1,7 +1,10 @@
 // Beam search's selection: the best (score, beam, token) of each sequence over the logits of its beams, total = score + (logit - log sum exp logits).
 //
-// Two launches.  The first reads every logit once: a block takes a piece of a row into registers, finds its largest value, the sum of exponentials under it and its `keep` best
-// logits: totals of a row are in the order of its logits.  The second joins the pieces of a sequence's rows in binary64 and picks among them.
+// Two launches.  The first reads every logit once: a block takes a piece of a row into registers, finds the sums of exponentials of its granules and its `keep` best
+// logits: totals of a row are in the order of its logits.  The second joins a sequence's rows in binary64 and picks among them.
+//
+// How a row is cut depends on the batch, its totals do not, nor on where the row begins: they are compared with other rows', where an equal total has to be equal in every bit.  Sums are formed over
+// granules of 64 vectors of 16 bytes from the row's first value on, each under its own largest value, and over blocks of eight granules, in the same order in every cut; a piece is one block or eight of them.
 //
 // The best of a piece: the `keep`-th largest of the maxima of its groups of threads is no more than the `keep`-th largest value of all.  What reaches it (18 values for keep = 16 and
 // logits in no order) goes to a list in LDS, which is ranked by counting.
@@ -19,8 +22,11 @@ constexpr int SLOTS = 128, ROOM = 512;                                // threads
 constexpr float LOG2E = 1.44269504088896340736f;                      // (1.3e-8 of it off: as much of the mean distance from the largest logit, 2e-7 at most)
 
 enum { F16 = 0, BF16 = 1, F32 = 2 };
+typedef int v4i_at_2 __attribute__((ext_vector_type(4), aligned(2)));              // 16 bytes at any value's address: one load, wherever they lie
+typedef int v4i_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 template <int T> struct Logit {
     static constexpr int SIZE = T == F32 ? 4 : 2, VEC = 16 / SIZE;
+    typedef typename std::conditional<T == F32, v4i_at_4, v4i_at_2>::type Raw;
     static constexpr unsigned MINUS_INF_BITS = T == F16 ? 0xfc00u : T == BF16 ? 0xff80u : 0xff800000u;
     static __device__ __forceinline__ float value(const v4i &raw, int e)
     {
@@ -35,14 +41,6 @@ template <int T> struct Logit {
         else return (float)static_cast<const _Float16 *>(at)[i];
     }
 };
-// (the compiler's own maxima quiet signalling NaN in front: another instruction each)
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-template <int CTRL> __device__ __forceinline__ float other_lane(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); }
 __device__ __forceinline__ float max_of_wave(float x)
 {
     x = max3(x, x, other_lane<0xb1>(x));                              // lanes 1 0 3 2, then 2 3 0 1 of four, eight mirrored, sixteen mirrored
@@ -53,19 +51,28 @@ __device__ __forceinline__ float max_of_wave(float x)
     const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 32)), d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 48));
     return max3(max3(a, b, c), d, d);
 }
-__device__ __forceinline__ float sum_of_wave(float x)
+// Of each of N values the largest (the sum) over the wave, in the lanes GRAIN n .. GRAIN n + GRAIN - 1 that of value n.  Lanes meet in the same order for every N
+template <bool MAX> __device__ __forceinline__ float met(const Met &m) { return MAX ? max3(m.x, m.x, m.y) : m.x + m.y; }
+template <bool MAX, int N> __device__ __forceinline__ float of_each(float (&x)[N], int lane)
 {
-    x += other_lane<0xb1>(x);
-    x += other_lane<0x4e>(x);
-    x += other_lane<0x141>(x);
-    x += other_lane<0x140>(x);
-    const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 0)), b = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 16));
-    const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 32)), d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 48));
-    return (a + b) + (c + d);
+    static_assert(N == 2 || N == 8, "pieces have two vectors a thread or eight");
+    constexpr int A = N / 2, B = N == 8 ? 2 : 1;
+    float a[A], b[B], c;
+    if constexpr (MAX) settle(x);
+#pragma unroll
+    for (int i = 0; i < A; i++) a[i] = met<MAX>(meet<32>(x[i], x[i + A], lane));
+    if constexpr (MAX) settle(a);
+#pragma unroll
+    for (int i = 0; i < B; i++) b[i] = met<MAX>(meet<16>(a[i], a[i + (N == 8 ? B : 0)], lane));
+    c = met<MAX>(meet<8>(b[0], b[B - 1], lane));
+    c = met<MAX>(Met{c, other_lane<0x141>(c)});                       // eight mirrored, then lanes 2 3 0 1 of four, 1 0 3 2
+    c = met<MAX>(Met{c, other_lane<0x4e>(c)});
+    return met<MAX>(Met{c, other_lane<0xb1>(c)});
 }
 
 struct Candidate { float logit; int token; };                         // token -1: none
-struct PieceSum { float top, sum; };                                  // sum of exp(x - top)
+constexpr int BLOCK_OF = 8;                                           // granules of a block
+struct BlockSum { float top, sum; };                                  // sum of exp(x - top)
 // A number of the order of the value (one zero; not for NaN); with the place behind it, the lower one first
 __device__ __forceinline__ unsigned order_of(float x)
 {
@@ -113,45 +120,46 @@ __device__ __forceinline__ bool row_counts(const float *scores, const uint8_t *f
 
 // One piece of one row: what bounds it is HBM where there are rows enough (512 rows of 128256, of which a quarter are finished or have no score and are not read: 97 MB, 24.2 us, 4.0 TB/s;
 // the vector ALUs issue half of that time, nine instructions a logit), else its chain of one trip to memory, two reductions and the list: 35 rows of 50265
-// binary32 6.4 us, 4 rows of 21128 4.6.  Vectors of 16 bytes are numbered from the aligned address at or before the row's first value; what of them lies outside the row counts as minus infinity.
+// binary32 6.4 us, 4 rows of 21128 4.6.  Vectors of 16 bytes are counted from the row's first value, wherever that lies; what of the last one lies behind the row counts as minus infinity.
 template <int T, int THREADS, int VECTORS, int GROUPS>
 __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__restrict__ logits, long ld, const float *__restrict__ scores,
                                                               const uint8_t *__restrict__ finished, int vocab, int keep, int chunks,
-                                                              PieceSum *__restrict__ sums, Candidate *__restrict__ best)
+                                                              BlockSum *__restrict__ sums, Candidate *__restrict__ best)
 {
     typedef Logit<T> L;
-    constexpr int VEC = L::VEC, PER = VECTORS * VEC, TEAM = THREADS / GROUPS, WAVES = THREADS / 64;
+    constexpr int VEC = L::VEC, PER = VECTORS * VEC, TEAM = THREADS / GROUPS, WAVES = THREADS / 64, GRANULES = WAVES * VECTORS, GRAIN = 64 / VECTORS;
+    static_assert(GRANULES % BLOCK_OF == 0 && GRANULES <= 64, "whole blocks, a granule a lane");
     static_assert(GROUPS == 64 || (GROUPS % 64 == 0 && TEAM <= 2), "the same lane of every wave, or one or two neighbours");
     __shared__ __attribute__((aligned(16))) unsigned long long list[ROOM];
     __shared__ __attribute__((aligned(16))) v4i held[SLOTS][VECTORS];
     __shared__ int owner[SLOTS];
     __shared__ __attribute__((aligned(16))) float tops[GROUPS == 64 ? THREADS : GROUPS];
-    __shared__ float wave_top[WAVES], wave_sum[WAVES], least[GROUPS / 64];
+    __shared__ float granule_top[GRANULES], granule_sum[GRANULES], least[GROUPS / 64];
     __shared__ int slots, listed, wave_count[WAVES];
 
     const int row = blockIdx.x / chunks, piece = blockIdx.x - row * chunks;
     if (VECTORS > 2 && !row_counts(scores, finished, row)) return;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const char *from = logits + (size_t)row * ld * L::SIZE;
-    const int phase = (int)(reinterpret_cast<uintptr_t>(from) & 15) / L::SIZE;
-    const int first = piece * THREADS * PER - phase;                  // token of the piece's first place
+    const int first = piece * THREADS * PER;                          // the piece's first token
 
     v4i raw[VECTORS];
-    if (first >= 0 && first + THREADS * PER <= vocab) {
-        const v4i *const all = reinterpret_cast<const v4i *>(from + (long)first * L::SIZE) + tid;
+    typedef typename L::Raw Raw;
+    if (first + THREADS * PER <= vocab) {
+        const Raw *const all = reinterpret_cast<const Raw *>(from + (long)first * L::SIZE) + tid;
 #pragma unroll
         for (int i = 0; i < VECTORS; i++) raw[i] = all[i * THREADS];
     } else {
 #pragma unroll
         for (int i = 0; i < VECTORS; i++) {
             const int at = first + (i * THREADS + tid) * VEC;
-            if (at >= 0 && at + VEC <= vocab) raw[i] = *reinterpret_cast<const v4i *>(from + (long)at * L::SIZE);
+            if (at + VEC <= vocab) raw[i] = *reinterpret_cast<const Raw *>(from + (long)at * L::SIZE);
             else {
                 unsigned x[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; e++) {
                     x[e] = L::MINUS_INF_BITS;
-                    if (at + e >= 0 && at + e < vocab) {
+                    if (at + e < vocab) {
                         if constexpr (T == F32) x[e] = *reinterpret_cast<const unsigned *>(from + (long)(at + e) * 4);
                         else x[e] = *reinterpret_cast<const unsigned short *>(from + (long)(at + e) * 2);
                     }
@@ -164,17 +172,23 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
     // (a short piece waits for its logits and for the row's flags at the same time)
     if (VECTORS <= 2 && !row_counts(scores, finished, row)) return;
     if (tid == 0) slots = listed = 0;
-    float top = -INFINITY;
+    float each[VECTORS];
 #pragma unroll
-    for (int i = 0; i < VECTORS; i++)
+    for (int i = 0; i < VECTORS; i++) {
+        each[i] = max3(L::value(raw[i], 0), L::value(raw[i], 1), L::value(raw[i], 2));
 #pragma unroll
-        for (int e = 0; e < VEC; e += 2) top = max3(top, L::value(raw[i], e), L::value(raw[i], e + 1));
+        for (int e = 3; e < VEC; e += 2) each[i] = max3(each[i], L::value(raw[i], e), L::value(raw[i], min(e + 1, VEC - 1)));
+    }
+    float top = max3(each[0], each[0], each[1]);
+#pragma unroll
+    for (int i = 2; i < VECTORS; i += 2) top = max3(top, each[i], each[i + 1]);
     if constexpr (GROUPS == 64) tops[tid] = top;
     else {
         const float pair = TEAM == 2 ? max3(top, top, other_lane<0xb1>(top)) : top;
         if (tid % TEAM == 0) tops[tid / TEAM] = pair;
     }
-    float m = max_of_wave(top);
+    // the largest of the granule of vector lane / GRAIN of the wave's threads
+    float m = of_each<true>(each, lane);
     if (m == -INFINITY) m = 0.0f;
     // (converted again for each use: 32 registers, and waves enough to wait for memory.  With the values kept, 178 registers, 64 x 8 x 128256 took 84 us)
     auto again = [&]() {
@@ -184,27 +198,34 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
     again();
     // exp(x - m) as 2^(x log2(e) - reference), one multiply-add in front of each; the reference is m log2(e) but for its rounding, at most 1, which the sum makes
     // up for.  Of larger logits (a row of the type's lowest value) the difference comes first.
-    float part[4] = {}, sum;
-    if (__builtin_fabsf(m) < 0x1p24f) {
-        const float reference = m * LOG2E;
+    constexpr float PLAIN = 0x1p24f;
+    float sums_of[VECTORS];
 #pragma unroll
-        for (int i = 0; i < VECTORS; i++)
+    for (int i = 0; i < VECTORS; i++) {
+        const float reference = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), GRAIN * i)) * LOG2E;
+        float part[4] = {};
 #pragma unroll
-            for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(L::value(raw[i], e), LOG2E, -reference));
-        sum = ((part[0] + part[1]) + (part[2] + part[3])) * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, LOG2E, -reference));
-    } else {
+        for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(L::value(raw[i], e), LOG2E, -reference));
+        sums_of[i] = (part[0] + part[1]) + (part[2] + part[3]);
+    }
+    if (__any(!(__builtin_fabsf(m) < PLAIN))) {
         again();
 #pragma unroll
-        for (int i = 0; i < VECTORS; i++)
+        for (int i = 0; i < VECTORS; i++) {
+            const float of = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), GRAIN * i));
+            if (__builtin_fabsf(of) < PLAIN) continue;
+            float part[4] = {};
 #pragma unroll
-            for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f((L::value(raw[i], e) - m) * LOG2E);
-        sum = (part[0] + part[1]) + (part[2] + part[3]);
+            for (int e = 0; e < VEC; e++) part[e & 3] += __builtin_amdgcn_exp2f((L::value(raw[i], e) - of) * LOG2E);
+            sums_of[i] = (part[0] + part[1]) + (part[2] + part[3]);
+        }
     }
     again();
-    sum = sum_of_wave(sum);
-    if (lane == 0) {
-        wave_top[w] = m;
-        wave_sum[w] = sum;
+    float sum = of_each<false>(sums_of, lane);
+    if (__builtin_fabsf(m) < PLAIN) sum *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, LOG2E, -(m * LOG2E)));
+    if (lane % GRAIN == 0) {
+        granule_top[lane / GRAIN * WAVES + w] = m;
+        granule_sum[lane / GRAIN * WAVES + w] = sum;
     }
     __syncthreads();
     if (tid < GROUPS) {
@@ -227,10 +248,17 @@ __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__r
         if (lane == 0) least[w] = t;
     }
     if (w == WAVES - 1) {
-        const float u = lane < WAVES ? wave_top[lane] : -INFINITY, all = max_of_wave(lane < WAVES && wave_sum[lane] != 0.0f ? u : -INFINITY);
-        const float s = lane < WAVES && wave_sum[lane] != 0.0f ? wave_sum[lane] * __builtin_amdgcn_exp2f((u - all) * LOG2E) : 0.0f;
-        const float total = sum_of_wave(s);
-        if (lane == 0) sums[blockIdx.x] = PieceSum{all, total};
+        // eight neighbouring lanes have a block's granules
+        const bool some = lane < GRANULES && granule_sum[lane % GRANULES] != 0.0f;
+        const float u = some ? granule_top[lane % GRANULES] : -INFINITY;
+        float all = max3(u, u, other_lane<0xb1>(u));
+        all = max3(all, all, other_lane<0x4e>(all));
+        all = max3(all, all, other_lane<0x141>(all));
+        float s = some ? granule_sum[lane % GRANULES] * __builtin_amdgcn_exp2f((u - all) * LOG2E) : 0.0f;
+        s += other_lane<0xb1>(s);
+        s += other_lane<0x4e>(s);
+        s += other_lane<0x141>(s);
+        if (lane < GRANULES && lane % BLOCK_OF == 0) sums[(size_t)blockIdx.x * (GRANULES / BLOCK_OF) + lane / BLOCK_OF] = BlockSum{all, s};
     }
     __syncthreads();
     float limit = least[0];
@@ -421,8 +449,8 @@ template <class F> __device__ __forceinline__ void rank_best(const Entry *all, i
 }
 
 // A block a sequence.  A few dependent steps over some thousand numbers: 7.3 us for 64 sequences of 8 rows in 4 pieces each, keep = 16; 5.6 for one of 4 rows in 6.
-__global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restrict__ sums, const Candidate *__restrict__ best, const float *__restrict__ scores,
-                                                         const uint8_t *__restrict__ finished, int end, int beams, int keep, int chunks, float *__restrict__ out,
+__global__ __launch_bounds__(JOIN) void beam_join_kernel(const BlockSum *__restrict__ sums, const Candidate *__restrict__ best, const float *__restrict__ scores,
+                                                         const uint8_t *__restrict__ finished, int end, int beams, int keep, int chunks, int blocks, float *__restrict__ out,
                                                          int *__restrict__ parents, int *__restrict__ tokens)
 {
     extern __shared__ __attribute__((aligned(16))) Entry first[];
@@ -446,14 +474,14 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
     if (tid < keep) list_of[tid] = -1;
     if (tid == 0) there = 0, enough = 0;
     for (int r = w; r < beams; r += JOIN / 64) {
-        const PieceSum *const of = sums + (row0 + r) * chunks;
-        const PieceSum mine = lane < chunks ? of[lane] : PieceSum{0.0f, 0.0f};
+        const BlockSum *const of = sums + (row0 + r) * blocks;
+        const BlockSum mine = lane < blocks ? of[lane] : BlockSum{0.0f, 0.0f};
         float top = mine.sum == 0.0f ? -INFINITY : mine.top;          // (a sum of 0: nothing finite there)
-        for (int c = lane + 64; c < chunks; c += 64)
+        for (int c = lane + 64; c < blocks; c += 64)
             if (!(of[c].sum == 0.0f)) top = __builtin_fmaxf(top, of[c].top);
         top = wave_max(top);
         double sum = mine.sum == 0.0f ? 0.0 : (double)mine.sum * exp((double)mine.top - (double)top);
-        for (int c = lane + 64; c < chunks; c += 64)
+        for (int c = lane + 64; c < blocks; c += 64)
             if (!(of[c].sum == 0.0f)) sum += (double)of[c].sum * exp((double)of[c].top - (double)top);
         sum = wave_sum(sum);
         // (no finite logit: a sum of 0; NaN or plus infinity: a sum of NaN)
@@ -505,7 +533,7 @@ __global__ __launch_bounds__(JOIN) void beam_join_kernel(const PieceSum *__restr
 }
 
 template <int T, int THREADS, int VECTORS>
-void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, int chunks, PieceSum *sums, Candidate *best,
+void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, int chunks, BlockSum *sums, Candidate *best,
             hipStream_t st)
 {
     auto kern = keep <= 16 ? beam_pieces_kernel<T, THREADS, VECTORS, 64> : beam_pieces_kernel<T, THREADS, VECTORS, 256>;
@@ -513,7 +541,7 @@ void pieces(const void *logits, long ld, const float *scores, const uint8_t *fin
                        vocab, keep, chunks, sums, best);
 }
 template <int T>
-void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, BeamCut cut, PieceSum *sums, Candidate *best,
+void pieces(const void *logits, long ld, const float *scores, const uint8_t *finished, int rows, int vocab, int keep, BeamCut cut, BlockSum *sums, Candidate *best,
             hipStream_t st)
 {
     if (cut.large) pieces<T, LONG_PIECE.threads, LONG_PIECE.vectors>(logits, ld, scores, finished, rows, vocab, keep, cut.chunks, sums, best, st);
@@ -525,13 +553,15 @@ void pieces(const void *logits, long ld, const float *scores, const uint8_t *fin
 BeamCut beam_cut(int type, int rows, int vocab)
 {
     const bool wide = type == F32, large = long_pieces(wide, rows, vocab);
-    return BeamCut{large, piece_chunks(large ? LONG_PIECE : SHORT_PIECE, wide, vocab)};
+    const BeamPiece piece = large ? LONG_PIECE : SHORT_PIECE;
+    const int chunks = piece_chunks(piece, wide, vocab);
+    return BeamCut{large, chunks, chunks * (piece.threads * piece.vectors / 64 / BLOCK_OF)};
 }
 
 size_t beam_workspace(int type, int batch, int beams, int vocab, int keep)
 {
     const BeamCut cut = beam_cut(type, batch * beams, vocab);
-    return (size_t)batch * beams * cut.chunks * (sizeof(PieceSum) + (size_t)keep * sizeof(Candidate));
+    return (size_t)batch * beams * (cut.blocks * sizeof(BlockSum) + (size_t)cut.chunks * keep * sizeof(Candidate));
 }
 
 hipError_t launch_beam_select(const void *logits, long ld, int type, const float *scores, const uint8_t *finished, int end, int batch, int beams, int vocab, int keep,
@@ -540,14 +570,14 @@ hipError_t launch_beam_select(const void *logits, long ld, int type, const float
     const BeamCut cut = beam_cut(type, batch * beams, vocab);
     const int rows = batch * beams;
     Candidate *const candidates = static_cast<Candidate *>(ws);
-    PieceSum *const sums = reinterpret_cast<PieceSum *>(candidates + (size_t)rows * cut.chunks * keep);
+    BlockSum *const sums = reinterpret_cast<BlockSum *>(candidates + (size_t)rows * cut.chunks * keep);
     if (type == F16) pieces<F16>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
     else if (type == BF16) pieces<BF16>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
     else pieces<F32>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
     const size_t lds = sizeof(Entry) * ((size_t)beams * cut.chunks + (size_t)keep * (keep + 1) / 2);
     if (lds > 56 << 10)
         if (hipError_t err = hipFuncSetAttribute((const void *)beam_join_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return err;
-    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)batch), dim3(JOIN), lds, st, sums, candidates, scores, finished, end, beams, keep, cut.chunks, best, parents,
+    hipLaunchKernelGGL(beam_join_kernel, dim3((unsigned)batch), dim3(JOIN), lds, st, sums, candidates, scores, finished, end, beams, keep, cut.chunks, cut.blocks, best, parents,
                        tokens);
     return hipGetLastError();
 }

@@ -46,6 +46,42 @@ __device__ __forceinline__ int wave_scan(int x)
     return x;
 }
 
+// The larger of three.  (The compiler's own maxima quiet signalling NaN in front: another instruction each.)  A lane exchange that reads a result has to wait two states, for which the compiler
+// does not look into asm where the exchange is a swap of halves: settle() in front of those.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ void settle(float &a, float &b) { asm("s_nop 1" : "+v"(a), "+v"(b)); }
+__device__ __forceinline__ void settle(float &a, float &b, float &c, float &d) { asm("s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d)); }
+template <int N> __device__ __forceinline__ void settle(float (&x)[N])
+{
+    static_assert(N == 1 || N == 2 || N % 4 == 0, "one, two or fours");
+    if constexpr (N <= 2) settle(x[0], x[N - 1]);
+    else
+#pragma unroll
+        for (int i = 0; i < N; i += 4) settle(x[i], x[i + 1], x[i + 2], x[i + 3]);
+}
+template <int CTRL> __device__ __forceinline__ float other_lane(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); }
+// Lanes l and l ^ HALF of two values: the lower of the two lanes gets the first value of both, the upper the second
+struct Met { float x, y; };
+template <int HALF> __device__ __forceinline__ Met meet(float a, float b, int lane)
+{
+    if constexpr (HALF == 32) {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return Met{__uint_as_float(both[0]), __uint_as_float(both[1])};
+    } else if constexpr (HALF == 16) {
+        const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+        return Met{__uint_as_float(both[0]), __uint_as_float(both[1])};
+    } else {
+        const bool upper = lane & HALF;
+        const int give = __float_as_int(upper ? a : b);
+        return Met{upper ? b : a, __int_as_float(HALF == 8 ? __builtin_amdgcn_update_dpp(0, give, 0x128, 0xf, 0xf, true) : __builtin_amdgcn_ds_swizzle(give, HALF << 10 | 0x1f))};
+    }
+}
+
 // The largest magnitude of 16-bit values, by their bits (two running maxima, in the halves of a dword): infinities come above every number and NaN above them
 typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned max_halves(unsigned a, unsigned b)
@@ -147,7 +183,7 @@ hipError_t launch_causal_attention(const void *q, long ldq, const void *k, long 
                                    int head_dim, const int *cu, int batch, int max_len, int rows, float scale, void *out, hipStream_t st);
 
 // Beam search: type as in samp.h; the bytes of the workspace follow from how a row is cut
-struct BeamCut { bool large; int chunks; };                           // kind and number of a row's pieces
+struct BeamCut { bool large; int chunks, blocks; };                   // kind and number of a row's pieces; blocks whose exponentials are summed
 BeamCut beam_cut(int type, int rows, int vocab);
 size_t beam_workspace(int type, int batch, int beams, int vocab, int keep);
 hipError_t launch_beam_select(const void *logits, long ld, int type, const float *scores, const uint8_t *finished, int end, int batch, int beams, int vocab, int keep,

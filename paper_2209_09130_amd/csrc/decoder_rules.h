@@ -69,7 +69,7 @@ constexpr BeamPiece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
 inline int piece_chunks(BeamPiece p, bool wide, int vocab)
 {
     const int vector = wide ? 4 : 8, values = p.threads * p.vectors * vector;
-    return (vocab + vector - 1 + values - 1) / values;                // (a row may begin `vector` - 1 places behind an aligned address)
+    return (vocab + vector - 1 + values - 1) / values;                // (room for `vector` - 1 values more than a row has: a piece of those alone is empty)
 }
 inline bool long_pieces(bool wide, int rows, int vocab)
 {

@@ -259,3 +259,53 @@ def test_selection_in_graphs_and_on_two_streams(P):
         for _, out in graphs:
             assert all(torch.equal(a, b) for a, b in zip(out, other))
     check(P, x.cpu(), s.cpu(), 4, 8)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_a_sequence_has_the_same_results_alone_in_a_batch_and_at_any_alignment(P, dtype):
+    """The rows of a large batch are cut into long pieces, those of one sequence into short ones, and rows begin at any value: the totals have the same bits."""
+    B, W, V, keep = 66, 8, 45003, 64
+    g = gen(11)
+    rows = (torch.randn(W, V, generator=g) * 3).to(dtype)
+    rows[1, torch.rand(V, generator=g) < 0.3] = -math.inf
+    rows[2] += 5000 if dtype is F32 else 30                  # (references of another size)
+    rows[3, :100] = torch.finfo(dtype).min
+    if dtype is not F16:
+        rows[4] *= 2.0 ** 30
+    scores = -torch.rand(W, generator=g)
+    want = [t.cpu() for t in P.beam_select(rows.cuda(), scores.cuda(), W, keep)]
+    for row in range(W):                                     # (each row's own best, also where others are far ahead)
+        want_row = [t.cpu() for t in P.beam_select(rows[row:row + 1].cuda(), scores[row:row + 1].cuda(), 1, keep)]
+        for shift in range(8):
+            base = torch.zeros(V + shift, dtype=dtype)
+            base[shift:] = rows[row]
+            got = [t.cpu() for t in P.beam_select(base.cuda()[shift:][None], scores[row:row + 1].cuda(), 1, keep)]
+            assert all(torch.equal(a, b) for a, b in zip(got, want_row)), (row, shift)
+    batch, of = torch.randn(B * W, V, generator=g).to(dtype), -torch.rand(B * W, generator=g)
+    for b in (0, 17, 65):
+        batch[b * W:(b + 1) * W], of[b * W:(b + 1) * W] = rows, scores
+    for ld in (V, V + 5):
+        wide = torch.zeros(B * W, ld, dtype=dtype, device="cuda")
+        wide[:, :V] = batch.cuda()
+        best, parents, tokens = (t.cpu() for t in P.beam_select(wide[:, :V], of.cuda(), W, keep))
+        for b in (0, 17, 65):
+            assert torch.equal(best[b], want[0][0]) and torch.equal(parents[b] - b * W, want[1][0]) and torch.equal(tokens[b], want[2][0]), (ld, b)
+    single = [t.cpu() for t in P.beam_select(batch.cuda(), of.cuda(), 1, keep)]              # long pieces, a row each
+    for row in range(W):
+        alone = [t.cpu() for t in P.beam_select(rows[row:row + 1].cuda(), scores[row:row + 1].cuda(), 1, keep)]
+        assert torch.equal(single[0][17 * W + row], alone[0][0]) and torch.equal(single[2][17 * W + row], alone[2][0]), row
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_beams_that_are_alike_tie_wherever_their_rows_begin(P, dtype):
+    """Rows of one content, each at an alignment of its own, have one log-sum-exp: their totals are equal, and the lower row comes first."""
+    for V in (4001, 21127, 50257):
+        x = (torch.randn(1, V, generator=gen(V)) * 2).to(dtype).repeat(8, 1)
+        _, parents, tokens = P.beam_select(x.cuda(), torch.full((8,), -0.25, device="cuda"), 8, 64)
+        order = torch.sort(x[0].double(), descending=True, stable=True).indices
+        want, i = [], 0
+        while len(want) < 64:
+            same = [v for v in order[:200].tolist() if x[0, v] == x[0, order[i]]]
+            want += [(r, v) for r in range(8) for v in same]
+            i += len(same)
+        assert list(zip(parents[0].tolist(), tokens[0].tolist())) == want[:64], V
