@@ -191,9 +191,9 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
 #pragma unroll
         for (int i = 0; i < STEPS; i++) bf[t][i] = *reinterpret_cast<const v4i *>(from + 64 * i);
     }
-    unsigned best[TILES];                                             // of the lane's rows of queries
+    unsigned best[TILES];                                             // of the lane's rows of queries: minus infinity without any, as for a page that is none of the cache's
 #pragma unroll
-    for (int t = 0; t < TILES; t++) best[t] = 0;
+    for (int t = 0; t < TILES; t++) best[t] = order_of(-INFINITY);
     for (int r0 = 0; r0 < all; r0 += 16) {
         const unsigned top = max_of_16_lanes(bits_max16(raw));
         const RowQuant q = row_quant<BF>(top);

@@ -393,3 +393,25 @@ def test_more_new_tokens_than_the_maximum(P, lens, new, most, keep, H, G, D, pag
             check_attention(out[at:at + todo, heads], *want, dtype, F16, n, held[1].abs().max().item())
             if pages <= keep:
                 check_attention(whole[at:at + todo, heads], *want, dtype, F16, n, held[1].abs().max().item())
+
+
+@pytest.mark.parametrize("pages", [40, 256, 257, 600])
+def test_holes_of_a_sequence_without_new_tokens(P, pages):
+    """Without new tokens all pages score minus infinity, those that are none of the cache's too: the earlier ones are kept, however many pages there are."""
+    page, G, D, keep = 16, 2, 64, 9
+    plan = Plan(P, [16 * pages, 16 * pages - 5], [0, 1], G, D, page)
+    plan.fill(P, F16, 3)
+    bounds = P.KeyBounds.empty(plan.cache)
+    P.cache_bounds(plan.cache, bounds, plan.args[0], None, plan.args[2], 16 * pages)
+    table = plan.args[0].clone()
+    holes = [3, 7, pages // 2, pages - 9]
+    table[:, holes] = -1
+    q = torch.randn(1, 4, D, generator=gen(5)).half()
+    tables, lens = P.cache_select(q.cuda(), plan.cache, bounds, table, *plan.args[1:], 1, keep, 1, 2)
+    for b in range(2):
+        want = choose_definition(q[:b], bounds.codes.cpu(), bounds.steps.cpu(), table[b].cpu(), pages, keep, 1, 2, 4, G)
+        assert int(lens[b]) == 16 * pages - 5 * b - (pages - keep) * page
+        for g in range(G):
+            assert tables[b, g].tolist() == [int(table[b, j]) for j in want[g]], (b, g)
+        if b == 0:
+            assert want[0] == [0, 1, 2, 3, 4, 5, 6, pages - 2, pages - 1]
