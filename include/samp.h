@@ -514,7 +514,7 @@ enum { SAMP_TYPE_F32 = 2 };                /* logits only */
  * larger logit, then the lower token.  A total of minus infinity is no candidate; neither are those of a row whose score is
  * not finite, or whose logits hold NaN or plus infinity.
  * best dev float [batch, keep]: the totals; parents dev int32: rows; tokens dev int32.  Behind the last candidate: minus infinity, -1, -1.
- * beams <= SAMP_MAX_BEAMS, keep <= SAMP_MAX_KEEP, vocab <= SAMP_MAX_VOCAB, 1 to 8192 sequences.  workspace as in samp_linear_i8_tokens.        */
+ * beams <= SAMP_MAX_BEAMS, keep <= SAMP_MAX_KEEP, vocab <= SAMP_MAX_VOCAB, 1 to 8192 sequences; more logits than a launch of 2^32 threads takes are refused.  workspace as in samp_linear_i8_tokens.        */
 SAMP_API size_t samp_beam_select_workspace_bytes(int32_t type, int32_t batch, int32_t beams, int32_t vocab, int32_t keep);
 SAMP_API int samp_beam_select(const void *logits, int64_t ld, int32_t type, const float *scores, const uint8_t *finished, int32_t end, int32_t batch,
                               int32_t beams, int32_t vocab, int32_t keep, float *best, int32_t *parents, int32_t *tokens, void *workspace,
@@ -570,7 +570,7 @@ SAMP_API int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_boun
  * binary32; NaN counts as plus infinity, a page number that is none of the cache's as minus infinity.
  * Of a sequence with more new tokens than max_new, and more than `keep` pages, the pages are those up to the last row that is computed (no computed row sees a later position, except that a tree's word
  * may name a later draft: it is seen only if its page is kept), `recent` the last of them.
- * sinks >= 0, recent at least the pages that max_new positions can lie in ((max_new + page_len - 2) / page_len + 1), sinks + recent <= keep, width <= SAMP_MAX_TABLE.
+ * sinks >= 0, recent at least the pages that max_new positions can lie in ((max_new + page_len - 2) / page_len + 1), sinks + recent <= keep, width <= SAMP_MAX_TABLE, batch * kv_heads * ((width + 127) / 128) < 2^24 (a launch's threads).
  * workspace as in samp_linear_i8_tokens.                                                                     */
 SAMP_API size_t samp_cache_select_workspace_bytes(int32_t batch, int32_t kv_heads, int32_t width);
 SAMP_API int samp_cache_select(const uint16_t *q, int64_t ldq, int32_t type, int32_t heads, const samp_kv_cache_t *cache, const samp_key_bounds_t *bounds,

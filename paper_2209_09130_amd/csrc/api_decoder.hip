@@ -110,6 +110,7 @@ int check_beams(int32_t type, int32_t batch, int32_t beams, int32_t vocab, int32
     if (batch < 1 || batch > SAMP_MAX_BATCH || beams < 1 || beams > SAMP_MAX_BEAMS || vocab < 1 || vocab > SAMP_MAX_VOCAB || keep < 1 || keep > SAMP_MAX_KEEP)
         return fail(SAMP_ERR_SHAPE, "1 to %d sequences, 1 to %d beams, a vocabulary of 1 to %d and keep of 1 to %d are supported (%d, %d, %d, %d)", SAMP_MAX_BATCH,
                     SAMP_MAX_BEAMS, SAMP_MAX_VOCAB, SAMP_MAX_KEEP, batch, beams, vocab, keep);
+    if (!pieces_fit(type == SAMP_TYPE_F32, (long)batch * beams, vocab)) return fail(SAMP_ERR_SHAPE, "%d sequences x %d beams x %d logits are more threads than a launch has", batch, beams, vocab);
     return SAMP_OK;
 }
 
@@ -126,7 +127,7 @@ int check_choice(int32_t batch, int32_t kv_heads, int32_t width, int32_t page_le
     if (sinks < 0 || recent < need || keep < 1 || (long)sinks + recent > keep)
         return fail(SAMP_ERR_SHAPE, "sinks >= 0, recent >= %ld for max_new %d, and sinks + recent <= keep are needed (%d, %d, %d)", need, max_new, sinks, recent, keep);
     if (keep > SAMP_MAX_TABLE) return fail(SAMP_ERR_SHAPE, "keep is at most %d (%d)", SAMP_MAX_TABLE, keep);
-    if ((double)batch * kv_heads * (width / 64 + 1) > 2147483647.0) return fail(SAMP_ERR_SHAPE, "batch x key heads x pages is past 2^37");
+    if (!choice_fits(batch, kv_heads, width)) return fail(SAMP_ERR_SHAPE, "%d sequences x %d key heads x %d pages are more threads than a launch has", batch, kv_heads, width);
     return SAMP_OK;
 }
 
@@ -361,7 +362,7 @@ int samp_cache_bounds(const samp_kv_cache_t *cache, const samp_key_bounds_t *bou
 
 size_t samp_cache_select_workspace_bytes(int32_t batch, int32_t kv_heads, int32_t width)
 {
-    if (batch < 1 || batch > SAMP_MAX_BATCH || kv_heads < 1 || kv_heads > SAMP_MAX_HEADS || width < 1 || width > SAMP_MAX_TABLE) return 0;
+    if (batch < 1 || batch > SAMP_MAX_BATCH || kv_heads < 1 || kv_heads > SAMP_MAX_HEADS || width < 1 || width > SAMP_MAX_TABLE || !choice_fits(batch, kv_heads, width)) return 0;
     return up(cache_select_workspace(batch, kv_heads, width));
 }
 
@@ -400,7 +401,7 @@ size_t samp_attention_sparse_workspace_bytes(int32_t rows, int32_t batch, int32_
     Cut cut;
     if (check_page_len(page_len) || keep < 1 || keep > SAMP_MAX_TABLE || width < 1 || width > SAMP_MAX_TABLE) return 0;
     max_len = chosen_len(max_len, keep, page_len);
-    if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len, &cut)) return 0;
+    if (check_cached(rows, batch, heads, kv_heads, head_dim, max_new, max_len, &cut) || !choice_fits(batch, kv_heads, width)) return 0;
     const size_t choice = samp_cache_select_workspace_bytes(batch, kv_heads, width), attention = samp_attention_cache_workspace_bytes(rows, batch, heads, kv_heads, head_dim, max_new, max_len);
     return chosen_bytes(batch, kv_heads, keep) + (choice > attention ? choice : attention);
 }

@@ -574,6 +574,7 @@ hipError_t launch_beam_select(const void *logits, long ld, int type, const float
     if (type == F16) pieces<F16>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
     else if (type == BF16) pieces<BF16>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
     else pieces<F32>(logits, ld, scores, finished, rows, vocab, keep, cut, sums, candidates, st);
+    if (hipError_t err = hipGetLastError()) return err;               // (the join reads what they wrote)
     const size_t lds = sizeof(Entry) * ((size_t)beams * cut.chunks + (size_t)keep * (keep + 1) / 2);
     if (lds > 56 << 10)
         if (hipError_t err = hipFuncSetAttribute((const void *)beam_join_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return err;

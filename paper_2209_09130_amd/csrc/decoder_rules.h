@@ -77,6 +77,14 @@ inline bool long_pieces(bool wide, int rows, int vocab)
     return (long)rows * chunks >= (wide ? 128 : 512) && 2 * piece_chunks(SHORT_PIECE, wide, vocab) >= 11 * chunks;
 }
 
+// A launch has fewer than 2^32 threads in a direction
+constexpr long LAUNCH_THREADS = 1l << 32;
+inline bool pieces_fit(bool wide, long rows, int vocab)
+{
+    const BeamPiece p = rows < 1l << 31 && long_pieces(wide, (int)rows, vocab) ? LONG_PIECE : SHORT_PIECE;
+    return rows * piece_chunks(p, wide, vocab) * p.threads < LAUNCH_THREADS;
+}
+
 // ---- bookkeeping of pages ------------------------------------------------------------------------------
 // One block does a whole call where its counters fit the LDS of a CU (two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 bytes for each
 // old one; 6 bytes for each page) and its 16 waves are no slower than the launches of several.  us in a chain of calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 5.4 / 13.6,
@@ -94,5 +102,13 @@ inline bool compact_in_block(long pages, long entries) { return pages <= 8192 &&
 // block of sixteen waves for 1 x 8 x 1563 21 / 11.
 constexpr int SCORED_TOGETHER = 256;
 inline bool scores_apart(int width) { return width > SCORED_TOGETHER; }
+// Threads of a block that chooses among scores that are there, by the most pages that it can have
+inline int choice_threads(int width) { return width <= 512 ? 256 : width <= 1024 ? 512 : 1024; }
+// Of the two launches that of the scores, 256 threads for each 128 pages of a sequence and a key head, always has more threads
+constexpr int SCORES_BLOCK = 128;
+inline bool choice_fits(long batch, long kv_heads, int width)
+{
+    return batch * kv_heads * (scores_apart(width) ? (width + SCORES_BLOCK - 1) / SCORES_BLOCK : 1) * 256 < LAUNCH_THREADS;
+}
 
 }  // namespace samp

@@ -261,16 +261,16 @@ __device__ __forceinline__ Seen what_is_seen(const KvCache &c, const KvRows &row
 // scores [batch, kv_heads, width]; a wave has 32 pages of a sequence and a key head.  What bounds it is a chain of dependent loads (lengths and page numbers, bounds) and then HBM: 64 contexts of 900 to 32768 tokens in
 // pages of 64, 8 key heads of 128 (35 MB) 13.0 us, one of 100000 4.3; 25 of 85000 in pages of 32, 4 key heads, 35 rows of queries each (69 MB) 21 us, 37 where the bounds were read
 // again for every sixteen rows.  (64 pages a wave: 13.5 and 5.4; blocks of the key heads of a page on one XCD, which shares their steps: no difference.)
-constexpr int OF_WAVE = 32;
+constexpr int OF_WAVE = SCORES_BLOCK / 4;
 template <bool BF, int D>
 __global__ __launch_bounds__(256, 4) void page_scores_kernel(const char *__restrict__ Q, long ldq, KvCache c, KeyBounds bounds, KvRows rows, int group, int keep, int sinks,
                                                           int recent, unsigned *__restrict__ scores)
 {
     const int head = blockIdx.x % c.kv_heads, item = blockIdx.x / c.kv_heads, chunk = item / rows.batch, b = item - chunk * rows.batch;
-    const int first = chunk * 4 * OF_WAVE + __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * OF_WAVE), page = first + (threadIdx.x & 63);
+    const int first = chunk * SCORES_BLOCK + __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) * OF_WAVE), page = first + (threadIdx.x & 63);
     const int entry = rows.table[(size_t)b * rows.width + min(page, rows.width - 1)];              // (on its way with the lengths)
     const Seen seen = what_is_seen(c, rows, b, head, group, keep, sinks, recent);
-    if (seen.pages <= keep || chunk * 4 * OF_WAVE >= seen.pages) return;
+    if (seen.pages <= keep || chunk * SCORES_BLOCK >= seen.pages) return;
     unsigned *const to = scores + ((size_t)b * c.kv_heads + head) * rows.width;
     score_pages<BF, D, OF_WAVE / 16>(Q, ldq, c, bounds, seen, first, page < seen.pages ? entry : -1,
                        [&](int p, unsigned x) { to[p] = x; });
@@ -517,11 +517,11 @@ hipError_t select_pages(const void *q, long ldq, int heads, const KvCache &c, co
     }
     if (lds > 40 << 10)
         if (hipError_t e = hipFuncSetAttribute((const void *)select_scored_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
-    const unsigned items = (unsigned)((rows.width + 4 * OF_WAVE - 1) / (4 * OF_WAVE)) * rows.batch;
+    const unsigned items = (unsigned)((rows.width + SCORES_BLOCK - 1) / SCORES_BLOCK) * rows.batch;
     hipLaunchKernelGGL((page_scores_kernel<BF, D>), dim3(items * c.kv_heads), dim3(256), 0, st, (const char *)q, ldq, c, bounds, rows, group, keep, sinks, recent,
                        scores);
-    const int threads = rows.width <= 512 ? 256 : rows.width <= 1024 ? 512 : 1024;
-    hipLaunchKernelGGL(select_scored_kernel, grid, dim3(threads), lds, st, c, rows, keep, sinks, recent, scores, tables, lens_out);
+    if (hipError_t e = hipGetLastError()) return e;                   // (the choice reads what they wrote)
+    hipLaunchKernelGGL(select_scored_kernel, grid, dim3(choice_threads(rows.width)), lds, st, c, rows, keep, sinks, recent, scores, tables, lens_out);
     return hipGetLastError();
 }
 

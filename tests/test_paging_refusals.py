@@ -96,6 +96,26 @@ def test_cache_select_and_attention_sparse(L):
         ({"bytes": need - 1}, SPACE, b"workspace"), ({"workspace": AT + 8}, SPACE, b"workspace")])
 
 
+def test_launches_of_more_threads_than_there_are(L):
+    """A launch has fewer than 2^32 threads: one sequence below, the next thing that is wrong is named, the workspace."""
+    ok, kb, many = cache(kv_heads=8), bounds(), cache(kv_heads=1024)
+    head = [("q", AT), ("ldq", 1 << 17), ("type", 0), ("heads", 8), ("cache", C.addressof(ok)), ("bounds", C.addressof(kb)), ("table", AT), ("width", 32768), ("cu", AT), ("lens", AT),
+            ("batch", 8192), ("max_new", 1)]
+    tail = [("keep", 6), ("sinks", 1), ("recent", 1)]
+    choice = head + [("rows", 8192)] + tail + [("tables", AT), ("lens_out", AT + 64), ("workspace", None), ("bytes", 1 << 40), ("stream", None)]
+    sparse = head + [("max_len", 32), ("rows", 8192)] + tail + [("scale", 0.125), ("tree", None), ("out", AT), ("workspace", None), ("bytes", 1 << 40), ("stream", None)]
+    wide = {"cache": C.addressof(many), "heads": 1024}               # 256 threads for each 128 pages, or fewer: 2^24 blocks are one too many
+    cases = [({}, SHAPE, b"launch"), ({"batch": 8191}, SPACE, b"workspace"), ({"width": 32641}, SHAPE, b"launch"), ({"width": 32640}, SPACE, b"workspace"),
+             ({**wide, "width": 257, "batch": 5461}, SPACE, b"workspace"), ({**wide, "width": 257, "batch": 5462}, SHAPE, b"launch")]
+    refusals(L.samp_cache_select, choice, cases)
+    refusals(L.samp_attention_sparse, sparse, cases)
+    assert L.samp_cache_select_workspace_bytes(8192, 8, 32768) == 0 and L.samp_cache_select_workspace_bytes(8191, 8, 32768) >= 8191 * 8 * 32768 * 4
+    assert L.samp_attention_sparse_workspace_bytes(8192, 8192, 8, 8, 64, 16, 32768, 1, 32, 6) == 0 and L.samp_attention_sparse_workspace_bytes(8191, 8191, 8, 8, 64, 16, 32768, 1, 32, 6) > 0
+    base = [("logits", AT), ("ld", 1 << 19), ("type", 0), ("scores", AT), ("finished", None), ("end", 0), ("batch", 8192), ("beams", 64), ("vocab", 1 << 19), ("keep", 5), ("best", AT),
+            ("parents", AT), ("tokens", AT), ("workspace", None), ("bytes", 0), ("stream", None)]
+    refusals(L.samp_beam_select, base, [({}, SHAPE, b"launch"), ({"vocab": (1 << 19) - 7}, SHAPE, b"launch"), ({"vocab": (1 << 19) - 7 - (1 << 15)}, SPACE, b"workspace"), ({"type": 2}, SHAPE, b"launch"), ({"batch": 4096}, SPACE, b"workspace")])
+
+
 def test_the_binding_refuses_what_is_not_on_the_gpu():
     i = torch.zeros(2, 4, dtype=torch.int32)
     for call in (lambda: P.beam_select(torch.zeros(2, 8), torch.zeros(2), 1), lambda: P.pages_fork(i[0], i, i[:, 0], 16), lambda: P.pages_compact(i[0], i, 16),
