@@ -58,10 +58,10 @@ template <bool MAX, int N> __device__ __forceinline__ float of_each(float (&x)[N
     static_assert(N == 2 || N == 8, "pieces have two vectors a thread or eight");
     constexpr int A = N / 2, B = N == 8 ? 2 : 1;
     float a[A], b[B], c;
-    if constexpr (MAX) settle(x);
+    if constexpr (MAX) settle<N>(x);
 #pragma unroll
     for (int i = 0; i < A; i++) a[i] = met<MAX>(meet<32>(x[i], x[i + A], lane));
-    if constexpr (MAX) settle(a);
+    if constexpr (MAX) settle<A>(a);
 #pragma unroll
     for (int i = 0; i < B; i++) b[i] = met<MAX>(meet<16>(a[i], a[i + (N == 8 ? B : 0)], lane));
     c = met<MAX>(meet<8>(b[0], b[B - 1], lane));

@@ -46,7 +46,7 @@ __device__ __forceinline__ int wave_scan(int x)
     return x;
 }
 
-// The larger of three.  (The compiler's own maxima quiet signalling NaN in front: another instruction each.)  A lane exchange that reads a result has to wait two states, for which the compiler
+// The largest, the smallest of three.  (The compiler's own quiet signalling NaN in front: another instruction each.)  A lane exchange that reads a result has to wait two states, for which the compiler
 // does not look into asm where the exchange is a swap of halves: settle() in front of those.
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -54,15 +54,22 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
     return r;
 }
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float r;
+    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 __device__ __forceinline__ void settle(float &a, float &b) { asm("s_nop 1" : "+v"(a), "+v"(b)); }
 __device__ __forceinline__ void settle(float &a, float &b, float &c, float &d) { asm("s_nop 1" : "+v"(a), "+v"(b), "+v"(c), "+v"(d)); }
-template <int N> __device__ __forceinline__ void settle(float (&x)[N])
+// of the first M
+template <int M, int N> __device__ __forceinline__ void settle(float (&x)[N])
 {
-    static_assert(N == 1 || N == 2 || N % 4 == 0, "one, two or fours");
-    if constexpr (N <= 2) settle(x[0], x[N - 1]);
+    static_assert(M <= N && (M == 1 || M == 2 || M % 4 == 0), "one, two or fours");
+    if constexpr (M <= 2) settle(x[0], x[M - 1]);
     else
 #pragma unroll
-        for (int i = 0; i < N; i += 4) settle(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        for (int i = 0; i < M; i += 4) settle(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 template <int CTRL> __device__ __forceinline__ float other_lane(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); }
 // Lanes l and l ^ HALF of two values: the lower of the two lanes gets the first value of both, the upper the second

@@ -16,35 +16,11 @@ constexpr float INV_127 = 1.0f / 127.0f;
 // A wave takes a page of a key head: D / 16 lanes hold 16 channels each of 1024 / D keys at a time; then the lanes of the same channels meet and share them out, D / 64 of them a lane.
 // What bounds it is HBM for whole prompts (16 of 2000 to 8192 positions, 8 key heads of 128: 88 MB, 18.5 us, 4.8 TB/s), and the launch for a decode step (3.4 us), in which few pages become
 // full and the other waves end at once.
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
-__device__ __forceinline__ float min3(float a, float b, float c)
-{
-    float r;
-    asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
 // Of two channels the lower half of the lanes (or of each 32, 16, 8) gets the first, the upper the second, each from both halves
 template <int HALF, bool MAX> __device__ __forceinline__ float share(float a, float b, int lane)
 {
-    float x, y;
-    if constexpr (HALF == 32) {
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-        x = __uint_as_float(both[0]), y = __uint_as_float(both[1]);
-    } else if constexpr (HALF == 16) {
-        const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
-        x = __uint_as_float(both[0]), y = __uint_as_float(both[1]);
-    } else {
-        const bool upper = lane & HALF;
-        const int give = __float_as_int(upper ? a : b);
-        x = upper ? b : a;
-        y = __int_as_float(HALF == 8 ? __builtin_amdgcn_update_dpp(0, give, 0x128, 0xf, 0xf, true) : __builtin_amdgcn_ds_swizzle(give, HALF << 10 | 0x1f));
-    }
-    return MAX ? max3(x, x, y) : min3(x, x, y);
+    const Met m = meet<HALF>(a, b, lane);
+    return MAX ? max3(m.x, m.x, m.y) : min3(m.x, m.x, m.y);
 }
 
 // AT: keys at a time, 32, or 16 for pages of no more (138 MB in pages of 64 24.8 us; of 16 38.5, bound by the vector ALUs, and 49.0 by the kernel of 32, each key twice)
@@ -91,11 +67,15 @@ __global__ __launch_bounds__(256) void cache_bounds_kernel(KvCache c, KeyBounds 
         }
     }
     const bool bad = __any(!(odd == 0.0f));
+    settle<16>(high);
+    settle<16>(low);
 #pragma unroll
     for (int e = 0; e < 8; e++) {
         high[e] = share<32, true>(high[e], high[e + 8], lane);
         low[e] = share<32, false>(low[e], low[e + 8], lane);
     }
+    settle<8>(high);
+    settle<8>(low);
 #pragma unroll
     for (int e = 0; e < 4; e++) {
         high[e] = share<16, true>(high[e], high[e + 4], lane);
