@@ -73,16 +73,9 @@ template <bool MAX, int N> __device__ __forceinline__ float of_each(float (&x)[N
 struct Candidate { float logit; int token; };                         // token -1: none
 constexpr int BLOCK_OF = 8;                                           // granules of a block
 struct BlockSum { float top, sum; };                                  // sum of exp(x - top)
-// A number of the order of the value (one zero; not for NaN); with the place behind it, the lower one first
-__device__ __forceinline__ unsigned order_of(float x)
-{
-    const unsigned u = __float_as_uint(x + 0.0f);
-    return u >> 31 ? ~u : u | 1u << 31;
-}
+// The order of a value with the place behind it, the lower one first
 __device__ __forceinline__ unsigned long long listed_of(float x, int place) { return (unsigned long long)order_of(x) << 32 | (unsigned)~place; }
 __device__ __forceinline__ bool before(unsigned long long a, unsigned long long b) { return a > b; }
-// The value of a number whose order as an unsigned integer is the values' own (NaN outside the infinities: nothing reaches those)
-__device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t >> 31 ? t & 0x7fffffffu : ~t); }
 
 // How many of `all` come before `mine`, counted by 2^n lanes `step` that have each every step-th; and f(entry, how many come before it) for each of n entries, by THREADS threads.
 // Eight (numbers of 16 bytes: four) are read together; one at a time took 110 clocks each.

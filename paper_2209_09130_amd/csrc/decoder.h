@@ -89,6 +89,14 @@ template <int HALF> __device__ __forceinline__ Met meet(float a, float b, int la
     }
 }
 
+// A whole number of the order of the values, the two zeros the same (not for NaN), and back: numbers outside the infinities' are NaN, which nothing reaches
+__device__ __forceinline__ unsigned order_of(float x)
+{
+    const unsigned u = __float_as_uint(x + 0.0f);
+    return u >> 31 ? ~u : u | 1u << 31;
+}
+__device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t >> 31 ? t & 0x7fffffffu : ~t); }
+
 // The largest magnitude of 16-bit values, by their bits (two running maxima, in the halves of a dword): infinities come above every number and NaN above them
 typedef unsigned short v2u16 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ unsigned max_halves(unsigned a, unsigned b)

@@ -116,20 +116,14 @@ __global__ __launch_bounds__(256) void cache_bounds_kernel(KvCache c, KeyBounds 
 }
 
 // ---- choice ------------------------------------------------------------------------------------------
-// A binary32 number as a whole number of the same order; NaN counts as plus infinity
-__device__ __forceinline__ unsigned order_of(float x)
-{
-    const unsigned u = __float_as_uint(x);
-    if (x != x) return 0xff800000u;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
+// NaN counts as plus infinity
+__device__ __forceinline__ unsigned order_of_score(float x) { return x != x ? order_of(INFINITY) : order_of(x); }
 template <bool BF> __device__ __forceinline__ float largest(unsigned bits)
 {
     return BF ? __uint_as_float(bits << 16) : (float)__builtin_bit_cast(_Float16, (unsigned short)bits);
 }
 constexpr unsigned ALWAYS = 0xfffffffeu;                              // above the order of every number, and a number above it
 
-__device__ __forceinline__ float value_of_order(unsigned t) { return __uint_as_float(t & 0x80000000u ? t & 0x7fffffffu : ~t); }
 constexpr int BINS = 1024, LIST = 512, WORDS = SAMP_MAX_TABLE / 64;
 struct Scored { unsigned score; int page; };
 
@@ -209,7 +203,7 @@ __device__ __forceinline__ void score_pages(const char *__restrict__ Q, long ldq
             const float s = __shfl(page_step, 16 * t + r, 64);
 #pragma unroll
             for (int e = 0; e < 4; e++)
-                if (r0 + 4 * g + e < all) best[t] = max(best[t], order_of((float)sum[e] * (qs[e] * s)));
+                if (r0 + 4 * g + e < all) best[t] = max(best[t], order_of_score((float)sum[e] * (qs[e] * s)));
         }
     }
     unsigned mine = 0;

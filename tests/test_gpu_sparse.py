@@ -415,3 +415,17 @@ def test_holes_of_a_sequence_without_new_tokens(P, pages):
             assert tables[b, g].tolist() == [int(table[b, j]) for j in want[g]], (b, g)
         if b == 0:
             assert want[0] == [0, 1, 2, 3, 4, 5, 6, pages - 2, pages - 1]
+
+
+@pytest.mark.parametrize("pages", [40, 300])
+def test_scores_that_are_zeros_of_either_sign_are_equal(P, pages):
+    """Steps so small that the products of some pages are zeros, some of them negative ones: equal scores, of which the earlier pages are kept."""
+    page, G, D, keep = 16, 2, 64, 9
+    plan = Plan(P, [16 * pages], [1], G, D, page)
+    plan.fill(P, BF16, 3)
+    bounds = P.KeyBounds(torch.randint(-127, 128, (plan.cache.pages, G, 2, D), generator=gen(1), dtype=torch.int8).cuda(), torch.full((plan.cache.pages, G), 1e-38, device="cuda"))
+    q = (torch.randn(1, 4, D, generator=gen(5)) * 1e-15).bfloat16()
+    tables, _ = P.cache_select(q.cuda(), plan.cache, bounds, *plan.args, 1, keep, 1, 2)
+    want = choose_definition(q, bounds.codes.cpu(), bounds.steps.cpu(), plan.table[0], pages, keep, 1, 2, 4, G)
+    assert want == [[0, 1, 2, 3, 4, 5, 6, pages - 2, pages - 1]] * G
+    assert tables[0].tolist() == [[int(plan.table[0, j]) for j in want[g]] for g in range(G)]
