@@ -394,7 +394,7 @@ def pages_fork(refs: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, page
     refs_out, table_out, lens_out, copies, lacking = _parts(refs, (pages, rows * width, rows, 3 * rows, 1))
     need = _workspace_bytes("samp_pages_fork_workspace_bytes", pages, rows_from, width, rows)
     ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
-    rc = _fn("samp_pages_fork")(pr, pages, pt, pl, rows_from, width, page_len, pp, pc, _most(max_new), rows, refs_out.data_ptr(), table_out.data_ptr(),
+    rc = _fn("samp_pages_fork")(pr, pages, pt, pl, rows_from, width, _most(page_len), pp, pc, _most(max_new), rows, refs_out.data_ptr(), table_out.data_ptr(),
                                 lens_out.data_ptr(), copies.data_ptr(), lacking.data_ptr(), ws.data_ptr() if need else 0, need, _raw_stream(device))
     if rc:
         _raise(rc)
@@ -415,7 +415,7 @@ def pages_compact(refs: torch.Tensor, table: torch.Tensor, page_len: int) -> Tup
     refs_out, table_out, copies, used = _parts(refs, (pages, entries, 3 * n, 1))
     need = _workspace_bytes("samp_pages_compact_workspace_bytes", pages, entries)
     ws = refs.new_empty((need,), dtype=torch.uint8) if need else None
-    rc = _fn("samp_pages_compact")(pr, pages, pt, entries, page_len, refs_out.data_ptr(), table_out.data_ptr(), copies.data_ptr(), used.data_ptr(),
+    rc = _fn("samp_pages_compact")(pr, pages, pt, entries, _most(page_len), refs_out.data_ptr(), table_out.data_ptr(), copies.data_ptr(), used.data_ptr(),
                                    ws.data_ptr() if need else 0, need, _raw_stream(device))
     if rc:
         _raise(rc)
@@ -479,7 +479,7 @@ def cache_bounds(cache: KVCache, bounds: KeyBounds, table: torch.Tensor, cu: Opt
     if rows is None:
         rows = B * max_new if cu is None else 1 << 24
     if rows and B:
-        rc = _fn("samp_cache_bounds")(cache.address, kb, t, width, pcu, plens, B, max_new, rows, _raw_stream(device))
+        rc = _fn("samp_cache_bounds")(cache.address, kb, t, width, pcu, plens, B, max_new, _most(rows), _raw_stream(device))
         if rc:
             _raise(rc)
 

@@ -122,3 +122,40 @@ def test_the_binding_refuses_what_is_not_on_the_gpu():
                  lambda: P.KeyBounds(torch.zeros(1, 1, 2, 64, dtype=torch.int8), torch.zeros(1, 1))):
         with pytest.raises(P.SampError, match="GPU"):
             call()
+
+
+@pytest.fixture
+def passed(monkeypatch):
+    """What the binding hands to each entry point, on the CPU: nothing is called."""
+    seen = {}
+
+    def entry(name):
+        argtypes = D._SIGNATURES[name]
+
+        def call(*args):
+            assert len(args) == len(argtypes)
+            seen[name] = [t(a).value for t, a in zip(argtypes, args)]          # as ctypes converts them
+            return 0
+        return call
+
+    monkeypatch.setattr(D, "_fn", entry)
+    monkeypatch.setattr(D, "_device", lambda t: -1)
+    monkeypatch.setattr(D, "_current_device", lambda: -1)
+    monkeypatch.setattr(D, "_raw_stream", lambda device: 0)
+    D._workspace_bytes.cache_clear()
+    yield seen
+    D._workspace_bytes.cache_clear()
+
+
+def test_numbers_past_int32_are_not_cut(passed):
+    """ctypes passes the low 32 bits of a larger number: the entry has to see one that it refuses, or that counts as the largest."""
+    i = torch.zeros(2, 4, dtype=torch.int32)
+    most = 2 ** 31 - 1
+    for n, want in ((16, 16), ((1 << 32) + 16, most), (-(1 << 32) + 16, -1)):
+        P.pages_fork(i[0], i, i[0, :2], n)
+        assert passed["samp_pages_fork"][6] == want
+        P.pages_compact(i[0], i, n)
+        assert passed["samp_pages_compact"][4] == want
+        cache_ = P.KVCache.empty(4, 2, 16, 64, device="cpu")
+        P.cache_bounds(cache_, P.KeyBounds.empty(cache_), i, torch.zeros(3, dtype=torch.int32), i[0, :2], 3, rows=n)
+        assert passed["samp_cache_bounds"][8] == want
