@@ -111,9 +111,9 @@ __device__ __forceinline__ bool row_counts(const float *scores, const uint8_t *f
     return __builtin_isfinite(scores[row]) && !(finished && finished[row]);
 }
 
-// One piece of one row: what bounds it is HBM where there are rows enough (512 rows of 128256, of which a quarter are finished or have no score and are not read: 97 MB, 24.2 us, 4.0 TB/s;
-// the vector ALUs issue half of that time, nine instructions a logit), else its chain of one trip to memory, two reductions and the list: 35 rows of 50265
-// binary32 6.4 us, 4 rows of 21128 4.6.  Vectors of 16 bytes are counted from the row's first value, wherever that lies; what of the last one lies behind the row counts as minus infinity.
+// One piece of one row: what bounds it is HBM where there are rows enough (512 rows of 128256, of which a quarter are finished or have no score and are not read: 97 MB, 25.7 us, 3.8 TB/s;
+// the vector ALUs issue six tenths of that time, eleven instructions a logit), else its chain of one trip to memory, two reductions and the list: 35 rows of 50265
+// binary32 6.6 us, 4 rows of 21128 4.8.  Vectors of 16 bytes are counted from the row's first value, wherever that lies; what of the last one lies behind the row counts as minus infinity.
 template <int T, int THREADS, int VECTORS, int GROUPS>
 __global__ __launch_bounds__(THREADS, 8) void beam_pieces_kernel(const char *__restrict__ logits, long ld, const float *__restrict__ scores,
                                                               const uint8_t *__restrict__ finished, int vocab, int keep, int chunks,
@@ -441,7 +441,7 @@ template <class F> __device__ __forceinline__ void rank_best(const Entry *all, i
     if (mine == 0) f(best.at[i], e, better);
 }
 
-// A block a sequence.  A few dependent steps over some thousand numbers: 7.3 us for 64 sequences of 8 rows in 4 pieces each, keep = 16; 5.6 for one of 4 rows in 6.
+// A block a sequence.  A few dependent steps over some thousand numbers: 7.4 us for 64 sequences of 8 rows in 4 pieces each, keep = 16; 5.2 for one of 4 rows in 6.
 __global__ __launch_bounds__(JOIN) void beam_join_kernel(const BlockSum *__restrict__ sums, const Candidate *__restrict__ best, const float *__restrict__ scores,
                                                          const uint8_t *__restrict__ finished, int end, int beams, int keep, int chunks, int blocks, float *__restrict__ out,
                                                          int *__restrict__ parents, int *__restrict__ tokens)

@@ -59,11 +59,11 @@ inline int cache_passes(long rows, int kv_heads) { return rows * kv_heads >= 327
 
 // ---- beam search's selection -----------------------------------------------------------------------------
 // A row is cut into pieces of 512 threads with eight vectors of 16 bytes each where that makes enough of them, else of 256 with two.  us, both kernels, long / short pieces, rows x vocabulary:
-// 16 bits 64 x 32000 13.9 / 11.4, 256 x 32000 15.6 / 14.4, 512 x 32000 18.1 / 18.8, 64 x 128256 14.7 / 14.7, 128 x 128256 17.1 / 18.9; binary32, whose short pieces are half as many
-// values, 4 x 21128 11.3 / 9.7, 64 x 32000 12.4 / 12.0, 16 x 128256 12.2 / 14.7, 32 x 128256 13.3 / 16.1, 512 x 32000 20.8 / 25.0, 128 x 128256 20.8 / 27.4.
-// A long piece takes as long as five or six short ones, full or not: 16 bits 1024 x 1000 22.3 / 13.6, 1024 x 16000 21.7 / 19.7, 1024 x 21000 21.7 / 22.3, 1024 x 36000 30.3 / 27.7, 1024 x 50304
-// 29.4 / 36.5; binary32 1024 x 8000 19.0 / 18.3, 1024 x 12000 20.0 / 20.8, 512 x 12000 16.7 / 15.5, 512 x 21000 17.9 / 19.3.  (Long pieces of 256 threads take as long, with four
-// vectors of 512 up to 2 us longer: 512 x 128256 29.7 and 31.8.)
+// 16 bits 64 x 32000 14.0 / 10.8, 256 x 32000 14.3 / 14.0, 512 x 32000 17.8 / 18.9, 64 x 128256 13.6 / 14.3, 128 x 128256 16.9 / 19.5; binary32, whose short pieces are half as many
+// values, 4 x 21128 11.9 / 9.6, 64 x 32000 12.0 / 11.3, 16 x 128256 12.0 / 12.8, 32 x 128256 12.3 / 14.3, 512 x 32000 20.6 / 25.2, 128 x 128256 20.9 / 26.4.
+// A long piece takes as long as five or six short ones, full or not: 16 bits 1024 x 1000 21.4 / 13.4, 1024 x 16000 21.7 / 19.2, 1024 x 21000 23.0 / 23.3, 1024 x 36000 30.8 / 29.8, 1024 x 50304
+// 31.5 / 38.6; binary32 1024 x 8000 18.4 / 17.4, 1024 x 12000 19.9 / 21.5, 512 x 12000 15.4 / 15.1, 512 x 21000 18.6 / 20.2.  Around the border the other kind is up to 0.7 us faster (64 x 128256 of
+// 16 bits goes to the short ones, 64 x 32000 and 512 x 12000 of binary32 to the long ones).
 struct BeamPiece { int threads, vectors; };
 constexpr BeamPiece LONG_PIECE{512, 8}, SHORT_PIECE{256, 2};
 inline int piece_chunks(BeamPiece p, bool wide, int vocab)
@@ -87,9 +87,10 @@ inline bool pieces_fit(bool wide, long rows, int vocab)
 
 // ---- bookkeeping of pages ------------------------------------------------------------------------------
 // One block does a whole call where its counters fit the LDS of a CU (two of 4 bytes for each page and a list of 2, a plan of 32 bytes and a number for each new row and 16 bytes for each
-// old one; 6 bytes for each page) and its 16 waves are no slower than the launches of several.  us in a chain of calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 5.4 / 13.6,
+// old one; 6 bytes for each page) and its 16 waves are, called from the host, no slower than the launches of several, four more of which cost another 10 us there.  In a recorded graph they are, by up to a quarter, near the border:
+// us in a chain of recorded calls, one block / several kernels: pages forked, pages x rows x width, 300 x 4 x 20 5.4 / 13.6,
 // 4000 x 256 x 40 9.6 / 15.6, 14000 x 64 x 64 13.8 / 15.7, 13000 x 256 x 64 16.7 / 15.6, 12000 x 64 x 512 17.3 / 15.4, 6000 x 1024 x 32 21.1 / 16.8, 9000 x 1024 x 64 28.4 / 17.3
-// (from the host four more launches cost another 10 us, so draws go to one block); compacted, pages, 300 2.9 / 8.2,
+// compacted, pages, 300 2.9 / 8.2,
 // 4096 4.9 / 10.2, 8192 10.9 / 11.3, 16384 24.8 / 13.9.
 inline long fork_block_lds(long pages, long rows_from, long rows) { return 10 * ((pages + 3) & ~3l) + 16 * rows_from + (32 + 4) * rows; }
 inline bool fork_in_block(long pages, long rows_from, long width, long rows) { return fork_block_lds(pages, rows_from, rows) <= 150 << 10 && rows_from * width <= 32768; }
@@ -102,7 +103,8 @@ inline bool compact_in_block(long pages, long entries) { return pages <= 8192 &&
 // block of sixteen waves for 1 x 8 x 1563 21 / 11.
 constexpr int SCORED_TOGETHER = 256;
 inline bool scores_apart(int width) { return width > SCORED_TOGETHER; }
-// Threads of a block that chooses among scores that are there, by the most pages that it can have
+// Threads of a block that chooses among scores that are there, by the most pages that it can have.  us, scores and choice, with 256 / 512 / 1024, sequences x 8 key heads x pages: 1 x 300 8.1 / 7.8 / 8.2,
+// 64 x 512 20.3 / 20.4 / 21.6, 1 x 1000 9.2 / 8.4 / 8.9, 64 x 1000 34.6 / 34.2 / 35.0, 1 x 1563 11.0 / 9.2 / 9.1, 32 x 1563 30.6 / 28.1 / 28.2, 1 x 4000 15.4 / 11.7 / 10.4, 1 x 32768 84 / 54 / 42
 inline int choice_threads(int width) { return width <= 512 ? 256 : width <= 1024 ? 512 : 1024; }
 // Of the two launches that of the scores, 256 threads for each 128 pages of a sequence and a key head, always has more threads
 constexpr int SCORES_BLOCK = 128;

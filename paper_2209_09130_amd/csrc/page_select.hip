@@ -23,7 +23,8 @@ template <int HALF, bool MAX> __device__ __forceinline__ float share(float a, fl
     return MAX ? max3(m.x, m.x, m.y) : min3(m.x, m.x, m.y);
 }
 
-// AT: keys at a time, 32, or 16 for pages of no more (138 MB in pages of 64 24.8 us; of 16 38.5, bound by the vector ALUs, and 49.0 by the kernel of 32, each key twice)
+// AT: keys at a time, 32, or 16 for pages of no more (138 MB, inputs that change from call to call: in pages of 64 32.9 us, of 16 42.6, bound by the vector ALUs; the kernel of 32, each key twice,
+// takes a quarter longer for those)
 template <int D, int AT>
 __global__ __launch_bounds__(256) void cache_bounds_kernel(KvCache c, KeyBounds bounds, KvRows rows)
 {

@@ -429,3 +429,31 @@ def test_scores_that_are_zeros_of_either_sign_are_equal(P, pages):
     want = choose_definition(q, bounds.codes.cpu(), bounds.steps.cpu(), plan.table[0], pages, keep, 1, 2, 4, G)
     assert want == [[0, 1, 2, 3, 4, 5, 6, pages - 2, pages - 1]] * G
     assert tables[0].tolist() == [[int(plan.table[0, j]) for j in want[g]] for g in range(G)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("lens,new,page,keep", [([9000, 70, 20000, 4000], [1, 1, 1, 1], 16, 100), ([30000] * 3 + [900, 2000], [1] * 5, 64, 32), ([5001, 700, 1500], [5, 5, 2], 32, 20)])
+def test_calls_repeat_themselves(P, lens, new, page, keep, dtype):
+    """The same inputs give the same bits: again, after other memory's use for the workspace, beside another stream's work, and from a copy of all tensors."""
+    H, G, D = 16, 4, 128
+    plan = Plan(P, lens, new, G, D, page, 3)
+    k, v = (torch.randn(sum(lens), G, D, generator=gen(i)).to(dtype).cuda() for i in (1, 2))
+    q = (torch.randn(plan.total, H, D, generator=gen(3)) * 1.5).to(dtype).cuda()
+    P.cache_write(plan.cache, k, v, plan.args[0], offsets(lens).cuda(), plan.args[2], max(lens))
+    bounds = P.KeyBounds.empty(plan.cache)
+    P.cache_bounds(plan.cache, bounds, plan.args[0], offsets(lens).cuda(), plan.args[2], max(lens))
+    copy = P.KVCache(*(t.clone() for t in (plan.cache.k, plan.cache.v, plan.cache.k_step, plan.cache.v_step)))
+    both = P.KeyBounds(bounds.codes.clone(), bounds.steps.clone())
+    call = lambda c=plan.cache, b=bounds, x=q: P.attention_sparse(x, c, b, *plan.args, max(new), keep)
+    want, chosen = call(), P.cache_select(q, plan.cache, bounds, *plan.args, max(new), keep)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for i in range(6):
+        junk = torch.full((1 << 22,), math.nan, device="cuda")
+        del junk
+        with torch.cuda.stream(side):
+            other = [call(copy, both) for _ in range(3)]
+        got = [call(), call(copy, both, q.clone()), call()]
+        again = P.cache_select(q, copy, both, *plan.args, max(new), keep)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, want) for x in got + other) and all(torch.equal(a, b) for a, b in zip(chosen, again)), i
